@@ -59,8 +59,11 @@ typedef enum {
 #define ML2_MAX_DEPTH 32        /* longest root-to-leaf path, in splits */
 #define ML2_MAX_TREE_NODES 3062 /* nodes of one tree in the ragged layout */
 #define ML2_MAX_FEATURES 256    /* num_features of an ensemble */
-#define ML2_MAX_TOPK 16384      /* k of ml2_filter_topk; m and keep of ml2_rerank */
+#define ML2_MAX_TOPK 16384      /* k of ml2_filter_topk; m and keep of ml2_rerank; draws and
+                                   targets of a row */
 #define ML2_MAX_STREAM_K 4096   /* k of ml2_stream_explorer_create */
+#define ML2_MAX_ROWS 2097152    /* rows of scores of one call */
+#define ML2_MAX_WIDTH 65536     /* columns of ml2_embed and ml2_embed_grad */
 
 typedef struct ml2_ensemble ml2_ensemble; /* opaque; immutable after load */
 
@@ -368,6 +371,125 @@ ml2_status ml2_stream_explorer_chunk(ml2_stream_explorer *ex, const float *X, in
  * round), HIP. */
 ml2_status ml2_stream_explorer_end(ml2_stream_explorer *ex, int32_t *out_idx, float *out_score,
                                    int32_t *num_selected, void *stream);
+
+/* ---- drawing from scores, and learning from what was drawn ----------------
+ *
+ * The calls above answer with the best rows.  These draw rows in proportion
+ * to their scores instead, give the likelihood of rows and its gradient, and
+ * hold the tables that rows index: what an explorer that learns between its
+ * rounds needs (the paper names reinforcement learning for the explorer as
+ * future work).
+ *
+ * Scores are `rows` rows of n entries, element (r, i) at scores[r * ld + i],
+ * in one of the types below; rows = 1 is one pool of candidates.  Any element
+ * alignment and any ld >= n will do.  valid: uint8, element (r, i) at
+ * valid[r * valid_ld + i] (valid_ld = 0: one mask for every row), or NULL.
+ * An entry is INCLUDED iff its mask is nonzero, its score is not NaN and not
+ * -inf.  With m the best included score of the row, R = 1 / T in float32 and
+ * every operation rounded to float32, its exponent is
+ *   z_i = 0 where s_i == m, else (s_i - m) * R.
+ * temperature, top_k, top_p, min_p: device arrays [rows], or NULL for
+ * T = 1 and no such limit.  A row without an included entry is not an error.
+ */
+typedef enum { ML2_F32 = 0, ML2_BF16 = 1, ML2_F16 = 2 } ml2_dtype;
+
+/*
+ * Draws from the softmax of each row, by temperature, top-k, top-p and min-p,
+ * with given uniform numbers u[r * draws + j] in [0, 1).
+ *   weight   q_i = exp(z_i) * 2^31 rounded to the nearest integer (ties to
+ *            even), 0 where not included: sums of weights are exact, so a
+ *            draw does not depend on the order or split of the work
+ *   order    score descending, then index ascending (-0.0 == +0.0)
+ *   top-k    the first top_k entries of that order (top_k <= 0: all)
+ *   top-p    of those, the entries before which less than
+ *            ceil(top_p * their weight) of weight lies (in float64; at least
+ *            the first; top_p >= 1 or NaN: all)
+ *   min-p    of those, the entries with z_i >= log(min_p) (min_p <= 0 or NaN:
+ *            all; min_p > 1 is taken as 1)
+ *   draw     with M the weight kept: idx = the first index i at which the
+ *            weight of the kept entries 0 .. i exceeds
+ *            min(floor(u * M), M - 1)  (u * M in float64)
+ *   logprob  z_idx - log(M / 2^31): its log-probability among the kept
+ * T <= 0 or NaN takes the first entry of the order (greedy).  A row without
+ * an included entry gives idx = -1, logprob = -inf.  An entry whose weight
+ * is below 2^-32 of the best one's is never drawn.
+ * idx: int32 [rows][draws], logprob: float32 [rows][draws], workspace: at
+ * least ml2_sample_workspace_bytes(n, rows, draws) bytes of device memory,
+ * 256-byte aligned, used by this call until it completes.
+ * Errors: INVALID_ARG (unknown dtype, NULL scores, u, outputs or workspace
+ * where they are needed, n, rows, draws < 0, ld < n, valid_ld neither 0 nor
+ * >= n, n > INT32_MAX, misaligned scores, small workspace),
+ * UNSUPPORTED (draws > ML2_MAX_TOPK, rows > ML2_MAX_ROWS), HIP.
+ */
+ml2_status ml2_sample_workspace_bytes(int64_t n, int64_t rows, int32_t draws, size_t *bytes);
+ml2_status ml2_sample(int32_t dtype, const void *scores, int64_t n, int64_t ld, int64_t rows,
+                      const uint8_t *valid, int64_t valid_ld, const float *temperature,
+                      const int32_t *top_k, const float *top_p, const float *min_p,
+                      const float *u, int32_t draws, int32_t *idx, float *logprob,
+                      void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Log-probabilities of `targets` entries of each row (int32, element (r, j)
+ * at targets[r * per_row + j]) under the softmax of the row's included
+ * entries at temperature T (T <= 0 or NaN is taken as 1):
+ *   logprob = z_t - log(sum_i exp(z_i))
+ * A target outside [0, n) (the -1 padding of the selection calls) gives 0
+ * and has no part in the gradient; one that is not included gives -inf and
+ * has none either.  Sums are held in float32.
+ * ml2_logprob_grad also writes the gradient of sum_j weight_j * logprob_j to
+ * the scores, in their type, element (r, i) at grad[r * grad_ld + i]:
+ *   grad_i = R * (sum of weight_j over targets j = i
+ *                 - exp(z_i) / sum_k exp(z_k) * sum_j weight_j)
+ * and 0 where an entry is not included.  weight: float32 [rows][per_row];
+ * logprob: float32 [rows][per_row], or NULL in ml2_logprob_grad.  Weights of
+ * a repeated target are added in the order of j, so results are the same in
+ * every run.  Workspace as in ml2_sample.
+ * Errors as ml2_sample (per_row > ML2_MAX_TOPK: UNSUPPORTED; grad_ld < n:
+ * INVALID_ARG).
+ */
+ml2_status ml2_logprob_workspace_bytes(int64_t n, int64_t rows, int32_t per_row, size_t *bytes);
+ml2_status ml2_logprob(int32_t dtype, const void *scores, int64_t n, int64_t ld, int64_t rows,
+                       const uint8_t *valid, int64_t valid_ld, const float *temperature,
+                       const int32_t *targets, int32_t per_row, float *logprob, void *workspace,
+                       size_t workspace_bytes, void *stream);
+ml2_status ml2_logprob_grad(int32_t dtype, const void *scores, int64_t n, int64_t ld,
+                            int64_t rows, const uint8_t *valid, int64_t valid_ld,
+                            const float *temperature, const int32_t *targets,
+                            const float *weight, int32_t per_row, float *logprob, void *grad,
+                            int64_t grad_ld, void *workspace, size_t workspace_bytes,
+                            void *stream);
+
+/*
+ * Rows of a learned table, scaled: out row i = scale * table row ids[i]
+ * (float32 product, rounded once), zeros where ids[i] lies outside
+ * [0, table_rows).  table: [table_rows][ld] of dtype, columns 0..width-1 are
+ * read; ids: int32 [n]; out: [n][out_ld] of dtype.
+ * Errors: INVALID_ARG (unknown dtype, NULL pointers that are needed, sizes
+ * < 0 or > INT32_MAX, ld or out_ld < width, misaligned arrays), UNSUPPORTED
+ * (width > ML2_MAX_WIDTH), HIP.
+ */
+ml2_status ml2_embed(int32_t dtype, const void *table, int64_t table_rows, int64_t width,
+                     int64_t ld, const int32_t *ids, int64_t n, float scale, void *out,
+                     int64_t out_ld, void *stream);
+
+/*
+ * The gradient of that table: for every row v of [0, table_rows)
+ *   grad row v = scale * sum of dout row i over the i with ids[i] = v
+ * (zeros where there is none; ids outside the table have no part).  The sum
+ * is held in float32 over ids sorted stably, so results are the same in
+ * every run.  dout: [n][dout_ld] of dtype; grad: [table_rows][grad_ld] of
+ * grad_dtype, which is dtype or ML2_F32; every row is written.  workspace:
+ * at least ml2_embed_grad_workspace_bytes(n, table_rows, width) bytes of
+ * device memory, 256-byte aligned, used by this call until it completes.
+ * Errors as ml2_embed, and INVALID_ARG for another grad_dtype or a small
+ * workspace.
+ */
+ml2_status ml2_embed_grad_workspace_bytes(int64_t n, int64_t table_rows, int64_t width,
+                                          size_t *bytes);
+ml2_status ml2_embed_grad(int32_t dtype, const void *dout, int64_t n, int64_t width,
+                          int64_t dout_ld, const int32_t *ids, float scale, int32_t grad_dtype,
+                          void *grad, int64_t table_rows, int64_t grad_ld, void *workspace,
+                          size_t workspace_bytes, void *stream);
 
 /* Thread-local description of the last non-OK status on this thread. */
 const char *ml2_last_error(void);

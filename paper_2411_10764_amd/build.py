@@ -16,7 +16,8 @@ BUILD = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libml2.so")
 SOURCES = ["ml2_host.hip", "walk_kernels.hip", "rank_host.hip", "rank_validity.hip",
            "rank_perf.hip", "rank_ragged.hip", "topk_kernels.hip", "probe_kernels.hip", "pack.cpp",
-           "rank_pack.cpp", "rank_plan.cpp"]
+           "rank_pack.cpp", "rank_plan.cpp", "draw_host.hip", "sample_kernels.hip",
+           "logprob_kernels.hip", "embed_kernels.hip"]
 ARCH = os.environ.get("ML2_OFFLOAD_ARCH", "gfx950")
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")

@@ -1,0 +1,103 @@
+// Shared by the operators over rows of scores and over tables (sample_kernels,
+// logprob_kernels, embed_kernels): element types, launch arguments, and the
+// exponent every one of them takes of a score.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stddef.h>
+#include <stdint.h>
+
+#include "ml2.h"
+
+namespace ml2 {
+
+// Rows of scores with a mask (see ml2.h).
+struct ScoreRows {
+  const void *scores;
+  int64_t n, ld, rows;
+  const uint8_t *valid;  // or null
+  int64_t valid_ld;
+  const float *temperature;  // [rows] or null
+};
+
+struct SampleArgs {
+  ScoreRows s;
+  const int32_t *top_k;  // [rows] or null, as the next two
+  const float *top_p, *min_p;
+  const float *u;  // [rows][draws]
+  int32_t draws;
+  int32_t *idx;
+  float *logprob;
+};
+
+struct LogprobArgs {
+  ScoreRows s;
+  const int32_t *targets;  // [rows][per_row]
+  const float *weight;     // [rows][per_row], null without a gradient
+  int32_t per_row;
+  float *logprob;          // or null
+  void *grad;              // or null
+  int64_t grad_ld;
+};
+
+struct EmbedArgs {
+  const void *table;
+  int64_t table_rows, width, ld;
+  const int32_t *ids;
+  int64_t n;
+  float scale;
+  void *out;
+  int64_t out_ld;
+};
+
+struct EmbedGradArgs {
+  const void *dout;
+  int64_t n, width, dout_ld;
+  const int32_t *ids;
+  float scale;
+  void *grad;
+  int64_t table_rows, grad_ld;
+};
+
+size_t sample_workspace_bytes(int64_t n, int64_t rows, int32_t draws);
+hipError_t launch_sample(int dtype, const SampleArgs &a, void *ws, int cu_count, hipStream_t s);
+size_t logprob_workspace_bytes(int64_t n, int64_t rows, int32_t per_row);
+hipError_t launch_logprob(int dtype, const LogprobArgs &a, void *ws, int cu_count, hipStream_t s);
+hipError_t launch_embed(int dtype, const EmbedArgs &a, int cu_count, hipStream_t s);
+size_t embed_grad_workspace_bytes(int64_t n, int64_t table_rows, int64_t width);
+hipError_t launch_embed_grad(int dtype, int grad_dtype, const EmbedGradArgs &a, void *ws,
+                             int cu_count, hipStream_t s);
+
+// ---- device helpers ---------------------------------------------------------
+
+// Vectors of 16 bytes that need the alignment of one element only (the memory
+// system takes any address; the type keeps the compiler from assuming more).
+template <typename T>
+struct Vec {
+  static constexpr int kLen = 16 / (int)sizeof(T);
+  typedef T type __attribute__((ext_vector_type(kLen), aligned(sizeof(T))));
+};
+
+// A float32 value rounded to an element.  (The compiler would fold a product
+// and its rounding to fp16 into one instruction that rounds once, and only
+// where it sees both: results would depend on the path an element takes.)
+template <typename T>
+__device__ __forceinline__ T narrow(float x) {
+  if constexpr (sizeof(T) == 2) asm("" : "+v"(x));
+  return (T)x;
+}
+
+// A score as float32 with -0.0 canonicalised to +0.0, and -inf where the entry
+// is not included (so a NaN or a masked entry never competes).
+__device__ __forceinline__ float included(float s, bool valid) {
+  return valid && !__builtin_isnan(s) ? s + 0.0f : -__builtin_inff();
+}
+
+__device__ __forceinline__ float inverse_temperature(const float *temperature, int64_t row,
+                                                     bool *greedy) {
+  const float t = temperature ? temperature[row] : 1.0f;
+  *greedy = !(t > 0.0f);
+  return t > 0.0f ? 1.0f / t : 1.0f;
+}
+
+}  // namespace ml2

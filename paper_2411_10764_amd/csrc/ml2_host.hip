@@ -10,6 +10,7 @@
 #include <string.h>
 
 #include <algorithm>
+#include <atomic>
 #include <memory>
 #include <mutex>
 #include <new>
@@ -76,9 +77,9 @@ struct ml2_stream_explorer {
   void *a_ws;         // second-level leaves
 };
 
-namespace {
+namespace ml2 {
 
-thread_local std::string g_last_error;
+static thread_local std::string g_last_error;
 
 ml2_status fail(ml2_status st, const char *fmt, ...) {
   char buf[512];
@@ -100,18 +101,15 @@ ml2_status hip_fail(hipError_t e, const char *what) {
 
 // Compute-unit count per device, queried once.
 int cu_count(int device) {
-  static std::mutex mu;
-  static std::vector<int> cache;
-  std::lock_guard<std::mutex> lock(mu);
-  if ((int)cache.size() <= device) cache.resize(device + 1, 0);
-  if (cache[device] == 0) {
-    int v = 0;
-    if (hipDeviceGetAttribute(&v, hipDeviceAttributeMultiprocessorCount, device) != hipSuccess ||
-        v <= 0)
-      v = 256;
-    cache[device] = v;
-  }
-  return cache[device];
+  static std::atomic<int> cache[64];  // zero: not yet known
+  const bool kept = device >= 0 && device < 64;
+  int v = kept ? cache[device].load(std::memory_order_relaxed) : 0;
+  if (v > 0) return v;
+  if (hipDeviceGetAttribute(&v, hipDeviceAttributeMultiprocessorCount, device) != hipSuccess ||
+      v <= 0)
+    v = 256;
+  if (kept) cache[device].store(v, std::memory_order_relaxed);
+  return v;
 }
 
 ml2_status current_device(int *dev) {
@@ -119,6 +117,15 @@ ml2_status current_device(int *dev) {
   if (e != hipSuccess) return hip_fail(e, "hipGetDevice");
   return ML2_OK;
 }
+
+}  // namespace ml2
+
+namespace {
+
+using ml2::cu_count;
+using ml2::current_device;
+using ml2::fail;
+using ml2::hip_fail;
 
 // ---- descriptor validation ------------------------------------------------
 
@@ -405,7 +412,7 @@ ml2_status load_ensemble(const ml2_ensemble_desc *desc, ml2_ensemble **out) {
 
 extern "C" {
 
-const char *ml2_last_error(void) { return g_last_error.c_str(); }
+const char *ml2_last_error(void) { return ml2::g_last_error.c_str(); }
 
 ml2_status ml2_load_ensemble(const ml2_ensemble_desc *desc, ml2_ensemble **out) {
   try {

@@ -13,6 +13,14 @@
 
 namespace ml2 {
 
+// Error reporting of the entry points: fail() records the thread's message and
+// returns the status it was given.
+ml2_status fail(ml2_status st, const char *fmt, ...);
+ml2_status hip_fail(hipError_t e, const char *what);
+// Compute units of a device, queried once; the calling thread's device.
+int cu_count(int device);
+ml2_status current_device(int *dev);
+
 constexpr size_t kTreeSlack = 128 * 1024;  // readable zero bytes after the tree table
 
 // hipFuncSetAttribute(MaxDynamicSharedMemorySize) for kernel fn on the current

@@ -26,6 +26,9 @@ ML2_MAX_TREE_NODES = 3062
 ML2_MAX_FEATURES = 256
 ML2_MAX_TOPK = 16384
 ML2_MAX_STREAM_K = 4096
+ML2_MAX_ROWS = 2097152
+ML2_MAX_WIDTH = 65536
+ML2_F32, ML2_BF16, ML2_F16 = 0, 1, 2
 
 EXPORTED = (
     "ml2_load_ensemble", "ml2_free_ensemble", "ml2_ensemble_num_features",
@@ -37,6 +40,8 @@ EXPORTED = (
     "ml2_explorer_round", "ml2_stream_explorer_create", "ml2_stream_explorer_free",
     "ml2_stream_explorer_reset", "ml2_stream_explorer_rounds", "ml2_stream_explorer_begin",
     "ml2_stream_explorer_chunk", "ml2_stream_explorer_end", "ml2_last_error",
+    "ml2_sample_workspace_bytes", "ml2_sample", "ml2_logprob_workspace_bytes", "ml2_logprob",
+    "ml2_logprob_grad", "ml2_embed", "ml2_embed_grad_workspace_bytes", "ml2_embed_grad",
 )
 # include/ml2_probe.h: microbenchmarks behind the roofline figures
 EXPORTED_PROBE = ("ml2_probe_visit", "ml2_probe_lds", "ml2_probe_valu", "ml2_tune_walk_plan",
@@ -130,6 +135,19 @@ def lib():
         L.ml2_stream_explorer_chunk.argtypes = [P, P, I64, I64, I64, P]
         L.ml2_stream_explorer_end.restype = I32
         L.ml2_stream_explorer_end.argtypes = [P, P, P, P, P]
+        F32 = ctypes.c_float
+        for f, types in (
+                ("ml2_sample_workspace_bytes", [I64, I64, I32, ctypes.POINTER(SZ)]),
+                ("ml2_sample", [I32, P, I64, I64, I64, P, I64, P, P, P, P, P, I32, P, P, P, SZ, P]),
+                ("ml2_logprob_workspace_bytes", [I64, I64, I32, ctypes.POINTER(SZ)]),
+                ("ml2_logprob", [I32, P, I64, I64, I64, P, I64, P, P, I32, P, P, SZ, P]),
+                ("ml2_logprob_grad", [I32, P, I64, I64, I64, P, I64, P, P, P, I32, P, P, I64, P,
+                                      SZ, P]),
+                ("ml2_embed", [I32, P, I64, I64, I64, P, I64, F32, P, I64, P]),
+                ("ml2_embed_grad_workspace_bytes", [I64, I64, I64, ctypes.POINTER(SZ)]),
+                ("ml2_embed_grad", [I32, P, I64, I64, I64, P, F32, I32, P, I64, I64, P, SZ, P])):
+            getattr(L, f).restype = I32
+            getattr(L, f).argtypes = types
         L.ml2_last_error.restype = ctypes.c_char_p
         L.ml2_last_error.argtypes = []
         D = ctypes.POINTER(ctypes.c_double)
@@ -428,6 +446,241 @@ class Pipeline:
         ml2_score_perf(self.p, X, self.valid, self.score, stream)
         ml2_filter_topk(self.valid, self.score, self.k, self.idx, self.top, self.num, self.ws,
                         self.ws_bytes, self.n, stream)
+
+
+# ---- drawing from scores, and learning from what was drawn -----------------
+
+_DTYPES = {"torch.float32": ML2_F32, "torch.bfloat16": ML2_BF16, "torch.float16": ML2_F16}
+
+
+def _dtype(t) -> int:
+    d = _DTYPES.get(str(t))
+    if d is None:
+        raise ValueError(f"float32, bfloat16 or float16 expected, not {t}")
+    return d
+
+
+def _device(x, name: str) -> None:
+    if not x.is_cuda:
+        raise ValueError(f"{name} must be a device tensor")
+
+
+def _matrix(x, name: str):
+    """(pointer, rows, columns, row stride) of a 2-D device tensor whose
+    columns are contiguous; a single row may have any row stride."""
+    _device(x, name)
+    if x.dim() != 2 or (x.shape[0] > 0 and x.shape[1] > 1 and x.stride(1) != 1):
+        raise ValueError(f"{name} must be a 2-D tensor with unit column stride")
+    rows, n = x.shape
+    return x.data_ptr(), rows, n, x.stride(0) if rows > 1 and n > 0 else max(x.stride(0), n)
+
+
+def _flat(x, name: str, dtype: str, shape):
+    """Pointer of a contiguous device tensor of the given type and shape (or None)."""
+    if x is None:
+        return None
+    _device(x, name)
+    if str(x.dtype) != "torch." + dtype or tuple(x.shape) != tuple(shape) or not x.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous {dtype} tensor of shape {tuple(shape)}")
+    return x.data_ptr()
+
+
+def _mask(valid, rows: int, n: int):
+    """(pointer, row stride) of a uint8 mask [n] (shared) or [rows][n], or None."""
+    if valid is None:
+        return None, 0
+    if str(valid.dtype) not in ("torch.uint8", "torch.bool"):
+        raise ValueError("valid must be a uint8 or bool tensor")
+    _device(valid, "valid")
+    if valid.dim() == 1:
+        if valid.shape[0] != n or (n > 1 and valid.stride(0) != 1):
+            raise ValueError(f"valid must hold {n} contiguous entries")
+        return valid.data_ptr(), 0
+    p, r, c, ld = _matrix(valid, "valid")
+    if (r, c) != (rows, n):
+        raise ValueError(f"valid must be [{n}] or [{rows}][{n}]")
+    return p, ld
+
+
+def _on(device: str | None):
+    import torch
+    return torch.device("cuda") if device is None else torch.device(device)
+
+
+def _space(ws):
+    """(pointer, bytes) of a workspace tensor."""
+    _device(ws, "workspace")
+    return ws.data_ptr(), ws.numel() * ws.element_size()
+
+
+def _workspace(size: int, device):
+    import torch
+    ws = torch.empty(max(size, 256), dtype=torch.uint8, device=device)
+    if ws.data_ptr() % 256:  # holds for torch's caching allocator blocks
+        raise RuntimeError("workspace is not 256-byte aligned")
+    return ws
+
+
+def _bytes(fn, *sizes) -> int:
+    out = ctypes.c_size_t()
+    _check(fn(*sizes, ctypes.byref(out)))
+    return int(out.value)
+
+
+def ml2_sample_workspace_bytes(n: int, rows: int, draws: int) -> int:
+    return _bytes(lib().ml2_sample_workspace_bytes, n, rows, draws)
+
+
+def ml2_sample(scores, u, idx, logprob, workspace, valid=None, temperature=None, top_k=None,
+               top_p=None, min_p=None, stream=None) -> None:
+    """Draws from each row of scores [rows][n] with given uniforms u [rows][draws]."""
+    sp, rows, n, ld = _matrix(scores, "scores")
+    draws = u.shape[-1]
+    vp, vld = _mask(valid, rows, n)
+    _check(lib().ml2_sample(
+        _dtype(scores.dtype), sp, n, ld, rows, vp, vld,
+        _flat(temperature, "temperature", "float32", (rows,)),
+        _flat(top_k, "top_k", "int32", (rows,)), _flat(top_p, "top_p", "float32", (rows,)),
+        _flat(min_p, "min_p", "float32", (rows,)), _flat(u, "u", "float32", (rows, draws)), draws,
+        _flat(idx, "idx", "int32", (rows, draws)),
+        _flat(logprob, "logprob", "float32", (rows, draws)), *_space(workspace),
+        _stream(stream)))
+
+
+def ml2_logprob_workspace_bytes(n: int, rows: int, per_row: int) -> int:
+    return _bytes(lib().ml2_logprob_workspace_bytes, n, rows, per_row)
+
+
+def ml2_logprob(scores, targets, logprob, workspace, valid=None, temperature=None,
+                stream=None) -> None:
+    """Log-probabilities of targets [rows][per_row] under each row's masked softmax."""
+    sp, rows, n, ld = _matrix(scores, "scores")
+    shape = (rows, targets.shape[-1])
+    vp, vld = _mask(valid, rows, n)
+    _check(lib().ml2_logprob(
+        _dtype(scores.dtype), sp, n, ld, rows, vp, vld,
+        _flat(temperature, "temperature", "float32", (rows,)),
+        _flat(targets, "targets", "int32", shape), shape[1],
+        _flat(logprob, "logprob", "float32", shape), *_space(workspace),
+        _stream(stream)))
+
+
+def ml2_logprob_grad(scores, targets, weight, grad, workspace, logprob=None, valid=None,
+                     temperature=None, stream=None) -> None:
+    """The gradient of sum_j weight_j * logprob_j to the scores, in their type
+    (and the log-probabilities, where `logprob` is given)."""
+    sp, rows, n, ld = _matrix(scores, "scores")
+    gp, grows, gn, gld = _matrix(grad, "grad")
+    if (grows, gn) != (rows, n) or grad.dtype != scores.dtype:
+        raise ValueError("grad must have the shape and type of scores")
+    shape = (rows, targets.shape[-1])
+    vp, vld = _mask(valid, rows, n)
+    _check(lib().ml2_logprob_grad(
+        _dtype(scores.dtype), sp, n, ld, rows, vp, vld,
+        _flat(temperature, "temperature", "float32", (rows,)),
+        _flat(targets, "targets", "int32", shape), _flat(weight, "weight", "float32", shape),
+        shape[1], _flat(logprob, "logprob", "float32", shape), gp, gld, *_space(workspace),
+        _stream(stream)))
+
+
+def ml2_embed(table, ids, out, scale: float = 1.0, stream=None) -> None:
+    """out[i] = scale * table[ids[i]], zeros where ids[i] lies outside the table."""
+    tp, V, D, ld = _matrix(table, "table")
+    op, N, width, out_ld = _matrix(out, "out")
+    if width != D or out.dtype != table.dtype:
+        raise ValueError("out must have the table's width and type")
+    _check(lib().ml2_embed(_dtype(table.dtype), tp, V, D, ld, _flat(ids, "ids", "int32", (N,)), N,
+                           scale, op, out_ld, _stream(stream)))
+
+
+def ml2_embed_grad_workspace_bytes(n: int, table_rows: int, width: int) -> int:
+    return _bytes(lib().ml2_embed_grad_workspace_bytes, n, table_rows, width)
+
+
+def ml2_embed_grad(dout, ids, grad, workspace, scale: float = 1.0, stream=None) -> None:
+    """grad[v] = scale * sum of dout[i] over ids[i] == v, for every row of grad
+    (float32 or dout's type)."""
+    dp, N, D, ld = _matrix(dout, "dout")
+    gp, V, width, gld = _matrix(grad, "grad")
+    if width != D:
+        raise ValueError("grad must have dout's width")
+    _check(lib().ml2_embed_grad(_dtype(dout.dtype), dp, N, D, ld, _flat(ids, "ids", "int32", (N,)),
+                                scale, _dtype(grad.dtype), gp, V, gld, *_space(workspace),
+                                _stream(stream)))
+
+
+class Sampler:
+    """Buffers of ml2_sample for rows of n scores and `draws` draws a row."""
+
+    def __init__(self, rows: int, n: int, draws: int = 1, device=None):
+        import torch
+        device = _on(device)
+        self.idx = torch.empty(rows, draws, dtype=torch.int32, device=device)
+        self.logprob = torch.empty(rows, draws, dtype=torch.float32, device=device)
+        self.ws = _workspace(ml2_sample_workspace_bytes(n, rows, draws), device)
+
+    def run(self, scores, u, valid=None, temperature=None, top_k=None, top_p=None, min_p=None,
+            stream=None):
+        """(idx, logprob), both [rows][draws]: this sampler's own buffers."""
+        ml2_sample(scores, u, self.idx, self.logprob, self.ws, valid, temperature, top_k, top_p,
+                   min_p, stream)
+        return self.idx, self.logprob
+
+
+class LogProb:
+    """Buffers of ml2_logprob, and of ml2_logprob_grad where grad_dtype (the
+    scores' type) is given, for rows of n scores and per_row targets a row."""
+
+    def __init__(self, rows: int, n: int, per_row: int = 1, grad_dtype=None, device=None):
+        import torch
+        device = _on(device)
+        self.logprob = torch.empty(rows, per_row, dtype=torch.float32, device=device)
+        self.grad = None
+        if grad_dtype is not None:
+            self.grad = torch.empty(rows, n, dtype=grad_dtype, device=device)
+        self.ws = _workspace(ml2_logprob_workspace_bytes(n, rows, per_row), device)
+
+    def run(self, scores, targets, valid=None, temperature=None, stream=None):
+        """logprob [rows][per_row]: this object's own buffer."""
+        ml2_logprob(scores, targets, self.logprob, self.ws, valid, temperature, stream)
+        return self.logprob
+
+    def run_grad(self, scores, targets, weight, valid=None, temperature=None, stream=None):
+        """(logprob, grad): this object's own buffers."""
+        if self.grad is None:
+            raise ValueError("made without grad_dtype")
+        ml2_logprob_grad(scores, targets, weight, self.grad, self.ws, self.logprob, valid,
+                         temperature, stream)
+        return self.logprob, self.grad
+
+
+class Embedding:
+    """The output buffer of ml2_embed for n tokens of a table of one width."""
+
+    def __init__(self, n: int, width: int, dtype, device=None):
+        import torch
+        self.out = torch.empty(n, width, dtype=dtype, device=_on(device))
+
+    def run(self, table, ids, scale: float = 1.0, stream=None):
+        """out [n][width]: this object's own buffer."""
+        ml2_embed(table, ids, self.out, scale, stream)
+        return self.out
+
+
+class EmbeddingGrad:
+    """Buffers of ml2_embed_grad: the gradient [table_rows][width] in grad_dtype
+    for n tokens."""
+
+    def __init__(self, n: int, table_rows: int, width: int, grad_dtype, device=None):
+        import torch
+        device = _on(device)
+        self.grad = torch.empty(table_rows, width, dtype=grad_dtype, device=device)
+        self.ws = _workspace(ml2_embed_grad_workspace_bytes(n, table_rows, width), device)
+
+    def run(self, dout, ids, scale: float = 1.0, stream=None):
+        """grad [table_rows][width]: this object's own buffer."""
+        ml2_embed_grad(dout, ids, self.grad, self.ws, scale, stream)
+        return self.grad
 
 
 # ---- microbenchmarks (include/ml2_probe.h) ---------------------------------

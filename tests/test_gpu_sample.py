@@ -1,0 +1,232 @@
+"""ml2_sample against the definition in 64 bits: every type, limits alone and
+together, lengths from one entry to a pool, ties, rows without an entry,
+infinities and NaN in and out of the mask, strides and alignments.
+
+The kernel's weights are whole numbers of a float32 exp, the reference's of a
+64-bit one, so a draw that falls within 2 ulp of two entries' border could go
+to either; such draws are left out (the reference says which) and must be
+rare.  All others must be equal.  logprob: z and log(M) are float32 values of
+magnitude up to 23 with one rounding each and logf's 1 ulp, so 4 * 2^-24 * 23
+= 6e-6 absolute."""
+import numpy as np
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+from paper_2411_10764_amd import ml2  # noqa: E402
+from tests import drawutil  # noqa: E402
+
+DEV = "cuda:0"
+TYPES = [torch.float32, torch.bfloat16, torch.float16]
+TOL = 6e-6
+
+
+def _run(scores, u, valid=None, T=None, k=None, p=None, minp=None):
+    """The call and the reference on the same inputs (numpy parameters)."""
+    rows, n = scores.shape
+    par = [None if v is None else torch.tensor(v, dtype=t, device=DEV)
+           for v, t in ((T, torch.float32), (k, torch.int32), (p, torch.float32),
+                        (minp, torch.float32))]
+    s = ml2.Sampler(rows, n, u.shape[1])
+    s.idx.fill_(-77)
+    s.logprob.fill_(float("nan"))
+    idx, logp = s.run(scores, torch.from_numpy(u).to(DEV),
+                      None if valid is None else torch.from_numpy(valid).to(DEV), *par)
+    torch.cuda.synchronize()
+    full = [np.full(rows, d) if v is None else np.asarray(v)
+            for v, d in ((T, 1.0), (k, 0), (p, 1.0), (minp, 0.0))]
+    full[0], full[2], full[3] = (f.astype(np.float32) for f in (full[0], full[2], full[3]))
+    want = drawutil.sample(drawutil.as_float(scores), valid, *full, u)
+    return idx.cpu().numpy(), logp.cpu().numpy(), want
+
+
+def _check(got_idx, got_logp, want, unsure=0.02):
+    idx, logp, sure = want
+    # the second uniform lies within 2^-24 of the row's end: rarely a sure one
+    some = ~np.delete(sure, 1, 1)
+    assert some.sum() <= max(2, unsure * some.size)
+    assert np.array_equal(got_idx[sure], idx[sure])
+    fin = np.isfinite(logp) & sure
+    assert np.array_equal(np.isfinite(got_logp[sure]), np.isfinite(logp[sure]))
+    assert np.all(np.abs(got_logp[fin] - logp[fin]) <= TOL)
+    assert not np.isnan(got_logp).any()
+
+
+def _u(rng, rows, d):
+    u = rng.random((rows, d), dtype=np.float32)
+    u[:, 0] = 0.0
+    if d > 1:
+        u[:, 1] = np.nextafter(np.float32(1), np.float32(0))
+    return u
+
+
+LIMITS = [dict(), dict(k=1), dict(k=7), dict(p=0.9), dict(p=0.0), dict(minp=0.05),
+          dict(k=40, p=0.8), dict(k=1000, p=0.97, minp=0.001), dict(p=0.5, minp=2.0),
+          dict(T=0.0), dict(T=0.25, k=30), dict(T=3.0, p=0.99)]
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("n", [1, 2, 63, 64, 65, 513, 1000, 4096, 8191, 16389, 70001])
+def test_lengths(dtype, n):
+    print(f"[sample] {dtype} n={n}", flush=True)
+    rng = np.random.default_rng(n)
+    for j, lim in enumerate(LIMITS):
+        rows = 3
+        x = torch.from_numpy(rng.standard_normal((rows, n)).astype(np.float32) * 2.5)
+        valid = None if j % 2 else (rng.random((rows, n)) < 0.7).astype(np.uint8)
+        par = {a: np.full(rows, b) for a, b in lim.items()}
+        got = _run(x.to(dtype).to(DEV), _u(rng, rows, 9), valid, **par)
+        _check(*got)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_rows_with_their_own_settings(dtype):
+    rng = np.random.default_rng(5)
+    rows, n = 37, 5003
+    x = torch.from_numpy(rng.standard_normal((rows, n)).astype(np.float32) * 3).to(dtype).to(DEV)
+    got = _run(x, _u(rng, rows, 5), None, T=rng.choice([0.0, -1.0, np.nan, 0.3, 1.0, 1.7], rows),
+               k=rng.choice([-3, 0, 1, 2, 50, 5003, 9999], rows),
+               p=rng.choice([np.nan, 2.0, 1.0, 0.9, 0.2, 0.0, -1.0], rows),
+               minp=rng.choice([np.nan, -1.0, 0.0, 0.01, 0.5, 1.0, 7.0], rows))
+    _check(*got)
+
+
+@pytest.mark.parametrize("n", [100, 3001, 40000])
+@pytest.mark.parametrize("levels", [1, 2, 5])
+def test_ties_go_to_the_lowest_index(n, levels):
+    rng = np.random.default_rng(n + levels)
+    rows = 2
+    x = rng.integers(0, levels, (rows, n)).astype(np.float32)
+    x[x == 0] = rng.choice([0.0, -0.0], (x == 0).sum())
+    for lim in (dict(k=n // 3), dict(k=3), dict(p=0.4), dict(k=n // 2, p=0.3), dict()):
+        par = {a: np.full(rows, b) for a, b in lim.items()}
+        got = _run(torch.from_numpy(x).to(DEV), _u(rng, rows, 16), None, **par)
+        _check(*got, unsure=0.2 if n > 30000 else 0.05)
+
+
+def test_specials():
+    """Rows without an entry, one entry, infinities and NaN in and out of the
+    mask, masks of the type's lowest value."""
+    inf, nan, low = np.inf, np.nan, np.finfo(np.float32).min
+    rng = np.random.default_rng(1)
+    rows = []
+    for fill in ([nan] * 8, [-inf] * 8, [low] * 8, [-inf, nan, 1.5, -inf], [inf, 1.0, inf, -inf],
+                 [low, low, 3.0, low], [-low, -low, low, 0.0], [0.0, -0.0, 0.0, nan],
+                 [1e-45, 0.0, -1e-45, -inf], [inf, -low, 2.0, nan]):
+        rows.append((fill * 8)[:8])
+    x = np.array(rows, np.float32)
+    ones = np.ones_like(x, dtype=np.uint8)
+    none = np.zeros_like(ones)
+    half = (rng.random(x.shape) < 0.5).astype(np.uint8)
+    for valid in (None, ones, none, half):
+        for lim in (dict(), dict(k=3), dict(p=0.6), dict(minp=0.5), dict(T=0.0), dict(T=1e-38),
+                    dict(T=np.inf), dict(T=1e-45, k=2)):
+            par = {a: np.full(len(x), b) for a, b in lim.items()}
+            got = _run(torch.from_numpy(x).to(DEV), _u(rng, len(x), 6), valid, **par)
+            _check(*got, unsure=0.35)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("offset,pad", [(0, 0), (1, 0), (3, 5), (1, 1), (0, 64)])
+def test_strides_and_alignment(dtype, offset, pad):
+    rng = np.random.default_rng(offset * 7 + pad)
+    rows, n = 4, 2999
+    flat = torch.full((offset + rows * (n + pad),), 99.0, dtype=dtype, device=DEV)
+    x = flat[offset:].view(rows, n + pad)[:, :n]
+    x.copy_(torch.from_numpy(rng.standard_normal((rows, n)).astype(np.float32) * 2))
+    mask = np.zeros(offset + rows * (n + pad), np.uint8)
+    mask[:] = rng.random(mask.shape) < 0.8
+    md = torch.from_numpy(mask).to(DEV)[offset:].view(rows, n + pad)[:, :n]
+    u = _u(rng, rows, 4)
+    s = ml2.Sampler(rows, n, 4)
+    for valid, ref in ((md, md.cpu().numpy()), (md[1], md[1].cpu().numpy())):
+        k = torch.full((rows,), 100, dtype=torch.int32, device=DEV)
+        idx, logp = s.run(x, torch.from_numpy(u).to(DEV), valid, top_k=k)
+        torch.cuda.synchronize()
+        want = drawutil.sample(drawutil.as_float(x), ref, np.ones(rows, np.float32),
+                               np.full(rows, 100), np.ones(rows, np.float32),
+                               np.zeros(rows, np.float32), u)
+        _check(idx.cpu().numpy(), logp.cpu().numpy(), want)
+
+
+@pytest.mark.parametrize("n,lim", [(1 << 20, dict(k=5000, p=0.9)), (1 << 20, dict(p=0.99)),
+                                   (999983, dict(T=4.0, p=0.5)), (3000001, dict(k=100000)),
+                                   (1500007, dict(minp=0.01))])
+def test_pools(n, lim):
+    """Long rows, many draws, most of the pool rejected."""
+    rng = np.random.default_rng(n)
+    x = torch.from_numpy(rng.standard_normal((1, n)).astype(np.float32) * 2.5).to(DEV)
+    valid = (rng.random((1, n)) < 0.3).astype(np.uint8)
+    par = {a: np.full(1, b) for a, b in lim.items()}
+    got = _run(x, _u(rng, 1, 300), valid, **par)
+    _check(*got, unsure=0.25)
+
+
+def test_flat_pool_and_repeats_are_the_same():
+    """A pool of few distinct, nearly equal scores (long lists of ties), and the
+    same call again gives the same bits."""
+    rng = np.random.default_rng(3)
+    n = 600000
+    x = (rng.integers(0, 3, (1, n)) * 1e-3).astype(np.float32)
+    x[0, 17] = -30.0  # an outlier that stretches the row's range
+    x = torch.from_numpy(x).to(DEV)
+    u = _u(rng, 1, 200)
+    for lim in (dict(k=250000), dict(p=0.5), dict(k=400000, p=0.25)):
+        par = {a: np.full(1, b) for a, b in lim.items()}
+        a, b = _run(x, u, None, **par), _run(x, u, None, **par)
+        assert np.array_equal(a[0], b[0]) and np.array_equal(a[1], b[1])
+        # a weight's neighbours lie 2^31 off, the exp's error adds up to 2^9 * n
+        assert np.abs(a[0] - a[2][0]).max() <= 2 and np.allclose(a[1], a[2][1], atol=TOL)
+
+
+def test_uniforms_outside_their_interval_stay_inside_the_row():
+    x = torch.randn(1, 500, device=DEV)
+    u = torch.tensor([[-1.0, float("nan"), 1.0, 7.0, float("inf"), -float("inf")]], device=DEV)
+    s = ml2.Sampler(1, 500, 6)
+    idx, logp = s.run(x, u)
+    torch.cuda.synchronize()
+    i = idx.cpu().numpy()[0]
+    assert list(i[[0, 1, 5]]) == [0, 0, 0] and len(set(i[2:5])) == 1 and 0 <= i[2] < 500
+
+
+def test_frequencies():
+    """Many draws of one row come in proportion to exp(score / T)."""
+    p = np.array([0.5, 0.2, 0.15, 0.1, 0.05])
+    x = torch.from_numpy(np.log(p).astype(np.float32))[None].to(DEV) * 0.7
+    d = 16384
+    u = (torch.arange(d, device=DEV, dtype=torch.float32)[None] + 0.5) / d
+    s = ml2.Sampler(1, 5, d)
+    idx, logp = s.run(x, u, temperature=torch.tensor([0.7], device=DEV))
+    torch.cuda.synchronize()
+    got = np.bincount(idx.cpu().numpy()[0], minlength=5) / d
+    assert np.all(np.abs(got - p) <= 2 / d)  # evenly spread uniforms
+    assert np.allclose(np.exp(logp.cpu().numpy()[0]), p[idx.cpu().numpy()[0]], rtol=1e-5)
+
+
+def test_streams_and_graph():
+    """On a stream of its own, and captured: every replay equals the eager call."""
+    rng = np.random.default_rng(9)
+    for rows, n, d in ((1, 300000, 64), (5, 2000, 1)):
+        x = torch.randn(rows, n, device=DEV)
+        u = torch.from_numpy(_u(rng, rows, d)).to(DEV)
+        p = torch.full((rows,), 0.9, device=DEV)
+        s = ml2.Sampler(rows, n, d)
+        want = [t.clone() for t in s.run(x, u, top_p=p)]
+        side = torch.cuda.Stream()
+        side.wait_stream(torch.cuda.current_stream())
+        s.run(x, u, top_p=p, stream=side)
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(want, (s.idx, s.logprob)))
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            s.run(x, u, top_p=p)
+        for _ in range(4):
+            s.idx.fill_(-5)
+            s.ws.fill_(255)
+            torch.cuda.synchronize()
+            g.replay()
+            torch.cuda.synchronize()
+            assert all(torch.equal(a, b) for a, b in zip(want, (s.idx, s.logprob)))
+            x.mul_(0.9)
+            want = [t.clone() for t in s.run(x, u, top_p=p)]
