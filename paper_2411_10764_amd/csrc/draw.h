@@ -8,6 +8,7 @@
 #include <stdint.h>
 
 #include "ml2.h"
+#include "ml2_internal.h"
 
 namespace ml2 {
 

@@ -253,13 +253,17 @@ hipError_t ensure_dynamic_lds(const void *fn, size_t bytes) {
   int dev = 0;
   hipError_t e = hipGetDevice(&dev);
   if (e != hipSuccess) return e;
-  std::lock_guard<std::mutex> lock(mu);
-  std::vector<size_t> &v = set[fn];
-  if ((int)v.size() <= dev) v.resize((size_t)dev + 1, 0);
-  if (bytes > v[(size_t)dev]) {
-    e = hipFuncSetAttribute(fn, hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
-    if (e != hipSuccess) return e;
-    v[(size_t)dev] = bytes;
+  try {
+    std::lock_guard<std::mutex> lock(mu);
+    std::vector<size_t> &v = set[fn];
+    if ((int)v.size() <= dev) v.resize((size_t)dev + 1, 0);
+    if (bytes > v[(size_t)dev]) {
+      e = hipFuncSetAttribute(fn, hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+      if (e != hipSuccess) return e;
+      v[(size_t)dev] = bytes;
+    }
+  } catch (const std::bad_alloc &) {
+    return hipErrorOutOfMemory;
   }
   return hipSuccess;
 }

@@ -5,13 +5,26 @@
 // ascending).  Every entry has a unique 64-bit key, larger is better,
 //   (ord(score) << 32) | (0xFFFFFFFF - index),
 // so a limit is a key: the cut.  Weights are whole numbers, so their sums are
-// exact in any order and every comparison of sums has one answer.
+// exact in any order and every comparison of sums has one answer, whatever
+// the split of the work and the order of the atomics.
 //
-// A cut is found in two steps.  Entries are counted and weighed in kBins bins
-// of equal width in z (of those that can be drawn: z above kLowest); the bin
-// in which the wanted count or weight is reached holds the cut.  Inside that
-// bin the interval of keys is split into kSub parts again and again until one
+// A cut is found in two steps.  Entries are counted and weighed in bins of
+// equal width in z (of those that can be drawn: z above kLowest); the bin in
+// which the wanted count or weight is reached holds the cut.  Inside that bin
+// the interval of keys is split into kSub parts again and again until one
 // entry is left or the wanted amount ends with a part.
+//
+// Rows of at most kRowMost entries: row_kernel, one workgroup and one launch,
+// scores and weights in LDS.  Longer rows are cut into chunks:
+//   range_kernel    a chunk's best and worst score (and clears the counts)
+//   count_kernel    counts and weights by bin, in LDS, then added up
+//   collect_kernel  lists the entries whose place the bins do not settle, and
+//                   weighs the others by tile of the row
+//   finish_kernel   a workgroup a row: the cuts from the list, the tiles'
+//                   running weights, and few draws
+//   draw_kernel     many draws: a wave a draw
+// top-k with a small k needs no weights before its cut is known: count_kernel
+// then only counts, and collect_kernel lists every entry down to the cut's bin.
 #include <algorithm>
 
 #include "draw.h"
@@ -19,10 +32,17 @@
 namespace ml2 {
 namespace {
 
-constexpr int kThreads = 1024;
-constexpr int kBins = 2048;
-constexpr int kSub = 512;           // parts of an interval of keys
-constexpr int kTiles = 1024;        // parts of a row whose kept weights are held
+constexpr int kBins = 2048;         // bins of a long row
+constexpr int kSub = 512;           // bins of a short row, parts of an interval of keys
+constexpr int kMaxTiles = 4096;     // tiles of a row
+constexpr int kTile = 512;          // smallest tile: 8 entries a lane
+constexpr int kChunk = 4 * kTile;   // smallest chunk: 4 waves
+constexpr int kPacked = 32768;      // entries that a packed LDS bin holds
+constexpr int kFew = 2048;          // k of top-k that lists everything it keeps
+constexpr int kList = 4096;         // list entries held in LDS
+constexpr int kFewDraws = 32;       // draws a row that finish_kernel makes itself
+constexpr int kRowMost = 16384;     // entries of a row in one workgroup's LDS
+constexpr int kBatch = 1024;        // long rows of one set of launches
 constexpr float kLowest = -22.25f;  // exp(z) * 2^31 rounds to 0 below -22.181
 constexpr float kOne = 2147483648.0f;
 
@@ -37,32 +57,68 @@ __device__ __forceinline__ u64 key_of(float x, int64_t i) {
   return ((u64)ordered(x) << 32) | (u64)(0xFFFFFFFFu - (uint32_t)i);
 }
 
+__device__ __forceinline__ float key_score(u64 key) {
+  const uint32_t o = (uint32_t)(key >> 32);
+  return __uint_as_float((o & 0x80000000u) ? o & 0x7FFFFFFFu : ~o);
+}
+
+__device__ __forceinline__ int64_t key_index(u64 key) {
+  return (int64_t)(0xFFFFFFFFu - (uint32_t)key);
+}
+
 // What all entries of a row share.
 struct RowLimits {
-  float m, r;      // best included score, 1 / T
-  float bin_scale; // bins per unit of z
-  float min_z;     // log(min_p), or -inf
-  int64_t k;       // entries top-k keeps (n: all)
-  double p;        // top_p, or 2 where it keeps all
+  float m, r;       // best included score (-inf: none), 1 / T
+  float range;      // z of interest reaches down to -range
+  float min_z;      // log(min_p), or -inf
+  int64_t k;        // entries top-k keeps (n: all)
+  float p;          // top_p, or 2 where it keeps all
 };
+
+// hi, lo: the row's best and worst included scores.
+__device__ __forceinline__ RowLimits row_limits(const SampleArgs &a, int64_t row, float hi,
+                                                float lo) {
+  RowLimits l;
+  bool greedy;
+  l.m = hi;
+  l.r = inverse_temperature(a.s.temperature, row, &greedy);
+  const float low = lo == hi ? 0.0f : (lo - hi) * l.r;
+  l.range = fminf(-kLowest, fmaxf(-low, 1e-20f));
+  const int32_t k = greedy ? 1 : a.top_k ? a.top_k[row] : 0;
+  l.k = k > 0 && k < a.s.n ? k : a.s.n;
+  const float p = a.top_p ? a.top_p[row] : 1.0f;
+  l.p = p < 1.0f ? p : 2.0f;
+  const float mp = a.min_p ? a.min_p[row] : 0.0f;
+  l.min_z = mp > 0.0f ? logf(fminf(mp, 1.0f)) : -__builtin_inff();
+  return l;
+}
 
 __device__ __forceinline__ float exponent(float x, const RowLimits &l) {
   return x == l.m ? 0.0f : (x - l.m) * l.r;
 }
 
+// 0 for an entry that is not included (x = -inf, or z NaN) too.
 __device__ __forceinline__ uint32_t weight(float z) {
   return z > kLowest ? (uint32_t)rintf(expf(z) * kOne) : 0u;
 }
 
-__device__ __forceinline__ int bin_of(float z, const RowLimits &l) {
-  return min(kBins - 1, (int)(-z * l.bin_scale));
+// Bin of an entry with z > kLowest, best first; scale = bins / range.
+template <int BINS>
+__device__ __forceinline__ int bin_of(float z, float scale) {
+  return min(BINS - 1, (int)(-z * scale));
+}
+
+// Weight that top-p wants of `total`.
+__device__ __forceinline__ u64 share_of(float p, u64 total) {
+  const double share = ceil((double)p * (double)total);
+  return share >= 1.0 ? (u64)share : 1ull;
 }
 
 struct Amount {
   u64 count, mass;
 };
 
-// Wave 0 looks through `bins` bins (a multiple of 64), best first, for the one
+// A wave looks through BINS bins (a multiple of 64), best first, for the one
 // in which the running amount reaches `need`: count where by_count, else mass.
 // *before: the amounts of better bins, on top of `base`.  The last bin where
 // `need` is never reached.
@@ -101,254 +157,815 @@ __device__ __forceinline__ int find_bin(const uint32_t *count, const u64 *mass, 
   return bin;
 }
 
-struct Shared {
-  uint32_t count[kBins];
-  u64 mass[kBins];
-  uint32_t sub_count[kSub];
-  u64 sub_mass[kSub];
-  u64 tile[kTiles + 1];
-  float fmax[16], fmin[16];
-  u64 lo, hi;       // interval of keys that holds the cut
+// State of a search for a cut, in LDS.
+struct Search {
+  uint32_t count[kSub];
+  u64 mass[kSub];
+  u64 lo, hi;    // interval of keys that holds the cut
   u64 need;
-  Amount above;     // amounts better than the interval
+  Amount above;  // amounts better than the interval
   int bin, done;
 };
 
-// The cut in the interval [sh.lo, sh.hi] of the keys that each(f) hands to
-// f(key, weight), given the smallest and the largest of those keys: afterwards
-// the entries with key >= sh.lo are kept (no entry of a worse bin has such a
-// key), and sh.above holds the amounts with them.
+// The cut among the keys that each(f) hands to f(key, weight), in which the
+// amount on top of `above` reaches `need`: entries with key >= the result are
+// kept.  The result is at least the smallest of those keys and may lie between
+// two of them.  Every thread of the workgroup calls it, with the same `above`
+// and `need`; each() hands out one key at least.
 template <typename Each>
-__device__ __forceinline__ void refine(Shared &sh, bool by_count, Each each) {
+__device__ __forceinline__ u64 find_cut(Search &s, bool by_count, Amount above, u64 need,
+                                        Each each) {
+  u64 first = ~0ull, last = 0;
+  each([&](u64 key, uint32_t) {
+    first = min(first, key);
+    last = max(last, key);
+  });
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    first = min(first, (u64)__shfl_xor(first, d));
+    last = max(last, (u64)__shfl_xor(last, d));
+  }
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    s.lo = ~0ull;
+    s.hi = 0;
+    s.need = need;
+    s.above = above;
+    s.done = 0;
+  }
+  __syncthreads();
+  if ((threadIdx.x & 63) == 0 && last) atomicMin(&s.lo, first), atomicMax(&s.hi, last);
   for (;;) {
+    for (int b = threadIdx.x; b < kSub; b += blockDim.x) s.count[b] = 0, s.mass[b] = 0;
     __syncthreads();
-    const u64 lo = sh.lo, hi = sh.hi;
-    if (sh.done) return;
-    const int width = 64 - __clzll((hi - lo) | 1ull);
+    const u64 lo = s.lo, hi = s.hi;
+    if (s.done || lo >= hi) break;
+    const int width = 64 - __clzll(hi - lo);
     const int shift = max(0, width - 9);
-    for (int b = threadIdx.x; b < kSub; b += kThreads) sh.sub_count[b] = 0, sh.sub_mass[b] = 0;
-    __syncthreads();
     each([&](u64 key, uint32_t q) {
       if (key < lo || key > hi) return;
       const int b = kSub - 1 - (int)((key - lo) >> shift);  // best first
-      atomicAdd(&sh.sub_count[b], 1u);
-      atomicAdd(&sh.sub_mass[b], (u64)q);
+      atomicAdd(&s.count[b], 1u);
+      atomicAdd(&s.mass[b], (u64)q);
     });
     __syncthreads();
     if (threadIdx.x < 64) {
       Amount before;
-      const int b = find_bin<kSub>(sh.sub_count, sh.sub_mass, by_count, sh.need, sh.above, &before);
+      const int b = find_bin<kSub>(s.count, s.mass, by_count, s.need, s.above, &before);
       if (threadIdx.x == 0) {
         const u64 part = (u64)(kSub - 1 - b);
-        const Amount with = {before.count + sh.sub_count[b], before.mass + sh.sub_mass[b]};
-        sh.lo = lo + (part << shift);
-        sh.hi = min(hi, sh.lo + ((1ull << shift) - 1));
+        const Amount with = {before.count + s.count[b], before.mass + s.mass[b]};
+        s.lo = lo + (part << shift);
+        s.hi = min(hi, s.lo + ((1ull << shift) - 1));
         // one entry, or all of the part is kept
-        sh.done = shift == 0 || sh.sub_count[b] <= 1 ||
-                  (by_count ? with.count : with.mass) == sh.need;
-        sh.above = sh.done ? with : before;
+        s.done = shift == 0 || s.count[b] <= 1 ||
+                 (by_count ? with.count : with.mass) == s.need;
+        s.above = before;
       }
     }
+    __syncthreads();
+  }
+  return s.lo;
+}
+
+// Eight consecutive entries i .. i+7 of a row of n: -inf where not included.
+template <typename T>
+__device__ __forceinline__ void load8(const T *scores, const uint8_t *valid, int64_t i, int64_t n,
+                                      float (&x)[8]) {
+  typedef T V __attribute__((ext_vector_type(8), aligned(sizeof(T))));
+  typedef u64 Mask __attribute__((aligned(1)));
+  if (i + 8 <= n) {
+    const V v = *reinterpret_cast<const V *>(scores + i);
+    const u64 mask = valid ? *reinterpret_cast<const Mask *>(valid + i) : ~0ull;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) x[j] = included((float)v[j], ((mask >> (8 * j)) & 0xFF) != 0);
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      x[j] = i + j < n ? included((float)scores[i + j], !valid || valid[i + j] != 0)
+                       : -__builtin_inff();
   }
 }
 
-template <typename T>
-__global__ __launch_bounds__(kThreads) void row_kernel(SampleArgs a) {
-  __shared__ Shared sh;
-  const int64_t row = blockIdx.x, n = a.s.n;
-  const T *scores = static_cast<const T *>(a.s.scores) + row * a.s.ld;
-  const uint8_t *valid = a.s.valid ? a.s.valid + row * a.s.valid_ld : nullptr;
-  const float ninf = -__builtin_inff();
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  auto load = [&](int64_t i) { return included((float)scores[i], !valid || valid[i] != 0); };
+// floor(u * total), kept inside [0, total).
+__device__ __forceinline__ u64 wanted(float u, u64 total) {
+  const double at = floor((double)u * (double)total);
+  return at >= 0.0 ? min(at < 9.0e18 ? (u64)at : total, total - 1) : 0;
+}
 
-  // the row's best and worst included scores
-  float hi = ninf, lo = __builtin_inff();
-  for (int64_t i = threadIdx.x; i < n; i += kThreads) {
-    const float x = load(i);
-    hi = fmaxf(hi, x);
-    if (x != ninf) lo = fminf(lo, x);
+__device__ __forceinline__ void no_entry(const SampleArgs &a, int64_t row) {
+  for (int j = threadIdx.x; j < a.draws; j += blockDim.x) {
+    a.idx[row * a.draws + j] = -1;
+    a.logprob[row * a.draws + j] = -__builtin_inff();
   }
+}
+
+__device__ __forceinline__ float log_total(u64 total) { return logf((float)total / kOne); }
+
+__device__ __forceinline__ u64 wave_prefix(u64 v) {  // inclusive
+  const int lane = threadIdx.x & 63;
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const u64 o = __shfl_up(v, d);
+    if (lane >= d) v += o;
+  }
+  return v;
+}
+
+// Best and worst over the workgroup, in every thread.
+__device__ __forceinline__ float2 block_range(float hi, float lo, float2 *lds) {
 #pragma unroll
   for (int d = 1; d < 64; d <<= 1) {
     hi = fmaxf(hi, __shfl_xor(hi, d));
     lo = fminf(lo, __shfl_xor(lo, d));
   }
-  if (lane == 0) sh.fmax[wave] = hi, sh.fmin[wave] = lo;
+  if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = make_float2(hi, lo);
   __syncthreads();
-  for (int w = 0; w < kThreads / 64; ++w) {
-    hi = fmaxf(hi, sh.fmax[w]);
-    lo = fminf(lo, sh.fmin[w]);
+  for (int w = 0; w < (int)blockDim.x >> 6; ++w) {
+    hi = fmaxf(hi, lds[w].x);
+    lo = fminf(lo, lds[w].y);
   }
-  if (hi == ninf) {
-    for (int j = threadIdx.x; j < a.draws; j += kThreads) {
-      a.idx[row * a.draws + j] = -1;
-      a.logprob[row * a.draws + j] = ninf;
+  __syncthreads();
+  return make_float2(hi, lo);
+}
+
+// ---- short rows: one workgroup -------------------------------------------------
+
+// The row's scores and weights in LDS: every entry is read from memory and
+// exponentiated once.
+template <typename T>
+__global__ __launch_bounds__(1024) void row_kernel(SampleArgs a) {
+  __shared__ Search s;
+  __shared__ float2 range[16];
+  __shared__ u64 wave_sum[16];
+  extern __shared__ char raw[];
+  const int64_t row = blockIdx.x;
+  const int n = (int)a.s.n, groups = (n + 7) / 8;
+  u64 *group_end = reinterpret_cast<u64 *>(raw);  // running weight after 8 entries
+  float *xs = reinterpret_cast<float *>(group_end + groups);
+  uint32_t *qs = reinterpret_cast<uint32_t *>(xs + groups * 8);
+  const T *scores = static_cast<const T *>(a.s.scores) + row * a.s.ld;
+  const uint8_t *valid = a.s.valid ? a.s.valid + row * a.s.valid_ld : nullptr;
+  const int threads = blockDim.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const float ninf = -__builtin_inff();
+
+  float hi = ninf, lo = __builtin_inff();
+  for (int g = threadIdx.x; g < groups; g += threads) {
+    float x[8];
+    load8(scores, valid, (int64_t)g * 8, n, x);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      xs[g * 8 + j] = x[j];
+      hi = fmaxf(hi, x[j]);
+      lo = fminf(lo, x[j] == ninf ? __builtin_inff() : x[j]);
     }
-    return;
   }
-  RowLimits l;
-  bool greedy;
-  l.m = hi;
-  l.r = inverse_temperature(a.s.temperature, row, &greedy);
-  const float range = fminf(-kLowest, fmaxf(-exponent(lo, l), 1e-20f));
-  l.bin_scale = (float)kBins / range;
-  const int32_t k = greedy ? 1 : a.top_k ? a.top_k[row] : 0;
-  l.k = k > 0 && k < n ? k : n;
-  const float p = a.top_p ? a.top_p[row] : 1.0f;
-  l.p = p < 1.0f ? (double)p : 2.0;
-  const float mp = a.min_p ? a.min_p[row] : 0.0f;
-  l.min_z = mp > 0.0f ? logf(fminf(mp, 1.0f)) : ninf;
+  const float2 ends = block_range(hi, lo, range);
+  if (ends.x == ninf) return no_entry(a, row);
+  const RowLimits l = row_limits(a, row, ends.x, ends.y);
+  for (int e = threadIdx.x; e < groups * 8; e += threads) qs[e] = weight(exponent(xs[e], l));
 
   u64 cut = 0;  // entries with a smaller key are not kept
-  if (l.k < n || l.p < 2.0) {
-    for (int b = threadIdx.x; b < kBins; b += kThreads) sh.count[b] = 0, sh.mass[b] = 0;
-    __syncthreads();
-    for (int64_t i = threadIdx.x; i < n; i += kThreads) {
-      const float x = load(i);
-      const float z = exponent(x, l);
-      const uint32_t q = weight(z);
-      if (x == ninf || q == 0) continue;
-      atomicAdd(&sh.count[bin_of(z, l)], 1u);
-      atomicAdd(&sh.mass[bin_of(z, l)], (u64)q);
-    }
-    __syncthreads();
-    // The cut among the entries of bin sh.bin with key >= cut.
-    auto search = [&](bool by_count, u64 need) {
+  if (l.k < n || l.p < 2.0f) {
+    const float scale = (float)kSub / l.range;
+    // The cut by count or weight among the entries with key >= cut: the bin
+    // that holds it, then find_cut inside that bin.
+    auto search = [&](bool by_count) {
+      for (int b = threadIdx.x; b < kSub; b += threads) s.count[b] = 0, s.mass[b] = 0;
+      __syncthreads();
+#pragma unroll 1
+      for (int e = threadIdx.x; e < n; e += threads) {
+        const uint32_t q = qs[e];
+        if (q == 0 || key_of(xs[e], e) < cut) continue;
+        const int b = bin_of<kSub>(exponent(xs[e], l), scale);
+        atomicAdd(&s.count[b], 1u);
+        atomicAdd(&s.mass[b], (u64)q);
+      }
+      __syncthreads();
       if (wave == 0) {
+        u64 want = (u64)l.k;
+        if (!by_count) {
+          Amount all;
+          find_bin<kSub>(s.count, s.mass, true, ~0ull, Amount{0, 0}, &all);
+          want = share_of(l.p, all.mass + s.mass[kSub - 1]);
+        }
         Amount before;
-        const int b = find_bin<kBins>(sh.count, sh.mass, by_count, need, Amount{0, 0}, &before);
+        const int b = find_bin<kSub>(s.count, s.mass, by_count, want, Amount{0, 0}, &before);
         if (lane == 0) {
-          sh.bin = b;
-          sh.need = need;
-          sh.above = before;
-          sh.lo = ~0ull;
-          sh.hi = 0;
-          sh.done = 0;
+          s.bin = (by_count ? before.count + s.count[b] : before.mass + s.mass[b]) < want ? -1 : b;
+          s.above = before;
+          s.need = want;
         }
       }
       __syncthreads();
-      const int bin = sh.bin;
-      auto each = [&](auto f) {
-        for (int64_t i = threadIdx.x; i < n; i += kThreads) {
-          const float x = load(i);
-          if (x == ninf) continue;
-          const float z = exponent(x, l);
-          const uint32_t q = weight(z);
-          const u64 key = key_of(x, i);
-          if (q != 0 && bin_of(z, l) == bin && key >= cut) f(key, q);
+      const int bin = s.bin;
+      const Amount above = s.above;
+      const u64 want = s.need, from = cut;
+      if (bin < 0) return;  // fewer entries than top-k keeps
+      cut = find_cut(s, by_count, above, want, [&](auto f) {
+#pragma unroll 1
+        for (int e = threadIdx.x; e < n; e += threads) {
+          const uint32_t q = qs[e];
+          if (q == 0) continue;
+          const float x = xs[e];
+          const u64 key = key_of(x, e);
+          if (key >= from && bin_of<kSub>(exponent(x, l), scale) == bin) f(key, q);
         }
-      };
-      u64 first = ~0ull, last = 0;
-      each([&](u64 key, uint32_t) {
-        first = min(first, key);
-        last = max(last, key);
       });
-      if (last) atomicMin(&sh.lo, first), atomicMax(&sh.hi, last);
-      refine(sh, by_count, each);
-      cut = sh.lo;
     };
-    u64 total = 0;
-    if (wave == 0) {
-      Amount all;
-      find_bin<kBins>(sh.count, sh.mass, true, ~0ull, Amount{0, 0}, &all);
-      if (lane == 0) {
-        sh.above.count = all.count + sh.count[kBins - 1];
-        sh.above.mass = all.mass + sh.mass[kBins - 1];
-      }
-    }
+    if (l.k < n) search(true);
     __syncthreads();
-    const Amount all = sh.above;
-    __syncthreads();
-    total = all.mass;
-    if ((u64)l.k < all.count) {
-      search(true, (u64)l.k);
-      total = sh.above.mass;
-      __syncthreads();
-    }
-    if (l.p < 2.0) {
-      const double share = ceil(l.p * (double)total);
-      search(false, share >= 1.0 ? (u64)share : 1ull);
-      __syncthreads();
-    }
+    if (l.p < 2.0f) search(false);
   }
-  auto kept = [&](float x, int64_t i, float *z) {
-    *z = exponent(x, l);
-    return x != ninf && key_of(x, i) >= cut && *z >= l.min_z ? weight(*z) : 0u;
-  };
+  __syncthreads();
 
-  // weights of the tiles, one wave a tile
-  const int64_t tile = ((n + kTiles - 1) / kTiles + 63) / 64 * 64;
-  const int tiles = (int)((n + tile - 1) / tile);
-  for (int t = wave; t < tiles; t += kThreads / 64) {
-    u64 sum = 0;
-    for (int64_t i = t * tile + lane; i < min(n, (t + 1) * tile); i += 64) {
-      float z;
-      sum += kept(load(i), i, &z);
-    }
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) sum += __shfl_xor(sum, d);
-    if (lane == 0) sh.tile[t + 1] = sum;
+  // running weights of the kept, each thread `per` groups in a row
+  auto kept = [&](int e) {
+    const uint32_t q = qs[e];
+    const float x = xs[e];
+    return q != 0 && exponent(x, l) >= l.min_z && key_of(x, e) >= cut ? q : 0u;
+  };
+  const int per = (groups + threads - 1) / threads;
+  const int g0 = min(groups, (int)threadIdx.x * per), g1 = min(groups, g0 + per);
+  u64 sum = 0;
+  for (int e = g0 * 8; e < g1 * 8; ++e) sum += kept(e);
+  const u64 incl = wave_prefix(sum);
+  if (lane == 63) wave_sum[wave] = incl;
+  __syncthreads();
+  u64 run = incl - sum, total = 0;
+  for (int w = 0; w < threads >> 6; ++w) {
+    if (w < wave) run += wave_sum[w];
+    total += wave_sum[w];
+  }
+  for (int g = g0; g < g1; ++g) {
+    for (int j = 0; j < 8; ++j) run += kept(g * 8 + j);
+    group_end[g] = run;
   }
   __syncthreads();
-  if (threadIdx.x == 0) {
-    sh.tile[0] = 0;
-    for (int t = 0; t < tiles; ++t) sh.tile[t + 1] += sh.tile[t];
-  }
-  __syncthreads();
-  const u64 total = sh.tile[tiles];
-  const float log_total = logf((float)total / kOne);
-  for (int j = wave; j < a.draws; j += kThreads / 64) {
-    const double at = floor((double)a.u[row * a.draws + j] * (double)total);
-    const u64 want = at >= 0.0 ? min(at < 9.0e18 ? (u64)at : total, total - 1) : 0;
-    int lo_t = 0, hi_t = tiles - 1;  // the tile whose end passes `want`
-    while (lo_t < hi_t) {
-      const int mid = (lo_t + hi_t) / 2;
-      if (sh.tile[mid + 1] > want) hi_t = mid; else lo_t = mid + 1;
+  const float lt = log_total(total);
+  for (int j = threadIdx.x; j < a.draws; j += threads) {
+    const u64 want = wanted(a.u[row * a.draws + j], total);
+    int first = 0, last = groups - 1;  // the group whose end passes `want`
+    while (first < last) {
+      const int mid = (first + last) / 2;
+      if (group_end[mid] > want) last = mid; else first = mid + 1;
     }
-    u64 run = sh.tile[lo_t];
-    for (int64_t base = lo_t * tile; base < n; base += 64) {
-      const int64_t i = base + lane;
-      float z = 0.0f;
-      u64 incl = i < n ? kept(load(i), i, &z) : 0u;
-#pragma unroll
-      for (int d = 1; d < 64; d <<= 1) {
-        const u64 o = __shfl_up(incl, d);
-        if (lane >= d) incl += o;
-      }
-      const u64 found = __ballot(run + incl > want);
-      if (found) {
-        if (lane == __ffsll(found) - 1) {
-          a.idx[row * a.draws + j] = (int32_t)i;
-          a.logprob[row * a.draws + j] = z - log_total;
-        }
-        break;
-      }
-      run += __shfl(incl, 63);
+    u64 now = first > 0 ? group_end[first - 1] : 0;
+    int e = first * 8;
+    for (;;) {
+      now += kept(e);
+      if (now > want || e == first * 8 + 7) break;
+      ++e;
     }
+    a.idx[row * a.draws + j] = e;
+    a.logprob[row * a.draws + j] = exponent(xs[e], l) - lt;
   }
 }
 
+// ---- long rows -------------------------------------------------------------------
+
+struct RowState {  // of one row, for draw_kernel
+  RowLimits l;
+  u64 cut, total;
+};
+
+struct Long {
+  SampleArgs a;
+  int64_t row0;              // first row of the batch
+  int64_t chunk, chunks;     // entries of a chunk, chunks of a row
+  int64_t tile, tiles;       // the same of tiles; a chunk is a number of tiles
+  uint32_t list_most;        // entries of a row's list
+  float2 *range;             // [rows][chunks]: best, worst
+  u64 *mass;                 // [rows][kBins]
+  uint32_t *count;           // [rows][kBins]
+  u64 *tile_mass;            // [rows][tiles], running sums after finish_kernel
+  u64 *list;                 // [rows][list_most] keys
+  uint32_t *listed;          // [rows]
+  RowState *state;           // [rows]
+};
+
 template <typename T>
-hipError_t launch(const SampleArgs &a, hipStream_t s) {
-  row_kernel<T><<<(uint32_t)a.s.rows, kThreads, 0, s>>>(a);
+__device__ __forceinline__ const T *row_scores(const Long &k, int64_t r) {
+  return static_cast<const T *>(k.a.s.scores) + (k.row0 + r) * k.a.s.ld;
+}
+
+__device__ __forceinline__ const uint8_t *row_mask(const Long &k, int64_t r) {
+  return k.a.s.valid ? k.a.s.valid + (k.row0 + r) * k.a.s.valid_ld : nullptr;
+}
+
+__device__ __forceinline__ RowLimits chunk_limits(const Long &k, int64_t r, float2 *lds) {
+  float hi = -__builtin_inff(), lo = __builtin_inff();
+  for (int64_t c = threadIdx.x; c < k.chunks; c += blockDim.x) {
+    const float2 v = k.range[r * k.chunks + c];
+    hi = fmaxf(hi, v.x);
+    lo = fminf(lo, v.y);
+  }
+  const float2 v = block_range(hi, lo, lds);
+  return row_limits(k.a, k.row0 + r, v.x, v.y);
+}
+
+template <typename T>
+__global__ __launch_bounds__(256) void range_kernel(Long k) {
+  __shared__ float2 lds[4];
+  const int64_t r = blockIdx.x / k.chunks, c = blockIdx.x % k.chunks;
+  for (int64_t b = c * 256 + threadIdx.x; b < kBins; b += k.chunks * 256) {
+    k.mass[r * kBins + b] = 0;
+    k.count[r * kBins + b] = 0;
+  }
+  if (c == 0 && threadIdx.x == 0) k.listed[r] = 0;
+  const T *scores = row_scores<T>(k, r);
+  const uint8_t *valid = row_mask(k, r);
+  const int64_t end = min(k.a.s.n, (c + 1) * k.chunk);
+  const float ninf = -__builtin_inff();
+  float hi = ninf, lo = __builtin_inff();
+  for (int64_t i = c * k.chunk + threadIdx.x * 8; i < end; i += 256 * 8) {
+    float x[8];
+    load8(scores, valid, i, k.a.s.n, x);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      hi = fmaxf(hi, x[j]);
+      lo = fminf(lo, x[j] == ninf ? __builtin_inff() : x[j]);
+    }
+  }
+  const float2 v = block_range(hi, lo, lds);
+  if (threadIdx.x == 0) k.range[blockIdx.x] = v;
+}
+
+// A row whose top-k needs no weights by bin: everything it keeps is listed.
+__device__ __forceinline__ bool lists_all(const RowLimits &l) { return l.k <= kFew; }
+
+template <typename T>
+__global__ __launch_bounds__(256) void count_kernel(Long k) {
+  __shared__ float2 lds[4];
+  __shared__ u64 bins[kBins];  // (weight << 17) | count: up to kPacked entries
+  const int64_t r = blockIdx.x / k.chunks, c = blockIdx.x % k.chunks;
+  const RowLimits l = chunk_limits(k, r, lds);
+  if (l.m == -__builtin_inff() || (l.k >= k.a.s.n && l.p >= 2.0f)) return;
+  const bool weigh = !lists_all(l);
+  const float scale = (float)kBins / l.range;
+  const T *scores = row_scores<T>(k, r);
+  const uint8_t *valid = row_mask(k, r);
+  const int64_t end = min(k.a.s.n, (c + 1) * k.chunk);
+  for (int64_t base = c * k.chunk; base < end; base += kPacked) {
+    for (int b = threadIdx.x; b < kBins; b += 256) bins[b] = 0;
+    __syncthreads();
+    const int64_t stop = min(end, base + kPacked);
+    for (int64_t i = base + threadIdx.x * 8; i < stop; i += 256 * 8) {
+      float x[8];
+      load8(scores, valid, i, k.a.s.n, x);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const float z = exponent(x[j], l);
+        if (weigh) {
+          const uint32_t q = weight(z);
+          if (q) atomicAdd(&bins[bin_of<kBins>(z, scale)], ((u64)q << 17) | 1ull);
+        } else if (z > kLowest) {
+          atomicAdd(reinterpret_cast<uint32_t *>(&bins[bin_of<kBins>(z, scale)]), 1u);
+        }
+      }
+    }
+    __syncthreads();
+    for (int b = threadIdx.x; b < kBins; b += 256) {
+      const u64 v = bins[b];
+      if (!v) continue;
+      atomicAdd(&k.count[r * kBins + b], (uint32_t)(v & 0x1FFFF));
+      if (weigh) atomicAdd(&k.mass[r * kBins + b], v >> 17);
+    }
+    __syncthreads();
+  }
+}
+
+// What the bins settle: entries of bins better than `sure` are kept, those of
+// bins [sure, last] and of bin `k_bin` are listed, the others dropped.
+struct Bins {
+  int k_bin;       // holds top-k's cut (kBins: none)
+  Amount k_above;  // better bins' amounts
+  int sure, last;
+};
+
+__device__ __forceinline__ Bins settle(const RowLimits &l, const uint32_t *count, const u64 *mass) {
+  Bins b = {kBins, {0, 0}, kBins, -1};
+  Amount all;
+  find_bin<kBins>(count, mass, true, ~0ull, Amount{0, 0}, &all);
+  all.count += count[kBins - 1];
+  all.mass += mass[kBins - 1];
+  u64 most = all.mass, least = all.mass;  // bounds of the weight that top-k keeps
+  if ((u64)l.k < all.count) {
+    b.k_bin = find_bin<kBins>(count, mass, true, (u64)l.k, Amount{0, 0}, &b.k_above);
+    least = b.k_above.mass;
+    most = least + mass[b.k_bin];
+    b.sure = b.last = b.k_bin;
+  }
+  if (lists_all(l)) {
+    // no weights yet: all down to the bin (to the last one where k keeps all)
+    if (b.k_bin == kBins) b.last = kBins - 1;
+    b.sure = 0;
+    return b;
+  }
+  if (l.p < 2.0f) {
+    Amount before;
+    const int from = find_bin<kBins>(count, mass, false, share_of(l.p, least), Amount{0, 0}, &before);
+    const int to = find_bin<kBins>(count, mass, false, share_of(l.p, most), Amount{0, 0}, &before);
+    b.sure = min(from, b.sure);
+    b.last = min(to, b.k_bin < kBins ? b.k_bin : kBins - 1);
+  }
+  return b;
+}
+
+template <typename T>
+__global__ __launch_bounds__(256) void collect_kernel(Long k) {
+  __shared__ float2 lds[4];
+  __shared__ uint32_t count[kBins];
+  __shared__ u64 mass[kBins];
+  __shared__ Bins sh;
+  const int64_t r = blockIdx.x / k.chunks, c = blockIdx.x % k.chunks;
+  const RowLimits l = chunk_limits(k, r, lds);
+  if (l.m == -__builtin_inff()) return;
+  Bins b = {kBins, {0, 0}, kBins, -1};
+  if (l.k < k.a.s.n || l.p < 2.0f) {
+    for (int j = threadIdx.x; j < kBins; j += 256) {
+      count[j] = k.count[r * kBins + j];
+      mass[j] = k.mass[r * kBins + j];
+    }
+    __syncthreads();
+    if (threadIdx.x < 64) {
+      const Bins found = settle(l, count, mass);
+      if (threadIdx.x == 0) sh = found;
+    }
+    __syncthreads();
+    b = sh;
+  }
+  const float scale = (float)kBins / l.range;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const T *scores = row_scores<T>(k, r);
+  const uint8_t *valid = row_mask(k, r);
+  u64 *list = k.list + (size_t)r * k.list_most;
+  const int64_t end = min(k.a.s.n, (c + 1) * k.chunk);
+  for (int64_t t = c * k.chunk + wave * k.tile; t < end; t += 4 * k.tile) {
+    u64 sum = 0;
+    const int64_t stop = min(end, t + k.tile);
+    for (int64_t i = t + lane * 8; i < t + k.tile; i += kTile) {
+      float x[8];
+      load8(scores, valid, i, stop, x);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const float z = exponent(x[j], l);
+        const bool in = z > kLowest;
+        const int bin = in ? bin_of<kBins>(z, scale) : kBins;
+        const bool wait = in && ((bin >= b.sure && bin <= b.last) || bin == b.k_bin);
+        if (in && bin < b.sure && z >= l.min_z) sum += weight(z);
+        const u64 ballot = __ballot(wait);
+        if (ballot) {
+          uint32_t at = 0;
+          if (lane == __ffsll(ballot) - 1)
+            at = atomicAdd(&k.listed[r], (uint32_t)__popcll(ballot));
+          at = __shfl(at, __ffsll(ballot) - 1) + (uint32_t)__popcll(ballot & ((1ull << lane) - 1));
+          if (wait && at < k.list_most) list[at] = key_of(x[j], i + j);
+        }
+      }
+    }
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) sum += __shfl_xor(sum, d);
+    if (lane == 0) k.tile_mass[r * k.tiles + t / k.tile] = sum;
+  }
+}
+
+// One draw by one wave: the tile whose running weight passes `want`, then the
+// entry inside it.
+template <typename T>
+__device__ __forceinline__ void draw_one(const Long &k, int64_t r, int j, const RowState &st,
+                                         const u64 *tile_end) {
+  const int lane = threadIdx.x & 63;
+  const int64_t at = (k.row0 + r) * k.a.draws + j;
+  const u64 want = wanted(k.a.u[at], st.total);
+  int first = 0, last = (int)k.tiles - 1;
+  while (first < last) {
+    const int mid = (first + last) / 2;
+    if (tile_end[mid] > want) last = mid; else first = mid + 1;
+  }
+  u64 run = first > 0 ? tile_end[first - 1] : 0;
+  const T *scores = row_scores<T>(k, r);
+  const uint8_t *valid = row_mask(k, r);
+  for (int64_t base = first * k.tile; base < k.a.s.n; base += kTile) {
+    const int64_t i = base + lane * 8;
+    float x[8];
+    load8(scores, valid, i, k.a.s.n, x);
+    uint32_t q[8];
+    u64 sum = 0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const float z = exponent(x[e], st.l);
+      q[e] = z >= st.l.min_z && key_of(x[e], i + e) >= st.cut ? weight(z) : 0u;
+      sum += q[e];
+    }
+    const u64 incl = wave_prefix(sum);
+    const u64 found = __ballot(run + incl > want);
+    if (found) {
+      if (lane == __ffsll(found) - 1) {
+        u64 now = run + incl - sum;
+        float z = 0.0f;
+        int e = 0;
+        bool done = false;
+#pragma unroll
+        for (int f = 0; f < 8; ++f) {
+          now += q[f];
+          if (!done && now > want) {
+            done = true;
+            e = f;
+            z = exponent(x[f], st.l);
+          }
+        }
+        k.a.idx[at] = (int32_t)(i + e);
+        k.a.logprob[at] = z - log_total(st.total);
+      }
+      return;
+    }
+    run += __shfl(incl, 63);
+  }
+}
+
+struct Finish {
+  Search s;
+  float2 range[16];
+  uint32_t count[kBins];
+  u64 mass[kBins];
+  u64 keys[kList];
+  u64 tile[kMaxTiles];
+  u64 wave_sum[16];
+  Bins bins;
+};
+
+template <typename T>
+__global__ __launch_bounds__(1024) void finish_kernel(Long k) {
+  extern __shared__ char raw[];
+  Finish &sh = *reinterpret_cast<Finish *>(raw);
+  const int64_t r = blockIdx.x, row = k.row0 + r, n = k.a.s.n;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const RowLimits l = chunk_limits(k, r, sh.range);
+  if (l.m == -__builtin_inff()) {
+    if (threadIdx.x == 0) k.state[r].l = l;
+    return no_entry(k.a, row);
+  }
+  const float scale = (float)kBins / l.range;
+  const T *scores = row_scores<T>(k, r);
+  const uint8_t *valid = row_mask(k, r);
+  const u64 *list = k.list + (size_t)r * k.list_most;
+  const uint32_t listed = k.listed[r];
+  for (int t = threadIdx.x; t < k.tiles; t += 1024) sh.tile[t] = k.tile_mass[r * k.tiles + t];
+  for (uint32_t e = threadIdx.x; e < min(listed, (uint32_t)kList); e += 1024) sh.keys[e] = list[e];
+
+  u64 cut = 0;
+  if (l.k < n || l.p < 2.0f) {
+    for (int j = threadIdx.x; j < kBins; j += 1024) {
+      sh.count[j] = k.count[r * kBins + j];
+      sh.mass[j] = k.mass[r * kBins + j];
+    }
+    __syncthreads();
+    if (wave == 0) {
+      const Bins found = settle(l, sh.count, sh.mass);
+      if (lane == 0) sh.bins = found;
+    }
+    __syncthreads();
+    const Bins b = sh.bins;
+    // f(key, weight, bin) for every listed entry.  A list that did not fit is
+    // read from the row again.
+    auto each = [&](auto f) {
+      auto one = [&](float x, int64_t i) {
+        const float z = exponent(x, l);
+        if (!(z > kLowest)) return;
+        const int bin = bin_of<kBins>(z, scale);
+        if ((bin >= b.sure && bin <= b.last) || bin == b.k_bin) f(key_of(x, i), weight(z), bin);
+      };
+      if (listed <= k.list_most) {
+        for (uint32_t e = threadIdx.x; e < listed; e += 1024) {
+          const u64 key = e < kList ? sh.keys[e] : list[e];
+          one(key_score(key), key_index(key));
+        }
+      } else {
+        for (int64_t i = (int64_t)threadIdx.x * 8; i < n; i += 8192) {
+          float x[8];
+          load8(scores, valid, i, n, x);
+#pragma unroll
+          for (int j = 0; j < 8; ++j) one(x[j], i + j);
+        }
+      }
+    };
+    if (b.k_bin < kBins)
+      cut = find_cut(sh.s, true, b.k_above, (u64)l.k, [&](auto f) {
+        each([&](u64 key, uint32_t q, int bin) {
+          if (bin == b.k_bin) f(key, q);
+        });
+      });
+    __syncthreads();
+    if (l.p < 2.0f) {
+      // the weight that top-k keeps: better bins' and the listed entries'
+      const bool everything = lists_all(l);
+      u64 part = 0;
+      each([&](u64 key, uint32_t q, int bin) {
+        if (everything ? key >= cut : (bin == b.k_bin && key >= cut)) part += q;
+      });
+#pragma unroll
+      for (int d = 1; d < 64; d <<= 1) part += __shfl_xor(part, d);
+      if (lane == 0) sh.wave_sum[wave] = part;
+      __syncthreads();
+      u64 total = 0;
+      for (int w = 0; w < 16; ++w) total += sh.wave_sum[w];
+      if (!everything) {
+        if (b.k_bin < kBins) {
+          total += b.k_above.mass;
+        } else {
+          total = 0;
+          if (wave == 0) {
+            Amount all;
+            find_bin<kBins>(sh.count, sh.mass, true, ~0ull, Amount{0, 0}, &all);
+            if (lane == 0) sh.s.need = all.mass + sh.mass[kBins - 1];
+          }
+          __syncthreads();
+          total = sh.s.need;
+        }
+      }
+      __syncthreads();
+      const u64 share = share_of(l.p, total);
+      if (everything) {
+        cut = find_cut(sh.s, false, Amount{0, 0}, share, [&](auto f) {
+          each([&](u64 key, uint32_t q, int) {
+            if (q && key >= cut) f(key, q);
+          });
+        });
+      } else {
+        if (wave == 0) {
+          Amount before;
+          const int bin = find_bin<kBins>(sh.count, sh.mass, false, share, Amount{0, 0}, &before);
+          if (lane == 0) {
+            sh.s.bin = bin;
+            sh.s.above = before;
+          }
+        }
+        __syncthreads();
+        const int p_bin = sh.s.bin;
+        const Amount above = sh.s.above;
+        const u64 from = cut;
+        cut = find_cut(sh.s, false, above, share, [&](auto f) {
+          each([&](u64 key, uint32_t q, int bin) {
+            if (q && bin == p_bin && key >= from) f(key, q);
+          });
+        });
+      }
+    }
+    __syncthreads();
+    // the listed entries that are kept join their tiles
+    each([&](u64 key, uint32_t q, int bin) {
+      if (q && key >= cut && bin >= b.sure && exponent(key_score(key), l) >= l.min_z)
+        atomicAdd(&sh.tile[key_index(key) / k.tile], (u64)q);
+    });
+  }
+  __syncthreads();
+  // running weights of the tiles, each thread four in a row
+  u64 own[kMaxTiles / 1024], sum = 0;
+#pragma unroll
+  for (int j = 0; j < kMaxTiles / 1024; ++j) {
+    const int t = threadIdx.x * (kMaxTiles / 1024) + j;
+    own[j] = t < k.tiles ? sh.tile[t] : 0;
+    sum += own[j];
+  }
+  const u64 incl = wave_prefix(sum);
+  if (lane == 63) sh.wave_sum[wave] = incl;
+  __syncthreads();
+  u64 run = incl - sum, total = 0;
+  for (int w = 0; w < 16; ++w) {
+    if (w < wave) run += sh.wave_sum[w];
+    total += sh.wave_sum[w];
+  }
+#pragma unroll
+  for (int j = 0; j < kMaxTiles / 1024; ++j) {
+    const int t = threadIdx.x * (kMaxTiles / 1024) + j;
+    run += own[j];
+    if (t < k.tiles) sh.tile[t] = run;
+  }
+  __syncthreads();
+  const RowState st = {l, cut, total};
+  if (k.a.draws <= kFewDraws) {
+    for (int j = wave; j < k.a.draws; j += 16) draw_one<T>(k, r, j, st, sh.tile);
+    return;
+  }
+  for (int t = threadIdx.x; t < k.tiles; t += 1024) k.tile_mass[r * k.tiles + t] = sh.tile[t];
+  if (threadIdx.x == 0) k.state[r] = st;
+}
+
+template <typename T>
+__global__ __launch_bounds__(256) void draw_kernel(Long k, int blocks) {
+  const int64_t r = blockIdx.x / blocks;
+  const int j = (int)(blockIdx.x % blocks) * 4 + (threadIdx.x >> 6);
+  const RowState st = k.state[r];
+  if (j >= k.a.draws || st.l.m == -__builtin_inff()) return;
+  draw_one<T>(k, r, j, st, k.tile_mass + r * k.tiles);
+}
+
+// ---- plans -------------------------------------------------------------------
+
+struct LongPlan {
+  int64_t batch, tile, tiles, most_chunks;
+  uint32_t list_most;
+  size_t range, mass, count, tile_mass, list, listed, state, bytes;
+};
+
+LongPlan long_plan(int64_t n, int64_t rows) {
+  LongPlan p{};
+  p.batch = std::min<int64_t>(rows, kBatch);
+  p.tile = std::max<int64_t>(kTile, ((n + kMaxTiles - 1) / kMaxTiles + kTile - 1) / kTile * kTile);
+  p.tiles = (n + p.tile - 1) / p.tile;
+  // as many chunks as workgroups may be wanted: 4,096 in all, one a row at least
+  p.most_chunks = std::max<int64_t>(1, 4096 / std::max<int64_t>(1, p.batch));
+  p.list_most = (uint32_t)(kList + n / 64);
+  size_t at = 0;
+  auto take = [&](size_t bytes) {
+    const size_t here = at;
+    at += (bytes + 255) & ~(size_t)255;
+    return here;
+  };
+  const size_t b = (size_t)p.batch;
+  p.range = take(b * p.most_chunks * sizeof(float2));
+  p.mass = take(b * kBins * 8);
+  p.count = take(b * kBins * 4);
+  p.tile_mass = take(b * p.tiles * 8);
+  p.list = take(b * p.list_most * 8);
+  p.listed = take(b * 4);
+  p.state = take(b * sizeof(RowState));
+  p.bytes = at;
+  return p;
+}
+
+template <typename T>
+hipError_t launch_long(const SampleArgs &a, void *ws, int cu_count, hipStream_t s) {
+  const LongPlan p = long_plan(a.s.n, a.s.rows);
+  char *base = static_cast<char *>(ws);
+  Long k{};
+  k.a = a;
+  k.tile = p.tile;
+  k.tiles = p.tiles;
+  k.list_most = p.list_most;
+  k.range = reinterpret_cast<float2 *>(base + p.range);
+  k.mass = reinterpret_cast<u64 *>(base + p.mass);
+  k.count = reinterpret_cast<uint32_t *>(base + p.count);
+  k.tile_mass = reinterpret_cast<u64 *>(base + p.tile_mass);
+  k.list = reinterpret_cast<u64 *>(base + p.list);
+  k.listed = reinterpret_cast<uint32_t *>(base + p.listed);
+  k.state = reinterpret_cast<RowState *>(base + p.state);
+  hipError_t e = ensure_dynamic_lds(reinterpret_cast<const void *>(finish_kernel<T>), sizeof(Finish));
+  if (e != hipSuccess) return e;
+  for (k.row0 = 0; k.row0 < a.s.rows; k.row0 += p.batch) {
+    const int64_t rows = std::min(p.batch, a.s.rows - k.row0);
+    // about four workgroups a CU, none over less than kChunk entries; chunks
+    // are whole tiles, a wave's at a time
+    const int64_t want = std::min(p.most_chunks, std::max<int64_t>(1, (int64_t)cu_count * 4 / rows));
+    const int64_t unit = std::max<int64_t>(kChunk, p.tile);
+    k.chunk = std::max<int64_t>(1, (a.s.n + want * unit - 1) / (want * unit)) * unit;
+    k.chunks = (a.s.n + k.chunk - 1) / k.chunk;
+    const uint32_t grid = (uint32_t)(rows * k.chunks);
+    range_kernel<T><<<grid, 256, 0, s>>>(k);
+    if (a.top_k || a.top_p || a.s.temperature) count_kernel<T><<<grid, 256, 0, s>>>(k);
+    collect_kernel<T><<<grid, 256, 0, s>>>(k);
+    finish_kernel<T><<<(uint32_t)rows, 1024, sizeof(Finish), s>>>(k);
+    if (a.draws > kFewDraws) {
+      const int blocks = (a.draws + 3) / 4;
+      draw_kernel<T><<<(uint32_t)(rows * blocks), 256, 0, s>>>(k, blocks);
+    }
+    e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
+}
+
+template <typename T>
+hipError_t launch_row(const SampleArgs &a, hipStream_t s) {
+  const int groups = (int)((a.s.n + 7) / 8);
+  const int threads = std::min(1024, std::max(64, (groups * 2 + 63) / 64 * 64));
+  const size_t lds = (size_t)groups * (8 + 8 * 8);
+  const hipError_t e = ensure_dynamic_lds(reinterpret_cast<const void *>(row_kernel<T>), lds);
+  if (e != hipSuccess) return e;
+  row_kernel<T><<<(uint32_t)a.s.rows, threads, lds, s>>>(a);
   return hipGetLastError();
+}
+
+template <typename T>
+hipError_t launch(const SampleArgs &a, void *ws, int cu_count, hipStream_t s) {
+  if (a.s.n <= kRowMost) return launch_row<T>(a, s);
+  return launch_long<T>(a, ws, cu_count, s);
 }
 
 }  // namespace
 
 size_t sample_workspace_bytes(int64_t n, int64_t rows, int32_t draws) {
-  (void)n, (void)rows, (void)draws;
-  return 256;
+  (void)draws;
+  return n <= kRowMost ? 256 : std::max<size_t>(256, long_plan(n, rows).bytes);
 }
 
 hipError_t launch_sample(int dtype, const SampleArgs &a, void *ws, int cu_count, hipStream_t s) {
-  (void)ws, (void)cu_count;
   if (a.s.rows == 0 || a.draws == 0) return hipSuccess;
   switch (dtype) {
-    case ML2_F32: return launch<float>(a, s);
-    case ML2_BF16: return launch<__bf16>(a, s);
-    default: return launch<_Float16>(a, s);
+    case ML2_F32: return launch<float>(a, ws, cu_count, s);
+    case ML2_BF16: return launch<__bf16>(a, ws, cu_count, s);
+    default: return launch<_Float16>(a, ws, cu_count, s);
   }
 }
 
