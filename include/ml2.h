@@ -63,6 +63,7 @@ typedef enum {
                                    targets of a row */
 #define ML2_MAX_STREAM_K 4096   /* k of ml2_stream_explorer_create */
 #define ML2_MAX_ROWS 2097152    /* rows of scores of one call */
+#define ML2_MAX_TOKENS 1073741824 /* n of ml2_embed_grad */
 #define ML2_MAX_WIDTH 65536     /* columns of ml2_embed and ml2_embed_grad */
 
 typedef struct ml2_ensemble ml2_ensemble; /* opaque; immutable after load */
@@ -481,8 +482,8 @@ ml2_status ml2_embed(int32_t dtype, const void *table, int64_t table_rows, int64
  * grad_dtype, which is dtype or ML2_F32; every row is written.  workspace:
  * at least ml2_embed_grad_workspace_bytes(n, table_rows, width) bytes of
  * device memory, 256-byte aligned, used by this call until it completes.
- * Errors as ml2_embed, and INVALID_ARG for another grad_dtype or a small
- * workspace.
+ * Errors as ml2_embed, UNSUPPORTED for n > ML2_MAX_TOKENS, and INVALID_ARG
+ * for another grad_dtype or a small workspace.
  */
 ml2_status ml2_embed_grad_workspace_bytes(int64_t n, int64_t table_rows, int64_t width,
                                           size_t *bytes);

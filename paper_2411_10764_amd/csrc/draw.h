@@ -67,7 +67,7 @@ hipError_t launch_logprob(int dtype, const LogprobArgs &a, void *ws, int cu_coun
 hipError_t launch_embed(int dtype, const EmbedArgs &a, int cu_count, hipStream_t s);
 size_t embed_grad_workspace_bytes(int64_t n, int64_t table_rows, int64_t width);
 hipError_t launch_embed_grad(int dtype, int grad_dtype, const EmbedGradArgs &a, void *ws,
-                             int cu_count, hipStream_t s);
+                             hipStream_t s);
 
 // ---- device helpers ---------------------------------------------------------
 

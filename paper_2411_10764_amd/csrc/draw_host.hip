@@ -185,6 +185,8 @@ static ml2_status check_grad_sizes(const char *call, int64_t n, int64_t table_ro
   if (width > ML2_MAX_WIDTH)
     return fail(ML2_ERR_UNSUPPORTED, "%s: width = %lld > %d", call, (long long)width,
                 ML2_MAX_WIDTH);
+  if (n > ML2_MAX_TOKENS)
+    return fail(ML2_ERR_UNSUPPORTED, "%s: n = %lld > %d", call, (long long)n, ML2_MAX_TOKENS);
   return ML2_OK;
 }
 
@@ -225,11 +227,8 @@ ml2_status ml2_embed_grad(int32_t dtype, const void *dout, int64_t n, int64_t wi
     return fail(ML2_ERR_INVALID_ARG, "ml2_embed_grad: workspace %zu < %zu bytes", workspace_bytes,
                 need);
   if (table_rows == 0 || width == 0) return ML2_OK;
-  int dev = 0;
-  st = ml2::current_device(&dev);
-  if (st != ML2_OK) return st;
   const ml2::EmbedGradArgs a = {dout, n, width, dout_ld, ids, scale, grad, table_rows, grad_ld};
-  const hipError_t e = ml2::launch_embed_grad(dtype, grad_dtype, a, workspace, ml2::cu_count(dev),
+  const hipError_t e = ml2::launch_embed_grad(dtype, grad_dtype, a, workspace,
                                               static_cast<hipStream_t>(stream));
   return e == hipSuccess ? ML2_OK : hip_fail(e, "ml2_embed_grad: kernel launch");
 }

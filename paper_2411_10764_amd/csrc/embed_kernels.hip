@@ -9,7 +9,12 @@
 // lanes adds the rows of one piece one after the other in registers.  A run
 // of one id that lies inside a piece is finished there; the parts of a run
 // that crosses pieces go to the workspace and are joined by join_kernel.  No
-// floating-point atomics, so results are the same in every run.
+// floating-point atomics, so results are the same in every run.  The rows
+// that no token names are cleared by further workgroups of the sums' launch.
+//
+// A table of few numbers (rows * width at most kFewCells, width at most
+// kFewWidth) needs no sort: every lane of a wave holds a table of its own in
+// LDS (few_kernel), and the lanes' and waves' tables are added up in order.
 #include <algorithm>
 
 #include "draw.h"
@@ -18,9 +23,11 @@ namespace ml2 {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kWaveKeys = 512;   // keys of one wave in a sort pass
 constexpr int kMaxBits = 9;      // digit of a sort pass
 constexpr int kMaxBins = 1 << kMaxBits;
+constexpr int kMaxTiles = 256;   // workgroups of a sort pass
+constexpr int kFewCells = 512;
+constexpr int kFewWidth = 4;
 
 // ---- lookup -------------------------------------------------------------------
 
@@ -62,12 +69,14 @@ __device__ __forceinline__ uint32_t token_key(const int32_t *ids, int64_t i, uin
   return id < rows ? id : rows;
 }
 
+// A pass sorts by one digit.  A workgroup takes a tile: `subs` times WAVES *
+// ROUNDS * 64 keys in a row.
 struct SortPass {
   const int32_t *ids;          // first pass: the tokens themselves
   const uint32_t *key, *pos;   // later passes: the last one's output
   uint32_t *key_out, *pos_out;
-  uint32_t *hist;              // [bins][tiles]
-  uint32_t n, rows, tiles;
+  uint32_t *hist;              // [tiles][bins]
+  uint32_t n, rows, tiles, subs;
   int shift, bits;
 };
 
@@ -75,46 +84,22 @@ __device__ __forceinline__ uint32_t pass_key(const SortPass &p, uint32_t i) {
   return p.ids ? token_key(p.ids, i, p.rows) : p.key[i];
 }
 
-template <int WAVES>
+template <int WAVES, int ROUNDS>
 __global__ __launch_bounds__(WAVES * 64) void sort_count(SortPass p) {
   __shared__ uint32_t h[kMaxBins];
   const uint32_t bins = 1u << p.bits;
   for (uint32_t b = threadIdx.x; b < bins; b += WAVES * 64) h[b] = 0;
   __syncthreads();
-  const uint32_t base = blockIdx.x * (uint32_t)(WAVES * kWaveKeys);
+  for (uint32_t sub = 0; sub < p.subs; ++sub) {
+    const uint64_t base = ((uint64_t)blockIdx.x * p.subs + sub) * (WAVES * ROUNDS * 64);
 #pragma unroll
-  for (int r = 0; r < kWaveKeys / 64; ++r) {
-    const uint64_t i = (uint64_t)base + (uint32_t)(r * WAVES * 64) + threadIdx.x;
-    if (i < p.n) atomicAdd(&h[(pass_key(p, (uint32_t)i) >> p.shift) & (bins - 1)], 1u);
+    for (int r = 0; r < ROUNDS; ++r) {
+      const uint64_t i = base + (uint32_t)(r * WAVES * 64) + threadIdx.x;
+      if (i < p.n) atomicAdd(&h[(pass_key(p, (uint32_t)i) >> p.shift) & (bins - 1)], 1u);
+    }
   }
   __syncthreads();
-  for (uint32_t b = threadIdx.x; b < bins; b += WAVES * 64)
-    p.hist[(size_t)b * p.tiles + blockIdx.x] = h[b];
-}
-
-// Exclusive prefix sum of h[0..total) in place: one workgroup.
-__global__ __launch_bounds__(1024) void sort_scan(uint32_t *h, uint32_t total) {
-  __shared__ uint32_t wave_sum[16];
-  const uint32_t per = (total + 1023) / 1024;
-  const uint32_t lo = min(total, threadIdx.x * per), hi = min(total, lo + per);
-  uint32_t sum = 0;
-  for (uint32_t i = lo; i < hi; ++i) sum += h[i];
-  uint32_t incl = sum;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const uint32_t o = __shfl_up(incl, d);
-    if (lane >= d) incl += o;
-  }
-  if (lane == 63) wave_sum[wave] = incl;
-  __syncthreads();
-  uint32_t run = incl - sum;
-  for (int w = 0; w < wave; ++w) run += wave_sum[w];
-  for (uint32_t i = lo; i < hi; ++i) {
-    const uint32_t v = h[i];
-    h[i] = run;
-    run += v;
-  }
+  for (uint32_t b = threadIdx.x; b < bins; b += WAVES * 64) p.hist[blockIdx.x * bins + b] = h[b];
 }
 
 // The lanes of this wave that hold the same digit.
@@ -127,50 +112,90 @@ __device__ __forceinline__ unsigned long long same_digit(uint32_t digit, int bit
   return peers;
 }
 
-template <int WAVES>
+template <int WAVES, int ROUNDS>
 __global__ __launch_bounds__(WAVES * 64) void sort_scatter(SortPass p) {
+  constexpr uint32_t kBlock = WAVES * 64;
   __shared__ uint32_t at[WAVES][kMaxBins];
+  __shared__ uint32_t base[kMaxBins], total[kMaxBins];
   const uint32_t bins = 1u << p.bits;
-  for (uint32_t b = threadIdx.x; b < WAVES * (uint32_t)kMaxBins; b += WAVES * 64)
-    (&at[0][0])[b] = 0;
-  __syncthreads();
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const uint64_t base = (uint64_t)blockIdx.x * (WAVES * kWaveKeys) + (uint32_t)(wave * kWaveKeys);
-  uint32_t key[kWaveKeys / 64], pos[kWaveKeys / 64], rank[kWaveKeys / 64];
-#pragma unroll
-  for (int r = 0; r < kWaveKeys / 64; ++r) {
-    const uint64_t i = base + (uint32_t)(r * 64 + lane);
-    const bool in = i < p.n;
-    key[r] = in ? pass_key(p, (uint32_t)i) : 0u;
-    pos[r] = !in ? 0u : p.ids ? (uint32_t)i : p.pos[i];
-  }
-#pragma unroll
-  for (int r = 0; r < kWaveKeys / 64; ++r) {
-    const bool in = base + (uint32_t)(r * 64 + lane) < p.n;
-    const uint32_t digit = (key[r] >> p.shift) & (bins - 1);
-    const unsigned long long peers = same_digit(digit, p.bits, in);
-    const unsigned long long below = peers & ((1ull << lane) - 1);
-    const int leader = __ffsll(peers | (1ull << 63)) - 1;  // a lane even where none is active
-    uint32_t old = 0;
-    if (in && below == 0) old = atomicAdd(&at[wave][digit], (uint32_t)__popcll(peers));
-    rank[r] = __shfl(old, leader) + (uint32_t)__popcll(below);
+  // Where this tile's keys of a digit go: all keys of smaller digits, and the
+  // earlier tiles' keys of the same.  Slices of threads share the tiles.
+  for (uint32_t b = threadIdx.x; b < bins; b += kBlock) base[b] = total[b] = 0;
+  __syncthreads();
+  const uint32_t slices = max(1u, kBlock >> p.bits);
+  const uint32_t per = (p.tiles + slices - 1) / slices;
+  for (uint32_t e = threadIdx.x; e < slices * bins; e += kBlock) {
+    const uint32_t b = e & (bins - 1), t0 = (e >> p.bits) * per, t1 = min(p.tiles, t0 + per);
+    uint32_t before = 0, all = 0;
+#pragma unroll 8
+    for (uint32_t t = t0; t < t1; ++t) {
+      const uint32_t c = p.hist[t * bins + b];
+      all += c;
+      before += t < blockIdx.x ? c : 0u;
+    }
+    atomicAdd(&total[b], all);
+    atomicAdd(&base[b], before);
   }
   __syncthreads();
-  for (uint32_t b = threadIdx.x; b < bins; b += WAVES * 64) {
-    uint32_t run = p.hist[(size_t)b * p.tiles + blockIdx.x];
-    for (int w = 0; w < WAVES; ++w) {
-      const uint32_t c = at[w][b];
-      at[w][b] = run;
-      run += c;
+  if (wave == 0) {
+    uint32_t carry = 0;
+    for (uint32_t b0 = 0; b0 < bins; b0 += 64) {
+      const uint32_t b = b0 + lane, own = b < bins ? total[b] : 0u;
+      uint32_t incl = own;
+#pragma unroll
+      for (int d = 1; d < 64; d <<= 1) {
+        const uint32_t o = __shfl_up(incl, d);
+        if (lane >= d) incl += o;
+      }
+      if (b < bins) base[b] += carry + incl - own;
+      carry += __shfl(incl, 63);
     }
   }
-  __syncthreads();
+  for (uint32_t sub = 0; sub < p.subs; ++sub) {
+    const uint64_t first = ((uint64_t)blockIdx.x * p.subs + sub) * (kBlock * ROUNDS);
+    if (first >= p.n) return;
+    __syncthreads();
+    for (uint32_t b = threadIdx.x; b < WAVES * (uint32_t)kMaxBins; b += kBlock) (&at[0][0])[b] = 0;
+    __syncthreads();
+    const uint64_t own = first + (uint32_t)(wave * ROUNDS * 64);
+    uint32_t key[ROUNDS], pos[ROUNDS], rank[ROUNDS];
 #pragma unroll
-  for (int r = 0; r < kWaveKeys / 64; ++r) {
-    if (base + (uint32_t)(r * 64 + lane) >= p.n) continue;
-    const uint32_t to = at[wave][(key[r] >> p.shift) & (bins - 1)] + rank[r];
-    p.key_out[to] = key[r];
-    p.pos_out[to] = pos[r];
+    for (int r = 0; r < ROUNDS; ++r) {
+      const uint64_t i = own + (uint32_t)(r * 64 + lane);
+      const bool in = i < p.n;
+      key[r] = in ? pass_key(p, (uint32_t)i) : 0u;
+      pos[r] = !in ? 0u : p.ids ? (uint32_t)i : p.pos[i];
+    }
+#pragma unroll
+    for (int r = 0; r < ROUNDS; ++r) {
+      const bool in = own + (uint32_t)(r * 64 + lane) < p.n;
+      const uint32_t digit = (key[r] >> p.shift) & (bins - 1);
+      const unsigned long long peers = same_digit(digit, p.bits, in);
+      const unsigned long long below = peers & ((1ull << lane) - 1);
+      const int leader = __ffsll(peers | (1ull << 63)) - 1;  // a lane even where none is active
+      uint32_t old = 0;
+      if (in && below == 0) old = atomicAdd(&at[wave][digit], (uint32_t)__popcll(peers));
+      rank[r] = __shfl(old, leader) + (uint32_t)__popcll(below);
+    }
+    __syncthreads();
+    for (uint32_t b = threadIdx.x; b < bins; b += kBlock) {
+      uint32_t run = base[b];
+      for (int w = 0; w < WAVES; ++w) {
+        const uint32_t c = at[w][b];
+        at[w][b] = run;
+        run += c;
+      }
+      base[b] = run;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int r = 0; r < ROUNDS; ++r) {
+      if (own + (uint32_t)(r * 64 + lane) >= p.n) continue;
+      const uint32_t to = at[wave][(key[r] >> p.shift) & (bins - 1)] + rank[r];
+      p.key_out[to] = key[r];
+      p.pos_out[to] = pos[r];
+    }
   }
 }
 
@@ -182,6 +207,7 @@ struct SumArgs {
   float *part;                // [pieces][2][width]: the run that entered a piece, the run that leaves it
   uint32_t n, rows, piece, pieces;
   int log_g;                  // lanes that share a row
+  uint32_t slabs, sum_blocks; // slabs of a row; workgroups that add, the others clear
 };
 
 template <typename T, typename O>
@@ -222,124 +248,14 @@ __device__ __forceinline__ void load_row(const T *src, int64_t c, int64_t width,
   }
 }
 
-template <typename T, typename O>
-__global__ __launch_bounds__(kThreads) void sum_kernel(SumArgs s) {
-  using V = typename Vec<T>::type;
-  constexpr int kLen = Vec<T>::kLen;
-  constexpr int kAhead = 4;
-  const int64_t c = ((int64_t)blockIdx.y << s.log_g) * kLen +
-                    (int64_t)(threadIdx.x & ((1 << s.log_g) - 1)) * kLen;
-  const uint32_t p = blockIdx.x * (uint32_t)(kThreads >> s.log_g) + (threadIdx.x >> s.log_g);
-  if (p >= s.pieces || c >= s.a.width) return;
-  const uint32_t lo = p * s.piece, hi = min(s.n, lo + s.piece);
-  const uint32_t before = lo > 0 ? s.key[lo - 1] : 0xFFFFFFFFu;
-  const uint32_t after = hi < s.n ? s.key[hi] : 0xFFFFFFFFu;
-  const T *dout = static_cast<const T *>(s.a.dout);
-  float acc[kLen] = {};
-  uint32_t cur = s.key[lo];
-  bool entered = cur == before;  // the current run began in an earlier piece
-  for (uint32_t e = lo; e < hi; e += kAhead) {
-    uint32_t key[kAhead];
-    V v[kAhead] = {};
-#pragma unroll
-    for (int j = 0; j < kAhead; ++j) {
-      key[j] = s.rows;
-      if (e + j < hi) {
-        key[j] = s.key[e + j];
-        if (key[j] < s.rows)
-          load_row<T>(dout + (int64_t)s.pos[e + j] * s.a.dout_ld, c, s.a.width, v[j]);
-      }
-    }
-#pragma unroll
-    for (int j = 0; j < kAhead; ++j) {
-      if (e + j >= hi) break;
-      if (key[j] != cur) {
-        if (entered)
-          store_part(s.part + (size_t)p * 2 * s.a.width, c, s.a.width, acc);
-        else
-          store_row<T, O>(s, cur, c, acc);
-        cur = key[j];
-        entered = false;
-#pragma unroll
-        for (int q = 0; q < kLen; ++q) acc[q] = 0.0f;
-      }
-#pragma unroll
-      for (int q = 0; q < kLen; ++q) acc[q] += (float)v[j][q];
-    }
-  }
-  if (cur >= s.rows) return;
-  if (entered)
-    store_part(s.part + (size_t)p * 2 * s.a.width, c, s.a.width, acc);
-  else if (cur == after)
-    store_part(s.part + ((size_t)p * 2 + 1) * s.a.width, c, s.a.width, acc);
-  else
-    store_row<T, O>(s, cur, c, acc);
-}
-
-// Joins the runs that cross pieces: a workgroup looks at 64 pieces and adds,
-// for each run that leaves one of them and did not enter it, the parts of the
-// pieces it reaches.  Groups of lanes take every 256/G-th part in order; their
-// sums are added in group order.
-template <typename T, typename O>
-__global__ __launch_bounds__(kThreads) void join_kernel(SumArgs s) {
-  constexpr int kLen = Vec<T>::kLen;
-  __shared__ float sums[kThreads][kLen];
-  const int lane = threadIdx.x & 63;
-  const uint32_t p0 = blockIdx.x * 64u;
-  bool starts = false;
-  {
-    const uint32_t p = p0 + lane;
-    if (p + 1 < s.pieces) {
-      const uint32_t lo = p * s.piece, hi = lo + s.piece, id = s.key[hi - 1];
-      starts = id < s.rows && s.key[hi] == id &&
-               (s.key[lo] != id || lo == 0 || s.key[lo - 1] != id);
-    }
-  }
-  unsigned long long todo = __ballot(starts);  // the same in every wave
-  const int g = 1 << s.log_g, groups = kThreads >> s.log_g;
-  const int group = threadIdx.x >> s.log_g;
-  const int64_t c = (int64_t)blockIdx.y * g * kLen + (int64_t)(threadIdx.x & (g - 1)) * kLen;
-  const bool live = c < s.a.width;
-  while (todo) {
-    const uint32_t p = p0 + (uint32_t)(__ffsll(todo) - 1);
-    todo &= todo - 1;
-    const uint32_t id = s.key[(p + 1) * s.piece - 1];
-    uint32_t lo = (p + 1) * s.piece, hi = s.n;  // first entry past the run
-    while (lo < hi) {
-      const uint32_t mid = lo + (hi - lo) / 2;
-      if (s.key[mid] == id) lo = mid + 1; else hi = mid;
-    }
-    const uint32_t last = (lo - 1) / s.piece;
-    float acc[kLen] = {};
-    if (live) {
-      for (uint32_t q = p + group; q <= last; q += groups) {
-        const float *src = s.part + ((size_t)q * 2 + (q == p ? 1 : 0)) * s.a.width;
-#pragma unroll
-        for (int j = 0; j < kLen; ++j)
-          if (c + j < s.a.width) acc[j] += src[c + j];
-      }
-    }
-    __syncthreads();
-#pragma unroll
-    for (int j = 0; j < kLen; ++j) sums[threadIdx.x][j] = acc[j];
-    __syncthreads();
-    if (group == 0 && live) {
-      for (int q = 1; q < groups; ++q)
-#pragma unroll
-        for (int j = 0; j < kLen; ++j) acc[j] += sums[(q << s.log_g) + threadIdx.x][j];
-      store_row<T, O>(s, id, c, acc);
-    }
-  }
-}
-
-// Zeros for the table rows that no token names: a wave looks 64 rows up in
-// the sorted list at once.
+// Zeros for the rows that no token names: a wave looks 64 rows up in the
+// sorted list at once.
 template <typename O>
-__global__ __launch_bounds__(kThreads) void fill_kernel(SumArgs s) {
-  typedef O OV __attribute__((ext_vector_type(16 / sizeof(O)), aligned(sizeof(O))));
-  constexpr int kLen = 16 / sizeof(O);
+__device__ __forceinline__ void clear_rows(const SumArgs &s, uint32_t block) {
+  constexpr int kLen = 16 / (int)sizeof(O);
+  typedef O OV __attribute__((ext_vector_type(kLen), aligned(sizeof(O))));
   const int lane = threadIdx.x & 63;
-  const int64_t r0 = ((int64_t)blockIdx.x * (kThreads / 64) + (threadIdx.x >> 6)) * 64;
+  const int64_t r0 = ((int64_t)block * (kThreads / 64) + (threadIdx.x >> 6)) * 64;
   if (r0 >= s.rows) return;
   const int64_t r = r0 + lane;
   uint32_t lo = 0, hi = s.n;
@@ -366,6 +282,217 @@ __global__ __launch_bounds__(kThreads) void fill_kernel(SumArgs s) {
   }
 }
 
+// The keys and positions of a workgroup's pieces go through LDS (read once,
+// in order); a row's load is then the only access to memory that an addition
+// waits for, and kAhead of them are in flight.
+template <typename T, typename O>
+__global__ __launch_bounds__(kThreads) void sum_kernel(SumArgs s) {
+  using V = typename Vec<T>::type;
+  constexpr int kLen = Vec<T>::kLen;
+  constexpr int kAhead = 8;
+  extern __shared__ uint32_t staged[];  // [groups][piece + 1] keys, then positions
+  if (blockIdx.x >= s.sum_blocks) return clear_rows<O>(s, blockIdx.x - s.sum_blocks);
+  const uint32_t block = blockIdx.x / s.slabs, slab = blockIdx.x % s.slabs;
+  const uint32_t groups = kThreads >> s.log_g, stride = s.piece + 1;
+  uint32_t *keys = staged, *poss = staged + groups * stride;
+  const uint32_t e0 = block * groups * s.piece;
+  for (uint32_t e = threadIdx.x; e < groups * s.piece && e0 + e < s.n; e += kThreads) {
+    const uint32_t at = e / s.piece * stride + e % s.piece;
+    keys[at] = s.key[e0 + e];
+    poss[at] = s.pos[e0 + e];
+  }
+  __syncthreads();
+  const int64_t c = ((int64_t)slab << s.log_g) * kLen +
+                    (int64_t)(threadIdx.x & ((1 << s.log_g) - 1)) * kLen;
+  const uint32_t group = threadIdx.x >> s.log_g, p = block * groups + group;
+  if (p >= s.pieces || c >= s.a.width) return;
+  const uint32_t lo = p * s.piece, hi = min(s.n, lo + s.piece);
+  const uint32_t before = lo > 0 ? s.key[lo - 1] : 0xFFFFFFFFu;
+  const uint32_t after = hi < s.n ? s.key[hi] : 0xFFFFFFFFu;
+  const T *dout = static_cast<const T *>(s.a.dout);
+  const uint32_t *key = keys + group * stride, *pos = poss + group * stride;
+  const int len = (int)(hi - lo);
+  float acc[kLen] = {};
+  uint32_t cur = key[0];
+  bool entered = cur == before;  // the current run began in an earlier piece
+  for (int e = 0; e < len; e += kAhead) {
+    V v[kAhead];
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) {
+      v[j] = V{};
+      if (e + j < len && key[e + j] < s.rows)
+        load_row<T>(dout + (int64_t)pos[e + j] * s.a.dout_ld, c, s.a.width, v[j]);
+    }
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) {
+      if (e + j < len && key[e + j] != cur) {
+        if (entered)
+          store_part(s.part + (size_t)p * 2 * s.a.width, c, s.a.width, acc);
+        else
+          store_row<T, O>(s, cur, c, acc);
+        cur = key[e + j];
+        entered = false;
+#pragma unroll
+        for (int q = 0; q < kLen; ++q) acc[q] = 0.0f;
+      }
+#pragma unroll
+      for (int q = 0; q < kLen; ++q) acc[q] += (float)v[j][q];
+    }
+  }
+  if (cur >= s.rows) return;
+  if (entered)
+    store_part(s.part + (size_t)p * 2 * s.a.width, c, s.a.width, acc);
+  else if (cur == after)
+    store_part(s.part + ((size_t)p * 2 + 1) * s.a.width, c, s.a.width, acc);
+  else
+    store_row<T, O>(s, cur, c, acc);
+}
+
+// Joins the runs that cross pieces: a workgroup looks at kJoin pieces and adds,
+// for each run that leaves one of them and did not enter it, the parts of the
+// pieces it reaches.  Groups of lanes take every 256/G-th part in order; their
+// sums are added in group order.
+constexpr int kJoin = 8;
+
+template <typename T, typename O>
+__global__ __launch_bounds__(kThreads) void join_kernel(SumArgs s) {
+  constexpr int kLen = Vec<T>::kLen;
+  typedef float Part __attribute__((ext_vector_type(kLen), aligned(4)));
+  __shared__ float sums[kThreads][kLen];
+  const uint32_t p0 = blockIdx.x * (uint32_t)kJoin;
+  bool starts = false;
+  {
+    const uint32_t p = p0 + (threadIdx.x & 63);
+    if ((threadIdx.x & 63) < kJoin && p + 1 < s.pieces) {
+      const uint32_t lo = p * s.piece, hi = lo + s.piece, id = s.key[hi - 1];
+      starts = id < s.rows && s.key[hi] == id &&
+               (s.key[lo] != id || lo == 0 || s.key[lo - 1] != id);
+    }
+  }
+  unsigned long long todo = __ballot(starts);  // the same in every wave
+  const int g = 1 << s.log_g, groups = kThreads >> s.log_g;
+  const int group = threadIdx.x >> s.log_g;
+  const int64_t c = (int64_t)blockIdx.y * g * kLen + (int64_t)(threadIdx.x & (g - 1)) * kLen;
+  const bool live = c < s.a.width, whole = c + kLen <= s.a.width;
+  while (todo) {
+    const uint32_t p = p0 + (uint32_t)(__ffsll(todo) - 1);
+    todo &= todo - 1;
+    const uint32_t id = s.key[(p + 1) * s.piece - 1];
+    uint32_t last = p + 1;  // the last piece that begins with the run's id
+    for (;;) {
+      const uint32_t q = last + 1 + (threadIdx.x & 63);
+      const unsigned long long on = __ballot(q < s.pieces && s.key[q * s.piece] == id);
+      last += on == ~0ull ? 64u : (uint32_t)__ffsll(~on) - 1;
+      if (on != ~0ull) break;
+    }
+    float acc[kLen] = {};
+    if (live) {
+#pragma unroll 4
+      for (uint32_t q = p + group; q <= last; q += groups) {
+        const float *src = s.part + ((size_t)q * 2 + (q == p ? 1 : 0)) * s.a.width + c;
+        if (whole) {
+          const Part v = *reinterpret_cast<const Part *>(src);
+#pragma unroll
+          for (int j = 0; j < kLen; ++j) acc[j] += v[j];
+        } else {
+#pragma unroll
+          for (int j = 0; j < kLen; ++j)
+            if (c + j < s.a.width) acc[j] += src[j];
+        }
+      }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < kLen; ++j) sums[threadIdx.x][j] = acc[j];
+    __syncthreads();
+    if (group == 0 && live) {
+      for (int q = 1; q < groups && q <= (int)(last - p); ++q)
+#pragma unroll
+        for (int j = 0; j < kLen; ++j) acc[j] += sums[(q << s.log_g) + threadIdx.x][j];
+      store_row<T, O>(s, id, c, acc);
+    }
+  }
+}
+
+// ---- tables of few numbers -------------------------------------------------------
+
+struct FewArgs {
+  EmbedGradArgs a;
+  float *part;       // [rows * width][waves]
+  uint32_t cells, waves;
+  int64_t per;       // tokens of a wave
+};
+
+// One wave a workgroup.  Number (v, d) of lane i's own table is
+// mine[(v * width + d) * 64 + i]: no two lanes share a bank or a number.
+// WIDTH: the row's width, or kFewWidth for all but the narrowest.
+template <typename T, int WIDTH>
+__global__ __launch_bounds__(64) void few_kernel(FewArgs f) {
+  constexpr int kAhead = 16 / WIDTH;
+  extern __shared__ float mine[];
+  const int lane = threadIdx.x, width = WIDTH == 1 ? 1 : (int)f.a.width;
+  const T *dout = static_cast<const T *>(f.a.dout);
+  const int64_t lo = blockIdx.x * f.per, hi = min(f.a.n, lo + f.per);
+  uint32_t id[kAhead];
+  T v[kAhead][WIDTH];
+  auto fetch = [&](int64_t i0) {
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) {
+      const int64_t i = i0 + j * 64;
+      id[j] = i < hi ? (uint32_t)f.a.ids[i] : 0xFFFFFFFFu;
+#pragma unroll
+      for (int d = 0; d < WIDTH; ++d)
+        v[j][d] = i < hi && d < width ? dout[i * f.a.dout_ld + d] : (T)0.0f;
+    }
+  };
+  fetch(lo + lane);
+  for (uint32_t c = lane; c < f.cells * 64; c += 64) mine[c] = 0.0f;
+  for (int64_t i0 = lo + lane; i0 - lane < hi; i0 += 64 * kAhead) {
+    uint32_t now[kAhead];
+    T add[kAhead][WIDTH];
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) {
+      now[j] = id[j];
+#pragma unroll
+      for (int d = 0; d < WIDTH; ++d) add[j][d] = v[j][d];
+    }
+    fetch(i0 + 64 * kAhead);
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) {
+      if (now[j] >= (uint32_t)f.a.table_rows) continue;
+      float *at = mine + (size_t)now[j] * width * 64 + lane;
+#pragma unroll
+      for (int d = 0; d < WIDTH; ++d)
+        if (d < width) at[d * 64] += (float)add[j][d];
+    }
+  }
+  __syncthreads();
+  for (uint32_t c = lane; c < f.cells; c += 64) {
+    float sum = 0.0f;
+#pragma unroll 16
+    for (int j = 0; j < 64; ++j) sum += mine[c * 64 + ((lane + j) & 63)];
+    f.part[(size_t)c * f.waves + blockIdx.x] = sum;
+  }
+}
+
+// The waves' sums of one number, added by a workgroup.
+template <typename O>
+__global__ __launch_bounds__(kThreads) void few_join(FewArgs f) {
+  __shared__ float sums[kThreads];
+  float sum = 0.0f;
+  for (uint32_t w = threadIdx.x; w < f.waves; w += kThreads)
+    sum += f.part[(size_t)blockIdx.x * f.waves + w];
+  sums[threadIdx.x] = sum;
+  __syncthreads();
+  for (int d = kThreads / 2; d > 0; d >>= 1) {
+    if ((int)threadIdx.x < d) sums[threadIdx.x] += sums[threadIdx.x + d];
+    __syncthreads();
+  }
+  if (threadIdx.x == 0)
+    static_cast<O *>(f.a.grad)[blockIdx.x / f.a.width * f.a.grad_ld + blockIdx.x % f.a.width] =
+        narrow<O>(sums[0] * f.a.scale);
+}
+
 // ---- plans -------------------------------------------------------------------
 
 // Lanes that share a row: enough 16-byte vectors for its width, at most `most`.
@@ -376,24 +503,37 @@ int log_group(int64_t width, int len, int most) {
 }
 
 struct GradPlan {
-  int bits, passes, waves;  // of a digit; sort passes; waves of a sort workgroup
-  uint32_t tiles, piece, pieces;
-  size_t keys, hist, part;  // byte offsets of the second key buffer, counts, parts
+  bool few;
+  uint32_t waves;              // few: waves, one a workgroup
+  int bits, passes, big;       // of a digit; sort passes; 16 waves a sort workgroup, else 4
+  uint32_t tiles, subs, piece, pieces;
+  size_t keys, hist, part;     // byte offsets of the second key buffer, counts, parts
   size_t bytes;
 };
 
+constexpr int kBigKeys = 16 * 8 * 64, kSmallKeys = 4 * 4 * 64;  // keys of a sort workgroup's step
+
 GradPlan grad_plan(int64_t n, int64_t rows, int64_t width) {
   GradPlan p{};
+  auto align = [](size_t b) { return (b + 255) & ~(size_t)255; };
+  p.few = n > 0 && width >= 1 && width <= kFewWidth && rows >= 1 && rows * width <= kFewCells;
+  if (p.few) {
+    // as many waves as 256 CUs' LDS holds tables, none for fewer than 512 tokens
+    const int64_t per_cu = std::min<int64_t>(8, (160 * 1024) / (rows * width * 256));
+    p.waves = (uint32_t)std::min<int64_t>(256 * per_cu, (n + 511) / 512);
+    p.bytes = align((size_t)(rows * width) * p.waves * 4);
+    return p;
+  }
   int bits = 1;
   while (((int64_t)1 << bits) <= rows) ++bits;  // keys 0 .. rows
   p.passes = (bits + kMaxBits - 1) / kMaxBits;
   p.bits = (bits + p.passes - 1) / p.passes;
-  p.waves = n > (1 << 18) ? 16 : 4;
-  const int64_t tile = (int64_t)p.waves * kWaveKeys;
-  p.tiles = (uint32_t)((n + tile - 1) / tile);
+  p.big = n > (int64_t)kMaxTiles * kSmallKeys;
+  const int64_t step = p.big ? kBigKeys : kSmallKeys;
+  p.subs = (uint32_t)std::max<int64_t>(1, (n + step * kMaxTiles - 1) / (step * kMaxTiles));
+  p.tiles = (uint32_t)((n + step * p.subs - 1) / (step * p.subs));
   p.piece = 32;
   p.pieces = (uint32_t)((n + p.piece - 1) / p.piece);
-  auto align = [](size_t b) { return (b + 255) & ~(size_t)255; };
   const size_t list = align((size_t)n * 4);
   p.keys = 2 * list;
   p.hist = 4 * list;
@@ -403,56 +543,32 @@ GradPlan grad_plan(int64_t n, int64_t rows, int64_t width) {
 }
 
 template <typename T, typename O>
-hipError_t launch_sums(const SumArgs &s, int64_t width, hipStream_t st) {
-  const uint32_t slabs = (uint32_t)((width + ((int64_t)Vec<T>::kLen << s.log_g) - 1) /
-                                    ((int64_t)Vec<T>::kLen << s.log_g));
-  const uint32_t per = kThreads >> s.log_g;
-  if (s.rows > 0)
-    fill_kernel<O><<<(s.rows + 255u) / 256u, kThreads, 0, st>>>(s);
-  if (s.n > 0) {
-    sum_kernel<T, O><<<dim3((s.pieces + per - 1) / per, slabs), kThreads, 0, st>>>(s);
-    if (s.pieces > 1)
-      join_kernel<T, O><<<dim3((s.pieces + 63) / 64, slabs), kThreads, 0, st>>>(s);
-  }
+hipError_t launch_few(const EmbedGradArgs &a, const GradPlan &g, void *ws, hipStream_t st) {
+  FewArgs f{};
+  f.a = a;
+  f.part = static_cast<float *>(ws);
+  f.cells = (uint32_t)(a.table_rows * a.width);
+  f.waves = g.waves;
+  f.per = ((a.n + g.waves - 1) / g.waves + 63) / 64 * 64;
+  const size_t lds = (size_t)f.cells * 256;
+  auto *kernel = a.width == 1 ? few_kernel<T, 1> : few_kernel<T, kFewWidth>;
+  const hipError_t e = ensure_dynamic_lds(reinterpret_cast<const void *>(kernel), lds);
+  if (e != hipSuccess) return e;
+  kernel<<<f.waves, 64, lds, st>>>(f);
+  few_join<O><<<f.cells, kThreads, 0, st>>>(f);
   return hipGetLastError();
 }
 
-template <typename T>
-hipError_t launch_lookup(const EmbedArgs &a, int cu_count, hipStream_t s) {
-  const int log_g = log_group(a.width, Vec<T>::kLen, 6);
-  const int64_t per = kThreads >> log_g;
-  const int64_t grid = std::min<int64_t>((a.n + per - 1) / per, (int64_t)cu_count * 32);
-  lookup_kernel<T><<<(uint32_t)grid, kThreads, 0, s>>>(a, log_g);
-  return hipGetLastError();
-}
-
-template <int WAVES>
+template <int WAVES, int ROUNDS>
 void launch_pass(const SortPass &p, hipStream_t st) {
-  sort_count<WAVES><<<p.tiles, WAVES * 64, 0, st>>>(p);
-  sort_scan<<<1, 1024, 0, st>>>(p.hist, p.tiles << p.bits);
-  sort_scatter<WAVES><<<p.tiles, WAVES * 64, 0, st>>>(p);
+  sort_count<WAVES, ROUNDS><<<p.tiles, WAVES * 64, 0, st>>>(p);
+  sort_scatter<WAVES, ROUNDS><<<p.tiles, WAVES * 64, 0, st>>>(p);
 }
 
-}  // namespace
-
-hipError_t launch_embed(int dtype, const EmbedArgs &a, int cu_count, hipStream_t s) {
-  if (a.n == 0 || a.width == 0) return hipSuccess;
-  switch (dtype) {
-    case ML2_F32: return launch_lookup<float>(a, cu_count, s);
-    case ML2_BF16: return launch_lookup<__bf16>(a, cu_count, s);
-    default: return launch_lookup<_Float16>(a, cu_count, s);
-  }
-}
-
-size_t embed_grad_workspace_bytes(int64_t n, int64_t table_rows, int64_t width) {
-  return std::max<size_t>(256, grad_plan(n, table_rows, width).bytes);
-}
-
-hipError_t launch_embed_grad(int dtype, int grad_dtype, const EmbedGradArgs &a, void *ws,
-                             int cu_count, hipStream_t st) {
-  (void)cu_count;
-  if (a.table_rows == 0 || a.width == 0) return hipSuccess;
+template <typename T, typename O>
+hipError_t launch_grad(const EmbedGradArgs &a, void *ws, hipStream_t st) {
   const GradPlan g = grad_plan(a.n, a.table_rows, a.width);
+  if (g.few) return launch_few<T, O>(a, g, ws, st);
   char *base = static_cast<char *>(ws);
   uint32_t *list[2] = {reinterpret_cast<uint32_t *>(base),
                        reinterpret_cast<uint32_t *>(base + g.keys)};
@@ -473,9 +589,10 @@ hipError_t launch_embed_grad(int dtype, int grad_dtype, const EmbedGradArgs &a, 
     p.n = (uint32_t)a.n;
     p.rows = (uint32_t)a.table_rows;
     p.tiles = g.tiles;
+    p.subs = g.subs;
     p.shift = pass * g.bits;
     p.bits = g.bits;
-    if (g.waves == 16) launch_pass<16>(p, st); else launch_pass<4>(p, st);
+    if (g.big) launch_pass<16, 8>(p, st); else launch_pass<4, 4>(p, st);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
@@ -488,16 +605,57 @@ hipError_t launch_embed_grad(int dtype, int grad_dtype, const EmbedGradArgs &a, 
   s.rows = (uint32_t)a.table_rows;
   s.piece = g.piece;
   s.pieces = g.pieces;
-  s.log_g = log_group(a.width, dtype == ML2_F32 ? 4 : 8, 6);
+  s.log_g = log_group(a.width, Vec<T>::kLen, 6);
+  const int64_t slab = (int64_t)Vec<T>::kLen << s.log_g;
+  s.slabs = (uint32_t)((a.width + slab - 1) / slab);
+  const uint32_t per = kThreads >> s.log_g;
+  s.sum_blocks = (s.pieces + per - 1) / per * s.slabs;
+  const uint32_t clear = (s.rows + kThreads - 1) / kThreads;
+  const size_t lds = (size_t)per * (g.piece + 1) * 8;
+  const hipError_t e = ensure_dynamic_lds(reinterpret_cast<const void *>(sum_kernel<T, O>), lds);
+  if (e != hipSuccess) return e;
+  sum_kernel<T, O><<<s.sum_blocks + clear, kThreads, lds, st>>>(s);
+  if (s.pieces > 1)
+    join_kernel<T, O><<<dim3((s.pieces + kJoin - 1) / kJoin, s.slabs), kThreads, 0, st>>>(s);
+  return hipGetLastError();
+}
+
+template <typename T>
+hipError_t launch_lookup(const EmbedArgs &a, int cu_count, hipStream_t s) {
+  const int log_g = log_group(a.width, Vec<T>::kLen, 6);
+  const int64_t per = kThreads >> log_g;
+  const int64_t grid = std::min<int64_t>((a.n + per - 1) / per, (int64_t)cu_count * 32);
+  lookup_kernel<T><<<(uint32_t)grid, kThreads, 0, s>>>(a, log_g);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_embed(int dtype, const EmbedArgs &a, int cu_count, hipStream_t s) {
+  if (a.n == 0 || a.width == 0) return hipSuccess;
+  switch (dtype) {
+    case ML2_F32: return launch_lookup<float>(a, cu_count, s);
+    case ML2_BF16: return launch_lookup<__bf16>(a, cu_count, s);
+    default: return launch_lookup<_Float16>(a, cu_count, s);
+  }
+}
+
+size_t embed_grad_workspace_bytes(int64_t n, int64_t table_rows, int64_t width) {
+  return std::max<size_t>(256, grad_plan(n, table_rows, width).bytes);
+}
+
+hipError_t launch_embed_grad(int dtype, int grad_dtype, const EmbedGradArgs &a, void *ws,
+                             hipStream_t st) {
+  if (a.table_rows == 0 || a.width == 0) return hipSuccess;
   const bool wide = grad_dtype == ML2_F32;
   switch (dtype) {
-    case ML2_F32: return launch_sums<float, float>(s, a.width, st);
+    case ML2_F32: return launch_grad<float, float>(a, ws, st);
     case ML2_BF16:
-      return wide ? launch_sums<__bf16, float>(s, a.width, st)
-                  : launch_sums<__bf16, __bf16>(s, a.width, st);
+      return wide ? launch_grad<__bf16, float>(a, ws, st)
+                  : launch_grad<__bf16, __bf16>(a, ws, st);
     default:
-      return wide ? launch_sums<_Float16, float>(s, a.width, st)
-                  : launch_sums<_Float16, _Float16>(s, a.width, st);
+      return wide ? launch_grad<_Float16, float>(a, ws, st)
+                  : launch_grad<_Float16, _Float16>(a, ws, st);
   }
 }
 

@@ -27,6 +27,7 @@ ML2_MAX_FEATURES = 256
 ML2_MAX_TOPK = 16384
 ML2_MAX_STREAM_K = 4096
 ML2_MAX_ROWS = 2097152
+ML2_MAX_TOKENS = 1073741824
 ML2_MAX_WIDTH = 65536
 ML2_F32, ML2_BF16, ML2_F16 = 0, 1, 2
 
@@ -450,11 +451,28 @@ class Pipeline:
 
 # ---- drawing from scores, and learning from what was drawn -----------------
 
-_DTYPES = {"torch.float32": ML2_F32, "torch.bfloat16": ML2_BF16, "torch.float16": ML2_F16}
+class _Types:
+    """torch's types that the operators take (torch is imported on first use)."""
+
+    def __init__(self):
+        import torch
+        self.f32, self.i32 = torch.float32, torch.int32
+        self.mask = (torch.uint8, torch.bool)
+        self.code = {torch.float32: ML2_F32, torch.bfloat16: ML2_BF16, torch.float16: ML2_F16}
+
+
+_types = None
+
+
+def _t() -> _Types:
+    global _types
+    if _types is None:
+        _types = _Types()
+    return _types
 
 
 def _dtype(t) -> int:
-    d = _DTYPES.get(str(t))
+    d = _t().code.get(t)
     if d is None:
         raise ValueError(f"float32, bfloat16 or float16 expected, not {t}")
     return d
@@ -469,19 +487,22 @@ def _matrix(x, name: str):
     """(pointer, rows, columns, row stride) of a 2-D device tensor whose
     columns are contiguous; a single row may have any row stride."""
     _device(x, name)
-    if x.dim() != 2 or (x.shape[0] > 0 and x.shape[1] > 1 and x.stride(1) != 1):
+    shape = x.shape
+    if len(shape) != 2:
         raise ValueError(f"{name} must be a 2-D tensor with unit column stride")
-    rows, n = x.shape
-    return x.data_ptr(), rows, n, x.stride(0) if rows > 1 and n > 0 else max(x.stride(0), n)
+    (rows, n), (ld, step) = shape, x.stride()
+    if step != 1 and rows > 0 and n > 1:
+        raise ValueError(f"{name} must be a 2-D tensor with unit column stride")
+    return x.data_ptr(), rows, n, ld if rows > 1 and n > 0 else max(ld, n)
 
 
-def _flat(x, name: str, dtype: str, shape):
+def _flat(x, name: str, dtype, shape):
     """Pointer of a contiguous device tensor of the given type and shape (or None)."""
     if x is None:
         return None
-    _device(x, name)
-    if str(x.dtype) != "torch." + dtype or tuple(x.shape) != tuple(shape) or not x.is_contiguous():
-        raise ValueError(f"{name} must be a contiguous {dtype} tensor of shape {tuple(shape)}")
+    if x.dtype is not dtype or x.shape != shape or not x.is_contiguous() or not x.is_cuda:
+        raise ValueError(f"{name} must be a contiguous {dtype} device tensor of shape "
+                         f"{tuple(shape)}")
     return x.data_ptr()
 
 
@@ -489,7 +510,7 @@ def _mask(valid, rows: int, n: int):
     """(pointer, row stride) of a uint8 mask [n] (shared) or [rows][n], or None."""
     if valid is None:
         return None, 0
-    if str(valid.dtype) not in ("torch.uint8", "torch.bool"):
+    if valid.dtype not in _t().mask:
         raise ValueError("valid must be a uint8 or bool tensor")
     _device(valid, "valid")
     if valid.dim() == 1:
@@ -539,11 +560,11 @@ def ml2_sample(scores, u, idx, logprob, workspace, valid=None, temperature=None,
     vp, vld = _mask(valid, rows, n)
     _check(lib().ml2_sample(
         _dtype(scores.dtype), sp, n, ld, rows, vp, vld,
-        _flat(temperature, "temperature", "float32", (rows,)),
-        _flat(top_k, "top_k", "int32", (rows,)), _flat(top_p, "top_p", "float32", (rows,)),
-        _flat(min_p, "min_p", "float32", (rows,)), _flat(u, "u", "float32", (rows, draws)), draws,
-        _flat(idx, "idx", "int32", (rows, draws)),
-        _flat(logprob, "logprob", "float32", (rows, draws)), *_space(workspace),
+        _flat(temperature, "temperature", _t().f32, (rows,)),
+        _flat(top_k, "top_k", _t().i32, (rows,)), _flat(top_p, "top_p", _t().f32, (rows,)),
+        _flat(min_p, "min_p", _t().f32, (rows,)), _flat(u, "u", _t().f32, (rows, draws)), draws,
+        _flat(idx, "idx", _t().i32, (rows, draws)),
+        _flat(logprob, "logprob", _t().f32, (rows, draws)), *_space(workspace),
         _stream(stream)))
 
 
@@ -559,9 +580,9 @@ def ml2_logprob(scores, targets, logprob, workspace, valid=None, temperature=Non
     vp, vld = _mask(valid, rows, n)
     _check(lib().ml2_logprob(
         _dtype(scores.dtype), sp, n, ld, rows, vp, vld,
-        _flat(temperature, "temperature", "float32", (rows,)),
-        _flat(targets, "targets", "int32", shape), shape[1],
-        _flat(logprob, "logprob", "float32", shape), *_space(workspace),
+        _flat(temperature, "temperature", _t().f32, (rows,)),
+        _flat(targets, "targets", _t().i32, shape), shape[1],
+        _flat(logprob, "logprob", _t().f32, shape), *_space(workspace),
         _stream(stream)))
 
 
@@ -577,9 +598,9 @@ def ml2_logprob_grad(scores, targets, weight, grad, workspace, logprob=None, val
     vp, vld = _mask(valid, rows, n)
     _check(lib().ml2_logprob_grad(
         _dtype(scores.dtype), sp, n, ld, rows, vp, vld,
-        _flat(temperature, "temperature", "float32", (rows,)),
-        _flat(targets, "targets", "int32", shape), _flat(weight, "weight", "float32", shape),
-        shape[1], _flat(logprob, "logprob", "float32", shape), gp, gld, *_space(workspace),
+        _flat(temperature, "temperature", _t().f32, (rows,)),
+        _flat(targets, "targets", _t().i32, shape), _flat(weight, "weight", _t().f32, shape),
+        shape[1], _flat(logprob, "logprob", _t().f32, shape), gp, gld, *_space(workspace),
         _stream(stream)))
 
 
@@ -589,7 +610,7 @@ def ml2_embed(table, ids, out, scale: float = 1.0, stream=None) -> None:
     op, N, width, out_ld = _matrix(out, "out")
     if width != D or out.dtype != table.dtype:
         raise ValueError("out must have the table's width and type")
-    _check(lib().ml2_embed(_dtype(table.dtype), tp, V, D, ld, _flat(ids, "ids", "int32", (N,)), N,
+    _check(lib().ml2_embed(_dtype(table.dtype), tp, V, D, ld, _flat(ids, "ids", _t().i32, (N,)), N,
                            scale, op, out_ld, _stream(stream)))
 
 
@@ -604,7 +625,7 @@ def ml2_embed_grad(dout, ids, grad, workspace, scale: float = 1.0, stream=None) 
     gp, V, width, gld = _matrix(grad, "grad")
     if width != D:
         raise ValueError("grad must have dout's width")
-    _check(lib().ml2_embed_grad(_dtype(dout.dtype), dp, N, D, ld, _flat(ids, "ids", "int32", (N,)),
+    _check(lib().ml2_embed_grad(_dtype(dout.dtype), dp, N, D, ld, _flat(ids, "ids", _t().i32, (N,)),
                                 scale, _dtype(grad.dtype), gp, V, gld, *_space(workspace),
                                 _stream(stream)))
 
