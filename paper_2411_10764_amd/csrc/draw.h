@@ -94,6 +94,25 @@ __device__ __forceinline__ float included(float s, bool valid) {
   return valid && !__builtin_isnan(s) ? s + 0.0f : -__builtin_inff();
 }
 
+// Eight consecutive entries i .. i+7 of a row of n: -inf where not included.
+template <typename T>
+__device__ __forceinline__ void load8(const T *scores, const uint8_t *valid, int64_t i, int64_t n,
+                                      float (&x)[8]) {
+  typedef T V __attribute__((ext_vector_type(8), aligned(sizeof(T))));
+  typedef unsigned long long Mask __attribute__((aligned(1)));
+  if (i + 8 <= n) {
+    const V v = *reinterpret_cast<const V *>(scores + i);
+    const unsigned long long mask = valid ? *reinterpret_cast<const Mask *>(valid + i) : ~0ull;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) x[j] = included((float)v[j], ((mask >> (8 * j)) & 0xFF) != 0);
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      x[j] = i + j < n ? included((float)scores[i + j], !valid || valid[i + j] != 0)
+                       : -__builtin_inff();
+  }
+}
+
 __device__ __forceinline__ float inverse_temperature(const float *temperature, int64_t row,
                                                      bool *greedy) {
   const float t = temperature ? temperature[row] : 1.0f;

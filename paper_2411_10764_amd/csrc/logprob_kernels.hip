@@ -5,10 +5,19 @@
 //   logprob_j = z_{t_j} - log l
 //   grad_i = R * (sum_{j: t_j = i} w_j - exp(z_i) / l * sum_j w_j)
 //
-// A row is cut into chunks.  stats_kernel reads a chunk once and keeps a
-// running maximum and sum (of exp of differences to that maximum); finish and
-// grad join the chunks' pairs in chunk order, so every workgroup of a row
-// arrives at the same m and l.  Weights are joined in the order of j.
+// Bytes bound it: a row is read once, its gradient written once.
+//
+// Rows that fit a workgroup's registers (row_kernel): one launch, the row's
+// scores stay as they came, in registers, between the maximum, the sum and
+// the gradient; two exponentials an entry cost less than the registers that
+// would hold the first ones in float32 (and with them the second workgroup
+// of a CU, whose loads run beside this one's arithmetic).
+//
+// Other rows are cut into chunks.  stats_kernel reads a chunk once and keeps
+// a running maximum and sum (of exp of differences to that maximum);
+// finish_kernel and grad_kernel join the chunks' pairs in chunk order, so
+// every workgroup of a row arrives at the same m and l.  Weights are joined
+// in the order of j inside a chunk, then in chunk order.
 #include <algorithm>
 
 #include "draw.h"
@@ -17,11 +26,20 @@ namespace ml2 {
 namespace {
 
 constexpr int kThreads = 256;
+constexpr int kChunk = 2048;      // smallest chunk
+constexpr int kPairs = 128;       // targets of a workgroup compared pair by pair
 constexpr float kLog2e = 1.44269504088896340736f;
 
 struct Stat {
   float m, l;  // maximum of the included scores, sum of exp((s - m) * R)
 };
+
+struct Part {
+  Stat s;
+  float w;     // weights of the included targets
+};
+
+__device__ __forceinline__ float ninf() { return -__builtin_inff(); }
 
 // exp(y * ln 2) of a difference to the maximum.  Where maximum and score are
 // both infinite their difference is NaN and the entry counts as the maximum.
@@ -30,9 +48,8 @@ __device__ __forceinline__ float weight_of(float x, float m, float c) {
 }
 
 __device__ __forceinline__ Stat join(Stat a, Stat b, float c) {
-  const float ninf = -__builtin_inff();
-  if (b.m == ninf) return a;
-  if (a.m == ninf) return b;
+  if (b.m == ninf()) return a;
+  if (a.m == ninf()) return b;
   const float m = fmaxf(a.m, b.m);
   return {m, a.l * weight_of(a.m, m, c) + b.l * weight_of(b.m, m, c)};
 }
@@ -54,142 +71,467 @@ __device__ __forceinline__ Stat block_join(Stat s, float c, Stat *lds) {
   return s;
 }
 
+__device__ __forceinline__ float block_sum(float v, float *lds) {
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) v += __shfl_xor(v, d);
+  __syncthreads();
+  if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
+  __syncthreads();
+  v = lds[0];
+  for (int w = 1; w < (int)blockDim.x >> 6; ++w) v += lds[w];
+  return v;
+}
+
 struct Rows {
   LogprobArgs a;
-  Stat *part;      // [rows][chunks]
+  Part *part;      // [rows][chunks]
   int64_t chunk;   // entries of a chunk
   int64_t chunks;
 };
 
 template <typename T>
-__device__ __forceinline__ float load_score(const Rows &k, int64_t row, int64_t i) {
-  const T *s = static_cast<const T *>(k.a.s.scores) + row * k.a.s.ld;
-  const bool ok = !k.a.s.valid || k.a.s.valid[row * k.a.s.valid_ld + i] != 0;
-  return included((float)s[i], ok);
+__device__ __forceinline__ const T *row_scores(const Rows &k, int64_t row) {
+  return static_cast<const T *>(k.a.s.scores) + row * k.a.s.ld;
+}
+
+__device__ __forceinline__ const uint8_t *row_mask(const Rows &k, int64_t row) {
+  return k.a.s.valid ? k.a.s.valid + row * k.a.s.valid_ld : nullptr;
 }
 
 template <typename T>
+__device__ __forceinline__ float load_score(const Rows &k, int64_t row, int64_t i) {
+  const uint8_t *valid = row_mask(k, row);
+  return included((float)row_scores<T>(k, row)[i], !valid || valid[i] != 0);
+}
+
+// log-probability of an included score
+__device__ __forceinline__ float logprob_of(float x, Stat st, float r) {
+  return x == ninf() ? x : (x == st.m ? 0.0f : (x - st.m) * r) - logf(st.l);
+}
+
+// ---- targets of a range of entries ----------------------------------------------
+
+// Handles the targets in [lo, hi): afterwards list[0..count) holds them as
+// (entry << 32) | j in the order of j.  Every thread of the workgroup calls it.
+__device__ __forceinline__ int list_targets(const int32_t *targets, int per_row, int64_t lo,
+                                            int64_t hi, unsigned long long *list, int *waves_at) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
+  int count = 0;
+  for (int j0 = 0; j0 < per_row; j0 += blockDim.x) {
+    const int j = j0 + threadIdx.x;
+    const int64_t t = j < per_row ? targets[j] : -1;
+    const bool mine = t >= lo && t < hi;
+    const unsigned long long on = __ballot(mine);
+    __syncthreads();
+    if (lane == 0) waves_at[wave] = __popcll(on);
+    __syncthreads();
+    int at = count;
+    for (int w = 0; w < waves; ++w) {
+      if (w == wave && mine)
+        list[at + __popcll(on & ((1ull << lane) - 1))] =
+            ((unsigned long long)t << 32) | (unsigned)j;
+      at += waves_at[w];
+    }
+    count = at;
+  }
+  __syncthreads();
+  return count;
+}
+
+// Calls f(entry, sum of weights) once for every entry the list names; weights
+// of one entry are added in the order of j.  Few targets are compared pair by
+// pair, many are sorted first (list has room for the next power of two).
+template <typename F>
+__device__ __forceinline__ void each_entry(unsigned long long *list, int count,
+                                           const float *weight, F f) {
+  const int threads = blockDim.x;
+  if (count <= kPairs) {
+    for (int a = threadIdx.x; a < count; a += threads) {
+      const uint32_t t = (uint32_t)(list[a] >> 32);
+      bool first = true;
+      for (int b = 0; b < a && first; ++b) first = (uint32_t)(list[b] >> 32) != t;
+      if (!first) continue;
+      float sum = weight[(uint32_t)list[a]];
+      for (int b = a + 1; b < count; ++b)
+        if ((uint32_t)(list[b] >> 32) == t) sum += weight[(uint32_t)list[b]];
+      f((int64_t)t, sum);
+    }
+    return;
+  }
+  int size = 256;
+  while (size < count) size <<= 1;
+  for (int a = count + threadIdx.x; a < size; a += threads) list[a] = ~0ull;
+  for (int k = 2; k <= size; k <<= 1) {
+    for (int d = k >> 1; d > 0; d >>= 1) {
+      __syncthreads();
+      for (int a = threadIdx.x; a < size / 2; a += threads) {
+        const int i = (a / d) * 2 * d + a % d, j = i + d;
+        const unsigned long long x = list[i], y = list[j];
+        if ((x > y) == ((i & k) == 0)) list[i] = y, list[j] = x;
+      }
+    }
+  }
+  __syncthreads();
+  for (int a = threadIdx.x; a < count; a += threads) {
+    const uint32_t t = (uint32_t)(list[a] >> 32);
+    if (a > 0 && (uint32_t)(list[a - 1] >> 32) == t) continue;
+    float sum = 0.0f;
+    for (int b = a; b < count && (uint32_t)(list[b] >> 32) == t; ++b)
+      sum += weight[(uint32_t)list[b]];
+    f((int64_t)t, sum);
+  }
+}
+
+// Weights of the listed targets that are included, added in an order that
+// depends on the list alone.
+template <typename T>
+__device__ __forceinline__ float listed_weight(const Rows &k, int64_t row, const float *weight,
+                                               const unsigned long long *list, int count,
+                                               float *lds) {
+  float w = 0.0f;
+  for (int a = threadIdx.x; a < count; a += blockDim.x)
+    if (load_score<T>(k, row, (int64_t)(list[a] >> 32)) != ninf())
+      w += weight[(uint32_t)list[a]];
+  return count > 0 ? block_sum(w, lds) : 0.0f;
+}
+
+// Log-probabilities of targets that lie outside the row.
+__device__ __forceinline__ void outside(const Rows &k, int64_t row) {
+  for (int j = threadIdx.x; j < k.a.per_row; j += blockDim.x) {
+    const int64_t t = k.a.targets[row * k.a.per_row + j];
+    if (t < 0 || t >= k.a.s.n) k.a.logprob[row * k.a.per_row + j] = 0.0f;
+  }
+}
+
+// The listed targets' log-probabilities and the gradient at their entries.
+// scale = -(sum of weights) / l * R, bias so that exp2((s - m) * c) is right.
+template <typename T>
+__device__ __forceinline__ void at_targets(const Rows &k, int64_t row, unsigned long long *list,
+                                           int count, Stat st, float r, float scale) {
+  const float *weight = k.a.weight + row * k.a.per_row;
+  if (k.a.logprob) {
+    for (int a = threadIdx.x; a < count; a += blockDim.x) {
+      const float x = load_score<T>(k, row, (int64_t)(list[a] >> 32));
+      k.a.logprob[row * k.a.per_row + (uint32_t)list[a]] = logprob_of(x, st, r);
+    }
+  }
+  if (count > kPairs) __syncthreads();  // the list is sorted in place
+  T *grad = static_cast<T *>(k.a.grad) + row * k.a.grad_ld;
+  each_entry(list, count, weight, [&](int64_t t, float sum) {
+    const float x = load_score<T>(k, row, t);
+    if (x != ninf())
+      grad[t] = narrow<T>(weight_of(x, st.m, r * kLog2e) * scale + sum * r);
+  });
+}
+
+// ---- rows in registers -----------------------------------------------------------
+
+// VECS vectors of 16 bytes a thread, as they came (64 registers a lane in all:
+// eight waves on a SIMD).  hold() keeps the compiler from carrying a pass's
+// float32 values over to the next one.
+template <typename T, int VECS, bool GRAD>
+__global__ __launch_bounds__(1024, 8) void row_kernel(Rows k) {
+  using V = typename Vec<T>::type;
+  typedef uint32_t Raw __attribute__((ext_vector_type(4)));
+  constexpr int kLen = Vec<T>::kLen;
+  Raw raw[VECS];
+  auto get = [&](int g) { return __builtin_bit_cast(V, raw[g]); };
+  auto hold = [&] {
+#pragma unroll
+    for (int g = 0; g < VECS; ++g) asm volatile("" : "+v"(raw[g]));
+  };
+  __shared__ float red[16];
+  __shared__ int waves_at[16];
+  extern __shared__ unsigned long long list[];
+  const int64_t row = blockIdx.x;
+  const int n = (int)k.a.s.n;
+  const T *scores = row_scores<T>(k, row);
+  const uint8_t *valid = row_mask(k, row);
+  const int threads = blockDim.x;
+  bool greedy;
+  const float r = inverse_temperature(k.a.s.temperature, row, &greedy), c = r * kLog2e;
+
+  // the targets first: nothing else is held in registers yet
+  const int32_t *targets = k.a.targets + row * k.a.per_row;
+  int count = 0;
+  float w = 0.0f;
+  if constexpr (GRAD) {
+    count = list_targets(targets, k.a.per_row, 0, n, list, waves_at);
+    w = listed_weight<T>(k, row, k.a.weight + row * k.a.per_row, list, count, red);
+    if (k.a.logprob && count < k.a.per_row) outside(k, row);
+    __syncthreads();
+  }
+
+  float m = ninf();
+#pragma unroll
+  for (int g = 0; g < VECS; ++g) {
+    const int i = (g * threads + (int)threadIdx.x) * kLen;
+    V v;
+    if (i + kLen <= n) {
+      v = *reinterpret_cast<const V *>(scores + i);
+    } else {
+#pragma unroll
+      for (int j = 0; j < kLen; ++j) v[j] = i + j < n ? scores[i + j] : (T)ninf();
+    }
+    raw[g] = __builtin_bit_cast(Raw, v);
+  }
+  if (valid) {
+#pragma unroll
+    for (int g = 0; g < VECS; ++g) {
+      const int i = (g * threads + (int)threadIdx.x) * kLen;
+      V v = get(g);
+#pragma unroll
+      for (int j = 0; j < kLen; ++j)
+        if (i + j < n && valid[i + j] == 0) v[j] = (T)ninf();
+      raw[g] = __builtin_bit_cast(Raw, v);
+    }
+  }
+#pragma unroll
+  for (int g = 0; g < VECS; ++g) {
+    const V v = get(g);
+#pragma unroll
+    for (int j = 0; j < kLen; ++j) m = fmaxf(m, (float)v[j]);  // a NaN never is the larger
+  }
+  hold();
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) m = fmaxf(m, __shfl_xor(m, d));
+  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = m;
+  __syncthreads();
+  for (int w = 0; w < threads >> 6; ++w) m = fmaxf(m, red[w]);
+
+  // exp2(s * c - b) with b = m * c rounded: one fused operation an entry.
+  // What b is off by is put right in l.  NaN scores, infinite maxima and
+  // temperatures that overflow c leave a sum that no row of finite scores has
+  // (the best entry alone counts 1): such a row is summed again, entry by entry.
+  const float b = m * c;
+  float l = 0.0f;
+#pragma unroll
+  for (int g = 0; g < VECS; ++g) {
+    const V v = get(g);
+#pragma unroll
+    for (int j = 0; j < kLen; ++j)
+      l += __builtin_amdgcn_exp2f(__builtin_fmaf((float)v[j], c, -b));
+  }
+  hold();
+  l = block_sum(l, red);
+  const bool plain = l >= 0.5f && l < __builtin_inff();
+  if (plain) {
+    l *= __builtin_amdgcn_exp2f(-__builtin_fmaf(m, c, -b));
+  } else {
+    l = 0.0f;
+#pragma unroll 1
+    for (int i = threadIdx.x; i < n; i += threads) {
+      const float x = load_score<T>(k, row, i);
+      if (x != ninf()) l += weight_of(x, m, c);
+    }
+    l = block_sum(l, red);
+  }
+  const Stat st = {m, l};
+  if constexpr (!GRAD) {
+    for (int j = threadIdx.x; j < k.a.per_row; j += threads) {
+      const int64_t t = targets[j];
+      k.a.logprob[row * k.a.per_row + j] =
+          t < 0 || t >= n ? 0.0f : logprob_of(load_score<T>(k, row, t), st, r);
+    }
+    return;
+  }
+  const float scale = -w / l * r;
+  T *grad = static_cast<T *>(k.a.grad) + row * k.a.grad_ld;
+  if (plain) {
+    const float fit = scale * __builtin_amdgcn_exp2f(-__builtin_fmaf(m, c, -b));
+#pragma unroll
+    for (int g = 0; g < VECS; ++g) {
+      const int i = (g * threads + (int)threadIdx.x) * kLen;
+      const V v = get(g);
+      V o;
+#pragma unroll
+      for (int j = 0; j < kLen; ++j)
+        o[j] = narrow<T>(__builtin_amdgcn_exp2f(__builtin_fmaf((float)v[j], c, -b)) * fit);
+      if (i + kLen <= n) {
+        *reinterpret_cast<V *>(grad + i) = o;
+      } else {
+#pragma unroll
+        for (int j = 0; j < kLen; ++j)
+          if (i + j < n) grad[i + j] = o[j];
+      }
+    }
+  } else {
+#pragma unroll 1
+    for (int i = threadIdx.x; i < n; i += threads) {
+      const float x = load_score<T>(k, row, i);
+      grad[i] = narrow<T>(x == ninf() ? 0.0f : weight_of(x, m, c) * scale);
+    }
+  }
+  __syncthreads();
+  at_targets<T>(k, row, list, count, st, r, scale);
+}
+
+// ---- rows in chunks ----------------------------------------------------------------
+
+template <typename T, bool GRAD>
 __global__ __launch_bounds__(kThreads) void stats_kernel(Rows k) {
   __shared__ Stat lds[kThreads / 64];
+  __shared__ float red[kThreads / 64];
+  __shared__ int waves_at[kThreads / 64];
+  extern __shared__ unsigned long long list[];
   const int64_t row = blockIdx.x / k.chunks, chunk = blockIdx.x % k.chunks;
   const int64_t lo = chunk * k.chunk, hi = min(k.a.s.n, lo + k.chunk);
+  const T *scores = row_scores<T>(k, row);
+  const uint8_t *valid = row_mask(k, row);
   bool greedy;
   const float c = inverse_temperature(k.a.s.temperature, row, &greedy) * kLog2e;
-  Stat s = {-__builtin_inff(), 0.0f};
-  for (int64_t i = lo + threadIdx.x; i < hi; i += kThreads) {
-    const float x = load_score<T>(k, row, i);
-    if (x == -__builtin_inff()) continue;
-    if (x > s.m) {
-      s.l = s.m == -__builtin_inff() ? 0.0f : s.l * weight_of(s.m, x, c);
-      s.m = x;
-    }
-    s.l += weight_of(x, s.m, c);
+  Stat s = {ninf(), 0.0f};
+  for (int64_t i = lo + threadIdx.x * 8; i < hi; i += kThreads * 8) {
+    float x[8];
+    load8(scores, valid, i, hi, x);
+    float m = s.m;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) m = fmaxf(m, x[j]);
+    if (m == ninf()) continue;
+    float l = s.m == ninf() ? 0.0f : s.l * weight_of(s.m, m, c);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) l += x[j] == ninf() ? 0.0f : weight_of(x[j], m, c);
+    s = {m, l};
   }
   s = block_join(s, c, lds);
-  if (threadIdx.x == 0) k.part[blockIdx.x] = s;
+  float w = 0.0f;
+  if constexpr (GRAD) {
+    const int count = list_targets(k.a.targets + row * k.a.per_row, k.a.per_row, lo, hi, list,
+                                   waves_at);
+    w = listed_weight<T>(k, row, k.a.weight + row * k.a.per_row, list, count, red);
+  }
+  if (threadIdx.x == 0) k.part[blockIdx.x] = {s, w};
 }
 
-// The row's maximum and sum, in every thread.
-__device__ __forceinline__ Stat row_stat(const Rows &k, int64_t row, float c, Stat *lds) {
-  Stat s = {-__builtin_inff(), 0.0f};
-  for (int64_t i = threadIdx.x; i < k.chunks; i += blockDim.x)
-    s = join(s, k.part[row * k.chunks + i], c);
-  return block_join(s, c, lds);
-}
-
-template <typename T>
-__device__ __forceinline__ float target_logprob(const Rows &k, int64_t row, int64_t t, Stat st,
-                                                float r) {
-  if (t < 0 || t >= k.a.s.n) return 0.0f;
-  const float x = load_score<T>(k, row, t);
-  if (x == -__builtin_inff()) return x;
-  return (x == st.m ? 0.0f : (x - st.m) * r) - logf(st.l);
+// The row's maximum, sum and weights, in every thread.
+__device__ __forceinline__ Part row_part(const Rows &k, int64_t row, float c, Stat *lds,
+                                         float *red) {
+  Part p = {{ninf(), 0.0f}, 0.0f};
+  for (int64_t i = threadIdx.x; i < k.chunks; i += blockDim.x) {
+    const Part o = k.part[row * k.chunks + i];
+    p.s = join(p.s, o.s, c);
+    p.w += o.w;
+  }
+  p.s = block_join(p.s, c, lds);
+  p.w = block_sum(p.w, red);
+  return p;
 }
 
 template <typename T>
 __global__ __launch_bounds__(kThreads) void finish_kernel(Rows k) {
   __shared__ Stat lds[kThreads / 64];
+  __shared__ float red[kThreads / 64];
   const int64_t row = blockIdx.x;
   bool greedy;
   const float r = inverse_temperature(k.a.s.temperature, row, &greedy);
-  const Stat st = row_stat(k, row, r * kLog2e, lds);
+  const Part p = row_part(k, row, r * kLog2e, lds, red);
   for (int j = threadIdx.x; j < k.a.per_row; j += kThreads) {
-    const int64_t at = row * k.a.per_row + j;
-    k.a.logprob[at] = target_logprob<T>(k, row, k.a.targets[at], st, r);
+    const int64_t t = k.a.targets[row * k.a.per_row + j];
+    k.a.logprob[row * k.a.per_row + j] =
+        t < 0 || t >= k.a.s.n ? 0.0f : logprob_of(load_score<T>(k, row, t), p.s, r);
   }
 }
 
 template <typename T>
 __global__ __launch_bounds__(kThreads) void grad_kernel(Rows k) {
+  typedef T V __attribute__((ext_vector_type(8), aligned(sizeof(T))));
   __shared__ Stat lds[kThreads / 64];
-  __shared__ float wsum[kThreads];
+  __shared__ float red[kThreads / 64];
+  __shared__ int waves_at[kThreads / 64];
+  extern __shared__ unsigned long long list[];
   const int64_t row = blockIdx.x / k.chunks, chunk = blockIdx.x % k.chunks;
   const int64_t lo = chunk * k.chunk, hi = min(k.a.s.n, lo + k.chunk);
+  const T *scores = row_scores<T>(k, row);
+  const uint8_t *valid = row_mask(k, row);
   bool greedy;
   const float r = inverse_temperature(k.a.s.temperature, row, &greedy), c = r * kLog2e;
-  const Stat st = row_stat(k, row, c, lds);
-  // The row's weights, summed in an order that every workgroup shares.
   const int32_t *targets = k.a.targets + row * k.a.per_row;
-  const float *weight = k.a.weight + row * k.a.per_row;
-  float w = 0.0f;
-  for (int j = threadIdx.x; j < k.a.per_row; j += kThreads) {
-    const float lp = target_logprob<T>(k, row, targets[j], st, r);
-    if (chunk == 0 && k.a.logprob) k.a.logprob[row * k.a.per_row + j] = lp;
-    const int64_t t = targets[j];
-    if (t >= 0 && t < k.a.s.n && load_score<T>(k, row, t) != -__builtin_inff()) w += weight[j];
-  }
-  wsum[threadIdx.x] = w;
-  __syncthreads();
-  for (int d = kThreads / 2; d > 0; d >>= 1) {
-    if ((int)threadIdx.x < d) wsum[threadIdx.x] += wsum[threadIdx.x + d];
-    __syncthreads();
-  }
-  const float scale = -wsum[0] / st.l;
+  const Part p = row_part(k, row, c, lds, red);
+  if (chunk == 0 && k.a.logprob) outside(k, row);
+  const float scale = -p.w / p.s.l * r;
   T *grad = static_cast<T *>(k.a.grad) + row * k.a.grad_ld;
-  for (int64_t i = lo + threadIdx.x; i < hi; i += kThreads) {
-    const float x = load_score<T>(k, row, i);
-    grad[i] = narrow<T>(x == -__builtin_inff() ? 0.0f : weight_of(x, st.m, c) * scale * r);
+  for (int64_t i = lo + threadIdx.x * 8; i < hi; i += kThreads * 8) {
+    float x[8];
+    load8(scores, valid, i, hi, x);
+    V o;
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      o[j] = narrow<T>(x[j] == ninf() ? 0.0f : weight_of(x[j], p.s.m, c) * scale);
+    if (i + 8 <= hi) {
+      *reinterpret_cast<V *>(grad + i) = o;
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        if (i + j < hi) grad[i + j] = o[j];
+    }
   }
-  __syncthreads();
-  // The targets of this chunk: the first of those that name an entry adds up
-  // the weights of all of them.
-  for (int j = threadIdx.x; j < k.a.per_row; j += kThreads) {
-    const int64_t t = targets[j];
-    if (t < lo || t >= hi) continue;
-    const float x = load_score<T>(k, row, t);
-    if (x == -__builtin_inff()) continue;
-    bool first = true;
-    for (int q = 0; q < j && first; ++q) first = targets[q] != t;
-    if (!first) continue;
-    float sum = weight[j];
-    for (int q = j + 1; q < k.a.per_row; ++q)
-      if (targets[q] == t) sum += weight[q];
-    grad[t] = narrow<T>((weight_of(x, st.m, c) * scale + sum) * r);
-  }
+  const int count = list_targets(targets, k.a.per_row, lo, hi, list, waves_at);
+  at_targets<T>(k, row, list, count, p.s, r, scale);
 }
 
-// Chunks of a row: enough workgroups for the device where rows are few, none
-// of them over fewer than 4,096 entries.
+// ---- plans -------------------------------------------------------------------
+
+// Chunks of a row: about four workgroups a CU where rows are few, none of them
+// over fewer than kChunk entries.
 void cut(int64_t n, int64_t rows, int cu_count, int64_t *chunk, int64_t *chunks) {
   const int64_t want = std::max<int64_t>(1, (int64_t)cu_count * 4 / std::max<int64_t>(1, rows));
-  const int64_t most = std::max<int64_t>(1, (n + 4095) / 4096);
+  const int64_t most = std::max<int64_t>(1, (n + kChunk - 1) / kChunk);
   const int64_t c = std::min(want, most);
   *chunk = std::max<int64_t>(1, ((n + c - 1) / c + 63) / 64 * 64);
   *chunks = std::max<int64_t>(1, (n + *chunk - 1) / *chunk);
+}
+
+// LDS of a list of targets: its own length, or the power of two it is sorted in.
+size_t list_bytes(int32_t per_row) {
+  size_t size = (size_t)per_row;
+  if (per_row > kPairs)
+    for (size = 256; size < (size_t)per_row;) size <<= 1;
+  return size * sizeof(unsigned long long);
+}
+
+template <typename T, int VECS>
+hipError_t launch_row(const Rows &k, hipStream_t s) {
+  const int64_t vecs = (k.a.s.n + Vec<T>::kLen - 1) / Vec<T>::kLen;
+  const int threads = (int)std::max<int64_t>(64, ((vecs + VECS - 1) / VECS + 63) / 64 * 64);
+  if (!k.a.grad) {
+    row_kernel<T, VECS, false><<<(uint32_t)k.a.s.rows, threads, 0, s>>>(k);
+    return hipGetLastError();
+  }
+  const size_t lds = list_bytes(k.a.per_row);
+  const hipError_t e =
+      ensure_dynamic_lds(reinterpret_cast<const void *>(row_kernel<T, VECS, true>), lds);
+  if (e != hipSuccess) return e;
+  row_kernel<T, VECS, true><<<(uint32_t)k.a.s.rows, threads, lds, s>>>(k);
+  return hipGetLastError();
 }
 
 template <typename T>
 hipError_t launch(const LogprobArgs &a, void *ws, int cu_count, hipStream_t s) {
   Rows k{};
   k.a = a;
-  k.part = static_cast<Stat *>(ws);
+  // A row in one workgroup's registers, unless its length would keep few
+  // workgroups busy for long.
+  const int64_t vecs = (a.s.n + Vec<T>::kLen - 1) / Vec<T>::kLen;
+  if (vecs <= 8 * 1024 && (vecs <= 1024 || a.s.rows * 4 >= cu_count)) {
+    if (vecs <= 1024) return launch_row<T, 1>(k, s);
+    if (vecs <= 2 * 1024) return launch_row<T, 2>(k, s);
+    if (vecs <= 4 * 1024) return launch_row<T, 4>(k, s);
+    return launch_row<T, 8>(k, s);
+  }
+  k.part = static_cast<Part *>(ws);
   cut(a.s.n, a.s.rows, cu_count, &k.chunk, &k.chunks);
   const uint32_t grid = (uint32_t)(a.s.rows * k.chunks);
-  stats_kernel<T><<<grid, kThreads, 0, s>>>(k);
-  if (a.grad)
-    grad_kernel<T><<<grid, kThreads, 0, s>>>(k);
-  else
+  if (!a.grad) {
+    stats_kernel<T, false><<<grid, kThreads, 0, s>>>(k);
     finish_kernel<T><<<(uint32_t)a.s.rows, kThreads, 0, s>>>(k);
+    return hipGetLastError();
+  }
+  const size_t lds = list_bytes(a.per_row);
+  hipError_t e = ensure_dynamic_lds(reinterpret_cast<const void *>(stats_kernel<T, true>), lds);
+  if (e == hipSuccess) e = ensure_dynamic_lds(reinterpret_cast<const void *>(grad_kernel<T>), lds);
+  if (e != hipSuccess) return e;
+  stats_kernel<T, true><<<grid, kThreads, lds, s>>>(k);
+  grad_kernel<T><<<grid, kThreads, lds, s>>>(k);
   return hipGetLastError();
 }
 
@@ -197,10 +539,10 @@ hipError_t launch(const LogprobArgs &a, void *ws, int cu_count, hipStream_t s) {
 
 size_t logprob_workspace_bytes(int64_t n, int64_t rows, int32_t per_row) {
   (void)per_row;
+  (void)n;
   // chunks: at most 4 workgroups a CU (of at most 1,024 CUs), or one a row
   const int64_t chunks = std::max<int64_t>(1, 4096 / std::max<int64_t>(1, rows));
-  (void)n;
-  return std::max<size_t>(256, (size_t)rows * chunks * sizeof(Stat));
+  return std::max<size_t>(256, (size_t)rows * chunks * sizeof(Part));
 }
 
 hipError_t launch_logprob(int dtype, const LogprobArgs &a, void *ws, int cu_count, hipStream_t s) {

@@ -228,25 +228,6 @@ __device__ __forceinline__ u64 find_cut(Search &s, bool by_count, Amount above, 
   return s.lo;
 }
 
-// Eight consecutive entries i .. i+7 of a row of n: -inf where not included.
-template <typename T>
-__device__ __forceinline__ void load8(const T *scores, const uint8_t *valid, int64_t i, int64_t n,
-                                      float (&x)[8]) {
-  typedef T V __attribute__((ext_vector_type(8), aligned(sizeof(T))));
-  typedef u64 Mask __attribute__((aligned(1)));
-  if (i + 8 <= n) {
-    const V v = *reinterpret_cast<const V *>(scores + i);
-    const u64 mask = valid ? *reinterpret_cast<const Mask *>(valid + i) : ~0ull;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) x[j] = included((float)v[j], ((mask >> (8 * j)) & 0xFF) != 0);
-  } else {
-#pragma unroll
-    for (int j = 0; j < 8; ++j)
-      x[j] = i + j < n ? included((float)scores[i + j], !valid || valid[i + j] != 0)
-                       : -__builtin_inff();
-  }
-}
-
 // floor(u * total), kept inside [0, total).
 __device__ __forceinline__ u64 wanted(float u, u64 total) {
   const double at = floor((double)u * (double)total);
