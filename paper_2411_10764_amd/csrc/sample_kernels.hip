@@ -18,8 +18,10 @@
 // scores and weights in LDS.  Longer rows are cut into chunks:
 //   range_kernel    a chunk's best and worst score (and clears the counts)
 //   count_kernel    counts and weights by bin, in LDS, then added up
+//   settle_kernel   a workgroup a row: the bins that hold the cuts, and the
+//                   scores at their ends
 //   collect_kernel  lists the entries whose place the bins do not settle, and
-//                   weighs the others by tile of the row
+//                   weighs those kept for sure by tile of the row
 //   finish_kernel   a workgroup a row: the cuts from the list, the tiles'
 //                   running weights, and few draws
 //   draw_kernel     many draws: a wave a draw
@@ -114,47 +116,60 @@ __device__ __forceinline__ u64 share_of(float p, u64 total) {
   return share >= 1.0 ? (u64)share : 1ull;
 }
 
-struct Amount {
-  u64 count, mass;
-};
+// v of the lane that the DPP control names, `none` where there is none.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ uint32_t lane_move(uint32_t v, uint32_t none) {
+  return (uint32_t)__builtin_amdgcn_update_dpp((int)none, (int)v, CTRL, ROWS, 0xF, false);
+}
 
-// A wave looks through BINS bins (a multiple of 64), best first, for the one
-// in which the running amount reaches `need`: count where by_count, else mass.
-// *before: the amounts of better bins, on top of `base`.  The last bin where
-// `need` is never reached.
-template <int BINS>
-__device__ __forceinline__ int find_bin(const uint32_t *count, const u64 *mass, bool by_count,
-                                        u64 need, Amount base, Amount *before) {
-  constexpr int kPer = BINS / 64;
+template <int CTRL, int ROWS>
+__device__ __forceinline__ u64 lane_move(u64 v, u64 none) {
+  return ((u64)lane_move<CTRL, ROWS>((uint32_t)(v >> 32), (uint32_t)(none >> 32)) << 32) |
+         lane_move<CTRL, ROWS>((uint32_t)v, (uint32_t)none);
+}
+
+// Folds v over the lanes up to and including the own one (DPP moves: shifts
+// inside rows of 16 lanes, then the rows' last lanes; an LDS shuffle a step
+// takes several times as long).  `none`: the neutral value.
+template <typename V, typename F>
+__device__ __forceinline__ V wave_fold(V v, V none, F f) {
+  v = f(v, lane_move<0x111, 0xF>(v, none));
+  v = f(v, lane_move<0x112, 0xF>(v, none));
+  v = f(v, lane_move<0x114, 0xF>(v, none));
+  v = f(v, lane_move<0x118, 0xF>(v, none));
+  v = f(v, lane_move<0x142, 0xA>(v, none));
+  return f(v, lane_move<0x143, 0xC>(v, none));
+}
+
+template <typename V>
+__device__ __forceinline__ V wave_prefix(V v) {  // inclusive
+  return wave_fold(v, (V)0, [](V a, V b) { return a + b; });
+}
+
+__device__ __forceinline__ u64 from_lane(u64 v, int lane) {
+  return ((u64)(uint32_t)__builtin_amdgcn_readlane((int)(v >> 32), lane) << 32) |
+         (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)v, lane);
+}
+
+__device__ __forceinline__ uint32_t from_lane(uint32_t v, int lane) {
+  return (uint32_t)__builtin_amdgcn_readlane((int)v, lane);
+}
+
+// Exclusive sum over the threads of a workgroup of at most 16 waves; *all: the
+// whole sum.  Ends without a barrier: `lds` may be written after the next one.
+__device__ __forceinline__ u64 block_prefix(u64 v, u64 *lds, u64 *all) {
   const int lane = threadIdx.x & 63;
-  Amount sum = {0, 0};
-  for (int j = 0; j < kPer; ++j) {
-    sum.count += count[lane * kPer + j];
-    sum.mass += mass[lane * kPer + j];
-  }
-  Amount incl = sum;
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const u64 c = __shfl_up(incl.count, d), q = __shfl_up(incl.mass, d);
-    if (lane >= d) incl.count += c, incl.mass += q;
-  }
-  Amount run = {base.count + incl.count - sum.count, base.mass + incl.mass - sum.mass};
-  const u64 reached = by_count ? base.count + incl.count : base.mass + incl.mass;
-  const u64 ballot = __ballot(reached >= need);
-  const int at = ballot ? __ffsll(ballot) - 1 : 63;
-  int bin = BINS - 1;
-  if (lane == at) {
-    for (int j = 0; j < kPer; ++j) {
-      const Amount next = {run.count + count[lane * kPer + j], run.mass + mass[lane * kPer + j]};
-      bin = lane * kPer + j;
-      if ((by_count ? next.count : next.mass) >= need || j == kPer - 1) break;
-      run = next;
-    }
-  }
-  bin = __shfl(bin, at);
-  before->count = __shfl(run.count, at);
-  before->mass = __shfl(run.mass, at);
-  return bin;
+  const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+  const u64 incl = wave_prefix(v);
+  if (lane == 63) lds[wave] = incl;
+  __syncthreads();
+  u64 w = lane < (int)(blockDim.x >> 6) ? lds[lane] : 0;
+  w += lane_move<0x111, 0xF>(w, 0);
+  w += lane_move<0x112, 0xF>(w, 0);
+  w += lane_move<0x114, 0xF>(w, 0);
+  w += lane_move<0x118, 0xF>(w, 0);
+  *all = from_lane(w, 15);
+  return incl - v + (wave > 0 ? from_lane(w, wave - 1) : 0);
 }
 
 // State of a search for a cut, in LDS.
@@ -162,39 +177,63 @@ struct Search {
   uint32_t count[kSub];
   u64 mass[kSub];
   u64 lo, hi;    // interval of keys that holds the cut
-  u64 need;
-  Amount above;  // amounts better than the interval
-  int bin, done;
+  int done;
+  u64 wave_sum[16];
+  int bin;       // of block_find: the bin found, or -1
+  u64 above;     // the amount of better ones
 };
 
+// Looks through `bins` bins, best first, for the one in which the running sum
+// of amount(b) on top of `base` reaches `need`.  s.bin and s.above say which
+// and what lies above it; the result is the sum of all, with base.  Every
+// thread of the workgroup calls it, after a barrier that completes the bins;
+// it ends with one.
+template <typename F>
+__device__ __forceinline__ u64 block_find(Search &s, int bins, u64 need, u64 base, F amount) {
+  const int per = (bins + blockDim.x - 1) / blockDim.x;
+  const int b0 = min(bins, (int)threadIdx.x * per), b1 = min(bins, b0 + per);
+  u64 sum = 0;
+  for (int b = b0; b < b1; ++b) sum += amount(b);
+  if (threadIdx.x == 0) s.bin = -1;
+  u64 all;
+  u64 run = base + block_prefix(sum, s.wave_sum, &all);
+  if (run < need && run + sum >= need) {  // one thread at most
+    for (int b = b0; b < b1; ++b) {
+      const u64 next = run + amount(b);
+      if (next >= need) {
+        s.bin = b;
+        s.above = run;
+        break;
+      }
+      run = next;
+    }
+  }
+  __syncthreads();
+  return base + all;
+}
+
 // The cut among the keys that each(f) hands to f(key, weight), in which the
-// amount on top of `above` reaches `need`: entries with key >= the result are
-// kept.  The result is at least the smallest of those keys and may lie between
-// two of them.  Every thread of the workgroup calls it, with the same `above`
-// and `need`; each() hands out one key at least.
+// count (by_count) or weight on top of `above` reaches `need`: entries with
+// key >= the result are kept.  The result is at least the smallest of those
+// keys and may lie between two of them.  Every thread of the workgroup calls
+// it, with the same `above` and `need`; each() hands out one key at least.
 template <typename Each>
-__device__ __forceinline__ u64 find_cut(Search &s, bool by_count, Amount above, u64 need,
+__device__ __forceinline__ u64 find_cut(Search &s, bool by_count, u64 above, u64 need,
                                         Each each) {
   u64 first = ~0ull, last = 0;
   each([&](u64 key, uint32_t) {
     first = min(first, key);
     last = max(last, key);
   });
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    first = min(first, (u64)__shfl_xor(first, d));
-    last = max(last, (u64)__shfl_xor(last, d));
-  }
-  __syncthreads();
+  first = wave_fold(first, ~0ull, [](u64 a, u64 b) { return min(a, b); });
+  last = wave_fold(last, 0ull, [](u64 a, u64 b) { return max(a, b); });
   if (threadIdx.x == 0) {
     s.lo = ~0ull;
     s.hi = 0;
-    s.need = need;
-    s.above = above;
     s.done = 0;
   }
   __syncthreads();
-  if ((threadIdx.x & 63) == 0 && last) atomicMin(&s.lo, first), atomicMax(&s.hi, last);
+  if ((threadIdx.x & 63) == 63 && last) atomicMin(&s.lo, first), atomicMax(&s.hi, last);
   for (;;) {
     for (int b = threadIdx.x; b < kSub; b += blockDim.x) s.count[b] = 0, s.mass[b] = 0;
     __syncthreads();
@@ -206,22 +245,19 @@ __device__ __forceinline__ u64 find_cut(Search &s, bool by_count, Amount above, 
       if (key < lo || key > hi) return;
       const int b = kSub - 1 - (int)((key - lo) >> shift);  // best first
       atomicAdd(&s.count[b], 1u);
-      atomicAdd(&s.mass[b], (u64)q);
+      if (!by_count) atomicAdd(&s.mass[b], (u64)q);
     });
     __syncthreads();
-    if (threadIdx.x < 64) {
-      Amount before;
-      const int b = find_bin<kSub>(s.count, s.mass, by_count, s.need, s.above, &before);
-      if (threadIdx.x == 0) {
-        const u64 part = (u64)(kSub - 1 - b);
-        const Amount with = {before.count + s.count[b], before.mass + s.mass[b]};
-        s.lo = lo + (part << shift);
-        s.hi = min(hi, s.lo + ((1ull << shift) - 1));
-        // one entry, or all of the part is kept
-        s.done = shift == 0 || s.count[b] <= 1 ||
-                 (by_count ? with.count : with.mass) == s.need;
-        s.above = before;
-      }
+    block_find(s, kSub, need, above, [&](int b) { return by_count ? (u64)s.count[b] : s.mass[b]; });
+    const int b = s.bin < 0 ? kSub - 1 : s.bin;  // the amount is always reached
+    above = s.above;
+    if (threadIdx.x == 0) {
+      const u64 part = lo + ((u64)(kSub - 1 - b) << shift);
+      s.lo = part;
+      s.hi = min(hi, part + ((1ull << shift) - 1));
+      // one entry, or all of the part is kept
+      s.done = shift == 0 || s.count[b] <= 1 ||
+               above + (by_count ? (u64)s.count[b] : s.mass[b]) == need;
     }
     __syncthreads();
   }
@@ -242,16 +278,6 @@ __device__ __forceinline__ void no_entry(const SampleArgs &a, int64_t row) {
 }
 
 __device__ __forceinline__ float log_total(u64 total) { return logf((float)total / kOne); }
-
-__device__ __forceinline__ u64 wave_prefix(u64 v) {  // inclusive
-  const int lane = threadIdx.x & 63;
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const u64 o = __shfl_up(v, d);
-    if (lane >= d) v += o;
-  }
-  return v;
-}
 
 // Best and worst over the workgroup, in every thread.
 __device__ __forceinline__ float2 block_range(float hi, float lo, float2 *lds) {
@@ -287,7 +313,7 @@ __global__ __launch_bounds__(1024) void row_kernel(SampleArgs a) {
   uint32_t *qs = reinterpret_cast<uint32_t *>(xs + groups * 8);
   const T *scores = static_cast<const T *>(a.s.scores) + row * a.s.ld;
   const uint8_t *valid = a.s.valid ? a.s.valid + row * a.s.valid_ld : nullptr;
-  const int threads = blockDim.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int threads = blockDim.x;
   const float ninf = -__builtin_inff();
 
   float hi = ninf, lo = __builtin_inff();
@@ -319,30 +345,17 @@ __global__ __launch_bounds__(1024) void row_kernel(SampleArgs a) {
         const uint32_t q = qs[e];
         if (q == 0 || key_of(xs[e], e) < cut) continue;
         const int b = bin_of<kSub>(exponent(xs[e], l), scale);
-        atomicAdd(&s.count[b], 1u);
-        atomicAdd(&s.mass[b], (u64)q);
+        if (by_count) atomicAdd(&s.count[b], 1u);
+        else atomicAdd(&s.mass[b], (u64)q);
       }
       __syncthreads();
-      if (wave == 0) {
-        u64 want = (u64)l.k;
-        if (!by_count) {
-          Amount all;
-          find_bin<kSub>(s.count, s.mass, true, ~0ull, Amount{0, 0}, &all);
-          want = share_of(l.p, all.mass + s.mass[kSub - 1]);
-        }
-        Amount before;
-        const int b = find_bin<kSub>(s.count, s.mass, by_count, want, Amount{0, 0}, &before);
-        if (lane == 0) {
-          s.bin = (by_count ? before.count + s.count[b] : before.mass + s.mass[b]) < want ? -1 : b;
-          s.above = before;
-          s.need = want;
-        }
-      }
-      __syncthreads();
+      auto amount = [&](int b) { return by_count ? (u64)s.count[b] : s.mass[b]; };
+      const u64 want = by_count ? (u64)l.k : share_of(l.p, block_find(s, kSub, ~0ull, 0, amount));
+      block_find(s, kSub, want, 0, amount);
       const int bin = s.bin;
-      const Amount above = s.above;
-      const u64 want = s.need, from = cut;
+      const u64 above = s.above, from = cut;
       if (bin < 0) return;  // fewer entries than top-k keeps
+      __syncthreads();
       cut = find_cut(s, by_count, above, want, [&](auto f) {
 #pragma unroll 1
         for (int e = threadIdx.x; e < n; e += threads) {
@@ -370,14 +383,8 @@ __global__ __launch_bounds__(1024) void row_kernel(SampleArgs a) {
   const int g0 = min(groups, (int)threadIdx.x * per), g1 = min(groups, g0 + per);
   u64 sum = 0;
   for (int e = g0 * 8; e < g1 * 8; ++e) sum += kept(e);
-  const u64 incl = wave_prefix(sum);
-  if (lane == 63) wave_sum[wave] = incl;
-  __syncthreads();
-  u64 run = incl - sum, total = 0;
-  for (int w = 0; w < threads >> 6; ++w) {
-    if (w < wave) run += wave_sum[w];
-    total += wave_sum[w];
-  }
+  u64 total;
+  u64 run = block_prefix(sum, wave_sum, &total);
   for (int g = g0; g < g1; ++g) {
     for (int j = 0; j < 8; ++j) run += kept(g * 8 + j);
     group_end[g] = run;
@@ -405,9 +412,23 @@ __global__ __launch_bounds__(1024) void row_kernel(SampleArgs a) {
 
 // ---- long rows -------------------------------------------------------------------
 
-struct RowState {  // of one row, for draw_kernel
+// What the bins settle: entries of bins better than `sure` are kept, those of
+// bins [sure, last] and of bin `k_bin` are listed, the others dropped.
+struct Bins {
+  int k_bin;       // holds top-k's cut (kBins: none)
+  u64 k_above, k_mass;  // better bins' count and weight
+  u64 all;         // all bins' weight
+  int sure, last;
+};
+
+// A row as settle_kernel leaves it, the same as scores: x_keep: kept for sure;
+// x_sure, x_last, x_k, x_k_end: the least of bins < sure, <= last, <= k_bin,
+// < k_bin (NaN: no score).
+struct RowState {
   RowLimits l;
-  u64 cut, total;
+  Bins b;
+  float x_keep, x_sure, x_last, x_k, x_k_end;
+  u64 cut, total;  // of finish_kernel
 };
 
 struct Long {
@@ -516,67 +537,118 @@ __global__ __launch_bounds__(256) void count_kernel(Long k) {
   }
 }
 
-// What the bins settle: entries of bins better than `sure` are kept, those of
-// bins [sure, last] and of bin `k_bin` are listed, the others dropped.
-struct Bins {
-  int k_bin;       // holds top-k's cut (kBins: none)
-  Amount k_above;  // better bins' amounts
-  int sure, last;
-};
+// The least score for which holds(score) is true, given that it is for the
+// row's best score and stays true as scores rise.  Sixteen lanes of a row of
+// lanes look for one score together, each row of lanes for its own.
+template <typename F>
+__device__ __forceinline__ float least_score(const RowLimits &l, F holds) {
+  const int lane = threadIdx.x & 63, row0 = lane & ~15;
+  uint32_t lo = ordered(-__builtin_inff()), hi = ordered(l.m);  // holds(hi)
+  while (__any(lo < hi)) {
+    // 16 probes in [lo, hi): the first that holds and the one before it
+    const uint32_t step = (hi - lo) / 17 + 1, at = lo + step * (uint32_t)(lane & 15);
+    const bool yes = at >= hi || holds(key_score((u64)at << 32));
+    const uint32_t rows = (uint32_t)(__ballot(yes) >> row0) & 0xFFFFu;
+    const int first = rows ? __ffs((int)rows) - 1 : 16;
+    if (lo < hi) {
+      const uint32_t low = first > 0 ? lo + step * (uint32_t)(first - 1) + 1 : lo;
+      if (first < 16) hi = min(hi, lo + step * (uint32_t)first);
+      lo = min(hi, low);
+    }
+  }
+  return key_score((u64)hi << 32);
+}
 
-__device__ __forceinline__ Bins settle(const RowLimits &l, const uint32_t *count, const u64 *mass) {
-  Bins b = {kBins, {0, 0}, kBins, -1};
-  Amount all;
-  find_bin<kBins>(count, mass, true, ~0ull, Amount{0, 0}, &all);
-  all.count += count[kBins - 1];
-  all.mass += mass[kBins - 1];
-  u64 most = all.mass, least = all.mass;  // bounds of the weight that top-k keeps
-  if ((u64)l.k < all.count) {
-    b.k_bin = find_bin<kBins>(count, mass, true, (u64)l.k, Amount{0, 0}, &b.k_above);
-    least = b.k_above.mass;
-    most = least + mass[b.k_bin];
-    b.sure = b.last = b.k_bin;
+// What the bins say of every entry, as scores to compare with: bins fall as
+// scores rise.  A workgroup a row.
+__global__ __launch_bounds__(1024) void settle_kernel(Long k) {
+  __shared__ Search s;
+  __shared__ float2 lds[16];
+  __shared__ uint32_t count[kBins];
+  __shared__ u64 mass[kBins];
+  __shared__ float edges[5];
+  const int64_t r = blockIdx.x;
+  if (k.a.top_k || k.a.top_p || k.a.s.temperature) {
+    for (int j = threadIdx.x; j < kBins; j += 1024) {
+      count[j] = k.count[r * kBins + j];
+      mass[j] = k.mass[r * kBins + j];
+    }
   }
-  if (lists_all(l)) {
-    // no weights yet: all down to the bin (to the last one where k keeps all)
-    if (b.k_bin == kBins) b.last = kBins - 1;
-    b.sure = 0;
-    return b;
+  const RowLimits l = chunk_limits(k, r, lds);  // ends with a barrier
+  if (l.m == -__builtin_inff()) {
+    if (threadIdx.x == 0) k.state[r].l = l;
+    return;
   }
-  if (l.p < 2.0f) {
-    Amount before;
-    const int from = find_bin<kBins>(count, mass, false, share_of(l.p, least), Amount{0, 0}, &before);
-    const int to = find_bin<kBins>(count, mass, false, share_of(l.p, most), Amount{0, 0}, &before);
-    b.sure = min(from, b.sure);
-    b.last = min(to, b.k_bin < kBins ? b.k_bin : kBins - 1);
+  Bins b = {kBins, 0, 0, 0, kBins, -1};
+  if (l.k < k.a.s.n || l.p < 2.0f) {
+    auto counted = [&](int j) { return (u64)count[j]; };
+    auto weighed = [&](int j) { return mass[j]; };
+    const bool weigh = !lists_all(l) && l.p < 2.0f;
+    const u64 entries = block_find(s, kBins, (u64)l.k, 0, counted);
+    if ((u64)l.k < entries) {
+      b.k_bin = s.bin;
+      b.k_above = s.above;
+      b.sure = b.last = b.k_bin;
+    }
+    __syncthreads();
+    if (lists_all(l)) {
+      // no weights yet: all down to the bin (to the last one where k keeps all)
+      if (b.k_bin == kBins) b.last = kBins - 1;
+      b.sure = 0;
+    } else if (weigh) {
+      b.all = block_find(s, kBins, ~0ull, 0, weighed);
+      u64 least = b.all, most = b.all;  // bounds of the weight that top-k keeps
+      if (b.k_bin < kBins) {
+        __syncthreads();
+        b.k_mass = least = block_find(s, b.k_bin, ~0ull, 0, weighed);
+        most = least + mass[b.k_bin];
+      }
+      __syncthreads();
+      block_find(s, kBins, share_of(l.p, least), 0, weighed);
+      b.sure = min(s.bin, b.sure);
+      __syncthreads();
+      block_find(s, kBins, share_of(l.p, most), 0, weighed);
+      b.last = min(s.bin, b.k_bin < kBins ? b.k_bin : kBins - 1);
+    }
   }
-  return b;
+  // the edges: a row of 16 lanes each
+  const float scale = (float)kBins / l.range;
+  const int which = (int)threadIdx.x >> 4;
+  if (threadIdx.x < 128) {
+    const int of = which == 0 ? b.sure - 1 : which == 1 ? b.last
+                 : b.k_bin == kBins ? -1 : which == 2 ? b.k_bin : b.k_bin - 1;
+    float edge;
+    if (threadIdx.x < 64)
+      edge = least_score(l, [&](float x) {
+        const float z = exponent(x, l);
+        return z > kLowest && bin_of<kBins>(z, scale) <= max(of, 0);
+      });
+    else
+      edge = least_score(l, [&](float x) { return exponent(x, l) >= l.min_z; });
+    if (which < 4 && of < 0) edge = __builtin_nanf("");
+    if ((threadIdx.x & 15) == 0 && which < 5) edges[which] = edge;
+  }
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    RowState &st = k.state[r];
+    st.l = l;
+    st.b = b;
+    st.x_sure = edges[0];
+    st.x_last = edges[1];
+    st.x_k = edges[2];
+    st.x_k_end = edges[3];
+    st.x_keep = edges[0] == edges[0] ? fmaxf(edges[0], edges[4]) : edges[0];
+  }
 }
 
 template <typename T>
 __global__ __launch_bounds__(256) void collect_kernel(Long k) {
-  __shared__ float2 lds[4];
-  __shared__ uint32_t count[kBins];
-  __shared__ u64 mass[kBins];
-  __shared__ Bins sh;
   const int64_t r = blockIdx.x / k.chunks, c = blockIdx.x % k.chunks;
-  const RowLimits l = chunk_limits(k, r, lds);
+  const RowState &st = k.state[r];
+  const RowLimits l = st.l;
   if (l.m == -__builtin_inff()) return;
-  Bins b = {kBins, {0, 0}, kBins, -1};
-  if (l.k < k.a.s.n || l.p < 2.0f) {
-    for (int j = threadIdx.x; j < kBins; j += 256) {
-      count[j] = k.count[r * kBins + j];
-      mass[j] = k.mass[r * kBins + j];
-    }
-    __syncthreads();
-    if (threadIdx.x < 64) {
-      const Bins found = settle(l, count, mass);
-      if (threadIdx.x == 0) sh = found;
-    }
-    __syncthreads();
-    b = sh;
-  }
-  const float scale = (float)kBins / l.range;
+  const float x_keep = st.x_keep, x_sure = st.x_sure, x_last = st.x_last, x_k = st.x_k,
+              x_k_end = st.x_k_end;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const T *scores = row_scores<T>(k, r);
   const uint8_t *valid = row_mask(k, r);
@@ -588,37 +660,45 @@ __global__ __launch_bounds__(256) void collect_kernel(Long k) {
     for (int64_t i = t + lane * 8; i < t + k.tile; i += kTile) {
       float x[8];
       load8(scores, valid, i, stop, x);
+      uint32_t wait = 0;
+      bool keep = false;
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        const float z = exponent(x[j], l);
-        const bool in = z > kLowest;
-        const int bin = in ? bin_of<kBins>(z, scale) : kBins;
-        const bool wait = in && ((bin >= b.sure && bin <= b.last) || bin == b.k_bin);
-        if (in && bin < b.sure && z >= l.min_z) sum += weight(z);
-        const u64 ballot = __ballot(wait);
-        if (ballot) {
-          uint32_t at = 0;
-          if (lane == __ffsll(ballot) - 1)
-            at = atomicAdd(&k.listed[r], (uint32_t)__popcll(ballot));
-          at = __shfl(at, __ffsll(ballot) - 1) + (uint32_t)__popcll(ballot & ((1ull << lane) - 1));
-          if (wait && at < k.list_most) list[at] = key_of(x[j], i + j);
+        keep |= x[j] >= x_keep;
+        wait |= ((x[j] >= x_last && !(x[j] >= x_sure)) || (x[j] >= x_k && !(x[j] >= x_k_end)))
+                    ? 1u << j : 0u;
+      }
+      if (__any(keep)) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) sum += x[j] >= x_keep ? weight(exponent(x[j], l)) : 0u;
+      }
+      if (__any(wait)) {
+        const uint32_t own = __popc(wait);
+        const uint32_t incl = wave_prefix(own);
+        uint32_t at = 0;
+        if (lane == 63) at = atomicAdd(&k.listed[r], incl);
+        at = from_lane(at, 63) + incl - own;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          if (!((wait >> j) & 1u)) continue;
+          if (at < k.list_most) list[at] = key_of(x[j], i + j);
+          ++at;
         }
       }
     }
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) sum += __shfl_xor(sum, d);
-    if (lane == 0) k.tile_mass[r * k.tiles + t / k.tile] = sum;
+    sum = wave_prefix(sum);
+    if (lane == 63) k.tile_mass[r * k.tiles + t / k.tile] = sum;
   }
 }
 
 // One draw by one wave: the tile whose running weight passes `want`, then the
 // entry inside it.
 template <typename T>
-__device__ __forceinline__ void draw_one(const Long &k, int64_t r, int j, const RowState &st,
-                                         const u64 *tile_end) {
+__device__ __forceinline__ void draw_one(const Long &k, int64_t r, int j, const RowLimits &l,
+                                         u64 cut, u64 total, const u64 *tile_end) {
   const int lane = threadIdx.x & 63;
   const int64_t at = (k.row0 + r) * k.a.draws + j;
-  const u64 want = wanted(k.a.u[at], st.total);
+  const u64 want = wanted(k.a.u[at], total);
   int first = 0, last = (int)k.tiles - 1;
   while (first < last) {
     const int mid = (first + last) / 2;
@@ -635,8 +715,8 @@ __device__ __forceinline__ void draw_one(const Long &k, int64_t r, int j, const 
     u64 sum = 0;
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      const float z = exponent(x[e], st.l);
-      q[e] = z >= st.l.min_z && key_of(x[e], i + e) >= st.cut ? weight(z) : 0u;
+      const float z = exponent(x[e], l);
+      q[e] = z >= l.min_z && key_of(x[e], i + e) >= cut ? weight(z) : 0u;
       sum += q[e];
     }
     const u64 incl = wave_prefix(sum);
@@ -653,27 +733,24 @@ __device__ __forceinline__ void draw_one(const Long &k, int64_t r, int j, const 
           if (!done && now > want) {
             done = true;
             e = f;
-            z = exponent(x[f], st.l);
+            z = exponent(x[f], l);
           }
         }
         k.a.idx[at] = (int32_t)(i + e);
-        k.a.logprob[at] = z - log_total(st.total);
+        k.a.logprob[at] = z - log_total(total);
       }
       return;
     }
-    run += __shfl(incl, 63);
+    run += from_lane(incl, 63);
   }
 }
 
 struct Finish {
   Search s;
-  float2 range[16];
-  uint32_t count[kBins];
   u64 mass[kBins];
   u64 keys[kList];
   u64 tile[kMaxTiles];
   u64 wave_sum[16];
-  Bins bins;
 };
 
 template <typename T>
@@ -681,12 +758,11 @@ __global__ __launch_bounds__(1024) void finish_kernel(Long k) {
   extern __shared__ char raw[];
   Finish &sh = *reinterpret_cast<Finish *>(raw);
   const int64_t r = blockIdx.x, row = k.row0 + r, n = k.a.s.n;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const RowLimits l = chunk_limits(k, r, sh.range);
-  if (l.m == -__builtin_inff()) {
-    if (threadIdx.x == 0) k.state[r].l = l;
-    return no_entry(k.a, row);
-  }
+  const int wave = threadIdx.x >> 6;
+  const RowState &settled = k.state[r];
+  const RowLimits l = settled.l;
+  if (l.m == -__builtin_inff()) return no_entry(k.a, row);
+  const Bins b = settled.b;
   const float scale = (float)kBins / l.range;
   const T *scores = row_scores<T>(k, r);
   const uint8_t *valid = row_mask(k, r);
@@ -697,17 +773,11 @@ __global__ __launch_bounds__(1024) void finish_kernel(Long k) {
 
   u64 cut = 0;
   if (l.k < n || l.p < 2.0f) {
-    for (int j = threadIdx.x; j < kBins; j += 1024) {
-      sh.count[j] = k.count[r * kBins + j];
-      sh.mass[j] = k.mass[r * kBins + j];
+    const bool everything = lists_all(l);
+    if (!everything && l.p < 2.0f) {
+      for (int j = threadIdx.x; j < kBins; j += 1024) sh.mass[j] = k.mass[r * kBins + j];
     }
     __syncthreads();
-    if (wave == 0) {
-      const Bins found = settle(l, sh.count, sh.mass);
-      if (lane == 0) sh.bins = found;
-    }
-    __syncthreads();
-    const Bins b = sh.bins;
     // f(key, weight, bin) for every listed entry.  A list that did not fit is
     // read from the row again.
     auto each = [&](auto f) {
@@ -740,51 +810,28 @@ __global__ __launch_bounds__(1024) void finish_kernel(Long k) {
     __syncthreads();
     if (l.p < 2.0f) {
       // the weight that top-k keeps: better bins' and the listed entries'
-      const bool everything = lists_all(l);
-      u64 part = 0;
-      each([&](u64 key, uint32_t q, int bin) {
-        if (everything ? key >= cut : (bin == b.k_bin && key >= cut)) part += q;
-      });
-#pragma unroll
-      for (int d = 1; d < 64; d <<= 1) part += __shfl_xor(part, d);
-      if (lane == 0) sh.wave_sum[wave] = part;
-      __syncthreads();
-      u64 total = 0;
-      for (int w = 0; w < 16; ++w) total += sh.wave_sum[w];
-      if (!everything) {
-        if (b.k_bin < kBins) {
-          total += b.k_above.mass;
-        } else {
-          total = 0;
-          if (wave == 0) {
-            Amount all;
-            find_bin<kBins>(sh.count, sh.mass, true, ~0ull, Amount{0, 0}, &all);
-            if (lane == 0) sh.s.need = all.mass + sh.mass[kBins - 1];
-          }
-          __syncthreads();
-          total = sh.s.need;
-        }
+      u64 total = b.all;
+      if (everything || b.k_bin < kBins) {
+        u64 part = 0;
+        each([&](u64 key, uint32_t q, int bin) {
+          if (key >= cut && (everything || bin == b.k_bin)) part += q;
+        });
+        block_prefix(part, sh.wave_sum, &total);
+        total += everything ? 0 : b.k_mass;
+        __syncthreads();
       }
-      __syncthreads();
       const u64 share = share_of(l.p, total);
       if (everything) {
-        cut = find_cut(sh.s, false, Amount{0, 0}, share, [&](auto f) {
+        cut = find_cut(sh.s, false, 0, share, [&](auto f) {
           each([&](u64 key, uint32_t q, int) {
             if (q && key >= cut) f(key, q);
           });
         });
       } else {
-        if (wave == 0) {
-          Amount before;
-          const int bin = find_bin<kBins>(sh.count, sh.mass, false, share, Amount{0, 0}, &before);
-          if (lane == 0) {
-            sh.s.bin = bin;
-            sh.s.above = before;
-          }
-        }
-        __syncthreads();
+        block_find(sh.s, kBins, share, 0, [&](int j) { return sh.mass[j]; });
         const int p_bin = sh.s.bin;
-        const Amount above = sh.s.above;
+        const u64 above = sh.s.above;
+        __syncthreads();
         const u64 from = cut;
         cut = find_cut(sh.s, false, above, share, [&](auto f) {
           each([&](u64 key, uint32_t q, int bin) {
@@ -809,14 +856,8 @@ __global__ __launch_bounds__(1024) void finish_kernel(Long k) {
     own[j] = t < k.tiles ? sh.tile[t] : 0;
     sum += own[j];
   }
-  const u64 incl = wave_prefix(sum);
-  if (lane == 63) sh.wave_sum[wave] = incl;
-  __syncthreads();
-  u64 run = incl - sum, total = 0;
-  for (int w = 0; w < 16; ++w) {
-    if (w < wave) run += sh.wave_sum[w];
-    total += sh.wave_sum[w];
-  }
+  u64 total;
+  u64 run = block_prefix(sum, sh.wave_sum, &total);
 #pragma unroll
   for (int j = 0; j < kMaxTiles / 1024; ++j) {
     const int t = threadIdx.x * (kMaxTiles / 1024) + j;
@@ -824,22 +865,25 @@ __global__ __launch_bounds__(1024) void finish_kernel(Long k) {
     if (t < k.tiles) sh.tile[t] = run;
   }
   __syncthreads();
-  const RowState st = {l, cut, total};
   if (k.a.draws <= kFewDraws) {
-    for (int j = wave; j < k.a.draws; j += 16) draw_one<T>(k, r, j, st, sh.tile);
+    for (int j = wave; j < k.a.draws; j += 16) draw_one<T>(k, r, j, l, cut, total, sh.tile);
     return;
   }
   for (int t = threadIdx.x; t < k.tiles; t += 1024) k.tile_mass[r * k.tiles + t] = sh.tile[t];
-  if (threadIdx.x == 0) k.state[r] = st;
+  if (threadIdx.x == 0) {
+    k.state[r].cut = cut;
+    k.state[r].total = total;
+  }
 }
 
 template <typename T>
 __global__ __launch_bounds__(256) void draw_kernel(Long k, int blocks) {
   const int64_t r = blockIdx.x / blocks;
   const int j = (int)(blockIdx.x % blocks) * 4 + (threadIdx.x >> 6);
-  const RowState st = k.state[r];
-  if (j >= k.a.draws || st.l.m == -__builtin_inff()) return;
-  draw_one<T>(k, r, j, st, k.tile_mass + r * k.tiles);
+  const RowState &st = k.state[r];
+  const RowLimits l = st.l;
+  if (j >= k.a.draws || l.m == -__builtin_inff()) return;
+  draw_one<T>(k, r, j, l, st.cut, st.total, k.tile_mass + r * k.tiles);
 }
 
 // ---- plans -------------------------------------------------------------------
@@ -905,6 +949,7 @@ hipError_t launch_long(const SampleArgs &a, void *ws, int cu_count, hipStream_t 
     const uint32_t grid = (uint32_t)(rows * k.chunks);
     range_kernel<T><<<grid, 256, 0, s>>>(k);
     if (a.top_k || a.top_p || a.s.temperature) count_kernel<T><<<grid, 256, 0, s>>>(k);
+    settle_kernel<<<(uint32_t)rows, 1024, 0, s>>>(k);
     collect_kernel<T><<<grid, 256, 0, s>>>(k);
     finish_kernel<T><<<(uint32_t)rows, 1024, sizeof(Finish), s>>>(k);
     if (a.draws > kFewDraws) {
