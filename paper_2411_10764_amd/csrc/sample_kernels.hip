@@ -39,19 +39,22 @@ constexpr int kSub = 512;           // bins of a short row, parts of an interval
 constexpr int kMaxTiles = 4096;     // tiles of a row
 constexpr int kTile = 512;          // smallest tile: 8 entries a lane
 constexpr int kChunk = 4 * kTile;   // smallest chunk: 4 waves
+constexpr int kSpan = 16 * kTile;   // smallest part of count_kernel: 16 waves
 constexpr int kPacked = 32768;      // entries that a packed LDS bin holds
 constexpr int kFew = 2048;          // k of top-k that lists everything it keeps
 constexpr int kList = 4096;         // list entries held in LDS
+constexpr int kOpen = 1024;         // list entries that collect_kernel gathers before it adds them
 constexpr int kFewDraws = 32;       // draws a row that finish_kernel makes itself
 constexpr int kRowMost = 16384;     // entries of a row in one workgroup's LDS
+constexpr int kRowList = 512;       // open entries of a short row held apart
 constexpr int kBatch = 1024;        // long rows of one set of launches
 constexpr float kLowest = -22.25f;  // exp(z) * 2^31 rounds to 0 below -22.181
 constexpr float kOne = 2147483648.0f;
 
 typedef unsigned long long u64;
 
-__device__ __forceinline__ uint32_t ordered(float x) {  // x is not NaN, not -0.0
-  const uint32_t b = __float_as_uint(x);
+__device__ __forceinline__ uint32_t ordered(float x) {  // x is not NaN
+  const uint32_t b = __float_as_uint(x + 0.0f);  // -0.0 is +0.0
   return (b & 0x80000000u) ? ~b : (b | 0x80000000u);
 }
 
@@ -77,21 +80,30 @@ struct RowLimits {
   float p;          // top_p, or 2 where it keeps all
 };
 
+// A row's own settings, read ahead of its scores.
+struct RowSettings {
+  float temperature, p, min_p;
+  int32_t k;
+};
+
+__device__ __forceinline__ RowSettings row_settings(const SampleArgs &a, int64_t row) {
+  return {a.s.temperature ? a.s.temperature[row] : 1.0f, a.top_p ? a.top_p[row] : 1.0f,
+          a.min_p ? a.min_p[row] : 0.0f, a.top_k ? a.top_k[row] : 0};
+}
+
 // hi, lo: the row's best and worst included scores.
-__device__ __forceinline__ RowLimits row_limits(const SampleArgs &a, int64_t row, float hi,
+__device__ __forceinline__ RowLimits row_limits(const RowSettings &s, int64_t n, float hi,
                                                 float lo) {
   RowLimits l;
-  bool greedy;
+  const bool greedy = !(s.temperature > 0.0f);
   l.m = hi;
-  l.r = inverse_temperature(a.s.temperature, row, &greedy);
+  l.r = greedy ? 1.0f : 1.0f / s.temperature;
   const float low = lo == hi ? 0.0f : (lo - hi) * l.r;
   l.range = fminf(-kLowest, fmaxf(-low, 1e-20f));
-  const int32_t k = greedy ? 1 : a.top_k ? a.top_k[row] : 0;
-  l.k = k > 0 && k < a.s.n ? k : a.s.n;
-  const float p = a.top_p ? a.top_p[row] : 1.0f;
-  l.p = p < 1.0f ? p : 2.0f;
-  const float mp = a.min_p ? a.min_p[row] : 0.0f;
-  l.min_z = mp > 0.0f ? logf(fminf(mp, 1.0f)) : -__builtin_inff();
+  const int32_t k = greedy ? 1 : s.k;
+  l.k = k > 0 && k < n ? k : n;
+  l.p = s.p < 1.0f ? s.p : 2.0f;
+  l.min_z = s.min_p > 0.0f ? logf(fminf(s.min_p, 1.0f)) : -__builtin_inff();
   return l;
 }
 
@@ -99,10 +111,47 @@ __device__ __forceinline__ float exponent(float x, const RowLimits &l) {
   return x == l.m ? 0.0f : (x - l.m) * l.r;
 }
 
-// 0 for an entry that is not included (x = -inf, or z NaN) too.
+// 0 for an entry that is not included (x = -inf or NaN, so z is) too.
 __device__ __forceinline__ uint32_t weight(float z) {
-  return z > kLowest ? (uint32_t)rintf(expf(z) * kOne) : 0u;
+  return (uint32_t)fmaxf(rintf(expf(z) * kOne), 0.0f);
 }
+
+// Eight consecutive entries of a row as they come from memory, so that the
+// next ones can be on their way while these are worked on.
+template <typename T>
+struct Eight {
+  typedef T V __attribute__((ext_vector_type(8), aligned(sizeof(T))));
+  typedef u64 Mask __attribute__((aligned(1)));
+  V v;
+  u64 mask;
+
+  // Entries i .. i+7 of a row that ends at n.
+  __device__ __forceinline__ void load(const T *scores, const uint8_t *valid, int64_t i,
+                                       int64_t n) {
+    if (i + 8 <= n) {
+      v = *reinterpret_cast<const V *>(scores + i);
+      if (valid) mask = *reinterpret_cast<const Mask *>(valid + i);
+    } else {
+      mask = 0;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        v[j] = i + j < n ? scores[i + j] : (T)-__builtin_inff();
+        if (valid && i + j < n) mask |= (u64)valid[i + j] << (8 * j);
+      }
+    }
+  }
+
+  // The scores, -inf where the mask excludes an entry; a NaN stays.
+  __device__ __forceinline__ void get(bool masked, float (&x)[8]) const {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) x[j] = (float)v[j];
+    if (masked) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        if (((mask >> (8 * j)) & 0xFF) == 0) x[j] = -__builtin_inff();
+    }
+  }
+};
 
 // Bin of an entry with z > kLowest, best first; scale = bins / range.
 template <int BINS>
@@ -176,6 +225,7 @@ __device__ __forceinline__ u64 block_prefix(u64 v, u64 *lds, u64 *all) {
 struct Search {
   uint32_t count[kSub];
   u64 mass[kSub];
+  u64 first[kSub], last[kSub];  // smallest and largest key of a part
   u64 lo, hi;    // interval of keys that holds the cut
   int done;
   u64 wave_sum[16];
@@ -184,12 +234,12 @@ struct Search {
 };
 
 // Looks through `bins` bins, best first, for the one in which the running sum
-// of amount(b) on top of `base` reaches `need`.  s.bin and s.above say which
-// and what lies above it; the result is the sum of all, with base.  Every
-// thread of the workgroup calls it, after a barrier that completes the bins;
-// it ends with one.
-template <typename F>
-__device__ __forceinline__ u64 block_find(Search &s, int bins, u64 need, u64 base, F amount) {
+// of amount(b) on top of `base` reaches need(sum of all, with base).  s.bin and
+// s.above say which and what lies above it; the result is the sum of all.
+// Every thread of the workgroup calls it, after a barrier that completes the
+// bins; it ends with one.
+template <typename F, typename N>
+__device__ __forceinline__ u64 block_find(Search &s, int bins, N need_of, u64 base, F amount) {
   const int per = (bins + blockDim.x - 1) / blockDim.x;
   const int b0 = min(bins, (int)threadIdx.x * per), b1 = min(bins, b0 + per);
   u64 sum = 0;
@@ -197,6 +247,7 @@ __device__ __forceinline__ u64 block_find(Search &s, int bins, u64 need, u64 bas
   if (threadIdx.x == 0) s.bin = -1;
   u64 all;
   u64 run = base + block_prefix(sum, s.wave_sum, &all);
+  const u64 need = need_of(base + all);
   if (run < need && run + sum >= need) {  // one thread at most
     for (int b = b0; b < b1; ++b) {
       const u64 next = run + amount(b);
@@ -214,9 +265,8 @@ __device__ __forceinline__ u64 block_find(Search &s, int bins, u64 need, u64 bas
 
 // The cut among the keys that each(f) hands to f(key, weight), in which the
 // count (by_count) or weight on top of `above` reaches `need`: entries with
-// key >= the result are kept.  The result is at least the smallest of those
-// keys and may lie between two of them.  Every thread of the workgroup calls
-// it, with the same `above` and `need`; each() hands out one key at least.
+// key >= the result are kept.  Every thread of the workgroup calls it, with
+// the same `above` and `need`; each() hands out one key at least.
 template <typename Each>
 __device__ __forceinline__ u64 find_cut(Search &s, bool by_count, u64 above, u64 need,
                                         Each each) {
@@ -235,7 +285,12 @@ __device__ __forceinline__ u64 find_cut(Search &s, bool by_count, u64 above, u64
   __syncthreads();
   if ((threadIdx.x & 63) == 63 && last) atomicMin(&s.lo, first), atomicMax(&s.hi, last);
   for (;;) {
-    for (int b = threadIdx.x; b < kSub; b += blockDim.x) s.count[b] = 0, s.mass[b] = 0;
+    for (int b = threadIdx.x; b < kSub; b += blockDim.x) {
+      s.count[b] = 0;
+      s.mass[b] = 0;
+      s.first[b] = ~0ull;
+      s.last[b] = 0;
+    }
     __syncthreads();
     const u64 lo = s.lo, hi = s.hi;
     if (s.done || lo >= hi) break;
@@ -246,22 +301,113 @@ __device__ __forceinline__ u64 find_cut(Search &s, bool by_count, u64 above, u64
       const int b = kSub - 1 - (int)((key - lo) >> shift);  // best first
       atomicAdd(&s.count[b], 1u);
       if (!by_count) atomicAdd(&s.mass[b], (u64)q);
+      atomicMin(&s.first[b], key);
+      atomicMax(&s.last[b], key);
     });
     __syncthreads();
-    block_find(s, kSub, need, above, [&](int b) { return by_count ? (u64)s.count[b] : s.mass[b]; });
+    block_find(s, kSub, [&](u64) { return need; }, above, [&](int b) { return by_count ? (u64)s.count[b] : s.mass[b]; });
     const int b = s.bin < 0 ? kSub - 1 : s.bin;  // the amount is always reached
     above = s.above;
     if (threadIdx.x == 0) {
-      const u64 part = lo + ((u64)(kSub - 1 - b) << shift);
-      s.lo = part;
-      s.hi = min(hi, part + ((1ull << shift) - 1));
+      s.lo = s.first[b];
+      s.hi = s.last[b];
       // one entry, or all of the part is kept
-      s.done = shift == 0 || s.count[b] <= 1 ||
-               above + (by_count ? (u64)s.count[b] : s.mass[b]) == need;
+      s.done = s.count[b] <= 1 || above + (by_count ? (u64)s.count[b] : s.mass[b]) == need;
     }
     __syncthreads();
   }
   return s.lo;
+}
+
+// What the bins settle: entries of bins better than `sure` are kept, those of
+// bins [sure, last] and of bin `k_bin` are listed, the others dropped.
+struct Bins {
+  int k_bin;       // holds top-k's cut (the number of bins: none)
+  u64 k_above, k_mass;  // better bins' count and weight
+  u64 all;         // all bins' weight
+  int sure, last;
+};
+
+__device__ __forceinline__ bool limited(const RowLimits &l, int64_t n) {
+  return l.k < n || l.p < 2.0f;
+}
+
+// counted(b), weighed(b): what lies in a bin.  everything: there are no weights
+// by bin, and all entries down to top-k's bin are listed.
+template <typename C, typename W>
+__device__ __forceinline__ Bins settle(Search &s, const RowLimits &l, int64_t n, int bins,
+                                       bool everything, C counted, W weighed) {
+  Bins b = {bins, 0, 0, 0, bins, -1};
+  if (l.k < n) {
+    const u64 entries = block_find(s, bins, [&](u64) { return (u64)l.k; }, 0, counted);
+    if ((u64)l.k < entries) {
+      b.k_bin = s.bin;
+      b.k_above = s.above;
+      b.sure = b.last = b.k_bin;
+    }
+    __syncthreads();
+  }
+  const auto share = [&](u64 all) { return share_of(l.p, all); };
+  if (everything) {
+    // all down to the bin (to the last one where k keeps all)
+    if (b.k_bin == bins) b.last = bins - 1;
+    b.sure = 0;
+  } else if (l.p < 2.0f) {
+    if (b.k_bin < bins) {
+      // between the weight of better bins and that with the cut's own
+      b.k_mass = block_find(s, b.k_bin, share, 0, weighed);
+      b.sure = min(s.bin < 0 ? 0 : s.bin, b.sure);
+      __syncthreads();
+      block_find(s, b.k_bin + 1, share, 0, weighed);
+    } else {
+      b.all = block_find(s, bins, share, 0, weighed);
+      b.sure = min(s.bin, b.sure);
+    }
+    b.last = min(s.bin, b.k_bin < bins ? b.k_bin : bins - 1);
+    __syncthreads();
+  }
+  return b;
+}
+
+// The cut of both limits.  each(f) calls f(key, weight, bin) for the listed entries.
+template <typename W, typename Each>
+__device__ __forceinline__ u64 find_cuts(Search &s, const RowLimits &l, const Bins &b, int bins,
+                                         bool everything, W weighed, Each each) {
+  u64 cut = 0;
+  if (b.k_bin < bins)
+    cut = find_cut(s, true, b.k_above, (u64)l.k, [&](auto f) {
+      each([&](u64 key, uint32_t q, int bin) {
+        if (bin == b.k_bin) f(key, q);
+      });
+    });
+  if (!(l.p < 2.0f)) return cut;
+  __syncthreads();
+  // the weight that top-k keeps: better bins' and the listed entries'
+  u64 total = b.all;
+  if (everything || b.k_bin < bins) {
+    u64 part = 0;
+    each([&](u64 key, uint32_t q, int bin) {
+      if (key >= cut && (everything || bin == b.k_bin)) part += q;
+    });
+    block_prefix(part, s.wave_sum, &total);
+    total += everything ? 0 : b.k_mass;
+    __syncthreads();
+  }
+  const u64 share = share_of(l.p, total);
+  int p_bin = -1;  // all bins
+  u64 above = 0;
+  if (!everything) {
+    block_find(s, bins, [&](u64) { return share; }, 0, weighed);
+    p_bin = s.bin;
+    above = s.above;
+    __syncthreads();
+  }
+  const u64 from = cut;
+  return find_cut(s, false, above, share, [&](auto f) {
+    each([&](u64 key, uint32_t q, int bin) {
+      if (q && (p_bin < 0 || bin == p_bin) && key >= from) f(key, q);
+    });
+  });
 }
 
 // floor(u * total), kept inside [0, total).
@@ -281,13 +427,19 @@ __device__ __forceinline__ float log_total(u64 total) { return logf((float)total
 
 // Best and worst over the workgroup, in every thread.
 __device__ __forceinline__ float2 block_range(float hi, float lo, float2 *lds) {
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    hi = fmaxf(hi, __shfl_xor(hi, d));
-    lo = fminf(lo, __shfl_xor(lo, d));
-  }
-  if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = make_float2(hi, lo);
+  const auto most = [](uint32_t a, uint32_t b) {
+    return __float_as_uint(fmaxf(__uint_as_float(a), __uint_as_float(b)));
+  };
+  const auto least = [](uint32_t a, uint32_t b) {
+    return __float_as_uint(fminf(__uint_as_float(a), __uint_as_float(b)));
+  };
+  const uint32_t inf = __float_as_uint(__builtin_inff());
+  hi = __uint_as_float(wave_fold(__float_as_uint(hi), inf | 0x80000000u, most));
+  lo = __uint_as_float(wave_fold(__float_as_uint(lo), inf, least));
+  if ((threadIdx.x & 63) == 63) lds[threadIdx.x >> 6] = make_float2(hi, lo);
   __syncthreads();
+  hi = -__builtin_inff();
+  lo = __builtin_inff();
   for (int w = 0; w < (int)blockDim.x >> 6; ++w) {
     hi = fmaxf(hi, lds[w].x);
     lo = fminf(lo, lds[w].y);
@@ -299,100 +451,137 @@ __device__ __forceinline__ float2 block_range(float hi, float lo, float2 *lds) {
 // ---- short rows: one workgroup -------------------------------------------------
 
 // The row's scores and weights in LDS: every entry is read from memory and
-// exponentiated once.
+// exponentiated once.  A thread's own entries are groups of 8.
 template <typename T>
 __global__ __launch_bounds__(1024) void row_kernel(SampleArgs a) {
   __shared__ Search s;
   __shared__ float2 range[16];
-  __shared__ u64 wave_sum[16];
+  __shared__ uint32_t count[kSub], list_q[kRowList], listed;
+  __shared__ u64 mass[kSub], list_key[kRowList];
+  __shared__ uint16_t list_bin[kRowList];
   extern __shared__ char raw[];
   const int64_t row = blockIdx.x;
   const int n = (int)a.s.n, groups = (n + 7) / 8;
-  u64 *group_end = reinterpret_cast<u64 *>(raw);  // running weight after 8 entries
-  float *xs = reinterpret_cast<float *>(group_end + groups);
-  uint32_t *qs = reinterpret_cast<uint32_t *>(xs + groups * 8);
+  float4 *xs = reinterpret_cast<float4 *>(raw);
+  uint4 *qs = reinterpret_cast<uint4 *>(xs + groups * 2);
+  u64 *group_end = reinterpret_cast<u64 *>(qs + groups * 2);  // running weight after 8 entries
   const T *scores = static_cast<const T *>(a.s.scores) + row * a.s.ld;
   const uint8_t *valid = a.s.valid ? a.s.valid + row * a.s.valid_ld : nullptr;
-  const int threads = blockDim.x;
+  const int threads = blockDim.x, t = threadIdx.x;
   const float ninf = -__builtin_inff();
+  const RowSettings set = row_settings(a, row);
+  const float u0 = t < a.draws ? a.u[row * a.draws + t] : 0.0f;
 
+  for (int b = t; b < kSub; b += threads) count[b] = 0, mass[b] = 0;
   float hi = ninf, lo = __builtin_inff();
-  for (int g = threadIdx.x; g < groups; g += threads) {
+  for (int g = t; g < groups; g += threads) {
     float x[8];
     load8(scores, valid, (int64_t)g * 8, n, x);
+    xs[g * 2] = make_float4(x[0], x[1], x[2], x[3]);
+    xs[g * 2 + 1] = make_float4(x[4], x[5], x[6], x[7]);
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      xs[g * 8 + j] = x[j];
       hi = fmaxf(hi, x[j]);
       lo = fminf(lo, x[j] == ninf ? __builtin_inff() : x[j]);
     }
   }
   const float2 ends = block_range(hi, lo, range);
   if (ends.x == ninf) return no_entry(a, row);
-  const RowLimits l = row_limits(a, row, ends.x, ends.y);
-  for (int e = threadIdx.x; e < groups * 8; e += threads) qs[e] = weight(exponent(xs[e], l));
+  const RowLimits l = row_limits(set, n, ends.x, ends.y);
+  const bool limits = limited(l, n);
+  const float scale = (float)kSub / l.range;
+  for (int h = t; h < groups * 2; h += threads) {
+    const float4 x = xs[h];
+    const float xv[4] = {x.x, x.y, x.z, x.w};
+    uint32_t q[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const float z = exponent(xv[j], l);
+      q[j] = weight(z);
+      if (limits && q[j]) {
+        const int b = bin_of<kSub>(z, scale);
+        atomicAdd(&count[b], 1u);
+        atomicAdd(&mass[b], (u64)q[j]);
+      }
+    }
+    qs[h] = make_uint4(q[0], q[1], q[2], q[3]);
+  }
+  __syncthreads();
 
   u64 cut = 0;  // entries with a smaller key are not kept
-  if (l.k < n || l.p < 2.0f) {
-    const float scale = (float)kSub / l.range;
-    // The cut by count or weight among the entries with key >= cut: the bin
-    // that holds it, then find_cut inside that bin.
-    auto search = [&](bool by_count) {
-      for (int b = threadIdx.x; b < kSub; b += threads) s.count[b] = 0, s.mass[b] = 0;
-      __syncthreads();
+  if (limits) {
+    auto weighed = [&](int j) { return mass[j]; };
+    const Bins b = settle(s, l, n, kSub, false, [&](int j) { return (u64)count[j]; }, weighed);
+    // f(index, score, weight, bin) for the entries that the bins do not settle
+    auto each_open = [&](auto f) {
 #pragma unroll 1
-      for (int e = threadIdx.x; e < n; e += threads) {
-        const uint32_t q = qs[e];
-        if (q == 0 || key_of(xs[e], e) < cut) continue;
-        const int b = bin_of<kSub>(exponent(xs[e], l), scale);
-        if (by_count) atomicAdd(&s.count[b], 1u);
-        else atomicAdd(&s.mass[b], (u64)q);
-      }
-      __syncthreads();
-      auto amount = [&](int b) { return by_count ? (u64)s.count[b] : s.mass[b]; };
-      const u64 want = by_count ? (u64)l.k : share_of(l.p, block_find(s, kSub, ~0ull, 0, amount));
-      block_find(s, kSub, want, 0, amount);
-      const int bin = s.bin;
-      const u64 above = s.above, from = cut;
-      if (bin < 0) return;  // fewer entries than top-k keeps
-      __syncthreads();
-      cut = find_cut(s, by_count, above, want, [&](auto f) {
-#pragma unroll 1
-        for (int e = threadIdx.x; e < n; e += threads) {
-          const uint32_t q = qs[e];
-          if (q == 0) continue;
-          const float x = xs[e];
-          const u64 key = key_of(x, e);
-          if (key >= from && bin_of<kSub>(exponent(x, l), scale) == bin) f(key, q);
+      for (int h = t; h < groups * 2; h += threads) {
+        const float4 x = xs[h];
+        const uint4 q = qs[h];
+        const float xv[4] = {x.x, x.y, x.z, x.w};
+        const uint32_t qv[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          if (qv[j] == 0) continue;
+          const int bin = bin_of<kSub>(exponent(xv[j], l), scale);
+          if ((bin >= b.sure && bin <= b.last) || bin == b.k_bin)
+            f(key_of(xv[j], h * 4 + j), qv[j], bin);
         }
-      });
+      }
     };
-    if (l.k < n) search(true);
+    if (t == 0) listed = 0;
     __syncthreads();
-    if (l.p < 2.0f) search(false);
+    each_open([&](u64 key, uint32_t q, int bin) {
+      const uint32_t at = atomicAdd(&listed, 1u);
+      if (at < kRowList) {
+        list_key[at] = key;
+        list_q[at] = q;
+        list_bin[at] = (uint16_t)bin;
+      }
+    });
+    __syncthreads();
+    const int open = (int)listed;
+    cut = find_cuts(s, l, b, kSub, false, weighed, [&](auto f) {
+      if (open > kRowList) return each_open(f);
+#pragma unroll 1
+      for (int e = t; e < open; e += threads) f(list_key[e], list_q[e], (int)list_bin[e]);
+    });
+    __syncthreads();
   }
-  __syncthreads();
 
-  // running weights of the kept, each thread `per` groups in a row
-  auto kept = [&](int e) {
-    const uint32_t q = qs[e];
-    const float x = xs[e];
-    return q != 0 && exponent(x, l) >= l.min_z && key_of(x, e) >= cut ? q : 0u;
-  };
-  const int per = (groups + threads - 1) / threads;
-  const int g0 = min(groups, (int)threadIdx.x * per), g1 = min(groups, g0 + per);
-  u64 sum = 0;
-  for (int e = g0 * 8; e < g1 * 8; ++e) sum += kept(e);
-  u64 total;
-  u64 run = block_prefix(sum, wave_sum, &total);
-  for (int g = g0; g < g1; ++g) {
-    for (int j = 0; j < 8; ++j) run += kept(g * 8 + j);
-    group_end[g] = run;
+  // running weights of the kept entries, a round of `threads` groups at a time
+  u64 total = 0;
+  for (int g0 = 0; g0 < groups; g0 += threads) {
+    const int g = g0 + t;
+    u64 sum = 0;
+    if (g < groups) {
+      uint32_t q[8];
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const float4 x = xs[g * 2 + h];
+        const uint4 w = qs[g * 2 + h];
+        const float xv[4] = {x.x, x.y, x.z, x.w};
+        const uint32_t wv[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          q[h * 4 + j] = exponent(xv[j], l) >= l.min_z && key_of(xv[j], g * 8 + h * 4 + j) >= cut
+                             ? wv[j] : 0u;
+          sum += q[h * 4 + j];
+        }
+      }
+      qs[g * 2] = make_uint4(q[0], q[1], q[2], q[3]);
+      qs[g * 2 + 1] = make_uint4(q[4], q[5], q[6], q[7]);
+    }
+    u64 all;
+    const u64 before = block_prefix(sum, s.wave_sum, &all);
+    if (g < groups) group_end[g] = total + before + sum;
+    total += all;
+    __syncthreads();
   }
-  __syncthreads();
   const float lt = log_total(total);
-  for (int j = threadIdx.x; j < a.draws; j += threads) {
-    const u64 want = wanted(a.u[row * a.draws + j], total);
+  const uint32_t *q1 = reinterpret_cast<const uint32_t *>(qs);
+  for (int j = t; j < a.draws; j += threads) {
+    const u64 want = wanted(j == t ? u0 : a.u[row * a.draws + j], total);
     int first = 0, last = groups - 1;  // the group whose end passes `want`
     while (first < last) {
       const int mid = (first + last) / 2;
@@ -400,26 +589,16 @@ __global__ __launch_bounds__(1024) void row_kernel(SampleArgs a) {
     }
     u64 now = first > 0 ? group_end[first - 1] : 0;
     int e = first * 8;
-    for (;;) {
-      now += kept(e);
-      if (now > want || e == first * 8 + 7) break;
-      ++e;
+    for (; e < first * 8 + 7; ++e) {
+      now += q1[e];
+      if (now > want) break;
     }
     a.idx[row * a.draws + j] = e;
-    a.logprob[row * a.draws + j] = exponent(xs[e], l) - lt;
+    a.logprob[row * a.draws + j] = exponent(reinterpret_cast<const float *>(xs)[e], l) - lt;
   }
 }
 
 // ---- long rows -------------------------------------------------------------------
-
-// What the bins settle: entries of bins better than `sure` are kept, those of
-// bins [sure, last] and of bin `k_bin` are listed, the others dropped.
-struct Bins {
-  int k_bin;       // holds top-k's cut (kBins: none)
-  u64 k_above, k_mass;  // better bins' count and weight
-  u64 all;         // all bins' weight
-  int sure, last;
-};
 
 // A row as settle_kernel leaves it, the same as scores: x_keep: kept for sure;
 // x_sure, x_last, x_k, x_k_end: the least of bins < sure, <= last, <= k_bin,
@@ -435,6 +614,7 @@ struct Long {
   SampleArgs a;
   int64_t row0;              // first row of the batch
   int64_t chunk, chunks;     // entries of a chunk, chunks of a row
+  int64_t span, spans;       // the same of count_kernel's parts
   int64_t tile, tiles;       // the same of tiles; a chunk is a number of tiles
   uint32_t list_most;        // entries of a row's list
   float2 *range;             // [rows][chunks]: best, worst
@@ -456,6 +636,7 @@ __device__ __forceinline__ const uint8_t *row_mask(const Long &k, int64_t r) {
 }
 
 __device__ __forceinline__ RowLimits chunk_limits(const Long &k, int64_t r, float2 *lds) {
+  const RowSettings set = row_settings(k.a, k.row0 + r);
   float hi = -__builtin_inff(), lo = __builtin_inff();
   for (int64_t c = threadIdx.x; c < k.chunks; c += blockDim.x) {
     const float2 v = k.range[r * k.chunks + c];
@@ -463,7 +644,7 @@ __device__ __forceinline__ RowLimits chunk_limits(const Long &k, int64_t r, floa
     lo = fminf(lo, v.y);
   }
   const float2 v = block_range(hi, lo, lds);
-  return row_limits(k.a, k.row0 + r, v.x, v.y);
+  return row_limits(set, k.a.s.n, v.x, v.y);
 }
 
 template <typename T>
@@ -480,13 +661,19 @@ __global__ __launch_bounds__(256) void range_kernel(Long k) {
   const int64_t end = min(k.a.s.n, (c + 1) * k.chunk);
   const float ninf = -__builtin_inff();
   float hi = ninf, lo = __builtin_inff();
-  for (int64_t i = c * k.chunk + threadIdx.x * 8; i < end; i += 256 * 8) {
-    float x[8];
-    load8(scores, valid, i, k.a.s.n, x);
+  for (int64_t i = c * k.chunk + threadIdx.x * 8; i < end; i += 256 * 16) {
+    Eight<T> e[2];
+    e[0].load(scores, valid, i, end);
+    e[1].load(scores, valid, i + 256 * 8, end);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      hi = fmaxf(hi, x[j]);
-      lo = fminf(lo, x[j] == ninf ? __builtin_inff() : x[j]);
+    for (int h = 0; h < 2; ++h) {
+      float x[8];
+      e[h].get(valid != nullptr, x);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        hi = fmaxf(hi, x[j]);  // a NaN is neither
+        lo = fminf(lo, x[j] == ninf ? __builtin_inff() : x[j]);
+      }
     }
   }
   const float2 v = block_range(hi, lo, lds);
@@ -496,41 +683,66 @@ __global__ __launch_bounds__(256) void range_kernel(Long k) {
 // A row whose top-k needs no weights by bin: everything it keeps is listed.
 __device__ __forceinline__ bool lists_all(const RowLimits &l) { return l.k <= kFew; }
 
-template <typename T>
-__global__ __launch_bounds__(256) void count_kernel(Long k) {
-  __shared__ float2 lds[4];
-  __shared__ u64 bins[kBins];  // (weight << 17) | count: up to kPacked entries
-  const int64_t r = blockIdx.x / k.chunks, c = blockIdx.x % k.chunks;
-  const RowLimits l = chunk_limits(k, r, lds);
-  if (l.m == -__builtin_inff() || (l.k >= k.a.s.n && l.p >= 2.0f)) return;
-  const bool weigh = !lists_all(l);
+// A row whose entries need no care: z is (s - m) * R as it stands.
+__device__ __forceinline__ bool ordinary(const RowLimits &l) {
+  return l.m < __builtin_inff() && l.r < __builtin_inff();
+}
+
+// Entries base .. stop-1 into the bins.
+template <typename T, bool WEIGH, bool ORDINARY>
+__device__ __forceinline__ void count_entries(const T *scores, const uint8_t *valid, int64_t base,
+                                              int64_t stop, const RowLimits &l, u64 *bins) {
   const float scale = (float)kBins / l.range;
-  const T *scores = row_scores<T>(k, r);
-  const uint8_t *valid = row_mask(k, r);
-  const int64_t end = min(k.a.s.n, (c + 1) * k.chunk);
-  for (int64_t base = c * k.chunk; base < end; base += kPacked) {
-    for (int b = threadIdx.x; b < kBins; b += 256) bins[b] = 0;
-    __syncthreads();
-    const int64_t stop = min(end, base + kPacked);
-    for (int64_t i = base + threadIdx.x * 8; i < stop; i += 256 * 8) {
-      float x[8];
-      load8(scores, valid, i, k.a.s.n, x);
+  int64_t i = base + threadIdx.x * 8;
+  Eight<T> next;
+  next.load(scores, valid, i, stop);
+  for (; i < stop; i += 1024 * 8) {
+    const Eight<T> now = next;
+    next.load(scores, valid, i + 1024 * 8, stop);
+    float x[8];
+    now.get(valid != nullptr, x);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const float z = exponent(x[j], l);
-        if (weigh) {
-          const uint32_t q = weight(z);
-          if (q) atomicAdd(&bins[bin_of<kBins>(z, scale)], ((u64)q << 17) | 1ull);
-        } else if (z > kLowest) {
-          atomicAdd(reinterpret_cast<uint32_t *>(&bins[bin_of<kBins>(z, scale)]), 1u);
-        }
+    for (int j = 0; j < 8; ++j) {
+      const float z = ORDINARY ? (x[j] - l.m) * l.r : exponent(x[j], l);
+      if constexpr (WEIGH) {
+        const uint32_t q = weight(z);
+        if (q) atomicAdd(&bins[bin_of<kBins>(z, scale)], ((u64)q << 17) | 1ull);
+      } else if (z > kLowest) {
+        atomicAdd(reinterpret_cast<uint32_t *>(&bins[bin_of<kBins>(z, scale)]), 1u);
       }
     }
+  }
+}
+
+// Adding a part's bins to the row's costs as much as some ten thousand
+// entries, so the parts are as long as still fill the device: sixteen waves
+// share the bins.  Counts serve top-k alone, weights top-p alone.
+template <typename T>
+__global__ __launch_bounds__(1024) void count_kernel(Long k) {
+  __shared__ float2 lds[16];
+  __shared__ u64 bins[kBins];  // (weight << 17) | count: up to kPacked entries
+  const int64_t r = blockIdx.x / k.spans, c = blockIdx.x % k.spans;
+  for (int b = threadIdx.x; b < kBins; b += 1024) bins[b] = 0;
+  const RowLimits l = chunk_limits(k, r, lds);
+  if (l.m == -__builtin_inff() || !limited(l, k.a.s.n)) return;
+  const bool weigh = !lists_all(l) && l.p < 2.0f, counts = l.k < k.a.s.n;
+  const T *scores = row_scores<T>(k, r);
+  const uint8_t *valid = row_mask(k, r);
+  const int64_t end = min(k.a.s.n, (c + 1) * k.span);
+  for (int64_t base = c * k.span; base < end; base += kPacked) {
+    const int64_t stop = min(end, base + kPacked);
+    if (!ordinary(l))
+      weigh ? count_entries<T, true, false>(scores, valid, base, stop, l, bins)
+            : count_entries<T, false, false>(scores, valid, base, stop, l, bins);
+    else
+      weigh ? count_entries<T, true, true>(scores, valid, base, stop, l, bins)
+            : count_entries<T, false, true>(scores, valid, base, stop, l, bins);
     __syncthreads();
-    for (int b = threadIdx.x; b < kBins; b += 256) {
+    for (int b = threadIdx.x; b < kBins; b += 1024) {
       const u64 v = bins[b];
       if (!v) continue;
-      atomicAdd(&k.count[r * kBins + b], (uint32_t)(v & 0x1FFFF));
+      bins[b] = 0;
+      if (counts) atomicAdd(&k.count[r * kBins + b], (uint32_t)(v & 0x1FFFF));
       if (weigh) atomicAdd(&k.mass[r * kBins + b], v >> 17);
     }
     __syncthreads();
@@ -580,37 +792,9 @@ __global__ __launch_bounds__(1024) void settle_kernel(Long k) {
     return;
   }
   Bins b = {kBins, 0, 0, 0, kBins, -1};
-  if (l.k < k.a.s.n || l.p < 2.0f) {
-    auto counted = [&](int j) { return (u64)count[j]; };
-    auto weighed = [&](int j) { return mass[j]; };
-    const bool weigh = !lists_all(l) && l.p < 2.0f;
-    const u64 entries = block_find(s, kBins, (u64)l.k, 0, counted);
-    if ((u64)l.k < entries) {
-      b.k_bin = s.bin;
-      b.k_above = s.above;
-      b.sure = b.last = b.k_bin;
-    }
-    __syncthreads();
-    if (lists_all(l)) {
-      // no weights yet: all down to the bin (to the last one where k keeps all)
-      if (b.k_bin == kBins) b.last = kBins - 1;
-      b.sure = 0;
-    } else if (weigh) {
-      b.all = block_find(s, kBins, ~0ull, 0, weighed);
-      u64 least = b.all, most = b.all;  // bounds of the weight that top-k keeps
-      if (b.k_bin < kBins) {
-        __syncthreads();
-        b.k_mass = least = block_find(s, b.k_bin, ~0ull, 0, weighed);
-        most = least + mass[b.k_bin];
-      }
-      __syncthreads();
-      block_find(s, kBins, share_of(l.p, least), 0, weighed);
-      b.sure = min(s.bin, b.sure);
-      __syncthreads();
-      block_find(s, kBins, share_of(l.p, most), 0, weighed);
-      b.last = min(s.bin, b.k_bin < kBins ? b.k_bin : kBins - 1);
-    }
-  }
+  if (limited(l, k.a.s.n))
+    b = settle(s, l, k.a.s.n, kBins, lists_all(l), [&](int j) { return (u64)count[j]; },
+               [&](int j) { return mass[j]; });
   // the edges: a row of 16 lanes each
   const float scale = (float)kBins / l.range;
   const int which = (int)threadIdx.x >> 4;
@@ -641,8 +825,17 @@ __global__ __launch_bounds__(1024) void settle_kernel(Long k) {
   }
 }
 
+// Where few of the entries are kept for sure, their scores go through a queue
+// in LDS, so that the exponentials run on full waves.  Listed entries are
+// gathered in LDS: an addition to the row's counter takes a microsecond, and
+// those of one row wait for one another.
 template <typename T>
 __global__ __launch_bounds__(256) void collect_kernel(Long k) {
+  __shared__ float queues[4][kTile / 2 + 64];
+  __shared__ u64 open[kOpen];
+  __shared__ uint32_t opened, open_at;
+  if (threadIdx.x == 0) opened = 0;
+  __syncthreads();
   const int64_t r = blockIdx.x / k.chunks, c = blockIdx.x % k.chunks;
   const RowState &st = k.state[r];
   const RowLimits l = st.l;
@@ -654,51 +847,92 @@ __global__ __launch_bounds__(256) void collect_kernel(Long k) {
   const uint8_t *valid = row_mask(k, r);
   u64 *list = k.list + (size_t)r * k.list_most;
   const int64_t end = min(k.a.s.n, (c + 1) * k.chunk);
+  const bool plain = ordinary(l);
+  float *queue = queues[wave];
+  int queued = 0;
   for (int64_t t = c * k.chunk + wave * k.tile; t < end; t += 4 * k.tile) {
     u64 sum = 0;
     const int64_t stop = min(end, t + k.tile);
+    Eight<T> next;
+    next.load(scores, valid, t + lane * 8, stop);
     for (int64_t i = t + lane * 8; i < t + k.tile; i += kTile) {
+      const Eight<T> now = next;
+      next.load(scores, valid, i + kTile, stop);
       float x[8];
-      load8(scores, valid, i, stop, x);
-      uint32_t wait = 0;
-      bool keep = false;
+      now.get(valid != nullptr, x);
+      u64 keep[8];
+      bool waits = false;
+      int kept = 0;
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        keep |= x[j] >= x_keep;
-        wait |= ((x[j] >= x_last && !(x[j] >= x_sure)) || (x[j] >= x_k && !(x[j] >= x_k_end)))
-                    ? 1u << j : 0u;
+        keep[j] = __ballot(x[j] >= x_keep);
+        kept += __popcll(keep[j]);
+        waits |= (x[j] >= x_last && !(x[j] >= x_sure)) || (x[j] >= x_k && !(x[j] >= x_k_end));
       }
-      if (__any(keep)) {
+      if (kept > kTile / 2) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) sum += x[j] >= x_keep ? weight(exponent(x[j], l)) : 0u;
+        for (int j = 0; j < 8; ++j)
+          sum += x[j] >= x_keep ? weight(plain ? (x[j] - l.m) * l.r : exponent(x[j], l)) : 0u;
+      } else if (kept) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          if (x[j] >= x_keep)
+            queue[queued + __builtin_amdgcn_mbcnt_hi((uint32_t)(keep[j] >> 32),
+                                                     __builtin_amdgcn_mbcnt_lo((uint32_t)keep[j], 0))] =
+                x[j];
+          queued += __popcll(keep[j]);
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        while (queued >= 64) {
+          queued -= 64;
+          sum += weight(exponent(queue[queued + lane], l));
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
       }
-      if (__any(wait)) {
-        const uint32_t own = __popc(wait);
-        const uint32_t incl = wave_prefix(own);
-        uint32_t at = 0;
-        if (lane == 63) at = atomicAdd(&k.listed[r], incl);
-        at = from_lane(at, 63) + incl - own;
+      if (__any(waits)) {
+        uint32_t wait = 0;
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+          wait |= ((x[j] >= x_last && !(x[j] >= x_sure)) || (x[j] >= x_k && !(x[j] >= x_k_end)))
+                      ? 1u << j : 0u;
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
           if (!((wait >> j) & 1u)) continue;
-          if (at < k.list_most) list[at] = key_of(x[j], i + j);
-          ++at;
+          const u64 key = key_of(x[j], i + j);
+          const uint32_t at = atomicAdd(&opened, 1u);
+          if (at < kOpen) {
+            open[at] = key;
+          } else {
+            const uint32_t to = atomicAdd(&k.listed[r], 1u);
+            if (to < k.list_most) list[to] = key;
+          }
         }
       }
     }
+    if (lane < queued) sum += weight(exponent(queue[lane], l));
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    queued = 0;
     sum = wave_prefix(sum);
     if (lane == 63) k.tile_mass[r * k.tiles + t / k.tile] = sum;
   }
+  __syncthreads();
+  const uint32_t count = min(opened, (uint32_t)kOpen);
+  if (count == 0) return;
+  if (threadIdx.x == 0) open_at = atomicAdd(&k.listed[r], count);
+  __syncthreads();
+  for (uint32_t e = threadIdx.x; e < count; e += 256)
+    if (open_at + e < k.list_most) list[open_at + e] = open[e];
 }
 
 // One draw by one wave: the tile whose running weight passes `want`, then the
 // entry inside it.
 template <typename T>
-__device__ __forceinline__ void draw_one(const Long &k, int64_t r, int j, const RowLimits &l,
-                                         u64 cut, u64 total, const u64 *tile_end) {
+__device__ __forceinline__ void draw_one(const Long &k, int64_t r, int j, float u,
+                                         const RowLimits &l, u64 cut, u64 total,
+                                         const u64 *tile_end) {
   const int lane = threadIdx.x & 63;
   const int64_t at = (k.row0 + r) * k.a.draws + j;
-  const u64 want = wanted(k.a.u[at], total);
+  const u64 want = wanted(u, total);
   int first = 0, last = (int)k.tiles - 1;
   while (first < last) {
     const int mid = (first + last) / 2;
@@ -749,6 +983,7 @@ struct Finish {
   Search s;
   u64 mass[kBins];
   u64 keys[kList];
+  uint32_t q[kList];
   u64 tile[kMaxTiles];
   u64 wave_sum[16];
 };
@@ -760,19 +995,22 @@ __global__ __launch_bounds__(1024) void finish_kernel(Long k) {
   const int64_t r = blockIdx.x, row = k.row0 + r, n = k.a.s.n;
   const int wave = threadIdx.x >> 6;
   const RowState &settled = k.state[r];
-  const RowLimits l = settled.l;
-  if (l.m == -__builtin_inff()) return no_entry(k.a, row);
-  const Bins b = settled.b;
-  const float scale = (float)kBins / l.range;
   const T *scores = row_scores<T>(k, r);
   const uint8_t *valid = row_mask(k, r);
   const u64 *list = k.list + (size_t)r * k.list_most;
   const uint32_t listed = k.listed[r];
+  const float u0 = wave < k.a.draws ? k.a.u[row * k.a.draws + wave] : 0.0f;
   for (int t = threadIdx.x; t < k.tiles; t += 1024) sh.tile[t] = k.tile_mass[r * k.tiles + t];
   for (uint32_t e = threadIdx.x; e < min(listed, (uint32_t)kList); e += 1024) sh.keys[e] = list[e];
+  const RowLimits l = settled.l;
+  if (l.m == -__builtin_inff()) return no_entry(k.a, row);
+  const Bins b = settled.b;
+  const float scale = (float)kBins / l.range;
+  for (uint32_t e = threadIdx.x; e < min(listed, (uint32_t)kList); e += 1024)
+    sh.q[e] = weight(exponent(key_score(sh.keys[e]), l));
 
   u64 cut = 0;
-  if (l.k < n || l.p < 2.0f) {
+  if (limited(l, n)) {
     const bool everything = lists_all(l);
     if (!everything && l.p < 2.0f) {
       for (int j = threadIdx.x; j < kBins; j += 1024) sh.mass[j] = k.mass[r * kBins + j];
@@ -788,10 +1026,14 @@ __global__ __launch_bounds__(1024) void finish_kernel(Long k) {
         if ((bin >= b.sure && bin <= b.last) || bin == b.k_bin) f(key_of(x, i), weight(z), bin);
       };
       if (listed <= k.list_most) {
-        for (uint32_t e = threadIdx.x; e < listed; e += 1024) {
-          const u64 key = e < kList ? sh.keys[e] : list[e];
-          one(key_score(key), key_index(key));
+#pragma unroll 1
+        for (uint32_t e = threadIdx.x; e < min(listed, (uint32_t)kList); e += 1024) {
+          const u64 key = sh.keys[e];
+          f(key, sh.q[e], bin_of<kBins>(exponent(key_score(key), l), scale));
         }
+#pragma unroll 1
+        for (uint32_t e = kList + threadIdx.x; e < listed; e += 1024)
+          one(key_score(list[e]), key_index(list[e]));
       } else {
         for (int64_t i = (int64_t)threadIdx.x * 8; i < n; i += 8192) {
           float x[8];
@@ -801,45 +1043,7 @@ __global__ __launch_bounds__(1024) void finish_kernel(Long k) {
         }
       }
     };
-    if (b.k_bin < kBins)
-      cut = find_cut(sh.s, true, b.k_above, (u64)l.k, [&](auto f) {
-        each([&](u64 key, uint32_t q, int bin) {
-          if (bin == b.k_bin) f(key, q);
-        });
-      });
-    __syncthreads();
-    if (l.p < 2.0f) {
-      // the weight that top-k keeps: better bins' and the listed entries'
-      u64 total = b.all;
-      if (everything || b.k_bin < kBins) {
-        u64 part = 0;
-        each([&](u64 key, uint32_t q, int bin) {
-          if (key >= cut && (everything || bin == b.k_bin)) part += q;
-        });
-        block_prefix(part, sh.wave_sum, &total);
-        total += everything ? 0 : b.k_mass;
-        __syncthreads();
-      }
-      const u64 share = share_of(l.p, total);
-      if (everything) {
-        cut = find_cut(sh.s, false, 0, share, [&](auto f) {
-          each([&](u64 key, uint32_t q, int) {
-            if (q && key >= cut) f(key, q);
-          });
-        });
-      } else {
-        block_find(sh.s, kBins, share, 0, [&](int j) { return sh.mass[j]; });
-        const int p_bin = sh.s.bin;
-        const u64 above = sh.s.above;
-        __syncthreads();
-        const u64 from = cut;
-        cut = find_cut(sh.s, false, above, share, [&](auto f) {
-          each([&](u64 key, uint32_t q, int bin) {
-            if (q && bin == p_bin && key >= from) f(key, q);
-          });
-        });
-      }
-    }
+    cut = find_cuts(sh.s, l, b, kBins, everything, [&](int j) { return sh.mass[j]; }, each);
     __syncthreads();
     // the listed entries that are kept join their tiles
     each([&](u64 key, uint32_t q, int bin) {
@@ -866,7 +1070,8 @@ __global__ __launch_bounds__(1024) void finish_kernel(Long k) {
   }
   __syncthreads();
   if (k.a.draws <= kFewDraws) {
-    for (int j = wave; j < k.a.draws; j += 16) draw_one<T>(k, r, j, l, cut, total, sh.tile);
+    for (int j = wave; j < k.a.draws; j += 16)
+      draw_one<T>(k, r, j, j == wave ? u0 : k.a.u[row * k.a.draws + j], l, cut, total, sh.tile);
     return;
   }
   for (int t = threadIdx.x; t < k.tiles; t += 1024) k.tile_mass[r * k.tiles + t] = sh.tile[t];
@@ -883,7 +1088,8 @@ __global__ __launch_bounds__(256) void draw_kernel(Long k, int blocks) {
   const RowState &st = k.state[r];
   const RowLimits l = st.l;
   if (j >= k.a.draws || l.m == -__builtin_inff()) return;
-  draw_one<T>(k, r, j, l, st.cut, st.total, k.tile_mass + r * k.tiles);
+  draw_one<T>(k, r, j, k.a.u[(k.row0 + r) * k.a.draws + j], l, st.cut, st.total,
+              k.tile_mass + r * k.tiles);
 }
 
 // ---- plans -------------------------------------------------------------------
@@ -940,15 +1146,20 @@ hipError_t launch_long(const SampleArgs &a, void *ws, int cu_count, hipStream_t 
   if (e != hipSuccess) return e;
   for (k.row0 = 0; k.row0 < a.s.rows; k.row0 += p.batch) {
     const int64_t rows = std::min(p.batch, a.s.rows - k.row0);
-    // about four workgroups a CU, none over less than kChunk entries; chunks
+    // about eight workgroups a CU, none over less than kChunk entries; chunks
     // are whole tiles, a wave's at a time
-    const int64_t want = std::min(p.most_chunks, std::max<int64_t>(1, (int64_t)cu_count * 4 / rows));
+    const int64_t want = std::min(p.most_chunks, std::max<int64_t>(1, (int64_t)cu_count * 8 / rows));
     const int64_t unit = std::max<int64_t>(kChunk, p.tile);
     k.chunk = std::max<int64_t>(1, (a.s.n + want * unit - 1) / (want * unit)) * unit;
     k.chunks = (a.s.n + k.chunk - 1) / k.chunk;
+    // the bins' parts: two workgroups a CU, of sixteen waves
+    const int64_t parts = std::max<int64_t>(1, (int64_t)cu_count * 2 / rows);
+    k.span = std::max<int64_t>(1, (a.s.n + parts * kSpan - 1) / (parts * kSpan)) * kSpan;
+    k.spans = (a.s.n + k.span - 1) / k.span;
     const uint32_t grid = (uint32_t)(rows * k.chunks);
     range_kernel<T><<<grid, 256, 0, s>>>(k);
-    if (a.top_k || a.top_p || a.s.temperature) count_kernel<T><<<grid, 256, 0, s>>>(k);
+    if (a.top_k || a.top_p || a.s.temperature) 
+      count_kernel<T><<<(uint32_t)(rows * k.spans), 1024, 0, s>>>(k);
     settle_kernel<<<(uint32_t)rows, 1024, 0, s>>>(k);
     collect_kernel<T><<<grid, 256, 0, s>>>(k);
     finish_kernel<T><<<(uint32_t)rows, 1024, sizeof(Finish), s>>>(k);
@@ -965,8 +1176,8 @@ hipError_t launch_long(const SampleArgs &a, void *ws, int cu_count, hipStream_t 
 template <typename T>
 hipError_t launch_row(const SampleArgs &a, hipStream_t s) {
   const int groups = (int)((a.s.n + 7) / 8);
-  const int threads = std::min(1024, std::max(64, (groups * 2 + 63) / 64 * 64));
-  const size_t lds = (size_t)groups * (8 + 8 * 8);
+  const int threads = std::min(1024, std::max(64, (groups + 63) / 64 * 64));
+  const size_t lds = (size_t)groups * (8 * 8 + 8);
   const hipError_t e = ensure_dynamic_lds(reinterpret_cast<const void *>(row_kernel<T>), lds);
   if (e != hipSuccess) return e;
   row_kernel<T><<<(uint32_t)a.s.rows, threads, lds, s>>>(a);
