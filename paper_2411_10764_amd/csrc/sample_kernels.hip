@@ -43,6 +43,7 @@ constexpr int kSpan = 16 * kTile;   // smallest part of count_kernel: 16 waves
 constexpr int kPacked = 32768;      // entries that a packed LDS bin holds
 constexpr int kFew = 2048;          // k of top-k that lists everything it keeps
 constexpr int kList = 4096;         // list entries held in LDS
+constexpr int kSegments = 32;       // of a row's list, at most
 constexpr int kOpen = 1024;         // list entries that collect_kernel gathers before it adds them
 constexpr int kFewDraws = 32;       // draws a row that finish_kernel makes itself
 constexpr int kRowMost = 16384;     // entries of a row in one workgroup's LDS
@@ -601,8 +602,8 @@ __global__ __launch_bounds__(1024) void row_kernel(SampleArgs a) {
 // ---- long rows -------------------------------------------------------------------
 
 // A row as settle_kernel leaves it, the same as scores: x_keep: kept for sure;
-// x_sure, x_last, x_k, x_k_end: the least of bins < sure, <= last, <= k_bin,
-// < k_bin (NaN: no score).
+// x_sure, x_last: the least of bins < sure, <= last; x_k, x_k_end: of bins
+// <= k_bin, < k_bin where that lies apart (NaN: no score).
 struct RowState {
   RowLimits l;
   Bins b;
@@ -616,13 +617,13 @@ struct Long {
   int64_t chunk, chunks;     // entries of a chunk, chunks of a row
   int64_t span, spans;       // the same of count_kernel's parts
   int64_t tile, tiles;       // the same of tiles; a chunk is a number of tiles
-  uint32_t list_most;        // entries of a row's list
+  uint32_t segments, segment_most;  // of a row's list: parts with a counter each
   float2 *range;             // [rows][chunks]: best, worst
   u64 *mass;                 // [rows][kBins]
   uint32_t *count;           // [rows][kBins]
   u64 *tile_mass;            // [rows][tiles], running sums after finish_kernel
-  u64 *list;                 // [rows][list_most] keys
-  uint32_t *listed;          // [rows]
+  u64 *list;                 // [rows][segments][segment_most] keys
+  uint32_t *listed;          // [rows][kSegments]
   RowState *state;           // [rows]
 };
 
@@ -655,7 +656,7 @@ __global__ __launch_bounds__(256) void range_kernel(Long k) {
     k.mass[r * kBins + b] = 0;
     k.count[r * kBins + b] = 0;
   }
-  if (c == 0 && threadIdx.x == 0) k.listed[r] = 0;
+  if (c == 0 && threadIdx.x < kSegments) k.listed[r * kSegments + threadIdx.x] = 0;
   const T *scores = row_scores<T>(k, r);
   const uint8_t *valid = row_mask(k, r);
   const int64_t end = min(k.a.s.n, (c + 1) * k.chunk);
@@ -798,9 +799,10 @@ __global__ __launch_bounds__(1024) void settle_kernel(Long k) {
   // the edges: a row of 16 lanes each
   const float scale = (float)kBins / l.range;
   const int which = (int)threadIdx.x >> 4;
+  const bool apart = b.k_bin < kBins && (b.k_bin < b.sure || b.k_bin > b.last);
   if (threadIdx.x < 128) {
     const int of = which == 0 ? b.sure - 1 : which == 1 ? b.last
-                 : b.k_bin == kBins ? -1 : which == 2 ? b.k_bin : b.k_bin - 1;
+                 : !apart ? -1 : which == 2 ? b.k_bin : b.k_bin - 1;
     float edge;
     if (threadIdx.x < 64)
       edge = least_score(l, [&](float x) {
@@ -827,8 +829,8 @@ __global__ __launch_bounds__(1024) void settle_kernel(Long k) {
 
 // Where few of the entries are kept for sure, their scores go through a queue
 // in LDS, so that the exponentials run on full waves.  Listed entries are
-// gathered in LDS: an addition to the row's counter takes a microsecond, and
-// those of one row wait for one another.
+// gathered in LDS and added to one of the row's segments: additions to one
+// counter wait for one another, some 20 ns each.
 template <typename T>
 __global__ __launch_bounds__(256) void collect_kernel(Long k) {
   __shared__ float queues[4][kTile / 2 + 64];
@@ -845,21 +847,26 @@ __global__ __launch_bounds__(256) void collect_kernel(Long k) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const T *scores = row_scores<T>(k, r);
   const uint8_t *valid = row_mask(k, r);
-  u64 *list = k.list + (size_t)r * k.list_most;
+  const uint32_t part = (uint32_t)c % k.segments;
+  u64 *list = k.list + ((size_t)r * k.segments + part) * k.segment_most;
+  uint32_t *listed = &k.listed[r * kSegments + part];
   const int64_t end = min(k.a.s.n, (c + 1) * k.chunk);
-  const bool plain = ordinary(l);
+  const bool plain = ordinary(l), apart = x_k == x_k;
   float *queue = queues[wave];
   int queued = 0;
-  for (int64_t t = c * k.chunk + wave * k.tile; t < end; t += 4 * k.tile) {
+  const int steps = (int)(k.tile / kTile);
+  const int64_t t0 = c * k.chunk + wave * k.tile;
+  Eight<T> next;
+  if (t0 < end) next.load(scores, valid, t0 + lane * 8, end);
+  for (int64_t t = t0; t < end; t += 4 * k.tile) {
     u64 sum = 0;
-    const int64_t stop = min(end, t + k.tile);
-    Eight<T> next;
-    next.load(scores, valid, t + lane * 8, stop);
-    for (int64_t i = t + lane * 8; i < t + k.tile; i += kTile) {
+    for (int step = 0; step < steps; ++step) {
+      const int64_t i = t + step * kTile + lane * 8;
       const Eight<T> now = next;
-      next.load(scores, valid, i + kTile, stop);
+      next.load(scores, valid, step + 1 < steps ? i + kTile : t + 4 * k.tile + lane * 8, end);
       float x[8];
       now.get(valid != nullptr, x);
+      // no short-circuits: comparisons go to scalar masks, without branches
       u64 keep[8];
       bool waits = false;
       int kept = 0;
@@ -867,7 +874,11 @@ __global__ __launch_bounds__(256) void collect_kernel(Long k) {
       for (int j = 0; j < 8; ++j) {
         keep[j] = __ballot(x[j] >= x_keep);
         kept += __popcll(keep[j]);
-        waits |= (x[j] >= x_last && !(x[j] >= x_sure)) || (x[j] >= x_k && !(x[j] >= x_k_end));
+        waits = waits | ((x[j] >= x_last) & !(x[j] >= x_sure));
+      }
+      if (apart) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) waits = waits | ((x[j] >= x_k) & !(x[j] >= x_k_end));
       }
       if (kept > kTile / 2) {
 #pragma unroll
@@ -893,7 +904,7 @@ __global__ __launch_bounds__(256) void collect_kernel(Long k) {
         uint32_t wait = 0;
 #pragma unroll
         for (int j = 0; j < 8; ++j)
-          wait |= ((x[j] >= x_last && !(x[j] >= x_sure)) || (x[j] >= x_k && !(x[j] >= x_k_end)))
+          wait |= (((x[j] >= x_last) & !(x[j] >= x_sure)) | ((x[j] >= x_k) & !(x[j] >= x_k_end)))
                       ? 1u << j : 0u;
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
@@ -903,8 +914,8 @@ __global__ __launch_bounds__(256) void collect_kernel(Long k) {
           if (at < kOpen) {
             open[at] = key;
           } else {
-            const uint32_t to = atomicAdd(&k.listed[r], 1u);
-            if (to < k.list_most) list[to] = key;
+            const uint32_t to = atomicAdd(listed, 1u);
+            if (to < k.segment_most) list[to] = key;
           }
         }
       }
@@ -918,10 +929,10 @@ __global__ __launch_bounds__(256) void collect_kernel(Long k) {
   __syncthreads();
   const uint32_t count = min(opened, (uint32_t)kOpen);
   if (count == 0) return;
-  if (threadIdx.x == 0) open_at = atomicAdd(&k.listed[r], count);
+  if (threadIdx.x == 0) open_at = atomicAdd(listed, count);
   __syncthreads();
   for (uint32_t e = threadIdx.x; e < count; e += 256)
-    if (open_at + e < k.list_most) list[open_at + e] = open[e];
+    if (open_at + e < k.segment_most) list[open_at + e] = open[e];
 }
 
 // One draw by one wave: the tile whose running weight passes `want`, then the
@@ -933,18 +944,28 @@ __device__ __forceinline__ void draw_one(const Long &k, int64_t r, int j, float 
   const int lane = threadIdx.x & 63;
   const int64_t at = (k.row0 + r) * k.a.draws + j;
   const u64 want = wanted(u, total);
-  int first = 0, last = (int)k.tiles - 1;
-  while (first < last) {
-    const int mid = (first + last) / 2;
-    if (tile_end[mid] > want) last = mid; else first = mid + 1;
+  // the first tile whose end passes `want`: 64 candidates at a time
+  int first = 0;
+  for (int width = 4096; width > 1; width >>= 6) {
+    const int part = width >> 6, last = first + lane * part + part - 1;
+    const u64 passed =
+        __ballot(last >= (int)k.tiles - 1 || tile_end[min(last, (int)k.tiles - 1)] > want);
+    first += part * (__ffsll(passed) - 1);
   }
   u64 run = first > 0 ? tile_end[first - 1] : 0;
   const T *scores = row_scores<T>(k, r);
   const uint8_t *valid = row_mask(k, r);
-  for (int64_t base = first * k.tile; base < k.a.s.n; base += kTile) {
+  const int64_t end = min(k.a.s.n, (first + 1) * k.tile);
+  Eight<T> next[2];
+  next[0].load(scores, valid, first * k.tile + lane * 8, end);
+  next[1].load(scores, valid, first * k.tile + kTile + lane * 8, end);
+  for (int64_t base = first * k.tile; base < end; base += kTile) {
     const int64_t i = base + lane * 8;
+    const Eight<T> now = next[0];
+    next[0] = next[1];
+    next[1].load(scores, valid, i + 2 * kTile, end);
     float x[8];
-    load8(scores, valid, i, k.a.s.n, x);
+    now.get(valid != nullptr, x);
     uint32_t q[8];
     u64 sum = 0;
 #pragma unroll
@@ -957,15 +978,13 @@ __device__ __forceinline__ void draw_one(const Long &k, int64_t r, int j, float 
     const u64 found = __ballot(run + incl > want);
     if (found) {
       if (lane == __ffsll(found) - 1) {
-        u64 now = run + incl - sum;
+        u64 now_at = run + incl - sum;
         float z = 0.0f;
-        int e = 0;
-        bool done = false;
+        int e = -1;
 #pragma unroll
         for (int f = 0; f < 8; ++f) {
-          now += q[f];
-          if (!done && now > want) {
-            done = true;
+          now_at += q[f];
+          if (e < 0 && now_at > want) {
             e = f;
             z = exponent(x[f], l);
           }
@@ -986,6 +1005,7 @@ struct Finish {
   uint32_t q[kList];
   u64 tile[kMaxTiles];
   u64 wave_sum[16];
+  uint32_t segment_end[kSegments];
 };
 
 template <typename T>
@@ -997,17 +1017,34 @@ __global__ __launch_bounds__(1024) void finish_kernel(Long k) {
   const RowState &settled = k.state[r];
   const T *scores = row_scores<T>(k, r);
   const uint8_t *valid = row_mask(k, r);
-  const u64 *list = k.list + (size_t)r * k.list_most;
-  const uint32_t listed = k.listed[r];
+  const u64 *list = k.list + (size_t)r * k.segments * k.segment_most;
+  const int lane = threadIdx.x & 63;
+  uint32_t part = lane < kSegments ? k.listed[r * kSegments + lane] : 0;
+  const bool fits = !__any(part > k.segment_most);
+  part = wave_prefix(part);
+  const uint32_t listed = from_lane(part, 63);
+  if (threadIdx.x < kSegments) sh.segment_end[threadIdx.x] = part;
+  // entry e of the list: its segment by the segments' ends
+  auto entry = [&](uint32_t e) {
+    uint32_t at = 0;
+#pragma unroll
+    for (uint32_t step = kSegments / 2; step; step >>= 1)
+      if (sh.segment_end[at + step - 1] <= e) at += step;
+    return list[(size_t)at * k.segment_most + (e - (at ? sh.segment_end[at - 1] : 0))];
+  };
+  __syncthreads();
   const float u0 = wave < k.a.draws ? k.a.u[row * k.a.draws + wave] : 0.0f;
   for (int t = threadIdx.x; t < k.tiles; t += 1024) sh.tile[t] = k.tile_mass[r * k.tiles + t];
-  for (uint32_t e = threadIdx.x; e < min(listed, (uint32_t)kList); e += 1024) sh.keys[e] = list[e];
+  if (fits)
+    for (uint32_t e = threadIdx.x; e < min(listed, (uint32_t)kList); e += 1024)
+      sh.keys[e] = entry(e);
   const RowLimits l = settled.l;
   if (l.m == -__builtin_inff()) return no_entry(k.a, row);
   const Bins b = settled.b;
   const float scale = (float)kBins / l.range;
-  for (uint32_t e = threadIdx.x; e < min(listed, (uint32_t)kList); e += 1024)
-    sh.q[e] = weight(exponent(key_score(sh.keys[e]), l));
+  if (fits)
+    for (uint32_t e = threadIdx.x; e < min(listed, (uint32_t)kList); e += 1024)
+      sh.q[e] = weight(exponent(key_score(sh.keys[e]), l));
 
   u64 cut = 0;
   if (limited(l, n)) {
@@ -1025,15 +1062,17 @@ __global__ __launch_bounds__(1024) void finish_kernel(Long k) {
         const int bin = bin_of<kBins>(z, scale);
         if ((bin >= b.sure && bin <= b.last) || bin == b.k_bin) f(key_of(x, i), weight(z), bin);
       };
-      if (listed <= k.list_most) {
+      if (fits) {
 #pragma unroll 1
         for (uint32_t e = threadIdx.x; e < min(listed, (uint32_t)kList); e += 1024) {
           const u64 key = sh.keys[e];
           f(key, sh.q[e], bin_of<kBins>(exponent(key_score(key), l), scale));
         }
 #pragma unroll 1
-        for (uint32_t e = kList + threadIdx.x; e < listed; e += 1024)
-          one(key_score(list[e]), key_index(list[e]));
+        for (uint32_t e = kList + threadIdx.x; e < listed; e += 1024) {
+          const u64 key = entry(e);
+          one(key_score(key), key_index(key));
+        }
       } else {
         for (int64_t i = (int64_t)threadIdx.x * 8; i < n; i += 8192) {
           float x[8];
@@ -1096,7 +1135,7 @@ __global__ __launch_bounds__(256) void draw_kernel(Long k, int blocks) {
 
 struct LongPlan {
   int64_t batch, tile, tiles, most_chunks;
-  uint32_t list_most;
+  uint32_t list_most;  // entries of a row's list
   size_t range, mass, count, tile_mass, list, listed, state, bytes;
 };
 
@@ -1107,7 +1146,7 @@ LongPlan long_plan(int64_t n, int64_t rows) {
   p.tiles = (n + p.tile - 1) / p.tile;
   // as many chunks as workgroups may be wanted: 4,096 in all, one a row at least
   p.most_chunks = std::max<int64_t>(1, 4096 / std::max<int64_t>(1, p.batch));
-  p.list_most = (uint32_t)(kList + n / 64);
+  p.list_most = (uint32_t)(2 * kList + n / 32);
   size_t at = 0;
   auto take = [&](size_t bytes) {
     const size_t here = at;
@@ -1120,7 +1159,7 @@ LongPlan long_plan(int64_t n, int64_t rows) {
   p.count = take(b * kBins * 4);
   p.tile_mass = take(b * p.tiles * 8);
   p.list = take(b * p.list_most * 8);
-  p.listed = take(b * 4);
+  p.listed = take(b * kSegments * 4);
   p.state = take(b * sizeof(RowState));
   p.bytes = at;
   return p;
@@ -1134,7 +1173,6 @@ hipError_t launch_long(const SampleArgs &a, void *ws, int cu_count, hipStream_t 
   k.a = a;
   k.tile = p.tile;
   k.tiles = p.tiles;
-  k.list_most = p.list_most;
   k.range = reinterpret_cast<float2 *>(base + p.range);
   k.mass = reinterpret_cast<u64 *>(base + p.mass);
   k.count = reinterpret_cast<uint32_t *>(base + p.count);
@@ -1152,6 +1190,8 @@ hipError_t launch_long(const SampleArgs &a, void *ws, int cu_count, hipStream_t 
     const int64_t unit = std::max<int64_t>(kChunk, p.tile);
     k.chunk = std::max<int64_t>(1, (a.s.n + want * unit - 1) / (want * unit)) * unit;
     k.chunks = (a.s.n + k.chunk - 1) / k.chunk;
+    k.segments = (uint32_t)std::min<int64_t>(kSegments, k.chunks);
+    k.segment_most = p.list_most / k.segments;
     // the bins' parts: two workgroups a CU, of sixteen waves
     const int64_t parts = std::max<int64_t>(1, (int64_t)cu_count * 2 / rows);
     k.span = std::max<int64_t>(1, (a.s.n + parts * kSpan - 1) / (parts * kSpan)) * kSpan;
