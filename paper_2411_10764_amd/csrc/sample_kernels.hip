@@ -38,10 +38,9 @@ constexpr int kBins = 2048;         // bins of a long row
 constexpr int kSub = 512;           // bins of a short row, parts of an interval of keys
 constexpr int kMaxTiles = 4096;     // tiles of a row
 constexpr int kTile = 512;          // smallest tile: 8 entries a lane
-constexpr int kChunk = 4 * kTile;   // smallest chunk: 4 waves
 constexpr int kSpan = 16 * kTile;   // smallest part of count_kernel: 16 waves
 constexpr int kPacked = 32768;      // entries that a packed LDS bin holds
-constexpr int kFew = 2048;          // k of top-k that lists everything it keeps
+constexpr int kFew = 256;           // k of top-k that lists everything it keeps
 constexpr int kList = 4096;         // list entries held in LDS
 constexpr int kSegments = 32;       // of a row's list, at most
 constexpr int kOpen = 1024;         // list entries that collect_kernel gathers before it adds them
@@ -112,9 +111,12 @@ __device__ __forceinline__ float exponent(float x, const RowLimits &l) {
   return x == l.m ? 0.0f : (x - l.m) * l.r;
 }
 
-// 0 for an entry that is not included (x = -inf or NaN, so z is) too.
+// 0 for an entry that is not included (x = -inf or NaN, so z is) too: the
+// instruction takes a NaN to 0, where C++ leaves the conversion undefined.
 __device__ __forceinline__ uint32_t weight(float z) {
-  return (uint32_t)fmaxf(rintf(expf(z) * kOne), 0.0f);
+  uint32_t q;
+  asm("v_cvt_u32_f32 %0, %1" : "=v"(q) : "v"(rintf(expf(z) * kOne)));
+  return q;
 }
 
 // Eight consecutive entries of a row as they come from memory, so that the
@@ -774,15 +776,15 @@ __device__ __forceinline__ float least_score(const RowLimits &l, F holds) {
 
 // What the bins say of every entry, as scores to compare with: bins fall as
 // scores rise.  A workgroup a row.
-__global__ __launch_bounds__(1024) void settle_kernel(Long k) {
+__global__ __launch_bounds__(512) void settle_kernel(Long k) {
   __shared__ Search s;
-  __shared__ float2 lds[16];
+  __shared__ float2 lds[8];
   __shared__ uint32_t count[kBins];
   __shared__ u64 mass[kBins];
   __shared__ float edges[5];
   const int64_t r = blockIdx.x;
   if (k.a.top_k || k.a.top_p || k.a.s.temperature) {
-    for (int j = threadIdx.x; j < kBins; j += 1024) {
+    for (int j = threadIdx.x; j < kBins; j += 512) {
       count[j] = k.count[r * kBins + j];
       mass[j] = k.mass[r * kBins + j];
     }
@@ -1003,6 +1005,7 @@ struct Finish {
   u64 mass[kBins];
   u64 keys[kList];
   uint32_t q[kList];
+  uint16_t bin[kList];
   u64 tile[kMaxTiles];
   u64 wave_sum[16];
   uint32_t segment_end[kSegments];
@@ -1013,7 +1016,7 @@ __global__ __launch_bounds__(1024) void finish_kernel(Long k) {
   extern __shared__ char raw[];
   Finish &sh = *reinterpret_cast<Finish *>(raw);
   const int64_t r = blockIdx.x, row = k.row0 + r, n = k.a.s.n;
-  const int wave = threadIdx.x >> 6;
+  const int wave = threadIdx.x >> 6, threads = blockDim.x, waves = threads >> 6;
   const RowState &settled = k.state[r];
   const T *scores = row_scores<T>(k, r);
   const uint8_t *valid = row_mask(k, r);
@@ -1034,23 +1037,26 @@ __global__ __launch_bounds__(1024) void finish_kernel(Long k) {
   };
   __syncthreads();
   const float u0 = wave < k.a.draws ? k.a.u[row * k.a.draws + wave] : 0.0f;
-  for (int t = threadIdx.x; t < k.tiles; t += 1024) sh.tile[t] = k.tile_mass[r * k.tiles + t];
+  for (int t = threadIdx.x; t < k.tiles; t += threads) sh.tile[t] = k.tile_mass[r * k.tiles + t];
   if (fits)
-    for (uint32_t e = threadIdx.x; e < min(listed, (uint32_t)kList); e += 1024)
+    for (uint32_t e = threadIdx.x; e < min(listed, (uint32_t)kList); e += threads)
       sh.keys[e] = entry(e);
   const RowLimits l = settled.l;
   if (l.m == -__builtin_inff()) return no_entry(k.a, row);
   const Bins b = settled.b;
   const float scale = (float)kBins / l.range;
   if (fits)
-    for (uint32_t e = threadIdx.x; e < min(listed, (uint32_t)kList); e += 1024)
-      sh.q[e] = weight(exponent(key_score(sh.keys[e]), l));
+    for (uint32_t e = threadIdx.x; e < min(listed, (uint32_t)kList); e += threads) {
+      const float z = exponent(key_score(sh.keys[e]), l);
+      sh.q[e] = weight(z);
+      sh.bin[e] = (uint16_t)bin_of<kBins>(z, scale);
+    }
 
   u64 cut = 0;
   if (limited(l, n)) {
     const bool everything = lists_all(l);
     if (!everything && l.p < 2.0f) {
-      for (int j = threadIdx.x; j < kBins; j += 1024) sh.mass[j] = k.mass[r * kBins + j];
+      for (int j = threadIdx.x; j < kBins; j += threads) sh.mass[j] = k.mass[r * kBins + j];
     }
     __syncthreads();
     // f(key, weight, bin) for every listed entry.  A list that did not fit is
@@ -1064,17 +1070,16 @@ __global__ __launch_bounds__(1024) void finish_kernel(Long k) {
       };
       if (fits) {
 #pragma unroll 1
-        for (uint32_t e = threadIdx.x; e < min(listed, (uint32_t)kList); e += 1024) {
-          const u64 key = sh.keys[e];
-          f(key, sh.q[e], bin_of<kBins>(exponent(key_score(key), l), scale));
+        for (uint32_t e = threadIdx.x; e < min(listed, (uint32_t)kList); e += threads) {
+          f(sh.keys[e], sh.q[e], (int)sh.bin[e]);
         }
 #pragma unroll 1
-        for (uint32_t e = kList + threadIdx.x; e < listed; e += 1024) {
+        for (uint32_t e = kList + threadIdx.x; e < listed; e += threads) {
           const u64 key = entry(e);
           one(key_score(key), key_index(key));
         }
       } else {
-        for (int64_t i = (int64_t)threadIdx.x * 8; i < n; i += 8192) {
+        for (int64_t i = (int64_t)threadIdx.x * 8; i < n; i += (int64_t)threads * 8) {
           float x[8];
           load8(scores, valid, i, n, x);
 #pragma unroll
@@ -1091,29 +1096,21 @@ __global__ __launch_bounds__(1024) void finish_kernel(Long k) {
     });
   }
   __syncthreads();
-  // running weights of the tiles, each thread four in a row
-  u64 own[kMaxTiles / 1024], sum = 0;
-#pragma unroll
-  for (int j = 0; j < kMaxTiles / 1024; ++j) {
-    const int t = threadIdx.x * (kMaxTiles / 1024) + j;
-    own[j] = t < k.tiles ? sh.tile[t] : 0;
-    sum += own[j];
-  }
+  // running weights of the tiles, each thread a few in a row
+  const int per = ((int)k.tiles + threads - 1) / threads;
+  const int first = min((int)k.tiles, (int)threadIdx.x * per), last = min((int)k.tiles, first + per);
+  u64 sum = 0;
+  for (int t = first; t < last; ++t) sum += sh.tile[t];
   u64 total;
   u64 run = block_prefix(sum, sh.wave_sum, &total);
-#pragma unroll
-  for (int j = 0; j < kMaxTiles / 1024; ++j) {
-    const int t = threadIdx.x * (kMaxTiles / 1024) + j;
-    run += own[j];
-    if (t < k.tiles) sh.tile[t] = run;
-  }
+  for (int t = first; t < last; ++t) sh.tile[t] = run += sh.tile[t];
   __syncthreads();
   if (k.a.draws <= kFewDraws) {
-    for (int j = wave; j < k.a.draws; j += 16)
+    for (int j = wave; j < k.a.draws; j += waves)
       draw_one<T>(k, r, j, j == wave ? u0 : k.a.u[row * k.a.draws + j], l, cut, total, sh.tile);
     return;
   }
-  for (int t = threadIdx.x; t < k.tiles; t += 1024) k.tile_mass[r * k.tiles + t] = sh.tile[t];
+  for (int t = threadIdx.x; t < k.tiles; t += threads) k.tile_mass[r * k.tiles + t] = sh.tile[t];
   if (threadIdx.x == 0) {
     k.state[r].cut = cut;
     k.state[r].total = total;
@@ -1142,7 +1139,10 @@ struct LongPlan {
 LongPlan long_plan(int64_t n, int64_t rows) {
   LongPlan p{};
   p.batch = std::min<int64_t>(rows, kBatch);
-  p.tile = std::max<int64_t>(kTile, ((n + kMaxTiles - 1) / kMaxTiles + kTile - 1) / kTile * kTile);
+  // A tile's sum costs a wave as much as a hundred of its entries a lane would:
+  // long tiles where there are waves enough.
+  const int64_t least = p.batch * n >= (int64_t)kTile * 4 * 4096 ? kTile * 4 : kTile;
+  p.tile = std::max<int64_t>(least, ((n + kMaxTiles - 1) / kMaxTiles + kTile - 1) / kTile * kTile);
   p.tiles = (n + p.tile - 1) / p.tile;
   // as many chunks as workgroups may be wanted: 4,096 in all, one a row at least
   p.most_chunks = std::max<int64_t>(1, 4096 / std::max<int64_t>(1, p.batch));
@@ -1184,10 +1184,10 @@ hipError_t launch_long(const SampleArgs &a, void *ws, int cu_count, hipStream_t 
   if (e != hipSuccess) return e;
   for (k.row0 = 0; k.row0 < a.s.rows; k.row0 += p.batch) {
     const int64_t rows = std::min(p.batch, a.s.rows - k.row0);
-    // about eight workgroups a CU, none over less than kChunk entries; chunks
+    // about eight workgroups a CU, none over less than four tiles; chunks
     // are whole tiles, a wave's at a time
     const int64_t want = std::min(p.most_chunks, std::max<int64_t>(1, (int64_t)cu_count * 8 / rows));
-    const int64_t unit = std::max<int64_t>(kChunk, p.tile);
+    const int64_t unit = 4 * p.tile;
     k.chunk = std::max<int64_t>(1, (a.s.n + want * unit - 1) / (want * unit)) * unit;
     k.chunks = (a.s.n + k.chunk - 1) / k.chunk;
     k.segments = (uint32_t)std::min<int64_t>(kSegments, k.chunks);
@@ -1196,13 +1196,16 @@ hipError_t launch_long(const SampleArgs &a, void *ws, int cu_count, hipStream_t 
     const int64_t parts = std::max<int64_t>(1, (int64_t)cu_count * 2 / rows);
     k.span = std::max<int64_t>(1, (a.s.n + parts * kSpan - 1) / (parts * kSpan)) * kSpan;
     k.spans = (a.s.n + k.span - 1) / k.span;
+    // What a row's workgroup does is a chain of short steps; waves beyond one a
+    // SIMD only pay where there is much to go through.
+    const int finish = a.s.n > (1 << 20) ? 1024 : 512;
     const uint32_t grid = (uint32_t)(rows * k.chunks);
     range_kernel<T><<<grid, 256, 0, s>>>(k);
     if (a.top_k || a.top_p || a.s.temperature) 
       count_kernel<T><<<(uint32_t)(rows * k.spans), 1024, 0, s>>>(k);
-    settle_kernel<<<(uint32_t)rows, 1024, 0, s>>>(k);
+    settle_kernel<<<(uint32_t)rows, 512, 0, s>>>(k);
     collect_kernel<T><<<grid, 256, 0, s>>>(k);
-    finish_kernel<T><<<(uint32_t)rows, 1024, sizeof(Finish), s>>>(k);
+    finish_kernel<T><<<(uint32_t)rows, finish, sizeof(Finish), s>>>(k);
     if (a.draws > kFewDraws) {
       const int blocks = (a.draws + 3) / 4;
       draw_kernel<T><<<(uint32_t)(rows * blocks), 256, 0, s>>>(k, blocks);
