@@ -5,12 +5,12 @@
 //
 // Both move data and little else.  The gradient adds in a fixed order: the
 // (id, position) pairs are sorted stably by id (least-significant-digit radix
-// sort), the sorted list is cut into pieces of equal length, and a group of
+// sort, in one workgroup up to kOneSort tokens), the sorted list is cut into pieces of equal length, and a group of
 // lanes adds the rows of one piece one after the other in registers.  A run
 // of one id that lies inside a piece is finished there; the parts of a run
 // that crosses pieces go to the workspace and are joined by join_kernel.  No
 // floating-point atomics, so results are the same in every run.  The rows
-// that no token names are cleared by further workgroups of the sums' launch.
+// that no token names are cleared by further workgroups of all those launches.
 //
 // A table of few numbers (rows * width at most kFewCells, width at most
 // kFewWidth) needs no sort: every lane of a wave holds a table of its own in
@@ -61,6 +61,38 @@ __global__ __launch_bounds__(kThreads) void lookup_kernel(EmbedArgs a, int log_g
   }
 }
 
+// ---- clearing beside the sort ------------------------------------------------------
+
+// The sort keeps few compute units busy.  Further workgroups of its launches
+// clear the table's first rows meanwhile, named by a token or not.
+struct Clear {
+  uint16_t *grad;          // in halves of 4 bytes: every type is a number of them
+  int64_t row0, row1;      // rows of this launch
+  int64_t width, ld;       // of a row, in halves
+  uint32_t first, blocks;  // workgroups first .. first + blocks - 1 clear
+};
+
+typedef uint16_t Halves __attribute__((ext_vector_type(8), aligned(2)));
+
+__device__ __forceinline__ void clear_part(const Clear &f) {
+  // rows that follow one another are one long row
+  const bool flat = f.ld == f.width;
+  const int64_t rows = flat ? 1 : f.row1 - f.row0;
+  const int64_t width = flat ? (f.row1 - f.row0) * f.width : f.width;
+  const int64_t step = (int64_t)f.blocks * blockDim.x * 8;
+  for (int64_t r = 0; r < rows; ++r) {
+    uint16_t *row = f.grad + (f.row0 + r) * f.ld;
+    for (int64_t c = ((int64_t)(blockIdx.x - f.first) * blockDim.x + threadIdx.x) * 8; c < width;
+         c += step) {
+      if (c + 8 <= width) {
+        __builtin_nontemporal_store(Halves{}, reinterpret_cast<Halves *>(row + c));
+      } else {
+        for (int64_t j = c; j < width; ++j) row[j] = 0;
+      }
+    }
+  }
+}
+
 // ---- stable sort of (id, position) by id ----------------------------------------
 
 // The key of position i: its id, or table_rows (sorted last) outside the table.
@@ -85,8 +117,9 @@ __device__ __forceinline__ uint32_t pass_key(const SortPass &p, uint32_t i) {
 }
 
 template <int WAVES, int ROUNDS>
-__global__ __launch_bounds__(WAVES * 64) void sort_count(SortPass p) {
+__global__ __launch_bounds__(WAVES * 64) void sort_count(SortPass p, Clear f) {
   __shared__ uint32_t h[kMaxBins];
+  if (blockIdx.x >= f.first) return clear_part(f);
   const uint32_t bins = 1u << p.bits;
   for (uint32_t b = threadIdx.x; b < bins; b += WAVES * 64) h[b] = 0;
   __syncthreads();
@@ -113,10 +146,11 @@ __device__ __forceinline__ unsigned long long same_digit(uint32_t digit, int bit
 }
 
 template <int WAVES, int ROUNDS>
-__global__ __launch_bounds__(WAVES * 64) void sort_scatter(SortPass p) {
+__global__ __launch_bounds__(WAVES * 64) void sort_scatter(SortPass p, Clear f) {
   constexpr uint32_t kBlock = WAVES * 64;
   __shared__ uint32_t at[WAVES][kMaxBins];
   __shared__ uint32_t base[kMaxBins], total[kMaxBins];
+  if (blockIdx.x >= f.first) return clear_part(f);
   const uint32_t bins = 1u << p.bits;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   // Where this tile's keys of a digit go: all keys of smaller digits, and the
@@ -199,6 +233,108 @@ __global__ __launch_bounds__(WAVES * 64) void sort_scatter(SortPass p) {
   }
 }
 
+// All passes over at most kOneSort tokens in one workgroup: keys and positions
+// stay in registers, LDS carries them from one order to the next.
+constexpr int kOneRounds = 8;
+constexpr int kOneSort = 1024 * kOneRounds;
+
+struct OneSort {
+  const int32_t *ids;
+  uint32_t *key_out, *pos_out;
+  uint32_t n, rows;
+  int passes, bits;
+};
+
+__global__ __launch_bounds__(1024) void sort_one(OneSort p, Clear f) {
+  __shared__ uint32_t at[16][kMaxBins], base[kMaxBins];
+  if (blockIdx.x >= f.first) return clear_part(f);
+  extern __shared__ uint32_t exchange[];  // [n rounded up to 1024]
+  const uint32_t bins = 1u << p.bits;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int rounds = (int)((p.n + 1023) / 1024);
+  const uint32_t own = (uint32_t)(wave * rounds * 64 + lane);  // a wave's keys are consecutive
+  uint32_t key[kOneRounds], pos[kOneRounds], to[kOneRounds];
+#pragma unroll
+  for (int r = 0; r < kOneRounds; ++r) {
+    const uint32_t i = own + (uint32_t)(r * 64);
+    key[r] = r < rounds && i < p.n ? token_key(p.ids, i, p.rows) : 0u;
+    pos[r] = i;
+  }
+  for (int pass = 0; pass < p.passes; ++pass) {
+    const int shift = pass * p.bits;
+    for (uint32_t b = threadIdx.x; b < 16u * kMaxBins; b += 1024) (&at[0][0])[b] = 0;
+    __syncthreads();
+#pragma unroll
+    for (int r = 0; r < kOneRounds; ++r) {
+      if (r >= rounds) break;
+      const bool in = own + (uint32_t)(r * 64) < p.n;
+      const uint32_t digit = (key[r] >> shift) & (bins - 1);
+      const unsigned long long peers = same_digit(digit, p.bits, in);
+      const unsigned long long below = peers & ((1ull << lane) - 1);
+      const int leader = __ffsll(peers | (1ull << 63)) - 1;
+      uint32_t old = 0;
+      if (in && below == 0) old = atomicAdd(&at[wave][digit], (uint32_t)__popcll(peers));
+      to[r] = __shfl(old, leader) + (uint32_t)__popcll(below);
+    }
+    __syncthreads();
+    if (threadIdx.x < bins) {
+      uint32_t run = 0;
+#pragma unroll
+      for (int w = 0; w < 16; ++w) {
+        const uint32_t c = at[w][threadIdx.x];
+        at[w][threadIdx.x] = run;
+        run += c;
+      }
+      base[threadIdx.x] = run;
+    }
+    __syncthreads();
+    if (wave == 0) {
+      uint32_t carry = 0;
+      for (uint32_t b0 = 0; b0 < bins; b0 += 64) {
+        const uint32_t b = b0 + lane, own_count = b < bins ? base[b] : 0u;
+        uint32_t incl = own_count;
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) {
+          const uint32_t o = __shfl_up(incl, d);
+          if (lane >= d) incl += o;
+        }
+        if (b < bins) base[b] = carry + incl - own_count;
+        carry += __shfl(incl, 63);
+      }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int r = 0; r < kOneRounds; ++r) {
+      const uint32_t digit = (key[r] >> shift) & (bins - 1);
+      if (r < rounds && own + (uint32_t)(r * 64) < p.n) {
+        to[r] += base[digit] + at[wave][digit];
+        exchange[to[r]] = key[r];
+      }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int r = 0; r < kOneRounds; ++r)
+      if (r < rounds && own + (uint32_t)(r * 64) < p.n) key[r] = exchange[own + (uint32_t)(r * 64)];
+    __syncthreads();
+#pragma unroll
+    for (int r = 0; r < kOneRounds; ++r)
+      if (r < rounds && own + (uint32_t)(r * 64) < p.n) exchange[to[r]] = pos[r];
+    __syncthreads();
+#pragma unroll
+    for (int r = 0; r < kOneRounds; ++r)
+      if (r < rounds && own + (uint32_t)(r * 64) < p.n) pos[r] = exchange[own + (uint32_t)(r * 64)];
+    __syncthreads();
+  }
+#pragma unroll
+  for (int r = 0; r < kOneRounds; ++r) {
+    const uint32_t i = own + (uint32_t)(r * 64);
+    if (r < rounds && i < p.n) {
+      p.key_out[i] = key[r];
+      p.pos_out[i] = pos[r];
+    }
+  }
+}
+
 // ---- sums over the sorted list ---------------------------------------------------
 
 struct SumArgs {
@@ -207,7 +343,11 @@ struct SumArgs {
   float *part;                // [pieces][2][width]: the run that entered a piece, the run that leaves it
   uint32_t n, rows, piece, pieces;
   int log_g;                  // lanes that share a row
-  uint32_t slabs, sum_blocks; // slabs of a row; workgroups that add, the others clear
+  uint32_t slabs;             // of a row
+  uint32_t sum_blocks, join_blocks;  // workgroups that add or join, the others clear
+  uint32_t join;              // pieces of a join workgroup
+  uint32_t cleared, split;    // rows below `cleared` are; those below `split` are beside the sums,
+                              // the others beside the joins
 };
 
 template <typename T, typename O>
@@ -251,19 +391,20 @@ __device__ __forceinline__ void load_row(const T *src, int64_t c, int64_t width,
 // Zeros for the rows that no token names: a wave looks 64 rows up in the
 // sorted list at once.
 template <typename O>
-__device__ __forceinline__ void clear_rows(const SumArgs &s, uint32_t block) {
+__device__ __forceinline__ void clear_rows(const SumArgs &s, uint32_t block, uint32_t row0,
+                                           uint32_t row1) {
   constexpr int kLen = 16 / (int)sizeof(O);
   typedef O OV __attribute__((ext_vector_type(kLen), aligned(sizeof(O))));
   const int lane = threadIdx.x & 63;
-  const int64_t r0 = ((int64_t)block * (kThreads / 64) + (threadIdx.x >> 6)) * 64;
-  if (r0 >= s.rows) return;
+  const int64_t r0 = row0 + ((int64_t)block * (kThreads / 64) + (threadIdx.x >> 6)) * 64;
+  if (r0 >= row1) return;
   const int64_t r = r0 + lane;
   uint32_t lo = 0, hi = s.n;
   while (lo < hi) {
     const uint32_t mid = lo + (hi - lo) / 2;
     if ((int64_t)s.key[mid] < r) lo = mid + 1; else hi = mid;
   }
-  const bool none = r < s.rows && !(lo < s.n && (int64_t)s.key[lo] == r);
+  const bool none = r < row1 && !(lo < s.n && (int64_t)s.key[lo] == r);
   O *grad = static_cast<O *>(s.a.grad);
   if (s.a.width <= 16) {
     if (none)
@@ -274,7 +415,7 @@ __device__ __forceinline__ void clear_rows(const SumArgs &s, uint32_t block) {
     O *dst = grad + (r0 + (__ffsll(todo) - 1)) * s.a.grad_ld;
     for (int64_t c = (int64_t)lane * kLen; c < s.a.width; c += 64 * kLen) {
       if (c + kLen <= s.a.width) {
-        *reinterpret_cast<OV *>(dst + c) = OV{};
+        __builtin_nontemporal_store(OV{}, reinterpret_cast<OV *>(dst + c));
       } else {
         for (int64_t j = c; j < s.a.width; ++j) dst[j] = (O)0.0f;
       }
@@ -291,7 +432,7 @@ __global__ __launch_bounds__(kThreads) void sum_kernel(SumArgs s) {
   constexpr int kLen = Vec<T>::kLen;
   constexpr int kAhead = 8;
   extern __shared__ uint32_t staged[];  // [groups][piece + 1] keys, then positions
-  if (blockIdx.x >= s.sum_blocks) return clear_rows<O>(s, blockIdx.x - s.sum_blocks);
+  if (blockIdx.x >= s.sum_blocks) return clear_rows<O>(s, blockIdx.x - s.sum_blocks, s.cleared, s.split);
   const uint32_t block = blockIdx.x / s.slabs, slab = blockIdx.x % s.slabs;
   const uint32_t groups = kThreads >> s.log_g, stride = s.piece + 1;
   uint32_t *keys = staged, *poss = staged + groups * stride;
@@ -348,22 +489,22 @@ __global__ __launch_bounds__(kThreads) void sum_kernel(SumArgs s) {
     store_row<T, O>(s, cur, c, acc);
 }
 
-// Joins the runs that cross pieces: a workgroup looks at kJoin pieces and adds,
+// Joins the runs that cross pieces: a workgroup looks at s.join pieces and adds,
 // for each run that leaves one of them and did not enter it, the parts of the
 // pieces it reaches.  Groups of lanes take every 256/G-th part in order; their
 // sums are added in group order.
-constexpr int kJoin = 8;
-
 template <typename T, typename O>
 __global__ __launch_bounds__(kThreads) void join_kernel(SumArgs s) {
   constexpr int kLen = Vec<T>::kLen;
   typedef float Part __attribute__((ext_vector_type(kLen), aligned(4)));
   __shared__ float sums[kThreads][kLen];
-  const uint32_t p0 = blockIdx.x * (uint32_t)kJoin;
+  if (blockIdx.x >= s.join_blocks)
+    return clear_rows<O>(s, blockIdx.x - s.join_blocks, s.split, s.rows);
+  const uint32_t p0 = blockIdx.x / s.slabs * s.join, slab = blockIdx.x % s.slabs;
   bool starts = false;
   {
     const uint32_t p = p0 + (threadIdx.x & 63);
-    if ((threadIdx.x & 63) < kJoin && p + 1 < s.pieces) {
+    if ((threadIdx.x & 63) < s.join && p + 1 < s.pieces) {
       const uint32_t lo = p * s.piece, hi = lo + s.piece, id = s.key[hi - 1];
       starts = id < s.rows && s.key[hi] == id &&
                (s.key[lo] != id || lo == 0 || s.key[lo - 1] != id);
@@ -372,7 +513,7 @@ __global__ __launch_bounds__(kThreads) void join_kernel(SumArgs s) {
   unsigned long long todo = __ballot(starts);  // the same in every wave
   const int g = 1 << s.log_g, groups = kThreads >> s.log_g;
   const int group = threadIdx.x >> s.log_g;
-  const int64_t c = (int64_t)blockIdx.y * g * kLen + (int64_t)(threadIdx.x & (g - 1)) * kLen;
+  const int64_t c = (int64_t)slab * g * kLen + (int64_t)(threadIdx.x & (g - 1)) * kLen;
   const bool live = c < s.a.width, whole = c + kLen <= s.a.width;
   while (todo) {
     const uint32_t p = p0 + (uint32_t)(__ffsll(todo) - 1);
@@ -505,13 +646,13 @@ int log_group(int64_t width, int len, int most) {
 struct GradPlan {
   bool few;
   uint32_t waves;              // few: waves, one a workgroup
-  int bits, passes, big;       // of a digit; sort passes; 16 waves a sort workgroup, else 4
+  int bits, passes, big;       // of a digit; sort passes; 8 keys a lane of a sort's step, else 2
   uint32_t tiles, subs, piece, pieces;
   size_t keys, hist, part;     // byte offsets of the second key buffer, counts, parts
   size_t bytes;
 };
 
-constexpr int kBigKeys = 16 * 8 * 64, kSmallKeys = 4 * 4 * 64;  // keys of a sort workgroup's step
+constexpr int kBigKeys = 16 * 8 * 64, kSmallKeys = 16 * 2 * 64;  // keys of a sort workgroup's step
 
 GradPlan grad_plan(int64_t n, int64_t rows, int64_t width) {
   GradPlan p{};
@@ -560,10 +701,14 @@ hipError_t launch_few(const EmbedGradArgs &a, const GradPlan &g, void *ws, hipSt
 }
 
 template <int WAVES, int ROUNDS>
-void launch_pass(const SortPass &p, hipStream_t st) {
-  sort_count<WAVES, ROUNDS><<<p.tiles, WAVES * 64, 0, st>>>(p);
-  sort_scatter<WAVES, ROUNDS><<<p.tiles, WAVES * 64, 0, st>>>(p);
+void launch_pass(const SortPass &p, const Clear &count, const Clear &scatter, hipStream_t st) {
+  sort_count<WAVES, ROUNDS><<<p.tiles + count.blocks, WAVES * 64, 0, st>>>(p, count);
+  sort_scatter<WAVES, ROUNDS><<<p.tiles + scatter.blocks, WAVES * 64, 0, st>>>(p, scatter);
 }
+
+// Bytes that a sort launch clears beside its own work: at 6.5 TB/s about the
+// time that the launch takes anyway.
+constexpr int64_t kClearBytes = (int64_t)40 << 20;
 
 template <typename T, typename O>
 hipError_t launch_grad(const EmbedGradArgs &a, void *ws, hipStream_t st) {
@@ -574,7 +719,27 @@ hipError_t launch_grad(const EmbedGradArgs &a, void *ws, hipStream_t st) {
                        reinterpret_cast<uint32_t *>(base + g.keys)};
   const size_t half = g.keys / 2 / 4;  // positions follow the keys
   int at = 0;
-  for (int pass = 0; pass < g.passes && a.n > 0; ++pass) {
+  const int64_t row_bytes = a.width * (int64_t)sizeof(O);
+  const int launches = a.n == 0 ? 0 : a.n <= kOneSort ? 1 : 2 * g.passes;
+  const int64_t cleared = std::min(a.table_rows, launches * kClearBytes / row_bytes);
+  // the part of launch i, after `own` workgroups of the sort
+  auto clear = [&](int i, uint32_t own) {
+    Clear f = {static_cast<uint16_t *>(a.grad), cleared * i / launches, cleared * (i + 1) / launches,
+               row_bytes / 2, a.grad_ld * (int64_t)sizeof(O) / 2, own, 0};
+    const int64_t vecs = (f.row1 - f.row0) * f.width / 8 + 1;
+    if (f.row1 > f.row0) f.blocks = (uint32_t)std::min<int64_t>((vecs + 1023) / 1024, 512);
+    return f;
+  };
+  if (a.n > 0 && a.n <= kOneSort) {
+    const OneSort p = {a.ids, list[0], list[0] + half, (uint32_t)a.n, (uint32_t)a.table_rows,
+                       g.passes, g.bits};
+    const hipError_t e =
+        ensure_dynamic_lds(reinterpret_cast<const void *>(sort_one), kOneSort * sizeof(uint32_t));
+    if (e != hipSuccess) return e;
+    const Clear f = clear(0, 1);
+    sort_one<<<1 + f.blocks, 1024, (size_t)((a.n + 1023) / 1024) * 4096, st>>>(p, f);
+  }
+  for (int pass = 0; pass < g.passes && a.n > kOneSort; ++pass) {
     SortPass p{};
     if (pass == 0) {
       p.ids = a.ids;
@@ -592,7 +757,9 @@ hipError_t launch_grad(const EmbedGradArgs &a, void *ws, hipStream_t st) {
     p.subs = g.subs;
     p.shift = pass * g.bits;
     p.bits = g.bits;
-    if (g.big) launch_pass<16, 8>(p, st); else launch_pass<4, 4>(p, st);
+    const Clear f[2] = {clear(2 * pass, p.tiles), clear(2 * pass + 1, p.tiles)};
+    if (g.big) launch_pass<16, 8>(p, f[0], f[1], st);
+    else launch_pass<16, 2>(p, f[0], f[1], st);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
@@ -610,13 +777,23 @@ hipError_t launch_grad(const EmbedGradArgs &a, void *ws, hipStream_t st) {
   s.slabs = (uint32_t)((a.width + slab - 1) / slab);
   const uint32_t per = kThreads >> s.log_g;
   s.sum_blocks = (s.pieces + per - 1) / per * s.slabs;
-  const uint32_t clear = (s.rows + kThreads - 1) / kThreads;
+  // Half of the other rows wait for the joins: both launches then keep writing.
+  s.cleared = (uint32_t)cleared;
+  s.split = s.pieces > 1 ? s.cleared + (s.rows - s.cleared) / 2 : s.rows;
+  const uint32_t clear1 = (s.split - s.cleared + kThreads - 1) / kThreads;
+  const uint32_t clear2 = (s.rows - s.split + kThreads - 1) / kThreads;
   const size_t lds = (size_t)per * (g.piece + 1) * 8;
   const hipError_t e = ensure_dynamic_lds(reinterpret_cast<const void *>(sum_kernel<T, O>), lds);
   if (e != hipSuccess) return e;
-  sum_kernel<T, O><<<s.sum_blocks + clear, kThreads, lds, st>>>(s);
-  if (s.pieces > 1)
-    join_kernel<T, O><<<dim3((s.pieces + kJoin - 1) / kJoin, s.slabs), kThreads, 0, st>>>(s);
+  if (s.sum_blocks + clear1 > 0)
+    sum_kernel<T, O><<<s.sum_blocks + clear1, kThreads, lds, st>>>(s);
+  if (s.pieces > 1) {
+    // a workgroup joins its runs one after the other: few pieces each while
+    // that keeps the launch short
+    s.join = s.pieces <= 16384 ? 2 : 16;
+    s.join_blocks = (s.pieces + s.join - 1) / s.join * s.slabs;
+    join_kernel<T, O><<<s.join_blocks + clear2, kThreads, 0, st>>>(s);
+  }
   return hipGetLastError();
 }
 

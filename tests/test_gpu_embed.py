@@ -58,7 +58,8 @@ def test_lookup(dtype, n, V, D, pad):
     (0, 7, 5, False), (1, 1, 1, False), (1, 1000, 3, False), (31, 4, 9, True), (64, 1, 1, False),
     (500, 2, 1, True), (2000, 81, 1, False), (4097, 300, 40, True), (3000, 5000, 129, False),
     (9000, 17, 256, True), (1025, 600, 513, True), (100, 70000, 16, True), (70001, 81, 2, True),
-    (300000, 7, 1, True), (270000, 100000, 3, False), (50, 9, 4099, True), (513, 200000, 1, False)])
+    (300000, 7, 1, True), (270000, 100000, 3, False), (50, 9, 4099, True), (513, 200000, 1, False),
+    (8192, 3000, 2, True), (8193, 70000, 5, False), (600000, 70000, 2, True)])
 def test_gradient(dtype, wide, n, V, D, skew):
     print(f"[embed_grad] {dtype} wide={wide} n={n} V={V} D={D}", flush=True)
     rng = np.random.default_rng(n + V + D)
