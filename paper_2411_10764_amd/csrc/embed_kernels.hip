@@ -234,9 +234,11 @@ __global__ __launch_bounds__(WAVES * 64) void sort_scatter(SortPass p, Clear f) 
 }
 
 // All passes over at most kOneSort tokens in one workgroup: keys and positions
-// stay in registers, LDS carries them from one order to the next.
+// stay in registers, LDS carries them from one order to the next.  PACKED: both
+// in one word, where the table's rows leave the bits.
 constexpr int kOneRounds = 8;
 constexpr int kOneSort = 1024 * kOneRounds;
+constexpr int kOneBits = 13;  // of a position
 
 struct OneSort {
   const int32_t *ids;
@@ -245,6 +247,7 @@ struct OneSort {
   int passes, bits;
 };
 
+template <bool PACKED>
 __global__ __launch_bounds__(1024) void sort_one(OneSort p, Clear f) {
   __shared__ uint32_t at[16][kMaxBins], base[kMaxBins];
   if (blockIdx.x >= f.first) return clear_part(f);
@@ -259,9 +262,10 @@ __global__ __launch_bounds__(1024) void sort_one(OneSort p, Clear f) {
     const uint32_t i = own + (uint32_t)(r * 64);
     key[r] = r < rounds && i < p.n ? token_key(p.ids, i, p.rows) : 0u;
     pos[r] = i;
+    if (PACKED) key[r] = key[r] << kOneBits | i;
   }
   for (int pass = 0; pass < p.passes; ++pass) {
-    const int shift = pass * p.bits;
+    const int shift = pass * p.bits + (PACKED ? kOneBits : 0);
     for (uint32_t b = threadIdx.x; b < 16u * kMaxBins; b += 1024) (&at[0][0])[b] = 0;
     __syncthreads();
 #pragma unroll
@@ -316,6 +320,7 @@ __global__ __launch_bounds__(1024) void sort_one(OneSort p, Clear f) {
     for (int r = 0; r < kOneRounds; ++r)
       if (r < rounds && own + (uint32_t)(r * 64) < p.n) key[r] = exchange[own + (uint32_t)(r * 64)];
     __syncthreads();
+    if (PACKED) continue;
 #pragma unroll
     for (int r = 0; r < kOneRounds; ++r)
       if (r < rounds && own + (uint32_t)(r * 64) < p.n) exchange[to[r]] = pos[r];
@@ -329,8 +334,8 @@ __global__ __launch_bounds__(1024) void sort_one(OneSort p, Clear f) {
   for (int r = 0; r < kOneRounds; ++r) {
     const uint32_t i = own + (uint32_t)(r * 64);
     if (r < rounds && i < p.n) {
-      p.key_out[i] = key[r];
-      p.pos_out[i] = pos[r];
+      p.key_out[i] = PACKED ? key[r] >> kOneBits : key[r];
+      p.pos_out[i] = PACKED ? key[r] & ((1u << kOneBits) - 1) : pos[r];
     }
   }
 }
@@ -345,7 +350,6 @@ struct SumArgs {
   int log_g;                  // lanes that share a row
   uint32_t slabs;             // of a row
   uint32_t sum_blocks, join_blocks;  // workgroups that add or join, the others clear
-  uint32_t join;              // pieces of a join workgroup
   uint32_t cleared, split;    // rows below `cleared` are; those below `split` are beside the sums,
                               // the others beside the joins
 };
@@ -396,7 +400,7 @@ __device__ __forceinline__ void clear_rows(const SumArgs &s, uint32_t block, uin
   constexpr int kLen = 16 / (int)sizeof(O);
   typedef O OV __attribute__((ext_vector_type(kLen), aligned(sizeof(O))));
   const int lane = threadIdx.x & 63;
-  const int64_t r0 = row0 + ((int64_t)block * (kThreads / 64) + (threadIdx.x >> 6)) * 64;
+  const int64_t r0 = row0 + ((int64_t)block * (blockDim.x / 64) + (threadIdx.x >> 6)) * 64;
   if (r0 >= row1) return;
   const int64_t r = r0 + lane;
   uint32_t lo = 0, hi = s.n;
@@ -489,69 +493,111 @@ __global__ __launch_bounds__(kThreads) void sum_kernel(SumArgs s) {
     store_row<T, O>(s, cur, c, acc);
 }
 
-// Joins the runs that cross pieces: a workgroup looks at s.join pieces and adds,
-// for each run that leaves one of them and did not enter it, the parts of the
-// pieces it reaches.  Groups of lanes take every 256/G-th part in order; their
-// sums are added in group order.
+// Joins the runs that cross pieces.  A group of lanes looks at one piece: a run
+// that leaves it without having entered it is the group's to add up, part after
+// part, where it reaches few pieces; a longer one is left to a wave, or to the
+// whole workgroup, whose groups take every so-many-th part in order and fold
+// their sums pairwise.
+constexpr int kJoinThreads = 1024;
+constexpr int kShortRun = 16;  // pieces that a group joins itself
+constexpr int kWaveRun = 32;   // pieces of each of a wave's groups that a wave joins itself
+
 template <typename T, typename O>
-__global__ __launch_bounds__(kThreads) void join_kernel(SumArgs s) {
+__global__ __launch_bounds__(kJoinThreads) void join_kernel(SumArgs s) {
   constexpr int kLen = Vec<T>::kLen;
   typedef float Part __attribute__((ext_vector_type(kLen), aligned(4)));
-  __shared__ float sums[kThreads][kLen];
+  __shared__ float sums[kJoinThreads * kLen];
+  // first pieces of longer runs, and the last ones of the longest
+  __shared__ uint32_t long_run[kJoinThreads / kShortRun + 1];
+  __shared__ uint32_t long_last[kJoinThreads / kShortRun + 1], longs;
   if (blockIdx.x >= s.join_blocks)
     return clear_rows<O>(s, blockIdx.x - s.join_blocks, s.split, s.rows);
-  const uint32_t p0 = blockIdx.x / s.slabs * s.join, slab = blockIdx.x % s.slabs;
-  bool starts = false;
-  {
-    const uint32_t p = p0 + (threadIdx.x & 63);
-    if ((threadIdx.x & 63) < s.join && p + 1 < s.pieces) {
-      const uint32_t lo = p * s.piece, hi = lo + s.piece, id = s.key[hi - 1];
-      starts = id < s.rows && s.key[hi] == id &&
-               (s.key[lo] != id || lo == 0 || s.key[lo - 1] != id);
+  const int groups = kJoinThreads >> s.log_g, group = threadIdx.x >> s.log_g;
+  const uint32_t block = blockIdx.x / s.slabs, slab = blockIdx.x % s.slabs;
+  const int in = threadIdx.x & ((1 << s.log_g) - 1);
+  const int64_t c = ((int64_t)slab << s.log_g) * kLen + (int64_t)in * kLen;
+  const bool live = c < s.a.width, whole = c + kLen <= s.a.width;
+  // adds the parts of pieces q, q + step, ... last
+  auto add = [&](float (&acc)[kLen], uint32_t p, uint32_t q, uint32_t step, uint32_t last) {
+#pragma unroll 8
+    for (; q <= last; q += step) {
+      const float *src = s.part + ((size_t)q * 2 + (q == p ? 1 : 0)) * s.a.width + c;
+      if (whole) {
+        const Part v = *reinterpret_cast<const Part *>(src);
+#pragma unroll
+        for (int j = 0; j < kLen; ++j) acc[j] += v[j];
+      } else {
+#pragma unroll
+        for (int j = 0; j < kLen; ++j)
+          if (c + j < s.a.width) acc[j] += src[j];
+      }
+    }
+  };
+  if (threadIdx.x == 0) longs = 0;
+  __syncthreads();
+  const uint32_t p = block * groups + group;
+  if (p + 1 < s.pieces) {
+    const uint32_t lo = p * s.piece, hi = lo + s.piece, id = s.key[hi - 1];
+    if (id < s.rows && s.key[hi] == id && (s.key[lo] != id || lo == 0 || s.key[lo - 1] != id)) {
+      uint32_t reach = 1;  // pieces that follow on and begin with the run's id
+#pragma unroll
+      for (uint32_t j = 2; j <= kShortRun; ++j)
+        if (p + j < s.pieces && s.key[(p + j) * s.piece] == id) reach = j;
+      if (reach < kShortRun) {
+        float acc[kLen] = {};
+        if (live) {
+          add(acc, p, p, 1, p + reach);
+          store_row<T, O>(s, id, c, acc);
+        }
+      } else if (in == 0) {
+        long_run[atomicAdd(&longs, 1u)] = p;  // whose turn is first changes no sum
+      }
     }
   }
-  unsigned long long todo = __ballot(starts);  // the same in every wave
-  const int g = 1 << s.log_g, groups = kThreads >> s.log_g;
-  const int group = threadIdx.x >> s.log_g;
-  const int64_t c = (int64_t)slab * g * kLen + (int64_t)(threadIdx.x & (g - 1)) * kLen;
-  const bool live = c < s.a.width, whole = c + kLen <= s.a.width;
-  while (todo) {
-    const uint32_t p = p0 + (uint32_t)(__ffsll(todo) - 1);
-    todo &= todo - 1;
-    const uint32_t id = s.key[(p + 1) * s.piece - 1];
-    uint32_t last = p + 1;  // the last piece that begins with the run's id
+  __syncthreads();
+  // runs of more pieces, a wave each: its groups of lanes side by side
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, side = 64 >> s.log_g;
+  for (uint32_t w = wave; w < longs; w += kJoinThreads / 64) {
+    const uint32_t first = long_run[w], id = s.key[(first + 1) * s.piece - 1];
+    uint32_t last = first + kShortRun;  // the last piece that begins with the run's id
     for (;;) {
-      const uint32_t q = last + 1 + (threadIdx.x & 63);
+      const uint32_t q = last + 1 + lane;
       const unsigned long long on = __ballot(q < s.pieces && s.key[q * s.piece] == id);
       last += on == ~0ull ? 64u : (uint32_t)__ffsll(~on) - 1;
       if (on != ~0ull) break;
     }
+    const bool wide = last - first >= (uint32_t)(kWaveRun * side);
+    if (lane == 0) long_last[w] = wide ? last : 0;
+    if (wide) continue;
     float acc[kLen] = {};
-    if (live) {
-#pragma unroll 4
-      for (uint32_t q = p + group; q <= last; q += groups) {
-        const float *src = s.part + ((size_t)q * 2 + (q == p ? 1 : 0)) * s.a.width + c;
-        if (whole) {
-          const Part v = *reinterpret_cast<const Part *>(src);
+    if (live) add(acc, first, first + (lane >> s.log_g), side, last);
+    for (int d = 1 << s.log_g; d < 64; d <<= 1) {
 #pragma unroll
-          for (int j = 0; j < kLen; ++j) acc[j] += v[j];
-        } else {
+      for (int j = 0; j < kLen; ++j) acc[j] += __shfl_xor(acc[j], d);
+    }
+    if (lane >> s.log_g == 0 && live) store_row<T, O>(s, id, c, acc);
+  }
+  __syncthreads();
+  // the longest, by the whole workgroup
+  for (uint32_t w = 0; w < longs; ++w) {
+    const uint32_t first = long_run[w], last = long_last[w];
+    if (last == 0) continue;
+    const uint32_t id = s.key[(first + 1) * s.piece - 1];
+    float acc[kLen] = {};
+    if (live) add(acc, first, first + group, groups, last);
+    for (int half = groups / 2; half > 0; half >>= 1) {
+      __syncthreads();
+      if (group >= half && group < 2 * half) {
 #pragma unroll
-          for (int j = 0; j < kLen; ++j)
-            if (c + j < s.a.width) acc[j] += src[j];
-        }
+        for (int j = 0; j < kLen; ++j) sums[(threadIdx.x - (half << s.log_g)) * kLen + j] = acc[j];
+      }
+      __syncthreads();
+      if (group < half) {
+#pragma unroll
+        for (int j = 0; j < kLen; ++j) acc[j] += sums[threadIdx.x * kLen + j];
       }
     }
-    __syncthreads();
-#pragma unroll
-    for (int j = 0; j < kLen; ++j) sums[threadIdx.x][j] = acc[j];
-    __syncthreads();
-    if (group == 0 && live) {
-      for (int q = 1; q < groups && q <= (int)(last - p); ++q)
-#pragma unroll
-        for (int j = 0; j < kLen; ++j) acc[j] += sums[(q << s.log_g) + threadIdx.x][j];
-      store_row<T, O>(s, id, c, acc);
-    }
+    if (group == 0 && live) store_row<T, O>(s, id, c, acc);
   }
 }
 
@@ -654,7 +700,7 @@ struct GradPlan {
 
 constexpr int kBigKeys = 16 * 8 * 64, kSmallKeys = 16 * 2 * 64;  // keys of a sort workgroup's step
 
-GradPlan grad_plan(int64_t n, int64_t rows, int64_t width) {
+GradPlan grad_plan(int64_t n, int64_t rows, int64_t width, int len) {
   GradPlan p{};
   auto align = [](size_t b) { return (b + 255) & ~(size_t)255; };
   p.few = n > 0 && width >= 1 && width <= kFewWidth && rows >= 1 && rows * width <= kFewCells;
@@ -673,7 +719,10 @@ GradPlan grad_plan(int64_t n, int64_t rows, int64_t width) {
   const int64_t step = p.big ? kBigKeys : kSmallKeys;
   p.subs = (uint32_t)std::max<int64_t>(1, (n + step * kMaxTiles - 1) / (step * kMaxTiles));
   p.tiles = (uint32_t)((n + step * p.subs - 1) / (step * p.subs));
-  p.piece = 32;
+  // Long pieces leave few parts, short ones more lanes at work: as long as
+  // 32,768 lanes (two waves a CU) have one each.
+  const int64_t vecs = (width + len - 1) / len;
+  p.piece = (uint32_t)std::min<int64_t>(32, std::max<int64_t>(8, n * vecs / 32768 / 8 * 8));
   p.pieces = (uint32_t)((n + p.piece - 1) / p.piece);
   const size_t list = align((size_t)n * 4);
   p.keys = 2 * list;
@@ -712,7 +761,7 @@ constexpr int64_t kClearBytes = (int64_t)40 << 20;
 
 template <typename T, typename O>
 hipError_t launch_grad(const EmbedGradArgs &a, void *ws, hipStream_t st) {
-  const GradPlan g = grad_plan(a.n, a.table_rows, a.width);
+  const GradPlan g = grad_plan(a.n, a.table_rows, a.width, Vec<T>::kLen);
   if (g.few) return launch_few<T, O>(a, g, ws, st);
   char *base = static_cast<char *>(ws);
   uint32_t *list[2] = {reinterpret_cast<uint32_t *>(base),
@@ -733,11 +782,12 @@ hipError_t launch_grad(const EmbedGradArgs &a, void *ws, hipStream_t st) {
   if (a.n > 0 && a.n <= kOneSort) {
     const OneSort p = {a.ids, list[0], list[0] + half, (uint32_t)a.n, (uint32_t)a.table_rows,
                        g.passes, g.bits};
+    auto *kernel = a.table_rows < (1 << (32 - kOneBits)) ? sort_one<true> : sort_one<false>;
     const hipError_t e =
-        ensure_dynamic_lds(reinterpret_cast<const void *>(sort_one), kOneSort * sizeof(uint32_t));
+        ensure_dynamic_lds(reinterpret_cast<const void *>(kernel), kOneSort * sizeof(uint32_t));
     if (e != hipSuccess) return e;
     const Clear f = clear(0, 1);
-    sort_one<<<1 + f.blocks, 1024, (size_t)((a.n + 1023) / 1024) * 4096, st>>>(p, f);
+    kernel<<<1 + f.blocks, 1024, (size_t)((a.n + 1023) / 1024) * 4096, st>>>(p, f);
   }
   for (int pass = 0; pass < g.passes && a.n > kOneSort; ++pass) {
     SortPass p{};
@@ -781,18 +831,16 @@ hipError_t launch_grad(const EmbedGradArgs &a, void *ws, hipStream_t st) {
   s.cleared = (uint32_t)cleared;
   s.split = s.pieces > 1 ? s.cleared + (s.rows - s.cleared) / 2 : s.rows;
   const uint32_t clear1 = (s.split - s.cleared + kThreads - 1) / kThreads;
-  const uint32_t clear2 = (s.rows - s.split + kThreads - 1) / kThreads;
+  const uint32_t clear2 = (s.rows - s.split + kJoinThreads - 1) / kJoinThreads;
   const size_t lds = (size_t)per * (g.piece + 1) * 8;
   const hipError_t e = ensure_dynamic_lds(reinterpret_cast<const void *>(sum_kernel<T, O>), lds);
   if (e != hipSuccess) return e;
   if (s.sum_blocks + clear1 > 0)
     sum_kernel<T, O><<<s.sum_blocks + clear1, kThreads, lds, st>>>(s);
   if (s.pieces > 1) {
-    // a workgroup joins its runs one after the other: few pieces each while
-    // that keeps the launch short
-    s.join = s.pieces <= 16384 ? 2 : 16;
-    s.join_blocks = (s.pieces + s.join - 1) / s.join * s.slabs;
-    join_kernel<T, O><<<s.join_blocks + clear2, kThreads, 0, st>>>(s);
+    const uint32_t join = kJoinThreads >> s.log_g;
+    s.join_blocks = (s.pieces + join - 1) / join * s.slabs;
+    join_kernel<T, O><<<s.join_blocks + clear2, kJoinThreads, 0, st>>>(s);
   }
   return hipGetLastError();
 }
@@ -818,7 +866,9 @@ hipError_t launch_embed(int dtype, const EmbedArgs &a, int cu_count, hipStream_t
 }
 
 size_t embed_grad_workspace_bytes(int64_t n, int64_t table_rows, int64_t width) {
-  return std::max<size_t>(256, grad_plan(n, table_rows, width).bytes);
+  // the type is not known here: vectors of 16-bit elements make the shorter pieces
+  return std::max<size_t>(256, std::max(grad_plan(n, table_rows, width, 4).bytes,
+                                        grad_plan(n, table_rows, width, 8).bytes));
 }
 
 hipError_t launch_embed_grad(int dtype, int grad_dtype, const EmbedGradArgs &a, void *ws,
