@@ -46,6 +46,7 @@ constexpr int kSegments = 32;       // of a row's list, at most
 constexpr int kOpen = 1024;         // list entries that collect_kernel gathers before it adds them
 constexpr int kFewDraws = 32;       // draws a row that finish_kernel makes itself
 constexpr int kRowMost = 16384;     // entries of a row in one workgroup's LDS
+constexpr int kRanked = 128;        // list entries that are ranked against one another
 constexpr int kRowList = 512;       // open entries of a short row held apart
 constexpr int kBatch = 1024;        // long rows of one set of launches
 constexpr float kLowest = -22.25f;  // exp(z) * 2^31 rounds to 0 below -22.181
@@ -329,6 +330,7 @@ struct Bins {
   u64 k_above, k_mass;  // better bins' count and weight
   u64 all;         // all bins' weight
   int sure, last;
+  u64 sure_mass;   // weight of bins better than `sure`
 };
 
 __device__ __forceinline__ bool limited(const RowLimits &l, int64_t n) {
@@ -340,7 +342,7 @@ __device__ __forceinline__ bool limited(const RowLimits &l, int64_t n) {
 template <typename C, typename W>
 __device__ __forceinline__ Bins settle(Search &s, const RowLimits &l, int64_t n, int bins,
                                        bool everything, C counted, W weighed) {
-  Bins b = {bins, 0, 0, 0, bins, -1};
+  Bins b = {bins, 0, 0, 0, bins, -1, 0};
   if (l.k < n) {
     const u64 entries = block_find(s, bins, [&](u64) { return (u64)l.k; }, 0, counted);
     if ((u64)l.k < entries) {
@@ -358,13 +360,17 @@ __device__ __forceinline__ Bins settle(Search &s, const RowLimits &l, int64_t n,
   } else if (l.p < 2.0f) {
     if (b.k_bin < bins) {
       // between the weight of better bins and that with the cut's own
-      b.k_mass = block_find(s, b.k_bin, share, 0, weighed);
-      b.sure = min(s.bin < 0 ? 0 : s.bin, b.sure);
+      b.k_mass = b.sure_mass = block_find(s, b.k_bin, share, 0, weighed);
+      if (s.bin >= 0) {  // (no weight above the cut's bin: that one is the first)
+        b.sure = s.bin;
+        b.sure_mass = s.above;
+      }
       __syncthreads();
       block_find(s, b.k_bin + 1, share, 0, weighed);
     } else {
       b.all = block_find(s, bins, share, 0, weighed);
-      b.sure = min(s.bin, b.sure);
+      b.sure = s.bin;
+      b.sure_mass = s.above;
     }
     b.last = min(s.bin, b.k_bin < bins ? b.k_bin : bins - 1);
     __syncthreads();
@@ -411,6 +417,60 @@ __device__ __forceinline__ u64 find_cuts(Search &s, const RowLimits &l, const Bi
       if (q && (p_bin < 0 || bin == p_bin) && key >= from) f(key, q);
     });
   });
+}
+
+// The same for a list of at most kRanked entries in LDS, one a thread: every
+// entry adds up those before it, which come from the wave's own registers, 64
+// at a time.  Steps without a barrier are quicker than the splitting of
+// intervals, which has seven a level.
+__device__ __forceinline__ u64 rank_cuts(Search &s, const RowLimits &l, const Bins &b, int bins,
+                                         bool everything, int open, const u64 *keys,
+                                         const uint32_t *qs, const uint16_t *bin_of_entry) {
+  const int e = threadIdx.x;
+  const u64 key = e < open ? keys[e] : 0;
+  const int bin = e < open ? bin_of_entry[e] : bins;
+  const uint32_t q = e < open ? qs[e] : 0;
+  u64 before = b.k_above, mass = b.sure_mass;
+  const int lane = threadIdx.x & 63;
+  if (e - lane < open) {
+    for (int j0 = 0; j0 < open; j0 += 64) {
+      const int mine = j0 + lane;
+      const u64 theirs = mine < open ? keys[mine] : 0;  // below every key
+      const uint32_t weight_of = mine < open ? qs[mine] : 0;
+      const u64 in_bin = __ballot(mine < open && bin_of_entry[mine] == b.k_bin);
+#pragma unroll 8
+      for (int j = 0; j < 64; ++j) {
+        const bool better = from_lane(theirs, j) > key;
+        mass += better ? from_lane(weight_of, j) : 0u;
+        if ((in_bin >> j) & 1) before += better ? 1u : 0u;
+      }
+    }
+  }
+  // kept by top-k
+  bool kept = e < open && (b.k_bin == bins || bin < b.k_bin || (bin == b.k_bin && before < (u64)l.k));
+  if (threadIdx.x == 0) s.lo = ~0ull;
+  if (l.p < 2.0f) {
+    u64 total = b.all;
+    if (everything || b.k_bin < bins) {
+      block_prefix(kept && (everything || bin == b.k_bin) ? q : 0u, s.wave_sum, &total);
+      total += everything ? 0 : b.k_mass;
+    }
+    kept = kept && q != 0 && bin >= b.sure && bin <= b.last && mass < share_of(l.p, total);
+  }
+  __syncthreads();
+  const u64 least = wave_fold(kept ? key : ~0ull, ~0ull, [](u64 a, u64 b) { return min(a, b); });
+  if ((threadIdx.x & 63) == 63 && least != ~0ull) atomicMin(&s.lo, least);
+  __syncthreads();
+  // None of the list kept: all that is kept lies in better bins, whose keys are larger.
+  const u64 cut = s.lo;
+  if (cut != ~0ull) return cut;
+  const u64 most = wave_fold(e < open ? key : 0, 0ull, [](u64 a, u64 b) { return max(a, b); });
+  __syncthreads();
+  if (threadIdx.x == 0) s.hi = 0;
+  __syncthreads();
+  if ((threadIdx.x & 63) == 63) atomicMax(&s.hi, most);
+  __syncthreads();
+  return s.hi + 1;
 }
 
 // floor(u * total), kept inside [0, total).
@@ -544,11 +604,14 @@ __global__ __launch_bounds__(1024) void row_kernel(SampleArgs a) {
     });
     __syncthreads();
     const int open = (int)listed;
-    cut = find_cuts(s, l, b, kSub, false, weighed, [&](auto f) {
-      if (open > kRowList) return each_open(f);
+    if (open <= min(kRanked, threads))
+      cut = rank_cuts(s, l, b, kSub, false, open, list_key, list_q, list_bin);
+    else
+      cut = find_cuts(s, l, b, kSub, false, weighed, [&](auto f) {
+        if (open > kRowList) return each_open(f);
 #pragma unroll 1
-      for (int e = t; e < open; e += threads) f(list_key[e], list_q[e], (int)list_bin[e]);
-    });
+        for (int e = t; e < open; e += threads) f(list_key[e], list_q[e], (int)list_bin[e]);
+      });
     __syncthreads();
   }
 
@@ -794,7 +857,7 @@ __global__ __launch_bounds__(512) void settle_kernel(Long k) {
     if (threadIdx.x == 0) k.state[r].l = l;
     return;
   }
-  Bins b = {kBins, 0, 0, 0, kBins, -1};
+  Bins b = {kBins, 0, 0, 0, kBins, -1, 0};
   if (limited(l, k.a.s.n))
     b = settle(s, l, k.a.s.n, kBins, lists_all(l), [&](int j) { return (u64)count[j]; },
                [&](int j) { return mass[j]; });
@@ -1087,7 +1150,10 @@ __global__ __launch_bounds__(1024) void finish_kernel(Long k) {
         }
       }
     };
-    cut = find_cuts(sh.s, l, b, kBins, everything, [&](int j) { return sh.mass[j]; }, each);
+    if (fits && listed <= (uint32_t)min(kRanked, threads))
+      cut = rank_cuts(sh.s, l, b, kBins, everything, (int)listed, sh.keys, sh.q, sh.bin);
+    else
+      cut = find_cuts(sh.s, l, b, kBins, everything, [&](int j) { return sh.mass[j]; }, each);
     __syncthreads();
     // the listed entries that are kept join their tiles
     each([&](u64 key, uint32_t q, int bin) {
