@@ -89,6 +89,12 @@ struct Rows {
   int64_t chunks;
 };
 
+enum Mode { kForward, kGradient, kGradientPastCache };
+
+// A gradient of more bytes than this (half of the last cache) is written past
+// the caches: 4,096 x 50,021 bf16 207 -> 191 us.
+constexpr int64_t kPastCache = (int64_t)128 << 20;
+
 template <typename T>
 __device__ __forceinline__ const T *row_scores(const Rows &k, int64_t row) {
   return static_cast<const T *>(k.a.s.scores) + row * k.a.s.ld;
@@ -229,10 +235,11 @@ __device__ __forceinline__ void at_targets(const Rows &k, int64_t row, unsigned 
 // VECS vectors of 16 bytes a thread, as they came (64 registers a lane in all:
 // eight waves on a SIMD).  hold() keeps the compiler from carrying a pass's
 // float32 values over to the next one.
-template <typename T, int VECS, bool GRAD>
+template <typename T, int VECS, Mode MODE>
 __global__ __launch_bounds__(1024, 8) void row_kernel(Rows k) {
   using V = typename Vec<T>::type;
   typedef uint32_t Raw __attribute__((ext_vector_type(4)));
+  constexpr bool GRAD = MODE != kForward;
   constexpr int kLen = Vec<T>::kLen;
   Raw raw[VECS];
   auto get = [&](int g) { return __builtin_bit_cast(V, raw[g]); };
@@ -348,7 +355,10 @@ __global__ __launch_bounds__(1024, 8) void row_kernel(Rows k) {
       for (int j = 0; j < kLen; ++j)
         o[j] = narrow<T>(__builtin_amdgcn_exp2f(__builtin_fmaf((float)v[j], c, -b)) * fit);
       if (i + kLen <= n) {
-        *reinterpret_cast<V *>(grad + i) = o;
+        if constexpr (MODE == kGradientPastCache)
+          __builtin_nontemporal_store(o, reinterpret_cast<V *>(grad + i));
+        else
+          *reinterpret_cast<V *>(grad + i) = o;
       } else {
 #pragma unroll
         for (int j = 0; j < kLen; ++j)
@@ -494,14 +504,15 @@ hipError_t launch_row(const Rows &k, hipStream_t s) {
   const int64_t vecs = (k.a.s.n + Vec<T>::kLen - 1) / Vec<T>::kLen;
   const int threads = (int)std::max<int64_t>(64, ((vecs + VECS - 1) / VECS + 63) / 64 * 64);
   if (!k.a.grad) {
-    row_kernel<T, VECS, false><<<(uint32_t)k.a.s.rows, threads, 0, s>>>(k);
+    row_kernel<T, VECS, kForward><<<(uint32_t)k.a.s.rows, threads, 0, s>>>(k);
     return hipGetLastError();
   }
+  auto *kernel = k.a.s.rows * k.a.s.n * (int64_t)sizeof(T) > kPastCache
+                     ? row_kernel<T, VECS, kGradientPastCache> : row_kernel<T, VECS, kGradient>;
   const size_t lds = list_bytes(k.a.per_row);
-  const hipError_t e =
-      ensure_dynamic_lds(reinterpret_cast<const void *>(row_kernel<T, VECS, true>), lds);
+  const hipError_t e = ensure_dynamic_lds(reinterpret_cast<const void *>(kernel), lds);
   if (e != hipSuccess) return e;
-  row_kernel<T, VECS, true><<<(uint32_t)k.a.s.rows, threads, lds, s>>>(k);
+  kernel<<<(uint32_t)k.a.s.rows, threads, lds, s>>>(k);
   return hipGetLastError();
 }
 
