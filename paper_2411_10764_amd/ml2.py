@@ -184,8 +184,10 @@ def _ptr(x):
 
 def _stream(stream):
     if stream is None:
+        # torch.cuda.current_stream() makes an object first, which takes longer
+        # than the rest of a call
         import torch
-        return torch.cuda.current_stream().cuda_stream
+        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
     if isinstance(stream, int):
         return stream
     return stream.cuda_stream
