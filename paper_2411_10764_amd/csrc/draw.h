@@ -71,6 +71,47 @@ hipError_t launch_embed_grad(int dtype, int grad_dtype, const EmbedGradArgs &a, 
 
 // ---- device helpers ---------------------------------------------------------
 
+typedef unsigned long long u64;
+
+// v of the lane that the DPP control names, `none` where there is none.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ uint32_t lane_move(uint32_t v, uint32_t none) {
+  return (uint32_t)__builtin_amdgcn_update_dpp((int)none, (int)v, CTRL, ROWS, 0xF, false);
+}
+
+template <int CTRL, int ROWS>
+__device__ __forceinline__ u64 lane_move(u64 v, u64 none) {
+  return ((u64)lane_move<CTRL, ROWS>((uint32_t)(v >> 32), (uint32_t)(none >> 32)) << 32) |
+         lane_move<CTRL, ROWS>((uint32_t)v, (uint32_t)none);
+}
+
+// Folds v over the lanes up to and including the own one (DPP moves: shifts
+// inside rows of 16 lanes, then the rows' last lanes; an LDS shuffle a step
+// takes several times as long).  `none`: the neutral value.
+template <typename V, typename F>
+__device__ __forceinline__ V wave_fold(V v, V none, F f) {
+  v = f(v, lane_move<0x111, 0xF>(v, none));
+  v = f(v, lane_move<0x112, 0xF>(v, none));
+  v = f(v, lane_move<0x114, 0xF>(v, none));
+  v = f(v, lane_move<0x118, 0xF>(v, none));
+  v = f(v, lane_move<0x142, 0xA>(v, none));
+  return f(v, lane_move<0x143, 0xC>(v, none));
+}
+
+template <typename V>
+__device__ __forceinline__ V wave_prefix(V v) {  // inclusive
+  return wave_fold(v, (V)0, [](V a, V b) { return a + b; });
+}
+
+__device__ __forceinline__ u64 from_lane(u64 v, int lane) {
+  return ((u64)(uint32_t)__builtin_amdgcn_readlane((int)(v >> 32), lane) << 32) |
+         (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)v, lane);
+}
+
+__device__ __forceinline__ uint32_t from_lane(uint32_t v, int lane) {
+  return (uint32_t)__builtin_amdgcn_readlane((int)v, lane);
+}
+
 // Vectors of 16 bytes that need the alignment of one element only (the memory
 // system takes any address; the type keeps the compiler from assuming more).
 template <typename T>

@@ -47,39 +47,37 @@ __device__ __forceinline__ float weight_of(float x, float m, float c) {
   return fminf(__builtin_amdgcn_exp2f((x - m) * c), 1.0f);
 }
 
-__device__ __forceinline__ Stat join(Stat a, Stat b, float c) {
-  if (b.m == ninf()) return a;
-  if (a.m == ninf()) return b;
-  const float m = fmaxf(a.m, b.m);
-  return {m, a.l * weight_of(a.m, m, c) + b.l * weight_of(b.m, m, c)};
-}
-
-// The workgroup's pairs joined (in thread order pairs of a tree); the result
-// in every thread.
-__device__ __forceinline__ Stat block_join(Stat s, float c, Stat *lds) {
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const Stat o = {__shfl_xor(s.m, d), __shfl_xor(s.l, d)};
-    s = (threadIdx.x & d) ? join(o, s, c) : join(s, o, c);
-  }
-  const int waves = blockDim.x >> 6;
+// Maximum and sum over the workgroup, in every thread; sums in the order of
+// the lanes and then of the waves.  They begin with the barrier that frees lds.
+__device__ __forceinline__ float block_max(float v, float *lds) {
+  const uint32_t none = __float_as_uint(ninf());
+  v = __uint_as_float(wave_fold(__float_as_uint(v), none, [](uint32_t a, uint32_t b) {
+    return __float_as_uint(fmaxf(__uint_as_float(a), __uint_as_float(b)));
+  }));
   __syncthreads();
-  if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = s;
+  if ((threadIdx.x & 63) == 63) lds[threadIdx.x >> 6] = v;
   __syncthreads();
-  s = lds[0];
-  for (int w = 1; w < waves; ++w) s = join(s, lds[w], c);
-  return s;
+  v = lds[0];
+  for (int w = 1; w < (int)blockDim.x >> 6; ++w) v = fmaxf(v, lds[w]);
+  return v;
 }
 
 __device__ __forceinline__ float block_sum(float v, float *lds) {
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) v += __shfl_xor(v, d);
+  v = __uint_as_float(wave_fold(__float_as_uint(v), 0u, [](uint32_t a, uint32_t b) {
+    return __float_as_uint(__uint_as_float(a) + __uint_as_float(b));
+  }));
   __syncthreads();
-  if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
+  if ((threadIdx.x & 63) == 63) lds[threadIdx.x >> 6] = v;
   __syncthreads();
   v = lds[0];
   for (int w = 1; w < (int)blockDim.x >> 6; ++w) v += lds[w];
   return v;
+}
+
+// The threads' pairs as one: their maximum, and their sums brought to it.
+__device__ __forceinline__ Stat block_join(Stat s, float c, float *lds) {
+  const float m = block_max(s.m, lds);
+  return {m, block_sum(s.m == ninf() ? 0.0f : s.l * weight_of(s.m, m, c), lds)};
 }
 
 struct Rows {
@@ -300,11 +298,7 @@ __global__ __launch_bounds__(1024, 8) void row_kernel(Rows k) {
     for (int j = 0; j < kLen; ++j) m = fmaxf(m, (float)v[j]);  // a NaN never is the larger
   }
   hold();
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) m = fmaxf(m, __shfl_xor(m, d));
-  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = m;
-  __syncthreads();
-  for (int w = 0; w < threads >> 6; ++w) m = fmaxf(m, red[w]);
+  m = block_max(m, red);
 
   // exp2(s * c - b) with b = m * c rounded: one fused operation an entry.
   // What b is off by is put right in l.  NaN scores, infinite maxima and
@@ -380,7 +374,6 @@ __global__ __launch_bounds__(1024, 8) void row_kernel(Rows k) {
 
 template <typename T, bool GRAD>
 __global__ __launch_bounds__(kThreads) void stats_kernel(Rows k) {
-  __shared__ Stat lds[kThreads / 64];
   __shared__ float red[kThreads / 64];
   __shared__ int waves_at[kThreads / 64];
   extern __shared__ unsigned long long list[];
@@ -391,9 +384,19 @@ __global__ __launch_bounds__(kThreads) void stats_kernel(Rows k) {
   bool greedy;
   const float c = inverse_temperature(k.a.s.temperature, row, &greedy) * kLog2e;
   Stat s = {ninf(), 0.0f};
+  float next[8];
+  load8(scores, valid, lo + threadIdx.x * 8, hi, next);
+  float w = 0.0f;
+  if constexpr (GRAD) {
+    const int count = list_targets(k.a.targets + row * k.a.per_row, k.a.per_row, lo, hi, list,
+                                   waves_at);
+    w = listed_weight<T>(k, row, k.a.weight + row * k.a.per_row, list, count, red);
+  }
   for (int64_t i = lo + threadIdx.x * 8; i < hi; i += kThreads * 8) {
     float x[8];
-    load8(scores, valid, i, hi, x);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) x[j] = next[j];
+    load8(scores, valid, i + kThreads * 8, hi, next);
     float m = s.m;
 #pragma unroll
     for (int j = 0; j < 8; ++j) m = fmaxf(m, x[j]);
@@ -403,38 +406,34 @@ __global__ __launch_bounds__(kThreads) void stats_kernel(Rows k) {
     for (int j = 0; j < 8; ++j) l += x[j] == ninf() ? 0.0f : weight_of(x[j], m, c);
     s = {m, l};
   }
-  s = block_join(s, c, lds);
-  float w = 0.0f;
-  if constexpr (GRAD) {
-    const int count = list_targets(k.a.targets + row * k.a.per_row, k.a.per_row, lo, hi, list,
-                                   waves_at);
-    w = listed_weight<T>(k, row, k.a.weight + row * k.a.per_row, list, count, red);
-  }
+  s = block_join(s, c, red);
   if (threadIdx.x == 0) k.part[blockIdx.x] = {s, w};
 }
 
 // The row's maximum, sum and weights, in every thread.
-__device__ __forceinline__ Part row_part(const Rows &k, int64_t row, float c, Stat *lds,
-                                         float *red) {
+__device__ __forceinline__ Part row_part(const Rows &k, int64_t row, float c, float *red) {
   Part p = {{ninf(), 0.0f}, 0.0f};
   for (int64_t i = threadIdx.x; i < k.chunks; i += blockDim.x) {
     const Part o = k.part[row * k.chunks + i];
-    p.s = join(p.s, o.s, c);
+    if (o.s.m != ninf()) {
+      const float m = fmaxf(p.s.m, o.s.m);
+      const float l = p.s.m == ninf() ? 0.0f : p.s.l * weight_of(p.s.m, m, c);
+      p.s = {m, l + o.s.l * weight_of(o.s.m, m, c)};
+    }
     p.w += o.w;
   }
-  p.s = block_join(p.s, c, lds);
-  p.w = block_sum(p.w, red);
+  p.s = block_join(p.s, c, red);
+  if (k.a.grad) p.w = block_sum(p.w, red);
   return p;
 }
 
 template <typename T>
 __global__ __launch_bounds__(kThreads) void finish_kernel(Rows k) {
-  __shared__ Stat lds[kThreads / 64];
   __shared__ float red[kThreads / 64];
   const int64_t row = blockIdx.x;
   bool greedy;
   const float r = inverse_temperature(k.a.s.temperature, row, &greedy);
-  const Part p = row_part(k, row, r * kLog2e, lds, red);
+  const Part p = row_part(k, row, r * kLog2e, red);
   for (int j = threadIdx.x; j < k.a.per_row; j += kThreads) {
     const int64_t t = k.a.targets[row * k.a.per_row + j];
     k.a.logprob[row * k.a.per_row + j] =
@@ -445,7 +444,6 @@ __global__ __launch_bounds__(kThreads) void finish_kernel(Rows k) {
 template <typename T>
 __global__ __launch_bounds__(kThreads) void grad_kernel(Rows k) {
   typedef T V __attribute__((ext_vector_type(8), aligned(sizeof(T))));
-  __shared__ Stat lds[kThreads / 64];
   __shared__ float red[kThreads / 64];
   __shared__ int waves_at[kThreads / 64];
   extern __shared__ unsigned long long list[];
@@ -456,13 +454,15 @@ __global__ __launch_bounds__(kThreads) void grad_kernel(Rows k) {
   bool greedy;
   const float r = inverse_temperature(k.a.s.temperature, row, &greedy), c = r * kLog2e;
   const int32_t *targets = k.a.targets + row * k.a.per_row;
-  const Part p = row_part(k, row, c, lds, red);
+  // what does not wait for the row's sum first: its first scores, its targets
+  float x[8];
+  load8(scores, valid, lo + threadIdx.x * 8, hi, x);
+  const int count = list_targets(targets, k.a.per_row, lo, hi, list, waves_at);
+  const Part p = row_part(k, row, c, red);
   if (chunk == 0 && k.a.logprob) outside(k, row);
   const float scale = -p.w / p.s.l * r;
   T *grad = static_cast<T *>(k.a.grad) + row * k.a.grad_ld;
   for (int64_t i = lo + threadIdx.x * 8; i < hi; i += kThreads * 8) {
-    float x[8];
-    load8(scores, valid, i, hi, x);
     V o;
 #pragma unroll
     for (int j = 0; j < 8; ++j)
@@ -474,8 +474,9 @@ __global__ __launch_bounds__(kThreads) void grad_kernel(Rows k) {
       for (int j = 0; j < 8; ++j)
         if (i + j < hi) grad[i + j] = o[j];
     }
+    load8(scores, valid, i + kThreads * 8, hi, x);
   }
-  const int count = list_targets(targets, k.a.per_row, lo, hi, list, waves_at);
+  __syncthreads();
   at_targets<T>(k, row, list, count, p.s, r, scale);
 }
 

@@ -52,8 +52,6 @@ constexpr int kBatch = 1024;        // long rows of one set of launches
 constexpr float kLowest = -22.25f;  // exp(z) * 2^31 rounds to 0 below -22.181
 constexpr float kOne = 2147483648.0f;
 
-typedef unsigned long long u64;
-
 __device__ __forceinline__ uint32_t ordered(float x) {  // x is not NaN
   const uint32_t b = __float_as_uint(x + 0.0f);  // -0.0 is +0.0
   return (b & 0x80000000u) ? ~b : (b | 0x80000000u);
@@ -167,45 +165,6 @@ __device__ __forceinline__ int bin_of(float z, float scale) {
 __device__ __forceinline__ u64 share_of(float p, u64 total) {
   const double share = ceil((double)p * (double)total);
   return share >= 1.0 ? (u64)share : 1ull;
-}
-
-// v of the lane that the DPP control names, `none` where there is none.
-template <int CTRL, int ROWS>
-__device__ __forceinline__ uint32_t lane_move(uint32_t v, uint32_t none) {
-  return (uint32_t)__builtin_amdgcn_update_dpp((int)none, (int)v, CTRL, ROWS, 0xF, false);
-}
-
-template <int CTRL, int ROWS>
-__device__ __forceinline__ u64 lane_move(u64 v, u64 none) {
-  return ((u64)lane_move<CTRL, ROWS>((uint32_t)(v >> 32), (uint32_t)(none >> 32)) << 32) |
-         lane_move<CTRL, ROWS>((uint32_t)v, (uint32_t)none);
-}
-
-// Folds v over the lanes up to and including the own one (DPP moves: shifts
-// inside rows of 16 lanes, then the rows' last lanes; an LDS shuffle a step
-// takes several times as long).  `none`: the neutral value.
-template <typename V, typename F>
-__device__ __forceinline__ V wave_fold(V v, V none, F f) {
-  v = f(v, lane_move<0x111, 0xF>(v, none));
-  v = f(v, lane_move<0x112, 0xF>(v, none));
-  v = f(v, lane_move<0x114, 0xF>(v, none));
-  v = f(v, lane_move<0x118, 0xF>(v, none));
-  v = f(v, lane_move<0x142, 0xA>(v, none));
-  return f(v, lane_move<0x143, 0xC>(v, none));
-}
-
-template <typename V>
-__device__ __forceinline__ V wave_prefix(V v) {  // inclusive
-  return wave_fold(v, (V)0, [](V a, V b) { return a + b; });
-}
-
-__device__ __forceinline__ u64 from_lane(u64 v, int lane) {
-  return ((u64)(uint32_t)__builtin_amdgcn_readlane((int)(v >> 32), lane) << 32) |
-         (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)v, lane);
-}
-
-__device__ __forceinline__ uint32_t from_lane(uint32_t v, int lane) {
-  return (uint32_t)__builtin_amdgcn_readlane((int)v, lane);
 }
 
 // Exclusive sum over the threads of a workgroup of at most 16 waves; *all: the
