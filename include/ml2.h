@@ -391,6 +391,8 @@ ml2_status ml2_stream_explorer_end(ml2_stream_explorer *ex, int32_t *out_idx, fl
  *   z_i = 0 where s_i == m, else (s_i - m) * R.
  * temperature, top_k, top_p, min_p: device arrays [rows], or NULL for
  * T = 1 and no such limit.  A row without an included entry is not an error.
+ * Like the calls above these only enqueue kernels, allocate nothing and may be
+ * captured into a HIP graph once each has run outside the capture.
  */
 typedef enum { ML2_F32 = 0, ML2_BF16 = 1, ML2_F16 = 2 } ml2_dtype;
 

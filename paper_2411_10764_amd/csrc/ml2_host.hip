@@ -259,7 +259,10 @@ hipError_t ensure_dynamic_lds(const void *fn, size_t bytes) {
     if ((int)v.size() <= dev) v.resize((size_t)dev + 1, 0);
     if (bytes > v[(size_t)dev]) {
       e = hipFuncSetAttribute(fn, hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
-      if (e != hipSuccess) return e;
+      if (e != hipSuccess) {
+        (void)hipGetLastError();  // the caller learns of it here, not from its next HIP call
+        return e;
+      }
       v[(size_t)dev] = bytes;
     }
   } catch (const std::bad_alloc &) {

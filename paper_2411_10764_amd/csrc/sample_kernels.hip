@@ -45,7 +45,7 @@ constexpr int kList = 4096;         // list entries held in LDS
 constexpr int kSegments = 32;       // of a row's list, at most
 constexpr int kOpen = 1024;         // list entries that collect_kernel gathers before it adds them
 constexpr int kFewDraws = 32;       // draws a row that finish_kernel makes itself
-constexpr int kRowMost = 16384;     // entries of a row in one workgroup's LDS
+constexpr int kRowMost = 14336;     // entries of a row in one workgroup's LDS, 9 bytes each
 constexpr int kRanked = 128;        // list entries that are ranked against one another
 constexpr int kRowList = 512;       // open entries of a short row held apart
 constexpr int kBatch = 1024;        // long rows of one set of launches

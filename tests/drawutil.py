@@ -35,7 +35,7 @@ def sample_row(x, valid, T, k, p, minp, u, lean=0.0):
     64 bits.  `lean` moves top-p's share by that part of the
     weight that is not exact (all but the best score's).  A draw
     is sure where its neighbours lie further off than what the float32 exp
-    (2 ulp) and the rounding of a weight (1) may move."""
+    (1 ulp) and the rounding of a weight (1) may move."""
     x = np.asarray(x, np.float32)
     ok = included(x, valid)
     d = len(u)
@@ -65,9 +65,9 @@ def sample_row(x, valid, T, k, p, minp, u, lean=0.0):
     pick = np.searchsorted(upto, want, side="right")
     low = np.where(pick > 0, upto[pick - 1], 0.0)
     high = upto[pick]
-    # weights other than the best score's may be off by 2 ulp and 1: a border
+    # weights other than the best score's may be off by 1 ulp and 1: a border
     # moves by those before it, floor(u * M) by u times those of the row
-    off = np.cumsum(np.where(z[kept] < 0, q[kept] * 2.0 ** -22 + 1, 0.0))
+    off = np.cumsum(np.where(z[kept] < 0, q[kept] * 2.0 ** -23 + 1, 0.0))
     moves = off[pick] + np.asarray(u, np.float64) * off[-1]
     sure = ((low == 0) | (want - low >= moves)) & ((high == M) | (high - want > moves))
     return kept[pick], z[kept[pick]] - math.log(M / ONE), sure
@@ -80,7 +80,7 @@ def sample(x, valid, T, k, p, minp, u):
     for r in range(x.shape[0]):
         v = None if valid is None else valid if valid.ndim == 1 else valid[r]
         a = sample_row(x[r], v, T[r], k[r], p[r], minp[r], u[r])
-        lean = [sample_row(x[r], v, T[r], k[r], p[r], minp[r], u[r], s * 2.0 ** -21)
+        lean = [sample_row(x[r], v, T[r], k[r], p[r], minp[r], u[r], s * 2.0 ** -22)
                 for s in (-1, 1)]
         idx.append(a[0])
         logp.append(a[1])

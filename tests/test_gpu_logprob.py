@@ -91,6 +91,7 @@ def _run(x, valid, targets, weight, T):
 @pytest.mark.parametrize("rows,n,d", [(1, 1, 1), (2, 2, 3), (3, 63, 5), (2, 65, 1), (5, 1000, 33),
                                       (2, 4097, 64), (300, 517, 2), (1, 50021, 17),
                                       (7, 20011, 1), (1, 300007, 1500), (600, 2048, 1),
+                                   (2, 100, 16384), (1, 50021, 16384), (1, 1000003, 5000),
                                       (2, 131072, 1), (40, 70001, 2)])
 def test_formula(dtype, rows, n, d):
     print(f"[logprob] {dtype} {rows} x {n}, {d}", flush=True)
@@ -206,3 +207,21 @@ def test_same_bits_every_run_and_in_a_graph():
             assert torch.equal(want[0], f.logprob) and torch.equal(want[1], f.grad)
             xd.mul_(0.95)
             want = [t.clone() for t in f.run_grad(xd, *dev)]
+
+
+def test_large_gradient():
+    """A gradient beyond what the caches hold (written past them): sampled rows."""
+    rows, n = 1400, 65536
+    g = torch.Generator(device=DEV)
+    g.manual_seed(3)
+    x = (torch.randn(rows, n, generator=g, device=DEV) * 2).to(torch.bfloat16)
+    targets = torch.randint(n, (rows, 2), generator=g, device=DEV, dtype=torch.int32)
+    weight = torch.randn(rows, 2, generator=g, device=DEV)
+    lp, grad = ml2.LogProb(rows, n, 2, grad_dtype=torch.bfloat16).run_grad(x, targets, weight)
+    torch.cuda.synchronize()
+    some = [0, 1, 255, 700, rows - 1]
+    xf, t, w = drawutil.as_float(x[some]), targets[some].cpu().numpy(), weight[some].cpu().numpy()
+    T = np.ones(len(some), np.float32)
+    want_lp, want = _reference(xf, None, T, t, w)
+    _check_logprob(lp[some].cpu().numpy(), want_lp)
+    _check_grad(drawutil.as_float(grad[some]), want, xf, None, T, t, w, torch.bfloat16)

@@ -3,7 +3,7 @@ together, lengths from one entry to a pool, ties, rows without an entry,
 infinities and NaN in and out of the mask, strides and alignments.
 
 The kernel's weights are whole numbers of a float32 exp, the reference's of a
-64-bit one, so a draw that falls within 2 ulp of two entries' border could go
+64-bit one, so a draw that falls within 1 ulp of two entries' border could go
 to either; such draws are left out (the reference says which) and must be
 rare.  All others must be equal.  logprob: z and log(M) are float32 values of
 magnitude up to 23 with one rounding each and logf's 1 ulp, so 4 * 2^-24 * 23
@@ -67,7 +67,8 @@ LIMITS = [dict(), dict(k=1), dict(k=7), dict(p=0.9), dict(p=0.0), dict(minp=0.05
 
 
 @pytest.mark.parametrize("dtype", TYPES)
-@pytest.mark.parametrize("n", [1, 2, 63, 64, 65, 513, 1000, 4096, 8191, 16389, 70001])
+@pytest.mark.parametrize("n", [1, 2, 63, 64, 65, 513, 1000, 4096, 8191, 14336, 14337,
+                               16384, 16389, 70001])
 def test_lengths(dtype, n):
     print(f"[sample] {dtype} n={n}", flush=True)
     rng = np.random.default_rng(n)
@@ -230,3 +231,83 @@ def test_streams_and_graph():
             assert all(torch.equal(a, b) for a, b in zip(want, (s.idx, s.logprob)))
             x.mul_(0.9)
             want = [t.clone() for t in s.run(x, u, top_p=p)]
+
+
+def _same(x, u, valid=None, **lim):
+    """The call against the definition, every draw."""
+    par = {a: np.full(x.shape[0], b) for a, b in lim.items()}
+    got = _run(torch.from_numpy(x).to(DEV), u, valid, **par)
+    _check(*got, unsure=0.3)
+
+
+@pytest.mark.parametrize("n", [3000, 16384, 16385, 120000])
+def test_long_lists(n):
+    """Cuts that the bins settle badly: thousands of nearly equal scores under
+    an outlier, so that the list beside the bins overflows and the row is read
+    again; the same with the scores sorted, all of one chunk."""
+    rng = np.random.default_rng(n)
+    x = (rng.standard_normal((1, n)) * 1e-4).astype(np.float32)
+    x[0, n // 2] = 9.0
+    u = _u(rng, 1, 40)
+    for y in (x, np.sort(x, axis=1), -np.sort(-x, axis=1)):
+        y = np.ascontiguousarray(y)
+        for lim in (dict(k=n // 2, T=3.0), dict(p=0.6, T=9.0), dict(k=n // 3, p=0.7, T=9.0),
+                    dict(k=200, T=9.0), dict(k=200, p=0.5, T=9.0)):
+            _same(y, u, **lim)
+
+
+@pytest.mark.parametrize("rows", [1, 3, 40])
+def test_sorted_rows(rows):
+    """The best scores all in one part of the row, each limit."""
+    rng = np.random.default_rng(rows)
+    n = 30000
+    x = -np.sort(-(rng.standard_normal((rows, n)) * 3).astype(np.float32), axis=1)
+    u = _u(rng, rows, 7)
+    for lim in (dict(), dict(k=50), dict(k=256), dict(k=257), dict(k=5000), dict(p=0.9),
+                dict(k=256, p=0.9), dict(k=9000, p=0.99, minp=0.01)):
+        _same(np.ascontiguousarray(x), u, **lim)
+
+
+@pytest.mark.parametrize("open_entries", [1, 2, 63, 64, 65, 127, 128, 129, 511, 513])
+def test_list_lengths(open_entries):
+    """Ties at the cut: as many entries wait for it, in short and long rows."""
+    for n in (4000, 40000):
+        rng = np.random.default_rng(n + open_entries)
+        x = np.full((1, n), -1.0, np.float32)
+        order = rng.permutation(n)
+        x[0, order[:100]] = 3.0
+        x[0, order[100:100 + open_entries]] = 1.0
+        u = _u(rng, 1, 30)
+        for lim in (dict(k=100 + (open_entries + 1) // 2), dict(k=100 + open_entries), dict(p=0.97),
+                    dict(k=99), dict(k=101 + open_entries, p=0.99)):
+            _same(x, u, **lim)
+
+
+def test_many_rows_and_batches():
+    """More long rows than one set of launches takes, some without an entry."""
+    rng = np.random.default_rng(12)
+    rows, n = 1100, 17001
+    x = torch.randn(rows, n, device=DEV) * 2
+    valid = torch.ones(rows, n, dtype=torch.uint8, device=DEV)
+    valid[::7] = 0
+    u = torch.from_numpy(_u(rng, rows, 2)).to(DEV)
+    k = torch.full((rows,), 40, dtype=torch.int32, device=DEV)
+    idx, logp = ml2.Sampler(rows, n, 2).run(x, u, valid, top_k=k)
+    torch.cuda.synchronize()
+    assert torch.all(idx[::7] == -1) and torch.all(torch.isneginf(logp[::7]))
+    some = [1, 2, 500, 1023, 1024, 1025, 1098]  # none of them masked out
+    want = drawutil.sample(x[some].cpu().numpy(), None, np.ones(7, np.float32), np.full(7, 40),
+                           np.ones(7, np.float32), np.zeros(7, np.float32), u[some].cpu().numpy())
+    _check(idx[some].cpu().numpy(), logp[some].cpu().numpy(), want)
+
+
+def test_draws_by_their_own_kernel():
+    """Few and many draws of one long row are the same draws."""
+    rng = np.random.default_rng(13)
+    x = torch.randn(2, 50000, device=DEV) * 2
+    u = torch.from_numpy(_u(rng, 2, 33)).to(DEV)
+    p = torch.full((2,), 0.9, device=DEV)
+    many = ml2.Sampler(2, 50000, 33).run(x, u, top_p=p)
+    few = ml2.Sampler(2, 50000, 32).run(x, u[:, :32].contiguous(), top_p=p)
+    torch.cuda.synchronize()
+    assert torch.equal(many[0][:, :32], few[0]) and torch.equal(many[1][:, :32], few[1])
