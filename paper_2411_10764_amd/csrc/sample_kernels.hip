@@ -186,11 +186,8 @@ __device__ __forceinline__ u64 block_prefix(u64 v, u64 *lds, u64 *all) {
 
 // State of a search for a cut, in LDS.
 struct Search {
-  uint32_t count[kSub];
-  u64 mass[kSub];
-  u64 first[kSub], last[kSub];  // smallest and largest key of a part
-  u64 lo, hi;    // interval of keys that holds the cut
-  int done;
+  u64 amount[kSub];  // count or weight of a part
+  u64 lo, hi;    // the smallest and largest key of the part that holds the cut
   u64 wave_sum[16];
   int bin;       // of block_find: the bin found, or -1
   u64 above;     // the amount of better ones
@@ -226,60 +223,77 @@ __device__ __forceinline__ u64 block_find(Search &s, int bins, N need_of, u64 ba
   return base + all;
 }
 
-// The cut among the keys that each(f) hands to f(key, weight), in which the
-// count (by_count) or weight on top of `above` reaches `need`: entries with
-// key >= the result are kept.  Every thread of the workgroup calls it, with
-// the same `above` and `need`; each() hands out one key at least.
-template <typename Each>
-__device__ __forceinline__ u64 find_cut(Search &s, bool by_count, u64 above, u64 need,
-                                        Each each) {
-  u64 first = ~0ull, last = 0;
-  each([&](u64 key, uint32_t) {
-    first = min(first, key);
-    last = max(last, key);
-  });
-  first = wave_fold(first, ~0ull, [](u64 a, u64 b) { return min(a, b); });
-  last = wave_fold(last, 0ull, [](u64 a, u64 b) { return max(a, b); });
+// Adds v (1, or an entry's weight) to amount[b] for every active lane.  Lanes of
+// one part whose v is the same, as entries of equal scores are, are one
+// addition: those of one address wait for one another.
+__device__ __forceinline__ void add_amount(u64 *amount, int b, uint32_t v) {
+  const int lane = threadIdx.x & 63;
+  for (u64 rest = __ballot(true); rest;) {
+    const int leader = __ffsll(rest) - 1;
+    const u64 same = __ballot(b == __builtin_amdgcn_readlane(b, leader) &&
+                              v == (uint32_t)__builtin_amdgcn_readlane((int)v, leader));
+    const int lanes = __popcll(same & rest);
+    if (lanes < 8) {
+      if ((rest >> lane) & 1) atomicAdd(&amount[b], (u64)v);
+      return;
+    }
+    if (lane == leader) atomicAdd(&amount[b], (u64)v * (uint32_t)lanes);
+    rest &= ~same;
+  }
+}
+
+// The cut among the keys that each(f) hands to f(key, weight(), bin()) and that
+// are at least `from` and inside(bin), in which the count (by_count) or weight
+// on top of `above` reaches `need`: entries with key >= the result are kept.
+// Keys between two that are inside are inside too.  Every thread of the
+// workgroup calls it, with the same `above` and `need`, and there is such a key.
+template <typename Each, typename In>
+__device__ __forceinline__ u64 find_cut(Search &s, bool by_count, u64 above, u64 need, u64 from,
+                                        Each each, In inside) {
+  u64 to = ~0ull;
+  bool known = false;  // that keys from .. to are inside
+  bool done = false;
   if (threadIdx.x == 0) {
     s.lo = ~0ull;
     s.hi = 0;
-    s.done = 0;
   }
-  __syncthreads();
-  if ((threadIdx.x & 63) == 63 && last) atomicMin(&s.lo, first), atomicMax(&s.hi, last);
   for (;;) {
-    for (int b = threadIdx.x; b < kSub; b += blockDim.x) {
-      s.count[b] = 0;
-      s.mass[b] = 0;
-      s.first[b] = ~0ull;
-      s.last[b] = 0;
-    }
+    for (int b = threadIdx.x; b < kSub; b += blockDim.x) s.amount[b] = 0;
+    // the smallest and largest key left
+    u64 first = ~0ull, last = 0;
+    each([&](u64 key, auto, auto bin) {
+      if (key < from || key > to || !(known || inside(bin))) return;
+      first = min(first, key);
+      last = max(last, key);
+    });
+    first = wave_fold(first, ~0ull, [](u64 a, u64 b) { return min(a, b); });
+    last = wave_fold(last, 0ull, [](u64 a, u64 b) { return max(a, b); });
+    __syncthreads();
+    if ((threadIdx.x & 63) == 63 && last) atomicMin(&s.lo, first), atomicMax(&s.hi, last);
     __syncthreads();
     const u64 lo = s.lo, hi = s.hi;
-    if (s.done || lo >= hi) break;
+    if (done || lo >= hi) return lo;  // all of the part is kept, or one entry
     const int width = 64 - __clzll(hi - lo);
     const int shift = max(0, width - 9);
-    each([&](u64 key, uint32_t q) {
+    each([&](u64 key, auto weight, auto) {
       if (key < lo || key > hi) return;
-      const int b = kSub - 1 - (int)((key - lo) >> shift);  // best first
-      atomicAdd(&s.count[b], 1u);
-      if (!by_count) atomicAdd(&s.mass[b], (u64)q);
-      atomicMin(&s.first[b], key);
-      atomicMax(&s.last[b], key);
+      // best first
+      add_amount(s.amount, kSub - 1 - (int)((key - lo) >> shift), by_count ? 1u : weight());
     });
     __syncthreads();
-    block_find(s, kSub, [&](u64) { return need; }, above, [&](int b) { return by_count ? (u64)s.count[b] : s.mass[b]; });
+    if (threadIdx.x == 0) {
+      s.lo = ~0ull;
+      s.hi = 0;
+    }
+    block_find(s, kSub, [&](u64) { return need; }, above, [&](int b) { return s.amount[b]; });
     const int b = s.bin < 0 ? kSub - 1 : s.bin;  // the amount is always reached
     above = s.above;
-    if (threadIdx.x == 0) {
-      s.lo = s.first[b];
-      s.hi = s.last[b];
-      // one entry, or all of the part is kept
-      s.done = s.count[b] <= 1 || above + (by_count ? (u64)s.count[b] : s.mass[b]) == need;
-    }
+    done = above + s.amount[b] == need;
+    known = true;
+    from = lo + ((u64)(kSub - 1 - b) << shift);
+    to = from + min((1ull << shift) - 1, ~from);
     __syncthreads();
   }
-  return s.lo;
 }
 
 // What the bins settle: entries of bins better than `sure` are kept, those of
@@ -337,25 +351,23 @@ __device__ __forceinline__ Bins settle(Search &s, const RowLimits &l, int64_t n,
   return b;
 }
 
-// The cut of both limits.  each(f) calls f(key, weight, bin) for the listed entries.
+// The cut of both limits.  each(f) calls f(key, weight, bin) for the listed
+// entries, where weight() and bin() are only worked out where they are needed.
 template <typename W, typename Each>
 __device__ __forceinline__ u64 find_cuts(Search &s, const RowLimits &l, const Bins &b, int bins,
                                          bool everything, W weighed, Each each) {
   u64 cut = 0;
   if (b.k_bin < bins)
-    cut = find_cut(s, true, b.k_above, (u64)l.k, [&](auto f) {
-      each([&](u64 key, uint32_t q, int bin) {
-        if (bin == b.k_bin) f(key, q);
-      });
-    });
+    cut = find_cut(s, true, b.k_above, (u64)l.k, 0, each,
+                   [&](auto bin) { return bin() == b.k_bin; });
   if (!(l.p < 2.0f)) return cut;
   __syncthreads();
   // the weight that top-k keeps: better bins' and the listed entries'
   u64 total = b.all;
   if (everything || b.k_bin < bins) {
     u64 part = 0;
-    each([&](u64 key, uint32_t q, int bin) {
-      if (key >= cut && (everything || bin == b.k_bin)) part += q;
+    each([&](u64 key, auto q, auto bin) {
+      if (key >= cut && (everything || bin() == b.k_bin)) part += q();
     });
     block_prefix(part, s.wave_sum, &total);
     total += everything ? 0 : b.k_mass;
@@ -370,12 +382,8 @@ __device__ __forceinline__ u64 find_cuts(Search &s, const RowLimits &l, const Bi
     above = s.above;
     __syncthreads();
   }
-  const u64 from = cut;
-  return find_cut(s, false, above, share, [&](auto f) {
-    each([&](u64 key, uint32_t q, int bin) {
-      if (q && (p_bin < 0 || bin == p_bin) && key >= from) f(key, q);
-    });
-  });
+  return find_cut(s, false, above, share, cut, each,
+                  [&](auto bin) { return p_bin < 0 || bin() == p_bin; });
 }
 
 // The same for a list of at most kRanked entries in LDS, one a thread: every
@@ -481,7 +489,7 @@ __global__ __launch_bounds__(1024) void row_kernel(SampleArgs a) {
   __shared__ uint32_t count[kSub], list_q[kRowList], listed;
   __shared__ u64 mass[kSub], list_key[kRowList];
   __shared__ uint16_t list_bin[kRowList];
-  extern __shared__ char raw[];
+  extern __shared__ __attribute__((aligned(16))) char raw[];
   const int64_t row = blockIdx.x;
   const int n = (int)a.s.n, groups = (n + 7) / 8;
   float4 *xs = reinterpret_cast<float4 *>(raw);
@@ -547,18 +555,18 @@ __global__ __launch_bounds__(1024) void row_kernel(SampleArgs a) {
           if (qv[j] == 0) continue;
           const int bin = bin_of<kSub>(exponent(xv[j], l), scale);
           if ((bin >= b.sure && bin <= b.last) || bin == b.k_bin)
-            f(key_of(xv[j], h * 4 + j), qv[j], bin);
+            f(key_of(xv[j], h * 4 + j), [&] { return qv[j]; }, [&] { return bin; });
         }
       }
     };
     if (t == 0) listed = 0;
     __syncthreads();
-    each_open([&](u64 key, uint32_t q, int bin) {
+    each_open([&](u64 key, auto q, auto bin) {
       const uint32_t at = atomicAdd(&listed, 1u);
       if (at < kRowList) {
         list_key[at] = key;
-        list_q[at] = q;
-        list_bin[at] = (uint16_t)bin;
+        list_q[at] = q();
+        list_bin[at] = (uint16_t)bin();
       }
     });
     __syncthreads();
@@ -569,7 +577,8 @@ __global__ __launch_bounds__(1024) void row_kernel(SampleArgs a) {
       cut = find_cuts(s, l, b, kSub, false, weighed, [&](auto f) {
         if (open > kRowList) return each_open(f);
 #pragma unroll 1
-        for (int e = t; e < open; e += threads) f(list_key[e], list_q[e], (int)list_bin[e]);
+        for (int e = t; e < open; e += threads)
+          f(list_key[e], [&] { return list_q[e]; }, [&] { return (int)list_bin[e]; });
       });
     __syncthreads();
   }
@@ -1035,7 +1044,7 @@ struct Finish {
 
 template <typename T>
 __global__ __launch_bounds__(1024) void finish_kernel(Long k) {
-  extern __shared__ char raw[];
+  extern __shared__ __attribute__((aligned(16))) char raw[];
   Finish &sh = *reinterpret_cast<Finish *>(raw);
   const int64_t r = blockIdx.x, row = k.row0 + r, n = k.a.s.n;
   const int wave = threadIdx.x >> 6, threads = blockDim.x, waves = threads >> 6;
@@ -1049,6 +1058,7 @@ __global__ __launch_bounds__(1024) void finish_kernel(Long k) {
   part = wave_prefix(part);
   const uint32_t listed = from_lane(part, 63);
   if (threadIdx.x < kSegments) sh.segment_end[threadIdx.x] = part;
+  const bool held = fits && listed <= (uint32_t)kList;
   // entry e of the list: its segment by the segments' ends
   auto entry = [&](uint32_t e) {
     uint32_t at = 0;
@@ -1060,15 +1070,14 @@ __global__ __launch_bounds__(1024) void finish_kernel(Long k) {
   __syncthreads();
   const float u0 = wave < k.a.draws ? k.a.u[row * k.a.draws + wave] : 0.0f;
   for (int t = threadIdx.x; t < k.tiles; t += threads) sh.tile[t] = k.tile_mass[r * k.tiles + t];
-  if (fits)
-    for (uint32_t e = threadIdx.x; e < min(listed, (uint32_t)kList); e += threads)
-      sh.keys[e] = entry(e);
+  if (held)
+    for (uint32_t e = threadIdx.x; e < listed; e += threads) sh.keys[e] = entry(e);
   const RowLimits l = settled.l;
   if (l.m == -__builtin_inff()) return no_entry(k.a, row);
   const Bins b = settled.b;
   const float scale = (float)kBins / l.range;
-  if (fits)
-    for (uint32_t e = threadIdx.x; e < min(listed, (uint32_t)kList); e += threads) {
+  if (held)
+    for (uint32_t e = threadIdx.x; e < listed; e += threads) {
       const float z = exponent(key_score(sh.keys[e]), l);
       sh.q[e] = weight(z);
       sh.bin[e] = (uint16_t)bin_of<kBins>(z, scale);
@@ -1081,31 +1090,49 @@ __global__ __launch_bounds__(1024) void finish_kernel(Long k) {
       for (int j = threadIdx.x; j < kBins; j += threads) sh.mass[j] = k.mass[r * kBins + j];
     }
     __syncthreads();
-    // f(key, weight, bin) for every listed entry.  A list that did not fit is
-    // read from the row again.
+    // f(key, weight, bin) for every listed entry.  A list longer than LDS holds
+    // stays in memory, its segments shared among the waves; one that did not
+    // fit there is read from the row again.
     auto each = [&](auto f) {
-      auto one = [&](float x, int64_t i) {
-        const float z = exponent(x, l);
-        if (!(z > kLowest)) return;
-        const int bin = bin_of<kBins>(z, scale);
-        if ((bin >= b.sure && bin <= b.last) || bin == b.k_bin) f(key_of(x, i), weight(z), bin);
+      auto one = [&](u64 key) {
+        const float z = exponent(key_score(key), l);
+        f(key, [&] { return weight(z); }, [&] { return bin_of<kBins>(z, scale); });
       };
-      if (fits) {
+      if (held) {
 #pragma unroll 1
-        for (uint32_t e = threadIdx.x; e < min(listed, (uint32_t)kList); e += threads) {
-          f(sh.keys[e], sh.q[e], (int)sh.bin[e]);
-        }
+        for (uint32_t e = threadIdx.x; e < listed; e += threads)
+          f(sh.keys[e], [&] { return sh.q[e]; }, [&] { return (int)sh.bin[e]; });
+      } else if (fits) {
+        const int segments = (int)k.segments;
 #pragma unroll 1
-        for (uint32_t e = kList + threadIdx.x; e < listed; e += threads) {
-          const u64 key = entry(e);
-          one(key_score(key), key_index(key));
+        for (int g = wave % segments; g < segments; g += waves) {
+          // the waves that share this segment, and which of them this one is
+          const int sharing = waves > segments ? (waves - g + segments - 1) / segments : 1;
+          const uint32_t from = g ? sh.segment_end[g - 1] : 0, count = sh.segment_end[g] - from;
+          const u64 *keys = list + (size_t)g * k.segment_most;
+#pragma unroll 1
+          for (uint32_t e = (uint32_t)(wave / segments * 64 + lane); e < count; e += sharing * 512) {
+            u64 key[8];  // on their way at once
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+              key[j] = e + j * sharing * 64 < count ? keys[e + j * sharing * 64] : 0;
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+              if (key[j]) one(key[j]);
+          }
         }
       } else {
+#pragma unroll 1
         for (int64_t i = (int64_t)threadIdx.x * 8; i < n; i += (int64_t)threads * 8) {
           float x[8];
           load8(scores, valid, i, n, x);
 #pragma unroll
-          for (int j = 0; j < 8; ++j) one(x[j], i + j);
+          for (int j = 0; j < 8; ++j) {
+            const float z = exponent(x[j], l);
+            if (!(z > kLowest)) continue;
+            const int bin = bin_of<kBins>(z, scale);
+            if ((bin >= b.sure && bin <= b.last) || bin == b.k_bin) one(key_of(x[j], i + j));
+          }
         }
       }
     };
@@ -1115,9 +1142,9 @@ __global__ __launch_bounds__(1024) void finish_kernel(Long k) {
       cut = find_cuts(sh.s, l, b, kBins, everything, [&](int j) { return sh.mass[j]; }, each);
     __syncthreads();
     // the listed entries that are kept join their tiles
-    each([&](u64 key, uint32_t q, int bin) {
-      if (q && key >= cut && bin >= b.sure && exponent(key_score(key), l) >= l.min_z)
-        atomicAdd(&sh.tile[key_index(key) / k.tile], (u64)q);
+    each([&](u64 key, auto q, auto bin) {
+      if (key >= cut && bin() >= b.sure && exponent(key_score(key), l) >= l.min_z)
+        atomicAdd(&sh.tile[key_index(key) / k.tile], (u64)q());
     });
   }
   __syncthreads();
