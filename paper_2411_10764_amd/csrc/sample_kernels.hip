@@ -27,7 +27,9 @@
 //   draw_kernel     many draws: a wave a draw
 // top-k with a small k needs no weights before its cut is known: count_kernel
 // then only counts, and collect_kernel lists every entry down to the cut's bin.
+// Long rows of 16-bit scores with one draw are counted by score instead (below).
 #include <algorithm>
+#include <type_traits>
 
 #include "draw.h"
 
@@ -1180,6 +1182,414 @@ __global__ __launch_bounds__(256) void draw_kernel(Long k, int blocks) {
               k.tile_mass + r * k.tiles);
 }
 
+// ---- long rows of 16-bit scores, one draw ----------------------------------------
+
+// Such a row has at most 65,536 different scores, and far fewer in practice: a
+// weight is worked out once for each of them and not for each entry.
+//   value_kernel  counts a part's entries by their bit pattern, in LDS, and
+//                 lists the (score, count) pairs
+//   pick_kernel   a workgroup a row: the cuts from the pairs, as a score and how
+//                 many of the entries that have it are kept; the parts' weights;
+//                 and a walk over the part that holds the draw
+// The row is read once, and one of its parts once more.  The chunked path reads
+// it three times and takes two exponentials an entry: 256 x 100,003 bf16 94 us
+// there and 47 here, 4 x 131,072 bf16 29 and 25, 16 x 50,000 fp16 at top_p
+// 0.95 38 and 37.  More draws walk more parts (four of 16 x 50,000 rows: 40 us
+// against 32), and longer rows have more pairs than one workgroup goes through
+// in that time: 16-bit floats of 10 bits an octave 200,000 entries a row at
+// top_p 0.95 71 us against 49, those of 7 bits 900,000 entries 52 against 51.
+constexpr int kPartVecs = 7;                      // vectors of 8 entries of a thread
+constexpr int kPartMost = kPartVecs * 1024 * 8;   // below 65,536: 16-bit counters
+constexpr int kPartLeast = 24576;                 // 16,384: 64 x 50,021 fp16 38.7 -> 41 us
+constexpr int kParts = 16;                        // of a row, at most
+constexpr int64_t kValueMostBf16 = 1 << 18, kValueMostF16 = 1 << 16;
+static_assert(kValueMostBf16 <= (int64_t)kParts * kPartMost);
+constexpr int64_t kValueBatch = (int64_t)1 << 25; // entries of one set of launches
+constexpr int kHeld = 28672;   // pairs of a row held in LDS
+constexpr int kWords = 32768;  // word i counts patterns i (low half) and i | 0x8000
+
+struct Values {
+  SampleArgs a;
+  int64_t row0;      // first row of the batch
+  int64_t part;      // entries of a part, a number of tiles
+  int parts;         // of a row
+  uint32_t *list;    // [rows][parts][part] (order << 16) | count
+  uint32_t *listed;  // [rows][parts]
+  uint32_t *best;    // [rows][parts] largest order listed, 0: none
+};
+
+// The place of a 16-bit pattern in the order of scores (-0.0 is +0.0), and back.
+__device__ __forceinline__ uint32_t order_of(uint32_t pattern) {
+  if (pattern == 0x8000u) pattern = 0;
+  return pattern & 0x8000u ? pattern ^ 0xFFFFu : pattern | 0x8000u;
+}
+
+template <typename T>
+__device__ __forceinline__ float score_of(uint32_t order) {
+  const uint16_t pattern = (uint16_t)(order & 0x8000u ? order ^ 0x8000u : order ^ 0xFFFFu);
+  return (float)__builtin_bit_cast(T, pattern);
+}
+
+template <typename T>
+__global__ __launch_bounds__(1024) void value_kernel(Values k) {
+  constexpr int kInfinity = std::is_same<T, _Float16>::value ? 0x7C00 : 0x7F80;
+  __shared__ uint32_t listed, best, least;
+  __shared__ uint32_t block_count[kWords / 512];  // of 512 words: both halves' sums
+  extern __shared__ __attribute__((aligned(16))) char raw[];
+  uint32_t *count = reinterpret_cast<uint32_t *>(raw);
+  const int64_t r = blockIdx.x / k.parts, c = blockIdx.x % k.parts, row = k.row0 + r;
+  const T *scores = static_cast<const T *>(k.a.s.scores) + row * k.a.s.ld;
+  const uint8_t *valid = k.a.s.valid ? k.a.s.valid + row * k.a.s.valid_ld : nullptr;
+  const int64_t lo = c * k.part, end = min(k.a.s.n, lo + k.part);
+  const int t = threadIdx.x, lane = t & 63;
+  const RowSettings set = row_settings(k.a, row);
+  const int32_t top_k = set.temperature > 0.0f ? set.k : 1;
+  // the whole part is on its way while the counters are cleared
+  Eight<T> e[kPartVecs];
+#pragma unroll
+  for (int v = 0; v < kPartVecs; ++v)
+    e[v].load(scores, valid, lo + (int64_t)(v * 1024 + t) * 8, end);
+  uint4 *clear = reinterpret_cast<uint4 *>(raw);
+  for (int w = t; w < kWords / 4; w += 1024) clear[w] = make_uint4(0, 0, 0, 0);
+  if (t == 0) listed = best = least = 0;
+  __syncthreads();
+#pragma unroll
+  for (int v = 0; v < kPartVecs; ++v) {
+    const int64_t i = lo + (int64_t)(v * 1024 + t) * 8;
+    if (i >= end) break;
+    const uint4 w4 = __builtin_bit_cast(uint4, e[v].v);
+    const uint32_t w[4] = {w4.x, w4.y, w4.z, w4.w};
+    const u64 mask = valid ? e[v].mask : ~0ull;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      // beyond the row's end there are entries of -inf, which are not listed
+      if (!valid || (mask >> (16 * j)) & 0xFF)
+        atomicAdd(&count[w[j] & 0x7FFFu], 1u << ((w[j] >> 11) & 16u));
+      if (!valid || (mask >> (16 * j + 8)) & 0xFF)
+        atomicAdd(&count[(w[j] >> 16) & 0x7FFFu], 1u << ((w[j] >> 27) & 16u));
+    }
+  }
+  __syncthreads();
+  // The row's best k entries are among the parts' best k: nothing worse than
+  // eight scores around a part's k-th is listed.
+  if (top_k > 0 && top_k < end - lo) {
+    for (int b = t >> 6; b * 512 <= kInfinity; b += 16) {
+      const uint4 x = clear[b * 128 + lane * 2], y = clear[b * 128 + lane * 2 + 1];
+      const uint32_t sum = wave_prefix(x.x + x.y + x.z + x.w + y.x + y.y + y.z + y.w);
+      if (lane == 63) block_count[b] = sum;
+    }
+    __syncthreads();
+    if (t < 64) {
+      // best first: the positive halves from the last block down, then the
+      // negative ones up
+      const uint32_t own = lane * 512 <= kInfinity ? block_count[lane] : 0;
+      const uint32_t low = own & 0xFFFFu, up = own >> 16;
+      const uint32_t low_upto = wave_prefix(low), lows = from_lane(low_upto, 63);
+      const uint32_t before_low = lows - low_upto, upto_up = lows + wave_prefix(up);
+      const u64 in_low = __ballot(before_low < (uint32_t)top_k && before_low + low >= (uint32_t)top_k);
+      const u64 in_up = __ballot(upto_up - up < (uint32_t)top_k && upto_up >= (uint32_t)top_k);
+      if (in_low | in_up) {
+        const bool negative = in_low == 0;
+        const int b = __ffsll(negative ? in_up : in_low) - 1;
+        const uint32_t before = negative ? from_lane(upto_up - up, b) : from_lane(before_low, b);
+        const uint4 x = clear[b * 128 + lane * 2], y = clear[b * 128 + lane * 2 + 1];
+        const uint32_t both = x.x + x.y + x.z + x.w + y.x + y.y + y.z + y.w;
+        const uint32_t here = negative ? both >> 16 : both & 0xFFFFu;
+        const uint32_t upto = wave_prefix(here), all = from_lane(upto, 63);
+        const uint32_t reached = before + (negative ? upto : all - upto + here);
+        const u64 yes = __ballot(reached >= (uint32_t)top_k);
+        const int at = negative ? __ffsll(yes) - 1 : 63 - __clzll(yes);
+        const uint32_t i = (uint32_t)(b * 512 + at * 8);
+        if (lane == 0) least = negative ? order_of((i + 7) | 0x8000u) : order_of(i);
+      }
+    }
+    __syncthreads();
+  }
+  const uint32_t drop = least;
+  // Patterns that follow one another are listed eight apart, as pick_kernel
+  // adds neighbours of the list to different bins.
+  uint32_t *list = k.list + (size_t)blockIdx.x * k.part;
+  uint32_t most = 0;
+  for (int w0 = (t >> 6) * 512; w0 <= kInfinity; w0 += 16 * 512) {
+    const uint4 a = clear[w0 / 4 + lane * 2], b = clear[w0 / 4 + lane * 2 + 1];
+    if (!__any((a.x | a.y | a.z | a.w | b.x | b.y | b.z | b.w) != 0)) continue;
+    uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+    u64 on[16];
+    int total = 0;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const int i = w0 + lane * 8 + j;
+      if (i > kInfinity) w[j] = 0;             // NaN
+      if (i == kInfinity) w[j] &= 0xFFFFu;     // -inf
+      if (order_of((uint32_t)i) < drop) w[j] &= 0xFFFF0000u;
+      if (order_of((uint32_t)i | 0x8000u) < drop) w[j] &= 0xFFFFu;
+      on[2 * j] = __ballot((w[j] & 0xFFFFu) != 0);
+      on[2 * j + 1] = __ballot((w[j] >> 16) != 0);
+      total += __popcll(on[2 * j]) + __popcll(on[2 * j + 1]);
+    }
+    if (total == 0) continue;
+    uint32_t at = 0;
+    if (lane == 0) at = atomicAdd(&listed, (uint32_t)total);
+    at = (uint32_t)__builtin_amdgcn_readfirstlane((int)at);
+#pragma unroll
+    for (int j = 0; j < 16; ++j) {
+      if (!on[j]) continue;
+      const uint32_t i = (uint32_t)(w0 + lane * 8 + j / 2);
+      const uint32_t here = j & 1 ? w[j / 2] >> 16 : w[j / 2] & 0xFFFFu;
+      if (here) {
+        const uint32_t order = order_of(j & 1 ? i | 0x8000u : i);
+        most = max(most, order);
+        list[at + __builtin_amdgcn_mbcnt_hi((uint32_t)(on[j] >> 32),
+                                            __builtin_amdgcn_mbcnt_lo((uint32_t)on[j], 0))] =
+            (order << 16) | here;
+      }
+      at += (uint32_t)__popcll(on[j]);
+    }
+  }
+  most = wave_fold(most, 0u, [](uint32_t a, uint32_t b) { return max(a, b); });
+  if (lane == 63 && most) atomicMax(&best, most);
+  __syncthreads();
+  if (t == 0) {
+    k.listed[blockIdx.x] = listed;
+    k.best[blockIdx.x] = best;
+  }
+}
+
+template <typename T>
+__global__ __launch_bounds__(1024) void pick_kernel(Values k) {
+  constexpr int kFine = 32;               // scores of a bin
+  constexpr int kCoarse = 65536 / kFine;  // bins, best first
+  __shared__ Search s;
+  __shared__ uint32_t count[kCoarse];
+  __shared__ u64 mass[kCoarse], fine[kFine];
+  __shared__ u64 part_mass[kParts], tile_mass[128];
+  __shared__ uint32_t part_ties[kParts], tile_ties[128];
+  extern __shared__ __attribute__((aligned(16))) char raw[];
+  const int64_t r = blockIdx.x, row = k.row0 + r, n = k.a.s.n;
+  const int t = threadIdx.x, lane = t & 63, parts = k.parts;
+  const int wave = __builtin_amdgcn_readfirstlane(t >> 6);
+  const T *scores = static_cast<const T *>(k.a.s.scores) + row * k.a.s.ld;
+  const uint8_t *valid = k.a.s.valid ? k.a.s.valid + row * k.a.s.valid_ld : nullptr;
+  const RowSettings set = row_settings(k.a, row);
+  // a part's list is shared by `sharing` waves
+  const int sharing = 16 / parts, mine = wave / sharing;
+  const uint32_t each_listed = lane < parts ? k.listed[r * parts + lane] : 0;
+  const uint32_t *list = k.list + (size_t)(r * parts + min(mine, parts - 1)) * k.part;
+  uint32_t order = lane < parts ? k.best[r * parts + lane] : 0;
+  const float u = k.a.u[row];
+  for (int b = t; b < kCoarse; b += 1024) count[b] = 0, mass[b] = 0;
+  if (t < kParts) part_mass[t] = 0, part_ties[t] = 0;
+  order = from_lane(wave_fold(order, 0u, [](uint32_t a, uint32_t b) { return max(a, b); }), 63);
+  if (order == 0) return no_entry(k.a, row);
+  const RowLimits l = row_limits(set, n, score_of<T>(order), -__builtin_inff());
+
+  // A thread's pairs are e0, e0 + step, ...: those it brings to LDS itself,
+  // unless all of the row's are too many.
+  const uint32_t listed_upto = wave_prefix(each_listed);
+  const uint32_t pairs = mine < parts ? from_lane(each_listed, min(mine, parts - 1)) : 0;
+  const bool held = from_lane(listed_upto, 63) <= (uint32_t)kHeld;
+  const uint32_t step = (uint32_t)sharing * 64, e0 = (uint32_t)(wave % sharing) * 64 + lane;
+  uint32_t *pair =
+      reinterpret_cast<uint32_t *>(raw) + from_lane(listed_upto - each_listed, min(mine, parts - 1));
+  if (held) {
+    for (uint32_t e = e0; e < pairs; e += 8 * step) {
+      uint32_t v[8];  // on their way at once
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] = e + j * step < pairs ? list[e + j * step] : 0;
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        if (v[j]) pair[e + j * step] = v[j];
+    }
+  }
+  __syncthreads();
+  // f(order, count) for the pairs of this thread
+  auto each = [&](auto f) {
+    auto walk = [&](const auto *from) {
+#pragma unroll 1
+      for (uint32_t e = e0; e < pairs; e += 4 * step) {
+        uint32_t v[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[j] = e + j * step < pairs ? from[e + j * step] : 0;
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          if (v[j]) f(v[j] >> 16, v[j] & 0xFFFFu);
+      }
+    };
+    if (held) walk(pair);
+    else walk(list);
+  };
+  auto weight_at = [&](uint32_t o) { return weight(exponent(score_of<T>(o), l)); };
+  auto bin = [&](uint32_t o) { return kCoarse - 1 - (int)(o / kFine); };
+
+  // Inside bin `b`, with `above` in better ones: the score at which the count or
+  // weight reaches `need`.  What better scores amount to goes back to `above`.
+  auto score_in = [&](int b, bool by_count, u64 need, u64 *above) {
+    if (t < kFine) fine[t] = 0;
+    __syncthreads();
+    each([&](uint32_t o, uint32_t c) {
+      if (bin(o) == b)
+        atomicAdd(&fine[kFine - 1 - (int)(o & (kFine - 1))], by_count ? c : (u64)c * weight_at(o));
+    });
+    __syncthreads();
+    const u64 v = lane < kFine ? fine[lane] : 0, upto = wave_prefix(v);
+    const int f = __ffsll(__ballot(lane < kFine && *above + upto >= need)) - 1;
+    *above += from_lane(upto - v, f);
+    return (uint32_t)((kCoarse - 1 - b) * kFine + kFine - 1 - f);
+  };
+
+  // The cut: entries of better scores than `edge` are kept, and the first
+  // `edge_kept` of those that have it.  top-k's needs no weights, and top-p's
+  // only those of what top-k keeps.
+  uint32_t at = 0;  // the edge's place in the order, 0: below all
+  u64 edge_kept = 0;
+  if (l.k < n) {
+    each([&](uint32_t o, uint32_t c) { atomicAdd(&count[bin(o)], c); });
+    __syncthreads();
+    block_find(s, kCoarse, [&](u64) { return (u64)l.k; }, 0,
+               [&](int b) { return (u64)count[b]; });
+    if (s.bin >= 0) {  // the row has k entries
+      u64 above = s.above;
+      at = score_in(s.bin, true, (u64)l.k, &above);
+      edge_kept = (u64)l.k - above;
+    }
+    __syncthreads();
+  }
+  if (l.p < 2.0f) {
+    each([&](uint32_t o, uint32_t c) {
+      if (o <= at) return;
+      const u64 q = (u64)c * weight_at(o);
+      if (q) atomicAdd(&mass[bin(o)], q);
+    });
+    if (t == 0 && at) atomicAdd(&mass[bin(at)], edge_kept * weight_at(at));
+    __syncthreads();
+    u64 need = 0;
+    block_find(s, kCoarse, [&](u64 all) { return need = share_of(l.p, all); }, 0,
+               [&](int b) { return mass[b]; });
+    u64 above = s.above;
+    at = score_in(s.bin, false, need, &above);
+    const uint32_t q = weight_at(at);
+    edge_kept = (need - above + q - 1) / q;
+  }
+  float edge = -__builtin_inff();
+  uint32_t edge_weight = 0;
+  if (at) {
+    edge = score_of<T>(at);
+    const float z = exponent(edge, l);
+    edge_weight = weight(z);
+    if (!(z >= l.min_z)) edge_kept = 0;
+  }
+  auto kept = [&](float x, float z) { return x > edge && z >= l.min_z; };
+
+  // what each part keeps: the weight of better scores, entries at the edge
+  u64 sum = 0;
+  uint32_t ties = 0;
+  each([&](uint32_t o, uint32_t c) {
+    if (o < at) return;
+    const float x = score_of<T>(o), z = exponent(x, l);
+    if (kept(x, z)) sum += (u64)c * weight(z);
+    if (x == edge) ties += c;
+  });
+  sum = wave_prefix(sum);
+  ties = wave_prefix(ties);
+  if (lane == 63 && mine < parts) {
+    atomicAdd(&part_mass[mine], sum);
+    atomicAdd(&part_ties[mine], ties);
+  }
+  __syncthreads();
+  // of `have` entries at the edge, `before` of them in earlier places
+  auto kept_ties = [](u64 have, u64 before, u64 most) {
+    return before >= most ? 0ull : min(have, most - before);
+  };
+  const u64 have = lane < parts ? part_ties[lane] : 0;
+  const u64 part_kept = kept_ties(have, wave_prefix(have) - have, edge_kept);
+  const u64 part_upto =
+      wave_prefix(lane < parts ? part_mass[lane] + part_kept * edge_weight : 0);
+  const u64 total = from_lane(part_upto, 63);
+
+  // The part that holds the draw, by tile.
+  u64 want = wanted(u, total);
+  const int p = __ffsll(__ballot(part_upto > want)) - 1;
+  if (p > 0) want -= from_lane(part_upto, p - 1);
+  const u64 keeps = from_lane(part_kept, p);  // entries at the edge
+  const int64_t lo = p * k.part, end = min(n, lo + k.part);
+  const int tiles = (int)((end - lo + kTile - 1) / kTile);
+  Eight<T> all[kPartVecs];
+#pragma unroll
+  for (int v = 0; v < kPartVecs; ++v)
+    all[v].load(scores, valid, lo + (v * 16 + wave) * kTile + lane * 8, end);
+#pragma unroll
+  for (int v = 0; v < kPartVecs; ++v) {
+    const int tile = v * 16 + wave;
+    if (tile >= tiles) break;
+    float x[8];
+    all[v].get(valid != nullptr, x);
+    u64 q = 0;
+    uint32_t at_edge = 0;
+    bool some = false;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) some = some | (x[i] >= edge);
+    if (__any(some)) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const float z = exponent(x[i], l);
+        q += kept(x[i], z) ? weight(z) : 0u;
+        at_edge += x[i] == edge ? 1u : 0u;
+      }
+      q = wave_prefix(q);
+      at_edge = wave_prefix(at_edge);
+    }
+    if (lane == 63) tile_mass[tile] = q, tile_ties[tile] = at_edge;
+  }
+  __syncthreads();
+  if (wave != 0) return;
+  // the tile, two a lane, and the entry inside it
+  const int t0 = lane * 2;
+  const u64 tie0 = t0 < tiles ? tile_ties[t0] : 0, tie1 = t0 + 1 < tiles ? tile_ties[t0 + 1] : 0;
+  const u64 before = wave_prefix(tie0 + tie1) - tie0 - tie1;
+  const u64 m0 = (t0 < tiles ? tile_mass[t0] : 0) + kept_ties(tie0, before, keeps) * edge_weight;
+  const u64 m1 = (t0 + 1 < tiles ? tile_mass[t0 + 1] : 0) +
+                 kept_ties(tie1, before + tie0, keeps) * edge_weight;
+  const u64 upto = wave_prefix(m0 + m1);
+  const int in = __ffsll(__ballot(upto > want)) - 1;
+  const u64 ahead = from_lane(upto - m0 - m1, in), first = from_lane(m0, in);
+  const bool second = ahead + first <= want;
+  want -= ahead + (second ? first : 0);
+  const u64 ties_before = from_lane(before + (second ? tie0 : 0), in);
+  const int64_t i = lo + (int64_t)(in * 2 + (second ? 1 : 0)) * kTile + lane * 8;
+  Eight<T> e;
+  e.load(scores, valid, i, end);
+  float x[8];
+  e.get(valid != nullptr, x);
+  uint32_t own = 0;
+#pragma unroll
+  for (int f = 0; f < 8; ++f) own += x[f] == edge ? 1u : 0u;
+  u64 tie = ties_before + wave_prefix(own) - own;
+  uint32_t q[8];
+  u64 weights = 0;
+#pragma unroll
+  for (int f = 0; f < 8; ++f) {
+    const float z = exponent(x[f], l);
+    q[f] = kept(x[f], z) ? weight(z) : 0u;
+    if (x[f] == edge) q[f] = tie++ < keeps ? edge_weight : 0u;
+    weights += q[f];
+  }
+  const u64 incl = wave_prefix(weights);
+  if (lane == __ffsll(__ballot(incl > want)) - 1) {
+    u64 now = incl - weights;
+    int f = 0;
+    float score = x[0];
+#pragma unroll
+    for (int g = 0; g < 8; ++g) {
+      now += q[g];
+      if (now <= want) f = g + 1;
+    }
+#pragma unroll
+    for (int g = 1; g < 8; ++g) score = g == f ? x[g] : score;
+    k.a.idx[row] = (int32_t)(i + f);
+    k.a.logprob[row] = exponent(score, l) - log_total(total);
+  }
+}
+
 // ---- plans -------------------------------------------------------------------
 
 struct LongPlan {
@@ -1268,6 +1678,57 @@ hipError_t launch_long(const SampleArgs &a, void *ws, int cu_count, hipStream_t 
   return hipSuccess;
 }
 
+struct ValuePlan {
+  int64_t batch, part;
+  int parts;
+  size_t list, listed, best, bytes;
+};
+
+bool by_values(int64_t n, int32_t draws, int64_t most) {
+  return n > kRowMost && n <= most && draws == 1;
+}
+
+// `cus` workgroups fill the device; 0: the plan of the most parts, for the workspace.
+ValuePlan value_plan(int64_t n, int64_t rows, int cus) {
+  ValuePlan p{};
+  p.batch = std::max<int64_t>(1, std::min(rows, kValueBatch / n));
+  const int64_t least = (n + kPartMost - 1) / kPartMost, most = std::max<int64_t>(1, n / kPartLeast);
+  const int64_t want = cus ? (cus + p.batch - 1) / p.batch : kParts;
+  p.parts = (int)std::max(least, std::min({want, most, (int64_t)kParts}));
+  p.part = ((n + p.parts - 1) / p.parts + kTile - 1) / kTile * kTile;
+  p.parts = (int)((n + p.part - 1) / p.part);
+  const size_t b = (size_t)p.batch;
+  auto aligned = [](size_t bytes) { return (bytes + 255) & ~(size_t)255; };
+  p.listed = aligned(b * (size_t)(n + kParts * kTile) * 4);
+  p.best = p.listed + aligned(b * kParts * 4);
+  p.bytes = p.best + aligned(b * kParts * 4);
+  return p;
+}
+
+template <typename T>
+hipError_t launch_values(const SampleArgs &a, void *ws, int cu_count, hipStream_t s) {
+  const ValuePlan p = value_plan(a.s.n, a.s.rows, cu_count);
+  char *base = static_cast<char *>(ws);
+  Values k{};
+  k.a = a;
+  k.part = p.part;
+  k.parts = p.parts;
+  k.list = reinterpret_cast<uint32_t *>(base + p.list);
+  k.listed = reinterpret_cast<uint32_t *>(base + p.listed);
+  k.best = reinterpret_cast<uint32_t *>(base + p.best);
+  const size_t lds = kWords * sizeof(uint32_t);
+  hipError_t e = ensure_dynamic_lds(reinterpret_cast<const void *>(value_kernel<T>), lds);
+  const size_t held = kHeld * sizeof(uint32_t);
+  if (e == hipSuccess) e = ensure_dynamic_lds(reinterpret_cast<const void *>(pick_kernel<T>), held);
+  for (k.row0 = 0; k.row0 < a.s.rows && e == hipSuccess; k.row0 += p.batch) {
+    const uint32_t rows = (uint32_t)std::min(p.batch, a.s.rows - k.row0);
+    value_kernel<T><<<rows * (uint32_t)k.parts, 1024, lds, s>>>(k);
+    pick_kernel<T><<<rows, 1024, held, s>>>(k);
+    e = hipGetLastError();
+  }
+  return e;
+}
+
 template <typename T>
 hipError_t launch_row(const SampleArgs &a, hipStream_t s) {
   const int groups = (int)((a.s.n + 7) / 8);
@@ -1282,14 +1743,19 @@ hipError_t launch_row(const SampleArgs &a, hipStream_t s) {
 template <typename T>
 hipError_t launch(const SampleArgs &a, void *ws, int cu_count, hipStream_t s) {
   if (a.s.n <= kRowMost) return launch_row<T>(a, s);
+  if constexpr (sizeof(T) == 2) {
+    const int64_t most = std::is_same<T, _Float16>::value ? kValueMostF16 : kValueMostBf16;
+    if (by_values(a.s.n, a.draws, most)) return launch_values<T>(a, ws, cu_count, s);
+  }
   return launch_long<T>(a, ws, cu_count, s);
 }
 
 }  // namespace
 
 size_t sample_workspace_bytes(int64_t n, int64_t rows, int32_t draws) {
-  (void)draws;
-  return n <= kRowMost ? 256 : std::max<size_t>(256, long_plan(n, rows).bytes);
+  if (n <= kRowMost || rows <= 0) return 256;
+  const size_t bytes = long_plan(n, rows).bytes;  // the type is not known here
+  return by_values(n, draws, kValueMostBf16) ? std::max(bytes, value_plan(n, rows, 0).bytes) : bytes;
 }
 
 hipError_t launch_sample(int dtype, const SampleArgs &a, void *ws, int cu_count, hipStream_t s) {
