@@ -79,17 +79,22 @@ __device__ __forceinline__ void clear_part(const Clear &f) {
   const bool flat = f.ld == f.width;
   const int64_t rows = flat ? 1 : f.row1 - f.row0;
   const int64_t width = flat ? (f.row1 - f.row0) * f.width : f.width;
-  const int64_t step = (int64_t)f.blocks * blockDim.x * 8;
-  for (int64_t r = 0; r < rows; ++r) {
+  // vector v of a row, then of the next: narrow rows keep all threads at work
+  const int64_t vecs = (width + 7) / 8, step = (int64_t)f.blocks * blockDim.x;
+  const int64_t first = (int64_t)(blockIdx.x - f.first) * blockDim.x + threadIdx.x;
+  int64_t r = first / vecs, v = first % vecs;
+  const int64_t down = step / vecs, along = step % vecs;
+  while (r < rows) {
     uint16_t *row = f.grad + (f.row0 + r) * f.ld;
-    for (int64_t c = ((int64_t)(blockIdx.x - f.first) * blockDim.x + threadIdx.x) * 8; c < width;
-         c += step) {
-      if (c + 8 <= width) {
-        __builtin_nontemporal_store(Halves{}, reinterpret_cast<Halves *>(row + c));
-      } else {
-        for (int64_t j = c; j < width; ++j) row[j] = 0;
-      }
+    const int64_t c = v * 8;
+    if (c + 8 <= width) {
+      __builtin_nontemporal_store(Halves{}, reinterpret_cast<Halves *>(row + c));
+    } else {
+      for (int64_t j = c; j < width; ++j) row[j] = 0;
     }
+    r += down;
+    v += along;
+    if (v >= vecs) v -= vecs, ++r;
   }
 }
 
@@ -775,7 +780,7 @@ hipError_t launch_grad(const EmbedGradArgs &a, void *ws, hipStream_t st) {
   auto clear = [&](int i, uint32_t own) {
     Clear f = {static_cast<uint16_t *>(a.grad), cleared * i / launches, cleared * (i + 1) / launches,
                row_bytes / 2, a.grad_ld * (int64_t)sizeof(O) / 2, own, 0};
-    const int64_t vecs = (f.row1 - f.row0) * f.width / 8 + 1;
+    const int64_t vecs = (f.row1 - f.row0) * (f.width / 8 + 1);
     if (f.row1 > f.row0) f.blocks = (uint32_t)std::min<int64_t>((vecs + 1023) / 1024, 512);
     return f;
   };
