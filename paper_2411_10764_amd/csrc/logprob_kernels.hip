@@ -144,20 +144,26 @@ __device__ __forceinline__ int list_targets(const int32_t *targets, int per_row,
 
 // Calls f(entry, sum of weights) once for every entry the list names; weights
 // of one entry are added in the order of j.  Few targets are compared pair by
-// pair, many are sorted first (list has room for the next power of two).
+// pair, many are sorted first (list has room for the next power of two).  Every
+// thread of the workgroup calls it.
 template <typename F>
 __device__ __forceinline__ void each_entry(unsigned long long *list, int count,
                                            const float *weight, F f) {
   const int threads = blockDim.x;
   if (count <= kPairs) {
+    // a repeated target's weights come from LDS, not one after the other from memory
+    __shared__ float weights[kPairs];
+    for (int a = threadIdx.x; a < count; a += threads) weights[a] = weight[(uint32_t)list[a]];
+    __syncthreads();
     for (int a = threadIdx.x; a < count; a += threads) {
       const uint32_t t = (uint32_t)(list[a] >> 32);
       bool first = true;
       for (int b = 0; b < a && first; ++b) first = (uint32_t)(list[b] >> 32) != t;
       if (!first) continue;
-      float sum = weight[(uint32_t)list[a]];
+      float sum = weights[a];
+#pragma unroll 4
       for (int b = a + 1; b < count; ++b)
-        if ((uint32_t)(list[b] >> 32) == t) sum += weight[(uint32_t)list[b]];
+        if ((uint32_t)(list[b] >> 32) == t) sum += weights[b];
       f((int64_t)t, sum);
     }
     return;
@@ -176,12 +182,25 @@ __device__ __forceinline__ void each_entry(unsigned long long *list, int count,
     }
   }
   __syncthreads();
+  // in order now: weights take the places of the j
+  for (int a = threadIdx.x; a < count; a += threads)
+    list[a] = (list[a] & ~0xFFFFFFFFull) | __float_as_uint(weight[(uint32_t)list[a]]);
+  __syncthreads();
   for (int a = threadIdx.x; a < count; a += threads) {
     const uint32_t t = (uint32_t)(list[a] >> 32);
     if (a > 0 && (uint32_t)(list[a - 1] >> 32) == t) continue;
     float sum = 0.0f;
-    for (int b = a; b < count && (uint32_t)(list[b] >> 32) == t; ++b)
-      sum += weight[(uint32_t)list[b]];
+    bool same = true;
+    for (int b = a; same; b += 8) {
+      unsigned long long x[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) x[j] = list[min(b + j, count - 1)];  // on their way at once
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        same = same & (b + j < count) & ((uint32_t)(x[j] >> 32) == t);
+        sum += same ? __uint_as_float((uint32_t)x[j]) : 0.0f;
+      }
+    }
     f((int64_t)t, sum);
   }
 }

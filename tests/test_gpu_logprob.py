@@ -225,3 +225,18 @@ def test_large_gradient():
     want_lp, want = _reference(xf, None, T, t, w)
     _check_logprob(lp[some].cpu().numpy(), want_lp)
     _check_grad(drawutil.as_float(grad[some]), want, xf, None, T, t, w, torch.bfloat16)
+
+
+@pytest.mark.parametrize("n,d", [(4096, 100), (4096, 500), (100, 16384), (300000, 128),
+                                 (300000, 5000)])
+def test_targets_that_mostly_repeat(n, d):
+    """Nine of ten targets are one entry, as where a sure policy draws one again and again."""
+    rng = np.random.default_rng(n + d)
+    x, valid, targets, weight, T = _case(rng, 2, n, d, torch.float32, False)
+    targets[:, : d - d // 10] = n // 2
+    a, b, g = _run(x, valid, targets, weight, T)
+    xf = drawutil.as_float(x)
+    lp, grad = _reference(xf, valid, T, targets, weight)
+    _check_logprob(a, lp)
+    _check_logprob(b, lp)
+    _check_grad(g, grad, xf, valid, T, targets, weight, torch.float32)
