@@ -415,6 +415,44 @@ __device__ __forceinline__ u64 find_cuts(Search &s, const RowLimits &l, const Bi
                   [&](auto bin) { return p_bin < 0 || bin() == p_bin; });
 }
 
+// The same for a list of at most 64 entries in LDS: one wave, an entry a lane,
+// without a barrier but the last (1 x 4,096 with 26 such entries: 12.3 us, 14.2
+// in the way below, which all waves go).
+__device__ __forceinline__ u64 wave_cuts(Search &s, const RowLimits &l, const Bins &b, int bins,
+                                         bool everything, int open, const u64 *keys,
+                                         const uint32_t *qs, const uint16_t *bin_of_entry) {
+  if (threadIdx.x < 64) {
+    const int lane = threadIdx.x;
+    const u64 key = lane < open ? keys[lane] : 0;  // 0: below every key
+    const int bin = lane < open ? bin_of_entry[lane] : bins;
+    const uint32_t q = lane < open ? qs[lane] : 0;
+    const u64 in_bin = __ballot(lane < open && bin == b.k_bin);
+    u64 before = b.k_above, mass = b.sure_mass;
+#pragma unroll 4
+    for (int j = 0; j < open; ++j) {
+      const bool better = from_lane(key, j) > key;
+      mass += better ? from_lane(q, j) : 0u;
+      before += better ? (uint32_t)(in_bin >> j) & 1u : 0u;
+    }
+    bool kept = lane < open &&
+                (b.k_bin == bins || bin < b.k_bin || (bin == b.k_bin && before < (u64)l.k));
+    if (l.p < 2.0f) {
+      u64 total = b.all;
+      if (everything || b.k_bin < bins) {
+        const u64 part = kept && (everything || bin == b.k_bin) ? q : 0u;
+        total = from_lane(wave_prefix(part), 63) + (everything ? 0 : b.k_mass);
+      }
+      kept = kept && q != 0 && bin >= b.sure && bin <= b.last && mass < share_of(l.p, total);
+    }
+    // None of the list kept: all that is kept lies in better bins, whose keys are larger.
+    const u64 least = wave_fold(kept ? key : ~0ull, ~0ull, [](u64 a, u64 b) { return min(a, b); });
+    const u64 most = wave_fold(key, 0ull, [](u64 a, u64 b) { return max(a, b); });
+    if (lane == 63) s.lo = least != ~0ull ? least : most + 1;
+  }
+  __syncthreads();
+  return s.lo;
+}
+
 // The same for a list of at most kRanked entries in LDS, one a thread: every
 // entry adds up those before it, which come from the wave's own registers, 64
 // at a time.  Steps without a barrier are quicker than the splitting of
@@ -600,7 +638,9 @@ __global__ __launch_bounds__(1024) void row_kernel(SampleArgs a) {
     });
     __syncthreads();
     const int open = (int)listed;
-    if (open <= min(kRanked, threads))
+    if (open <= 64)
+      cut = wave_cuts(s, l, b, kSub, false, open, list_key, list_q, list_bin);
+    else if (open <= min(kRanked, threads))
       cut = rank_cuts(s, l, b, kSub, false, open, list_key, list_q, list_bin);
     else
       cut = find_cuts(s, l, b, kSub, false, weighed, [&](auto f) {
@@ -1165,7 +1205,9 @@ __global__ __launch_bounds__(1024) void finish_kernel(Long k) {
         }
       }
     };
-    if (fits && listed <= (uint32_t)min(kRanked, threads))
+    if (fits && listed <= 64)
+      cut = wave_cuts(sh.s, l, b, kBins, everything, (int)listed, sh.keys, sh.q, sh.bin);
+    else if (fits && listed <= (uint32_t)min(kRanked, threads))
       cut = rank_cuts(sh.s, l, b, kBins, everything, (int)listed, sh.keys, sh.q, sh.bin);
     else
       cut = find_cuts(sh.s, l, b, kBins, everything, [&](int j) { return sh.mass[j]; }, each);
