@@ -129,6 +129,20 @@ __device__ __forceinline__ T narrow(float x) {
   return (T)x;
 }
 
+// An element as float32, a signaling NaN made a quiet one.  The compiler turns
+// fmaxf and comparisons joined by `or` into maxima, which give NaN where one
+// operand is signaling; it also counts on a cast from bfloat16, which is a shift
+// of the bits, to have quieted it.
+template <typename T>
+__device__ __forceinline__ float widen(T v) {
+  float x;
+  if constexpr (__is_same(T, __bf16))
+    x = __uint_as_float((uint32_t)__builtin_bit_cast(uint16_t, v) << 16);
+  else
+    x = (float)v;
+  return __builtin_canonicalizef(x);
+}
+
 // A score as float32 with -0.0 canonicalised to +0.0, and -inf where the entry
 // is not included (so a NaN or a masked entry never competes).
 __device__ __forceinline__ float included(float s, bool valid) {

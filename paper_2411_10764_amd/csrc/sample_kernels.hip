@@ -149,7 +149,7 @@ struct Eight {
   // The scores, -inf where the mask excludes an entry; a NaN stays.
   __device__ __forceinline__ void get(bool masked, float (&x)[8]) const {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) x[j] = (float)v[j];
+    for (int j = 0; j < 8; ++j) x[j] = widen<T>(v[j]);
     if (masked) {
 #pragma unroll
       for (int j = 0; j < 8; ++j)
@@ -1339,12 +1339,29 @@ __global__ __launch_bounds__(1024) void value_kernel(Values k) {
     }
   }
   __syncthreads();
+  // This lane's eight of 512 words from w0 on, without what is not included.
+  auto words = [&](int w0, uint32_t (&w)[8]) {
+    const uint4 x = clear[w0 / 4 + lane * 2], y = clear[w0 / 4 + lane * 2 + 1];
+    w[0] = x.x, w[1] = x.y, w[2] = x.z, w[3] = x.w;
+    w[4] = y.x, w[5] = y.y, w[6] = y.z, w[7] = y.w;
+    if (w0 + 512 <= kInfinity) return;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const int i = w0 + lane * 8 + j;
+      if (i > kInfinity) w[j] = 0;          // NaN
+      if (i == kInfinity) w[j] &= 0xFFFFu;  // -inf
+    }
+  };
+  auto sum_of = [](const uint32_t (&w)[8]) {
+    return w[0] + w[1] + w[2] + w[3] + w[4] + w[5] + w[6] + w[7];
+  };
   // The row's best k entries are among the parts' best k: nothing worse than
   // eight scores around a part's k-th is listed.
   if (top_k > 0 && top_k < end - lo) {
     for (int b = t >> 6; b * 512 <= kInfinity; b += 16) {
-      const uint4 x = clear[b * 128 + lane * 2], y = clear[b * 128 + lane * 2 + 1];
-      const uint32_t sum = wave_prefix(x.x + x.y + x.z + x.w + y.x + y.y + y.z + y.w);
+      uint32_t w[8];
+      words(b * 512, w);
+      const uint32_t sum = wave_prefix(sum_of(w));
       if (lane == 63) block_count[b] = sum;
     }
     __syncthreads();
@@ -1361,8 +1378,9 @@ __global__ __launch_bounds__(1024) void value_kernel(Values k) {
         const bool negative = in_low == 0;
         const int b = __ffsll(negative ? in_up : in_low) - 1;
         const uint32_t before = negative ? from_lane(upto_up - up, b) : from_lane(before_low, b);
-        const uint4 x = clear[b * 128 + lane * 2], y = clear[b * 128 + lane * 2 + 1];
-        const uint32_t both = x.x + x.y + x.z + x.w + y.x + y.y + y.z + y.w;
+        uint32_t w[8];
+        words(b * 512, w);
+        const uint32_t both = sum_of(w);
         const uint32_t here = negative ? both >> 16 : both & 0xFFFFu;
         const uint32_t upto = wave_prefix(here), all = from_lane(upto, 63);
         const uint32_t reached = before + (negative ? upto : all - upto + here);
@@ -1380,16 +1398,14 @@ __global__ __launch_bounds__(1024) void value_kernel(Values k) {
   uint32_t *list = k.list + (size_t)blockIdx.x * k.part;
   uint32_t most = 0;
   for (int w0 = (t >> 6) * 512; w0 <= kInfinity; w0 += 16 * 512) {
-    const uint4 a = clear[w0 / 4 + lane * 2], b = clear[w0 / 4 + lane * 2 + 1];
-    if (!__any((a.x | a.y | a.z | a.w | b.x | b.y | b.z | b.w) != 0)) continue;
-    uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+    uint32_t w[8];
+    words(w0, w);
+    if (!__any((w[0] | w[1] | w[2] | w[3] | w[4] | w[5] | w[6] | w[7]) != 0)) continue;
     u64 on[16];
     int total = 0;
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
       const int i = w0 + lane * 8 + j;
-      if (i > kInfinity) w[j] = 0;             // NaN
-      if (i == kInfinity) w[j] &= 0xFFFFu;     // -inf
       if (order_of((uint32_t)i) < drop) w[j] &= 0xFFFF0000u;
       if (order_of((uint32_t)i | 0x8000u) < drop) w[j] &= 0xFFFFu;
       on[2 * j] = __ballot((w[j] & 0xFFFFu) != 0);
@@ -1619,7 +1635,9 @@ __global__ __launch_bounds__(1024) void pick_kernel(Values k) {
   const u64 m1 = (t0 + 1 < tiles ? tile_mass[t0 + 1] : 0) +
                  kept_ties(tie1, before + tie0, keeps) * edge_weight;
   const u64 upto = wave_prefix(m0 + m1);
-  const int in = __ffsll(__ballot(upto > want)) - 1;
+  // (always found; with scores that another stream rewrites meanwhile it may be
+  // the last lane, which reads nothing)
+  const int in = __ffsll(__ballot(upto > want) | (1ull << 63)) - 1;
   const u64 ahead = from_lane(upto - m0 - m1, in), first = from_lane(m0, in);
   const bool second = ahead + first <= want;
   want -= ahead + (second ? first : 0);

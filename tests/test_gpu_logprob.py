@@ -240,3 +240,29 @@ def test_targets_that_mostly_repeat(n, d):
     _check_logprob(a, lp)
     _check_logprob(b, lp)
     _check_grad(g, grad, xf, valid, T, targets, weight, torch.float32)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("n", [60, 3001, 50021, 300007])
+def test_signaling_nan_is_like_any_nan(dtype, n):
+    """Scores of a bit pattern that operations quieten: draws, log-probabilities
+    and gradients are those of the same row with quiet ones."""
+    rng = np.random.default_rng(n)
+    x = torch.from_numpy(rng.standard_normal((2, n)).astype(np.float32) * 2).to(dtype)
+    bits = torch.int32 if dtype == torch.float32 else torch.int16
+    signaling = torch.tensor(torch.inf, dtype=dtype).view(bits) + 1
+    at = torch.from_numpy(rng.random((2, n)) < 0.4)
+    at[:, n // 2:n // 2 + 3] = torch.tensor([True, False, True])
+    x[:, n // 2 + 1] = 9.0  # the best, between two of them
+    loud = x.view(bits).where(~at, signaling.expand_as(at)).view(dtype).to(DEV)
+    quiet = x.masked_fill(at, float("nan")).to(DEV)
+    t = torch.from_numpy(rng.integers(0, n, (2, 7)).astype(np.int32)).to(DEV)
+    w = torch.from_numpy(rng.standard_normal((2, 7)).astype(np.float32)).to(DEV)
+    p = torch.full((2,), 0.8, device=DEV)
+    for d in (1, 40):
+        u = torch.from_numpy(rng.random((2, d), dtype=np.float32)).to(DEV)
+        got = [[v.clone() for v in ml2.Sampler(2, n, d).run(s, u, top_p=p)] for s in (loud, quiet)]
+        assert torch.equal(got[0][0], got[1][0]) and torch.equal(got[0][1], got[1][1])
+    f = [ml2.LogProb(2, n, 7, grad_dtype=dtype) for _ in range(2)]
+    got = [a.run_grad(s, t, w) for a, s in zip(f, (loud, quiet))]
+    assert torch.equal(got[0][0], got[1][0]) and torch.equal(got[0][1], got[1][1])

@@ -123,6 +123,24 @@ def test_specials_in_long_rows(dtype):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
+def test_every_bit_pattern(dtype):
+    """All 65,536 patterns, both signs of every NaN among them, in every place."""
+    rng = np.random.default_rng(11)
+    rows = 4
+    bits = np.stack([rng.permutation(65536) for _ in range(rows)])
+    bits[1, bits[1] % 3 > 0] = 0x7FFF      # two thirds NaN, positive
+    bits[2, bits[2] % 3 > 0] = 0xFFFF      # negative
+    bits[3, rng.random(65536) < 0.5] = torch.tensor(torch.inf, dtype=dtype).view(torch.int16) + 1
+    x = torch.from_numpy(bits.astype(np.uint16).view(np.int16)).to(DEV).view(dtype)
+    finite = x.float().where(x.float().abs() < 1000, torch.nan).to(dtype)
+    for scores in (x, finite):
+        for seed, lim in enumerate((dict(), dict(top_k=3), dict(top_k=1000), dict(top_k=20000),
+                                    dict(top_k=60000), dict(top_p=0.9),
+                                    dict(top_k=500, top_p=0.5), dict(temperature=0.0))):
+            _both(scores, None, seed, **lim)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("offset,pad", [(1, 0), (3, 5), (1, 1), (0, 64)])
 def test_strides_alignment_and_shared_mask(dtype, offset, pad):
     rng = np.random.default_rng(offset * 7 + pad)
