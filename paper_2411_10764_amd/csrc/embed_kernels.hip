@@ -569,12 +569,15 @@ __global__ __launch_bounds__(kJoinThreads) void join_kernel(SumArgs s) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, side = 64 >> s.log_g;
   for (uint32_t w = wave; w < longs; w += kJoinThreads / 64) {
     const uint32_t first = long_run[w], id = s.key[(first + 1) * s.piece - 1];
-    uint32_t last = first + kShortRun;  // the last piece that begins with the run's id
-    for (;;) {
-      const uint32_t q = last + 1 + lane;
-      const unsigned long long on = __ballot(q < s.pieces && s.key[q * s.piece] == id);
-      last += on == ~0ull ? 64u : (uint32_t)__ffsll(~on) - 1;
-      if (on != ~0ull) break;
+    // the last piece that begins with the run's id, between `last` and `end`: 64
+    // places in between are looked at at once (60,526 tokens into 30 x 16: the
+    // launch 15 us, 19 with 64 pieces after the other)
+    uint32_t last = first + kShortRun, end = s.pieces;
+    while (end - last > 1) {
+      const uint32_t step = (end - last - 1 + 63) / 64, q = last + (lane + 1) * step;
+      const uint32_t on = __popcll(__ballot(q < end && s.key[q * s.piece] == id));
+      end = min(end, last + (on + 1) * step);
+      last += on * step;
     }
     const bool wide = last - first >= (uint32_t)(kWaveRun * side);
     if (lane == 0) long_last[w] = wide ? last : 0;
