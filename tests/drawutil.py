@@ -116,6 +116,54 @@ def logprob_row(x, valid, T, targets, weight=None):
     return logp, grad / T
 
 
+def gradient_tolerance(x, valid, T, targets, weight, round_to, tiny):
+    """What a float32 computation of one row's gradient may be off by.
+
+    The two terms of an entry are p * W / T and the weights of the targets that
+    name it / T.  An exponent z is two float32 roundings from its value and the
+    exponential adds one, (|z| + 2) 2^-23 of p, and the sum that p is divided by
+    is within 330 * 2^-23 of its value: 8e-5 of both terms, which also covers
+    the sums of weights.  A p below 2^-125 may be taken as 0.  `round_to` and
+    `tiny`: half an ulp of the result's type, relative, and where that ends."""
+    ok = included(x, valid)
+    t = float(T) if T > 0 else 1.0
+    w = np.where([0 <= j < len(x) and bool(ok[j]) for j in targets],
+                 np.abs(np.asarray(weight, np.float64)), 0.0)
+    z = np.full(len(x), -np.inf)
+    if ok.any():
+        v = x[ok].astype(np.float64)
+        with np.errstate(all="ignore"):
+            z[ok] = np.where(v == v.max(), 0.0, (v - v.max()) / t)
+        z -= math.log(np.exp(z).sum())
+    with np.errstate(over="ignore"):
+        size = np.exp(z) * w.sum() / t
+        for j, q in zip(targets, w):
+            if 0 <= j < len(x):
+                size[j] += q / t
+        _, want = logprob_row(x, valid, T, targets, weight)
+        return 8e-5 * size + 2.0 ** -125 * w.sum() / t + round_to * np.abs(want) + tiny
+
+
+def check_gradient(got, x, valid, T, targets, weight, round_to, tiny, most):
+    """Asserts that `got` is the gradient of logprob_row, row by row: within the
+    tolerance at every entry (a NaN is within none), infinite only where the
+    value passes `most`, the largest number of its type, and 0 at an entry that
+    is not included."""
+    for r in range(x.shape[0]):
+        v = None if valid is None else valid if valid.ndim == 1 else valid[r]
+        with np.errstate(over="ignore"):
+            _, want = logprob_row(x[r], v, T[r], targets[r], weight[r])
+        assert not np.isnan(want).any(), "the formula itself has no value here"
+        ok = included(x[r], v)
+        assert np.all(got[r][~ok] == 0.0), (r, "not included", np.nonzero(got[r][~ok] != 0)[0][:5])
+        tol = gradient_tolerance(x[r], v, T[r], targets[r], weight[r], round_to, tiny)
+        with np.errstate(invalid="ignore"):
+            near = np.abs(got[r].astype(np.float64) - want) <= tol
+        beyond = np.isinf(got[r]) & (np.sign(got[r]) == np.sign(want)) & (np.abs(want) + tol > most)
+        bad = ~(near & np.isfinite(got[r]) | beyond)
+        assert not bad.any(), (r, np.nonzero(bad)[0][:5], got[r][bad][:5], want[bad][:5])
+
+
 def embed(table, ids, scale):
     out = np.zeros((len(ids), table.shape[1]))
     for i, v in enumerate(ids):
