@@ -78,7 +78,7 @@ def test_specials(dtype, n):
                      [low, 3, low, low, nan, 1], [-low, low, -low, 0, 1, 2],
                      [0.0, -0.0, nan, -inf, inf, 5]])
     rng = np.random.default_rng(n)
-    x = head[:, rng.integers(0, 6, n)]
+    x = np.ascontiguousarray(head[:, rng.integers(0, 6, n)])
     x[:, :6] = head
     x = torch.from_numpy(x).to(dtype)
     targets = rng.integers(-1, 12, (len(x), 9)).astype(np.int32)
