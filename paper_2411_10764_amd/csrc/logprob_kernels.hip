@@ -33,6 +33,7 @@ constexpr int kThreads = 256;
 constexpr int kChunk = 2048;      // smallest chunk
 constexpr int kPairs = 128;       // targets of a workgroup compared pair by pair
 constexpr float kLog2e = 1.44269504088896340736f;
+constexpr float kPlainMost = 4294967296.0f;  // 2^32: what row_kernel's fast sum stays below
 
 struct Stat {
   float m, l;  // maximum of the included scores, sum of exp((s - m) * R)
@@ -324,9 +325,13 @@ __global__ __launch_bounds__(1024, 8) void row_kernel(Rows k) {
   m = block_max(m, red);
 
   // exp2(s * c - b) with b = m * c rounded: one fused operation an entry.
-  // What b is off by is put right in l.  NaN scores, infinite maxima and
-  // temperatures that overflow c leave a sum that no row of finite scores has
-  // (the best entry alone counts 1): such a row is summed again, entry by entry.
+  // What b is off by is put right in l.  Where m / T passes 2^24 that can be
+  // many powers of two, in either direction; NaN scores, infinite maxima and
+  // temperatures that overflow c leave a NaN or nothing.  So the sum has to be
+  // from 1/2 to 2^32: with the at most 2^16 entries of a row here the best one
+  // then counts 2^-17 to 2^32, and factors that mend that are far from the ends
+  // of float32.  Any other row is summed again, entry by entry, as differences to
+  // the maximum.
   const float b = m * c;
   float l = 0.0f;
 #pragma unroll
@@ -338,7 +343,7 @@ __global__ __launch_bounds__(1024, 8) void row_kernel(Rows k) {
   }
   hold();
   l = block_sum(l, red);
-  const bool plain = l >= 0.5f && l < __builtin_inff();
+  const bool plain = l >= 0.5f && l < kPlainMost;
   if (plain) {
     l *= __builtin_amdgcn_exp2f(-__builtin_fmaf(m, c, -b));
   } else {
