@@ -443,7 +443,8 @@ ml2_status ml2_sample(int32_t dtype, const void *scores, int64_t n, int64_t ld, 
  * the scores, in their type, element (r, i) at grad[r * grad_ld + i]:
  *   grad_i = R * (sum of weight_j over targets j = i
  *                 - exp(z_i) / sum_k exp(z_k) * sum_j weight_j)
- * and 0 where an entry is not included.  weight: float32 [rows][per_row];
+ * (0 where the difference is, whatever R), and 0 where an entry is not
+ * included.  weight: float32 [rows][per_row];
  * logprob: float32 [rows][per_row], or NULL in ml2_logprob_grad.  Weights of
  * a repeated target are added in the order of j, so results are the same in
  * every run.  Workspace as in ml2_sample.

@@ -52,6 +52,13 @@ __device__ __forceinline__ float weight_of(float x, float m, float c) {
   return fminf(__builtin_amdgcn_exp2f((x - m) * c), 1.0f);
 }
 
+// A part of the gradient times R = 1 / T, which comes last: what is 0 (an entry
+// without probability, a target that holds all of it) stays 0 where R, or R times
+// the weights, passes float32.
+__device__ __forceinline__ float times_r(float part, float r) {
+  return part == 0.0f ? 0.0f : part * r;
+}
+
 // Maximum and sum over the workgroup, in every thread; sums in the order of
 // the lanes and then of the waves.  They begin with the barrier that frees lds.
 __device__ __forceinline__ float block_max(float v, float *lds) {
@@ -231,11 +238,11 @@ __device__ __forceinline__ void outside(const Rows &k, int64_t row) {
   }
 }
 
-// The listed targets' log-probabilities and the gradient at their entries.
-// scale = -(sum of weights) / l * R, bias so that exp2((s - m) * c) is right.
+// The listed targets' log-probabilities and the gradient at their entries;
+// share = (sum of weights) / l.
 template <typename T>
 __device__ __forceinline__ void at_targets(const Rows &k, int64_t row, unsigned long long *list,
-                                           int count, Stat st, float r, float scale) {
+                                           int count, Stat st, float r, float share) {
   const float *weight = k.a.weight + row * k.a.per_row;
   if (k.a.logprob) {
     for (int a = threadIdx.x; a < count; a += blockDim.x) {
@@ -248,7 +255,7 @@ __device__ __forceinline__ void at_targets(const Rows &k, int64_t row, unsigned 
   each_entry(list, count, weight, [&](int64_t t, float sum) {
     const float x = load_score<T>(k, row, t);
     if (x != ninf())
-      grad[t] = narrow<T>(weight_of(x, st.m, r * kLog2e) * scale + sum * r);
+      grad[t] = narrow<T>(times_r(sum - weight_of(x, st.m, r * kLog2e) * share, r));
   });
 }
 
@@ -343,7 +350,8 @@ __global__ __launch_bounds__(1024, 8) void row_kernel(Rows k) {
   }
   hold();
   l = block_sum(l, red);
-  const bool plain = l >= 0.5f && l < kPlainMost;
+  const float fast = l;
+  const bool plain = fast >= 0.5f && fast < kPlainMost;
   if (plain) {
     l *= __builtin_amdgcn_exp2f(-__builtin_fmaf(m, c, -b));
   } else {
@@ -364,10 +372,12 @@ __global__ __launch_bounds__(1024, 8) void row_kernel(Rows k) {
     }
     return;
   }
-  const float scale = -w / l * r;
+  const float share = w / l;
   T *grad = static_cast<T *>(k.a.grad) + row * k.a.grad_ld;
-  if (plain) {
-    const float fit = scale * __builtin_amdgcn_exp2f(-__builtin_fmaf(m, c, -b));
+  // what the fast weights are off by, the fast sum is too.  A factor that passes
+  // float32 would make a NaN of a weight of 0: the way entry by entry, then.
+  const float fit = -w / fast * r;
+  if (plain && __builtin_fabsf(fit) < __builtin_inff()) {
 #pragma unroll
     for (int g = 0; g < VECS; ++g) {
       const int i = (g * threads + (int)threadIdx.x) * kLen;
@@ -391,11 +401,11 @@ __global__ __launch_bounds__(1024, 8) void row_kernel(Rows k) {
 #pragma unroll 1
     for (int i = threadIdx.x; i < n; i += threads) {
       const float x = load_score<T>(k, row, i);
-      grad[i] = narrow<T>(x == ninf() ? 0.0f : weight_of(x, m, c) * scale);
+      grad[i] = narrow<T>(x == ninf() ? 0.0f : times_r(weight_of(x, m, c) * -share, r));
     }
   }
   __syncthreads();
-  at_targets<T>(k, row, list, count, st, r, scale);
+  at_targets<T>(k, row, list, count, st, r, share);
 }
 
 // ---- rows in chunks ----------------------------------------------------------------
@@ -488,13 +498,13 @@ __global__ __launch_bounds__(kThreads) void grad_kernel(Rows k) {
   const int count = list_targets(targets, k.a.per_row, lo, hi, list, waves_at);
   const Part p = row_part(k, row, c, red);
   if (chunk == 0 && k.a.logprob) outside(k, row);
-  const float scale = -p.w / p.s.l * r;
+  const float share = p.w / p.s.l;
   T *grad = static_cast<T *>(k.a.grad) + row * k.a.grad_ld;
   for (int64_t i = lo + threadIdx.x * 8; i < hi; i += kThreads * 8) {
     V o;
 #pragma unroll
     for (int j = 0; j < 8; ++j)
-      o[j] = narrow<T>(x[j] == ninf() ? 0.0f : weight_of(x[j], p.s.m, c) * scale);
+      o[j] = narrow<T>(x[j] == ninf() ? 0.0f : times_r(weight_of(x[j], p.s.m, c) * -share, r));
     if (i + 8 <= hi) {
       *reinterpret_cast<V *>(grad + i) = o;
     } else {
@@ -505,7 +515,7 @@ __global__ __launch_bounds__(kThreads) void grad_kernel(Rows k) {
     load8(scores, valid, i + kThreads * 8, hi, x);
   }
   __syncthreads();
-  at_targets<T>(k, row, list, count, p.s, r, scale);
+  at_targets<T>(k, row, list, count, p.s, r, share);
 }
 
 // ---- plans -------------------------------------------------------------------

@@ -86,3 +86,29 @@ def test_specials(dtype, n):
     T = np.array([1, 1, 2, 1, 0.5, 1, 0], np.float32)
     for valid in (None, np.zeros(n, np.uint8), (rng.random(x.shape) < 0.5).astype(np.uint8)):
         _check(x, valid, targets, weight, T)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("n", [6, 3001, 70001])
+def test_not_included_is_zero_whatever_the_weights(dtype, n):
+    """Weights whose sum or share over a small temperature passes float32's range:
+    entries that are not included get 0 all the same, and so do those without
+    probability and a target that holds all of it."""
+    rng = np.random.default_rng(n)
+    rows = 8
+    x = torch.from_numpy(rng.uniform(-9, -1, (rows, n)).astype(np.float32)).to(dtype)
+    x[:, 0] = 0.0
+    x[4:, 1] = 0.0  # two that share the probability
+    x[:, 2] = -np.inf
+    x[1::2, 3] = np.nan
+    valid = np.ones((rows, n), np.uint8)
+    valid[:, 4] = 0
+    targets = np.array([[0, -1, 4, n]] * rows, np.int32)
+    weight = np.array([[10.0, 3.0, 5.0, 2.0]] * rows, np.float32)
+    T = np.full(rows, 1e-38, np.float32)
+    T[2:4] = 3e-39
+    T[6:] = 1e-45  # 1 / T itself is infinite
+    _check(x, valid, targets, weight, T)
+    weight[:] = 3e38
+    T[:] = 1.0
+    _check(x, valid, targets, weight, T)
