@@ -46,10 +46,12 @@ struct Part {
 
 __device__ __forceinline__ float ninf() { return -__builtin_inff(); }
 
-// exp(y * ln 2) of a difference to the maximum.  Where maximum and score are
-// both infinite their difference is NaN and the entry counts as the maximum.
-__device__ __forceinline__ float weight_of(float x, float m, float c) {
-  return fminf(__builtin_amdgcn_exp2f((x - m) * c), 1.0f);
+// exp(z) of a score against the maximum.  Where both are infinite their
+// difference is NaN and the entry counts as the maximum.  R is multiplied before
+// log2(e): their product passes float32 where R alone, at temperatures below
+// 4.3e-39, does not.
+__device__ __forceinline__ float weight_of(float x, float m, float r) {
+  return fminf(__builtin_amdgcn_exp2f((x - m) * r * kLog2e), 1.0f);
 }
 
 // A part of the gradient times R = 1 / T, which comes last: what is 0 (an entry
@@ -87,9 +89,9 @@ __device__ __forceinline__ float block_sum(float v, float *lds) {
 }
 
 // The threads' pairs as one: their maximum, and their sums brought to it.
-__device__ __forceinline__ Stat block_join(Stat s, float c, float *lds) {
+__device__ __forceinline__ Stat block_join(Stat s, float r, float *lds) {
   const float m = block_max(s.m, lds);
-  return {m, block_sum(s.m == ninf() ? 0.0f : s.l * weight_of(s.m, m, c), lds)};
+  return {m, block_sum(s.m == ninf() ? 0.0f : s.l * weight_of(s.m, m, r), lds)};
 }
 
 struct Rows {
@@ -255,7 +257,7 @@ __device__ __forceinline__ void at_targets(const Rows &k, int64_t row, unsigned 
   each_entry(list, count, weight, [&](int64_t t, float sum) {
     const float x = load_score<T>(k, row, t);
     if (x != ninf())
-      grad[t] = narrow<T>(times_r(sum - weight_of(x, st.m, r * kLog2e) * share, r));
+      grad[t] = narrow<T>(times_r(sum - weight_of(x, st.m, r) * share, r));
   });
 }
 
@@ -359,7 +361,7 @@ __global__ __launch_bounds__(1024, 8) void row_kernel(Rows k) {
 #pragma unroll 1
     for (int i = threadIdx.x; i < n; i += threads) {
       const float x = load_score<T>(k, row, i);
-      if (x != ninf()) l += weight_of(x, m, c);
+      if (x != ninf()) l += weight_of(x, m, r);
     }
     l = block_sum(l, red);
   }
@@ -401,7 +403,7 @@ __global__ __launch_bounds__(1024, 8) void row_kernel(Rows k) {
 #pragma unroll 1
     for (int i = threadIdx.x; i < n; i += threads) {
       const float x = load_score<T>(k, row, i);
-      grad[i] = narrow<T>(x == ninf() ? 0.0f : times_r(weight_of(x, m, c) * -share, r));
+      grad[i] = narrow<T>(x == ninf() ? 0.0f : times_r(weight_of(x, m, r) * -share, r));
     }
   }
   __syncthreads();
@@ -420,7 +422,7 @@ __global__ __launch_bounds__(kThreads) void stats_kernel(Rows k) {
   const T *scores = row_scores<T>(k, row);
   const uint8_t *valid = row_mask(k, row);
   bool greedy;
-  const float c = inverse_temperature(k.a.s.temperature, row, &greedy) * kLog2e;
+  const float r = inverse_temperature(k.a.s.temperature, row, &greedy);
   Stat s = {ninf(), 0.0f};
   float next[8];
   load8(scores, valid, lo + threadIdx.x * 8, hi, next);
@@ -439,28 +441,28 @@ __global__ __launch_bounds__(kThreads) void stats_kernel(Rows k) {
 #pragma unroll
     for (int j = 0; j < 8; ++j) m = fmaxf(m, x[j]);
     if (m == ninf()) continue;
-    float l = s.m == ninf() ? 0.0f : s.l * weight_of(s.m, m, c);
+    float l = s.m == ninf() ? 0.0f : s.l * weight_of(s.m, m, r);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) l += x[j] == ninf() ? 0.0f : weight_of(x[j], m, c);
+    for (int j = 0; j < 8; ++j) l += x[j] == ninf() ? 0.0f : weight_of(x[j], m, r);
     s = {m, l};
   }
-  s = block_join(s, c, red);
+  s = block_join(s, r, red);
   if (threadIdx.x == 0) k.part[blockIdx.x] = {s, w};
 }
 
 // The row's maximum, sum and weights, in every thread.
-__device__ __forceinline__ Part row_part(const Rows &k, int64_t row, float c, float *red) {
+__device__ __forceinline__ Part row_part(const Rows &k, int64_t row, float r, float *red) {
   Part p = {{ninf(), 0.0f}, 0.0f};
   for (int64_t i = threadIdx.x; i < k.chunks; i += blockDim.x) {
     const Part o = k.part[row * k.chunks + i];
     if (o.s.m != ninf()) {
       const float m = fmaxf(p.s.m, o.s.m);
-      const float l = p.s.m == ninf() ? 0.0f : p.s.l * weight_of(p.s.m, m, c);
-      p.s = {m, l + o.s.l * weight_of(o.s.m, m, c)};
+      const float l = p.s.m == ninf() ? 0.0f : p.s.l * weight_of(p.s.m, m, r);
+      p.s = {m, l + o.s.l * weight_of(o.s.m, m, r)};
     }
     p.w += o.w;
   }
-  p.s = block_join(p.s, c, red);
+  p.s = block_join(p.s, r, red);
   if (k.a.grad) p.w = block_sum(p.w, red);
   return p;
 }
@@ -471,7 +473,7 @@ __global__ __launch_bounds__(kThreads) void finish_kernel(Rows k) {
   const int64_t row = blockIdx.x;
   bool greedy;
   const float r = inverse_temperature(k.a.s.temperature, row, &greedy);
-  const Part p = row_part(k, row, r * kLog2e, red);
+  const Part p = row_part(k, row, r, red);
   for (int j = threadIdx.x; j < k.a.per_row; j += kThreads) {
     const int64_t t = k.a.targets[row * k.a.per_row + j];
     k.a.logprob[row * k.a.per_row + j] =
@@ -490,13 +492,13 @@ __global__ __launch_bounds__(kThreads) void grad_kernel(Rows k) {
   const T *scores = row_scores<T>(k, row);
   const uint8_t *valid = row_mask(k, row);
   bool greedy;
-  const float r = inverse_temperature(k.a.s.temperature, row, &greedy), c = r * kLog2e;
+  const float r = inverse_temperature(k.a.s.temperature, row, &greedy);
   const int32_t *targets = k.a.targets + row * k.a.per_row;
   // what does not wait for the row's sum first: its first scores, its targets
   float x[8];
   load8(scores, valid, lo + threadIdx.x * 8, hi, x);
   const int count = list_targets(targets, k.a.per_row, lo, hi, list, waves_at);
-  const Part p = row_part(k, row, c, red);
+  const Part p = row_part(k, row, r, red);
   if (chunk == 0 && k.a.logprob) outside(k, row);
   const float share = p.w / p.s.l;
   T *grad = static_cast<T *>(k.a.grad) + row * k.a.grad_ld;
@@ -504,7 +506,7 @@ __global__ __launch_bounds__(kThreads) void grad_kernel(Rows k) {
     V o;
 #pragma unroll
     for (int j = 0; j < 8; ++j)
-      o[j] = narrow<T>(x[j] == ninf() ? 0.0f : times_r(weight_of(x[j], p.s.m, c) * -share, r));
+      o[j] = narrow<T>(x[j] == ninf() ? 0.0f : times_r(weight_of(x[j], p.s.m, r) * -share, r));
     if (i + 8 <= hi) {
       *reinterpret_cast<V *>(grad + i) = o;
     } else {

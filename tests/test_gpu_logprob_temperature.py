@@ -53,3 +53,20 @@ def test_small_temperatures(dtype, T, n):
     valid[np.arange(rows), at] = 1
     for v in (None, valid):
         _check(x, v, targets, weight, np.full(rows, T, np.float32))
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("n", [40, 3001, 70001])
+@pytest.mark.parametrize("T", [1e-38, 4e-39, 3.2e-39])
+def test_temperatures_as_small_as_the_scores(dtype, n, T):
+    """Scores of about T where 1 / T is finite, log2(e) / T not: the exponents are
+    ordinary numbers.  Scores are whole numbers of 2^-133, bfloat16's smallest."""
+    rng = np.random.default_rng(n)
+    x = torch.from_numpy(rng.integers(-250, 20, (3, n)).astype(np.float32) * 2.0 ** -133).to(dtype)
+    x[:, 0] = 40 * 2.0 ** -133
+    valid = (rng.random((3, n)) < 0.6).astype(np.uint8)
+    valid[:, 0] = 1
+    targets = rng.integers(-1, n + 1, (3, 5)).astype(np.int32)
+    targets[:, 0] = 0
+    weight = (rng.standard_normal((3, 5)) * 0.01).astype(np.float32)
+    _check(x, valid, targets, weight, np.full(3, T, np.float32))
