@@ -392,7 +392,8 @@ ml2_status ml2_stream_explorer_end(ml2_stream_explorer *ex, int32_t *out_idx, fl
  * temperature, top_k, top_p, min_p: device arrays [rows], or NULL for
  * T = 1 and no such limit.  A row without an included entry is not an error.
  * Like the calls above these only enqueue kernels, allocate nothing and may be
- * captured into a HIP graph once each has run outside the capture.
+ * captured into a HIP graph once each has run outside the capture.  What a call
+ * writes (outputs and workspace) shares no memory with what else it is given.
  */
 typedef enum { ML2_F32 = 0, ML2_BF16 = 1, ML2_F16 = 2 } ml2_dtype;
 
@@ -448,8 +449,11 @@ ml2_status ml2_sample(int32_t dtype, const void *scores, int64_t n, int64_t ld, 
  * logprob: float32 [rows][per_row], or NULL in ml2_logprob_grad.  Weights of
  * a repeated target are added in the order of j, so results are the same in
  * every run.  Workspace as in ml2_sample.
- * Errors as ml2_sample (per_row > ML2_MAX_TOPK: UNSUPPORTED; grad_ld < n:
- * INVALID_ARG).
+ * A gradient in the scores' own memory, in whole or in part, is refused: scores
+ * are read again at the targets after it is written (columns beside theirs in
+ * one buffer will do).  So is logprob in the memory of targets or weight.
+ * Errors as ml2_sample (per_row > ML2_MAX_TOPK: UNSUPPORTED; grad_ld < n and
+ * shared memory: INVALID_ARG).
  */
 ml2_status ml2_logprob_workspace_bytes(int64_t n, int64_t rows, int32_t per_row, size_t *bytes);
 ml2_status ml2_logprob(int32_t dtype, const void *scores, int64_t n, int64_t ld, int64_t rows,

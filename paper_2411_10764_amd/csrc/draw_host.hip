@@ -48,6 +48,31 @@ ml2_status check_rows(const char *call, int32_t dtype, const ml2::ScoreRows &s, 
   return ML2_OK;
 }
 
+// Whether two matrices of `rows` rows of n elements of `size` bytes, lda and ldb
+// elements apart and aligned to their elements, have one in common.  Columns of
+// one buffer lie between one another without that.
+bool overlap(const void *a, int64_t lda, const void *b, int64_t ldb, int64_t rows, int64_t n,
+             size_t size) {
+  if (!a || !b || rows <= 0 || n <= 0) return false;
+  const uintptr_t pa = reinterpret_cast<uintptr_t>(a), pb = reinterpret_cast<uintptr_t>(b);
+  if (pa > pb) return overlap(b, ldb, a, lda, rows, n, size);
+  const uint64_t d = (pb - pa) / size;  // b's first element, counted from a's
+  const uint64_t la = (uint64_t)lda, lb = (uint64_t)ldb, len = (uint64_t)n;
+  if (d >= (uint64_t)(rows - 1) * la + len) return false;
+  if (la == lb) {
+    // row r of b begins in row r + d / la of a, or behind its end and reaches on
+    // into the next
+    const uint64_t at = d % la, row = d / la;
+    return at < len || (row + 1 < (uint64_t)rows && at + len > la);
+  }
+  for (uint64_t i = 0, j = 0; i < (uint64_t)rows && j < (uint64_t)rows;) {
+    const uint64_t x = i * la, y = d + j * lb;
+    if (x < y + len && y < x + len) return true;
+    if (x < y) ++i; else ++j;
+  }
+  return false;
+}
+
 // n, rows and per_row of a workspace query.
 ml2_status check_sizes(const char *call, int64_t n, int64_t rows, int32_t per_row,
                        const size_t *bytes) {
@@ -144,6 +169,14 @@ ml2_status ml2_logprob_grad(int32_t dtype, const void *scores, int64_t n, int64_
                 "not aligned to its type", (long long)grad_ld, (long long)n);
   if (rows > 0 && per_row > 0 && !weight)
     return fail(ML2_ERR_INVALID_ARG, "ml2_logprob_grad: weight is NULL");
+  const bool sizes = size_ok(n) && size_ok(rows) && rows <= ML2_MAX_ROWS && per_row >= 0 &&
+                     per_row <= ML2_MAX_TOPK && ld >= n && ld <= (int64_t)1 << 40;  // else refused below
+  if (sizes && overlap(scores, ld, grad, grad_ld, rows, n, size))
+    return fail(ML2_ERR_INVALID_ARG, "ml2_logprob_grad: grad overlaps scores");
+  const int64_t items = sizes ? rows * per_row : 0;
+  if (overlap(logprob_out, items, targets, items, 1, items, 4) ||
+      overlap(logprob_out, items, weight, items, 1, items, 4))
+    return fail(ML2_ERR_INVALID_ARG, "ml2_logprob_grad: logprob overlaps targets or weight");
   // n = 0: no gradient to write, log-probabilities all the same
   const ml2::LogprobArgs a = {{scores, n, ld, rows, valid, valid_ld, temperature},
                               targets, weight, per_row, logprob_out, grad, grad_ld};

@@ -112,3 +112,25 @@ def test_not_included_is_zero_whatever_the_weights(dtype, n):
     weight[:] = 3e38
     T[:] = 1.0
     _check(x, valid, targets, weight, T)
+
+
+@pytest.mark.parametrize("rows,n", [(5, 3001), (2, 70001)])
+def test_scores_and_gradient_in_one_buffer(rows, n):
+    """Columns of one buffer are taken; the scores' own memory is refused."""
+    rng = np.random.default_rng(n)
+    x, valid, targets, weight, T = _case(rng, rows, n, 6, torch.float32, True)
+    both = torch.full((rows, 2 * n), 3.0, device=DEV)
+    both[:, :n] = x.to(DEV)
+    t, v, w, at = [torch.from_numpy(a).to(DEV) for a in (targets, valid, weight, T)]
+    ws = ml2.LogProb(rows, n, 6).ws
+    ml2.ml2_logprob_grad(both[:, :n], t, w, both[:, n:], ws, None, v, at)
+    torch.cuda.synchronize()
+    assert torch.equal(both[:, :n].cpu(), x)
+    drawutil.check_gradient(both[:, n:].cpu().numpy(), x.numpy(), valid, T, targets, weight,
+                            ROUND[torch.float32], TINY[torch.float32],
+                            float(np.finfo(np.float32).max))
+    for grad in (both[:, :n], both[:, 1:n + 1]):
+        with pytest.raises(ml2.Ml2Error, match="overlaps"):
+            ml2.ml2_logprob_grad(both[:, :n], t, w, grad, ws, None, v, at)
+    torch.cuda.synchronize()
+    assert torch.equal(both[:, :n].cpu(), x)
