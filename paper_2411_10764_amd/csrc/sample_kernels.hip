@@ -1753,16 +1753,13 @@ hipError_t launch_long(const SampleArgs &a, void *ws, int cu_count, hipStream_t 
     const int64_t parts = std::max<int64_t>(1, (int64_t)cu_count * 2 / rows);
     k.span = std::max<int64_t>(1, (a.s.n + parts * kSpan - 1) / (parts * kSpan)) * kSpan;
     k.spans = (a.s.n + k.span - 1) / k.span;
-    // What a row's workgroup does is a chain of short steps; waves beyond one a
-    // SIMD only pay where there is much to go through.
-    const int finish = a.s.n > (1 << 20) ? 1024 : 512;
     const uint32_t grid = (uint32_t)(rows * k.chunks);
     range_kernel<T><<<grid, 256, 0, s>>>(k);
-    if (a.top_k || a.top_p || a.s.temperature) 
+    if (a.top_k || a.top_p || a.s.temperature)
       count_kernel<T><<<(uint32_t)(rows * k.spans), 1024, 0, s>>>(k);
     settle_kernel<<<(uint32_t)rows, 512, 0, s>>>(k);
     collect_kernel<T><<<grid, 256, 0, s>>>(k);
-    finish_kernel<T><<<(uint32_t)rows, finish, sizeof(Finish), s>>>(k);
+    finish_kernel<T><<<(uint32_t)rows, 1024, sizeof(Finish), s>>>(k);
     if (a.draws > kFewDraws) {
       const int blocks = (a.draws + 3) / 4;
       draw_kernel<T><<<(uint32_t)(rows * blocks), 256, 0, s>>>(k, blocks);
