@@ -1269,15 +1269,26 @@ __global__ __launch_bounds__(256) void draw_kernel(Long k, int blocks) {
 //                 many of the entries that have it are kept; the parts' weights;
 //                 and a walk over the part that holds the draw
 // The row is read once, and one of its parts once more.  The chunked path reads
-// it three times and takes two exponentials an entry: 256 x 100,003 bf16 94 us
-// there and 47 here, 4 x 131,072 bf16 29 and 25, 16 x 50,000 fp16 at top_p
-// 0.95 38 and 37.  More draws walk more parts (four of 16 x 50,000 rows: 40 us
-// against 32), and longer rows have more pairs than one workgroup goes through
-// in that time: 16-bit floats of 10 bits an octave 200,000 entries a row at
-// top_p 0.95 71 us against 49, those of 7 bits 900,000 entries 52 against 51.
+// it three times and takes two exponentials an entry, but a workgroup a row goes
+// through all its pairs here, of which 16-bit floats of 10 bits an octave have
+// more.  The settings are the device's, so length and type decide.  Times in us,
+// here / there, of normal scores of deviation 2.5 at top-k 50 and top-p 0.9, at
+// top-p 0.95, and with no limit:
+//                     4 rows                64 rows               256 rows
+//   fp16   65,536   25/31 41/37 34/25     26/42 44/50 37/32     39/53 59/72 51/46
+//   fp16   98,304   26/30 47/36 35/23     27/41 52/51 40/32     42/64 66/87 58/56
+//   bf16  131,072   25/32 32/34 27/25     27/45 34/54 29/37     49/77 56/106 51/68
+//   bf16  262,144   24/33 42/37 33/25     36/53 49/70 43/45     95/116 118/166 107/107
+//   bf16  524,288   26/36 45/43 34/27     47/74 70/105 61/66
+// fp16 ends where a row of top-p alone no longer gains in any number of rows but
+// the largest, bf16 where a few such rows have lost as much.  More draws walk more
+// parts: four of 16 x 50,000 rows 40 us against 32.
 constexpr int kPartVecs = 7;                      // vectors of 8 entries of a thread
 constexpr int kPartMost = kPartVecs * 1024 * 8;   // below 65,536: 16-bit counters
-constexpr int kPartLeast = 24576;                 // 16,384: 64 x 50,021 fp16 38.7 -> 41 us
+// Smallest part: 64 rows of 50,021 at top-p 0.95 with 16,384, this, 32,768: fp16
+// 43.9, 41.4, 42.0 us, bf16 28.4, 29.1, 34.2; of 32,768 fp16 36.4, 35.5, 35.4, bf16
+// 26.7, 28.4, 28.2.
+constexpr int kPartLeast = 24576;
 constexpr int kParts = 16;                        // of a row, at most
 constexpr int64_t kValueMostBf16 = 1 << 18, kValueMostF16 = 1 << 16;
 static_assert(kValueMostBf16 <= (int64_t)kParts * kPartMost);
