@@ -471,7 +471,8 @@ ml2_status ml2_logprob_grad(int32_t dtype, const void *scores, int64_t n, int64_
  * Rows of a learned table, scaled: out row i = scale * table row ids[i]
  * (float32 product, rounded once), zeros where ids[i] lies outside
  * [0, table_rows).  table: [table_rows][ld] of dtype, columns 0..width-1 are
- * read; ids: int32 [n]; out: [n][out_ld] of dtype.
+ * read; ids: int32 [n]; out: [n][out_ld] of dtype; scale: a finite number, as
+ * in ml2_embed_grad.
  * Errors: INVALID_ARG (unknown dtype, NULL pointers that are needed, sizes
  * < 0 or > INT32_MAX, ld or out_ld < width, misaligned arrays), UNSUPPORTED
  * (width > ML2_MAX_WIDTH), HIP.

@@ -16,6 +16,8 @@
 // A table of few numbers (rows * width at most kFewCells, width at most
 // kFewWidth) needs no sort: every lane of a wave holds a table of its own in
 // LDS (few_kernel), and the lanes' and waves' tables are added up in order.
+// More numbers do not fit the LDS of a compute unit: 4,194,304 tokens into 512
+// float32 numbers 52 us, into 513, sorted, 160.
 //
 // Measured: lookup of 32,768 x 1,024 bf16 22 us; its gradient into 131,072
 // float32 rows 149 us (604 MB, 4.1 TB/s, most of it the clearing); 4,194,304

@@ -19,9 +19,16 @@
 // every workgroup of a row arrives at the same m and l.  Weights are joined
 // in the order of j inside a chunk, then in chunk order.
 //
+// Weights below 2^-126 of the best entry's are 0, as the exp2 instruction flushes
+// them: the sum, which is at least 1, does not show it, and such an entry's own
+// gradient is 0.
+//
 // Measured: 4,096 x 50,021 bf16 gradient 191 us (820 MB, 4.3 TB/s of a copy's
-// 4.65); 1 x 4,194,304 float32 with 512 targets 12 us; 1 x 262,144 gradient with
-// 128 targets 15 us, two launches of dependent loads.
+// 4.65; rows padded to 50,024 entries, 231 where they follow one another); 1 x
+// 4,194,304 float32 with 512 targets 12 us; 1 x 262,144 gradient with 128 targets
+// 15 us, two launches of dependent loads.  What a second read of the scores costs:
+// 4,096 rows of 65,536 bf16 211 us, of 65,537 384; of 32,768 float32 191, of
+// 32,769 357.
 #include <algorithm>
 
 #include "draw.h"
@@ -104,7 +111,10 @@ struct Rows {
 enum Mode { kForward, kGradient, kGradientPastCache };
 
 // A gradient of more bytes than this (half of the last cache) is written past
-// the caches: 4,096 x 50,021 bf16 207 -> 191 us.
+// the caches; a smaller one stays there for whoever reads it next.  50,021 bf16
+// entries a row, past the caches and not: 700 rows (67 MiB) 36 and 38 us, 1,300
+// (124 MiB) 67 and 71, 1,400 (134 MiB) 66 and 80, 2,680 (256 MiB) 124 and 161,
+// 4,096 (391 MiB) 231 and 240.
 constexpr int64_t kPastCache = (int64_t)128 << 20;
 
 template <typename T>

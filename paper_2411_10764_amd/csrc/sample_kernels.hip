@@ -1169,7 +1169,10 @@ __global__ __launch_bounds__(1024) void finish_kernel(Long k) {
     __syncthreads();
     // f(key, weight, bin) for every listed entry.  A list longer than LDS holds
     // stays in memory, its segments shared among the waves; one that did not
-    // fit there is read from the row again.
+    // fit there is read from the row again, by this one workgroup and once a
+    // step: where more entries than the list holds have nearly the score of a
+    // cut.  Equal scores are the worst of it: 1 x 65,536 of them 0.2 ms, 1 x
+    // 1,048,576 2 ms, 1 x 16,777,216 40 ms.
     auto each = [&](auto f) {
       auto one = [&](u64 key) {
         const float z = exponent(key_score(key), l);
