@@ -64,7 +64,9 @@ typedef enum {
 #define ML2_MAX_STREAM_K 4096   /* k of ml2_stream_explorer_create */
 #define ML2_MAX_ROWS 2097152    /* rows of scores of one call */
 #define ML2_MAX_TOKENS 1073741824 /* n of ml2_embed_grad */
-#define ML2_MAX_WIDTH 65536     /* columns of ml2_embed and ml2_embed_grad */
+#define ML2_MAX_WIDTH 65536     /* columns of ml2_embed, ml2_layer_norm and their gradients */
+#define ML2_MAX_TENSORS 65536   /* count of ml2_grad_norm and ml2_adamw */
+#define ML2_STATE_BLOCK 256     /* elements that share a scale in an 8-bit state */
 
 typedef struct ml2_ensemble ml2_ensemble; /* opaque; immutable after load */
 
@@ -499,6 +501,160 @@ ml2_status ml2_embed_grad(int32_t dtype, const void *dout, int64_t n, int64_t wi
                           int64_t dout_ld, const int32_t *ids, float scale, int32_t grad_dtype,
                           void *grad, int64_t table_rows, int64_t grad_ld, void *workspace,
                           size_t workspace_bytes, void *stream);
+
+/*
+ * Layer norm of every row: with m the mean and V the variance (over width) of
+ * the columns 0..width-1 of row r, and rstd = 1 / sqrt(V + eps),
+ *   out_i = (x_i - m) * rstd * weight_i + bias_i
+ * in float32, rounded once at the end.  x: [rows][ld] of dtype, out: [rows]
+ * [out_ld] of dtype.  weight, bias: [width] of param_dtype, which is dtype or
+ * ML2_F32, or NULL (1 and 0).  mean, rstd: float32 [rows], what the gradient
+ * takes, or NULL.  eps: a positive finite number.  A row that holds a NaN or an
+ * infinity gives NaN throughout; a row of one value gives bias.
+ * out may be x itself (the same pointer and row stride), and shares no other
+ * memory with what the call reads or writes.
+ * Errors: INVALID_ARG (unknown dtype or param_dtype, NULL x or out that is
+ * needed, sizes < 0 or > INT32_MAX, ld or out_ld < width, misaligned arrays,
+ * eps, shared memory), UNSUPPORTED (width > ML2_MAX_WIDTH), HIP.
+ */
+ml2_status ml2_layer_norm(int32_t dtype, const void *x, int64_t rows, int64_t width, int64_t ld,
+                          int32_t param_dtype, const void *weight, const void *bias, float eps,
+                          void *out, int64_t out_ld, float *mean, float *rstd, void *stream);
+
+/*
+ * The gradients of that: with xhat_i = (x_i - m) * rstd and g_i = dout_i *
+ * weight_i,
+ *   dx_i      = rstd * (g_i - avg(g) - xhat_i * avg(g * xhat))   averages over the row
+ *   dweight_i = sum over rows of dout_i * xhat_i
+ *   dbias_i   = sum over rows of dout_i
+ * mean, rstd: what ml2_layer_norm wrote for these rows.  (m is taken to more
+ * than float32's precision: mean plus the average of x_i - mean.)  dout:
+ * [rows][dout_ld] and dx: [rows][dx_ld] of dtype; dweight, dbias: [width] of
+ * grad_dtype, which is dtype or ML2_F32; any of the three may be NULL.  Sums
+ * are held in float32 in an order that depends on the sizes and the device
+ * alone, so results are the same in every run.  rows = 0 gives zeros.
+ * dx may be x or dout itself (the same pointer and row stride); nothing else
+ * that is written shares memory with what the call reads or writes.
+ * workspace: at least ml2_layer_norm_grad_workspace_bytes(rows, width) bytes of
+ * device memory, 256-byte aligned, used by this call until it completes.
+ * Errors as ml2_layer_norm; INVALID_ARG for another grad_dtype or a small
+ * workspace.
+ */
+ml2_status ml2_layer_norm_grad_workspace_bytes(int64_t rows, int64_t width, size_t *bytes);
+ml2_status ml2_layer_norm_grad(int32_t dtype, const void *x, int64_t rows, int64_t width,
+                               int64_t ld, const void *dout, int64_t dout_ld, int32_t param_dtype,
+                               const void *weight, const float *mean, const float *rstd, void *dx,
+                               int64_t dx_ld, int32_t grad_dtype, void *dweight, void *dbias,
+                               void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * The norm of `count` gradients together, and what a step multiplies them by so
+ * that it is at most max_norm:
+ *   norm   = scale * sqrt(sum of all elements' squares)
+ *   factor = scale * min(1, max_norm / norm)
+ * scale > 0: what gradients of a scaled loss are multiplied by, otherwise 1;
+ * max_norm > 0: infinity for a norm alone.  Where the norm is not finite the
+ * factor is NaN, which makes ml2_adamw leave everything as it was; where it is
+ * finite and step is not NULL, the device's *step is raised by one.
+ * grads, sizes: HOST arrays of `count` device pointers (contiguous tensors of
+ * dtype) and element counts.  norm, factor: float32 [1] on the device, either may be
+ * NULL; step: int32 [1] on the device, or NULL.  Squares are summed in 64 bits in
+ * an order that depends on the sizes alone.  workspace: at least
+ * ml2_grad_norm_workspace_bytes(sizes, count) bytes of device memory, 256-byte
+ * aligned, used by this call until it completes.
+ * Errors: INVALID_ARG (unknown dtype, count or a size < 0, NULL or misaligned
+ * pointers, scale or max_norm, small workspace, norm, factor or step in the
+ * memory of a gradient or of one another), UNSUPPORTED (count >
+ * ML2_MAX_TENSORS, a size > 2^40), HIP.
+ */
+ml2_status ml2_grad_norm_workspace_bytes(const int64_t *sizes, int32_t count, size_t *bytes);
+ml2_status ml2_grad_norm(int32_t dtype, const void *const *grads, const int64_t *sizes,
+                         int32_t count, float scale, float max_norm, float *norm, float *factor,
+                         int32_t *step, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * A tensor of ml2_adamw: contiguous device arrays of n elements.
+ *   param, grad    param_dtype and grad_dtype
+ *   m, v           the state: float32 [n] each, or 8-bit states (below)
+ *   param_out, m_out, v_out   where the new ones go: NULL for in place.  Where
+ *                  one of them is another array, the old one stays as it was.
+ *   copy           grad_dtype [n], the new parameter rounded to it, or NULL
+ *   weight_decay   of this tensor, finite
+ */
+typedef struct ml2_adamw_tensor {
+  void *param;
+  const void *grad;
+  void *m, *v;
+  void *param_out, *m_out, *v_out;
+  void *copy;
+  int64_t n;
+  float weight_decay;
+} ml2_adamw_tensor;
+
+/*
+ * What a step's tensors share.
+ *   beta1, beta2   in [0, 1);  eps: positive and finite, in float32 too
+ *   lr, step       the learning rate (finite) and the number t of this step, 1 to
+ *                  INT32_MAX; where
+ *                  lr_device (float32 [1]) or step_device (int32 [1]) is not
+ *                  NULL the device's value is taken when the step runs (a step
+ *                  below 1 as 1), so a captured step can be replayed
+ *   factor         float32 [1] on the device, what gradients are multiplied by
+ *                  (ml2_grad_norm writes one), or NULL for 1.  Where it is not
+ *                  finite, parameters and states keep their values.
+ *   seed           of 8-bit states' rounding
+ */
+typedef struct ml2_adamw_options {
+  double lr, beta1, beta2, eps;
+  int64_t step;
+  const float *lr_device;
+  const int32_t *step_device;
+  const float *factor;
+  uint64_t seed;
+} ml2_adamw_options;
+
+/*
+ * A step of AdamW over `count` tensors (HOST arrays of descriptors, read during
+ * the call).  In float32, for every element:
+ *   g  = grad * factor
+ *   m' = beta1 * m + (1 - beta1) * g
+ *   v' = beta2 * v + (1 - beta2) * g * g
+ *   p' = p - (lr * weight_decay * p
+ *             + lr / (1 - beta1^t) * m' / (sqrt(v') / sqrt(1 - beta2^t) + eps))
+ * p' is rounded once to param_dtype, and once to grad_dtype for the copy.
+ *
+ * state_bits 32: m and v as they are.  state_bits 8: m and r = sqrt(v) as
+ * e4m3 numbers (1 sign, 4 exponent and 3 mantissa bits, bias 7) times a float32
+ * scale that each block of ML2_STATE_BLOCK consecutive elements has of its own:
+ * scale = max(largest size in the block / 448, 2^-100).  A state of n elements
+ * is one array, aligned to 4 bytes, of ceil(n / 256) * 256 bytes (those behind
+ * the n-th are neither read nor written) followed by ceil(n / 256) scales;
+ * ml2_adamw_state_bytes(8, n).  All bytes 0 stand for zeros.
+ * Rounding to the nearest of so few numbers would stop a slow average for good,
+ * so sizes are rounded up or down at random, unbiased: up where the 20 bits
+ * below the last one kept, plus 16 hashed bits times 16, plus 8, pass 2^20
+ * (at most 448; an r that is not 0 does not become 0, so that no element loses
+ * its denominator).  The hashed bits depend on seed, t, the tensor's place in
+ * `tensors` and the element's index alone: m takes the upper 16 and r the lower
+ * 16 bits of
+ *   h = (K + index * 0x9E3779B9) mod 2^32;  h ^= h >> 15;
+ *   h = h * 0xC13FA9A9 mod 2^32;            h ^= h >> 16
+ * with K from folding the words seed mod 2^32, seed >> 32, t, the place and
+ * (from index 2^32 on) index >> 32, by K = mix(K + word + 0x9E3779B9) from 0,
+ * mix(k): k ^= k >> 16; k *= 0x9E3779B9; k ^= k >> 15; k *= 0xC13FA9A9;
+ * k ^= k >> 16.  A block with a gradient that is NaN or infinite gets a scale of
+ * NaN.
+ *
+ * A tensor's arrays share no memory with one another or with another tensor's,
+ * but for an output that is its own input, and gradients.
+ * Errors: INVALID_ARG (unknown types or state_bits, count or n < 0, NULL or
+ * misaligned arrays, options out of range, shared memory), UNSUPPORTED (count >
+ * ML2_MAX_TENSORS, n > 2^40), HIP.
+ */
+ml2_status ml2_adamw_state_bytes(int32_t state_bits, int64_t n, size_t *bytes);
+ml2_status ml2_adamw(int32_t param_dtype, int32_t grad_dtype, int32_t state_bits,
+                     const ml2_adamw_tensor *tensors, int32_t count,
+                     const ml2_adamw_options *options, void *stream);
 
 /* Thread-local description of the last non-OK status on this thread. */
 const char *ml2_last_error(void);

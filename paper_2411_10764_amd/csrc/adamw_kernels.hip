@@ -1,0 +1,553 @@
+// The norm of many gradients together, and a step of AdamW over many tensors.
+//
+//   g = grad f,  m' = b1 m + (1 - b1) g,  v' = b2 v + (1 - b2) g g
+//   p' = p - (lr decay p + lr / (1 - b1^t) m' / (sqrt(v') / sqrt(1 - b2^t) + eps))
+//
+// Bytes bound both.  A launch takes a table of tensors by value (no copy to the
+// device, nothing to keep until it has run); a workgroup finds its tensor by one
+// comparison of all first workgroups with its own number.
+#include <math.h>
+
+#include <algorithm>
+
+#include "train.h"
+
+namespace ml2 {
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int64_t kMostBlocks = 1 << 20;  // of a launch, and a bit: the rest are loops
+
+// The last tensor of `count` whose first workgroup is not behind `block`.
+template <int MOST>
+__device__ __forceinline__ int find_tensor(const uint32_t (&first)[MOST], int count,
+                                           uint32_t block) {
+  int n = 0;
+#pragma unroll
+  for (int i = 0; i < MOST; i += 64) {
+    const int at = i + (int)(threadIdx.x & 63);
+    n += __popcll(__ballot(at < count && at < MOST && first[at < MOST ? at : 0] <= block));
+  }
+  return __builtin_amdgcn_readfirstlane(n - 1);
+}
+
+// ---- norm ------------------------------------------------------------------------
+
+constexpr int kNormTensors = 128;
+constexpr int kNormVecs = 4;       // vectors of a thread in flight
+constexpr int kNormParts = 2048;   // about as many parts, and one for each tensor
+constexpr int64_t kNormLeast = 16384;
+
+struct NormTable {
+  const void *grad[kNormTensors];
+  int64_t n[kNormTensors];
+  uint32_t first[kNormTensors];  // workgroup
+  int count;
+  int64_t chunk;                 // elements of a workgroup
+  double *part;
+};
+static_assert(sizeof(NormTable) <= 3968, "kernel arguments");
+
+__device__ __forceinline__ double block_sum(double v, double *lds) {
+  const int wave = threadIdx.x >> 6;
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) v += __shfl_xor(v, d);
+  if ((threadIdx.x & 63) == 0) lds[wave] = v;
+  __syncthreads();
+  v = lds[0];
+  for (int w = 1; w < (int)(blockDim.x >> 6); ++w) v += lds[w];
+  return v;
+}
+
+// The squares of elements a .. b - 1, a thread's share.
+template <typename T>
+__device__ __forceinline__ double squares(const T *g, int64_t a, int64_t b) {
+  constexpr int kLen = Vec<T>::kLen;
+  double s[kNormVecs] = {};
+  for (int64_t i = a + (int64_t)threadIdx.x * kLen; i < b;
+       i += (int64_t)blockDim.x * kLen * kNormVecs) {
+    float x[kNormVecs][kLen];
+#pragma unroll
+    for (int k = 0; k < kNormVecs; ++k)
+      load_floats(g, i + (int64_t)k * blockDim.x * kLen, b, x[k]);
+#pragma unroll
+    for (int k = 0; k < kNormVecs; ++k) {
+#pragma unroll
+      for (int j = 0; j < kLen; ++j) s[k] = fma((double)x[k][j], (double)x[k][j], s[k]);
+    }
+  }
+  return (s[0] + s[1]) + (s[2] + s[3]);
+}
+
+template <typename T>
+__global__ __launch_bounds__(kThreads) void square_kernel(NormTable t) {
+  __shared__ double lds[kThreads / 64];
+  const int i = find_tensor(t.first, t.count, blockIdx.x);
+  const int64_t a = (int64_t)(blockIdx.x - t.first[i]) * t.chunk;
+  const double s = block_sum(
+      squares(static_cast<const T *>(t.grad[i]), a, min(t.n[i], a + t.chunk)), lds);
+  if (threadIdx.x == 0) t.part[blockIdx.x] = s;
+}
+
+struct NormOut {
+  float scale, max_norm;
+  float *norm, *factor;
+  int32_t *step;
+};
+
+__device__ __forceinline__ void finish(const NormOut &o, double sum) {
+  const double norm = (double)o.scale * sqrt(sum);
+  const bool finite = fabs((float)norm) < __builtin_inff();
+  if (o.norm) *o.norm = (float)norm;
+  if (o.factor)
+    *o.factor = finite ? (float)((double)o.scale * fmin(1.0, (double)o.max_norm / norm))
+                       : __builtin_nanf("");
+  if (o.step && finite) *o.step += 1;
+}
+
+__global__ __launch_bounds__(1024) void finish_kernel(const double *part, int64_t parts,
+                                                      NormOut o) {
+  __shared__ double lds[16];
+  double v = 0.0;
+#pragma unroll 4
+  for (int64_t i = threadIdx.x; i < parts; i += 1024) v += part[i];
+  v = block_sum(v, lds);
+  if (threadIdx.x == 0) finish(o, v);
+}
+
+// Few elements in all: one workgroup, one launch.
+template <typename T>
+__global__ __launch_bounds__(1024) void norm_one_kernel(NormTable t, NormOut o) {
+  __shared__ double lds[16];
+  double v = 0.0;
+  for (int i = 0; i < t.count; ++i) v += squares(static_cast<const T *>(t.grad[i]), 0, t.n[i]);
+  v = block_sum(v, lds);
+  if (threadIdx.x == 0) finish(o, v);
+}
+
+constexpr int64_t kNormOne = 65536;  // elements
+
+int64_t norm_chunk(const int64_t *sizes, int32_t count) {
+  int64_t total = 0;
+  for (int32_t i = 0; i < count; ++i) total += sizes[i] / kNormParts + 1;
+  return std::max(kNormLeast, (total + 4095) / 4096 * 4096);
+}
+
+int64_t norm_parts(const int64_t *sizes, int32_t count, int64_t chunk) {
+  int64_t parts = 0;
+  for (int32_t i = 0; i < count; ++i) parts += (sizes[i] + chunk - 1) / chunk;
+  return parts;
+}
+
+template <typename T>
+hipError_t launch_norm(const void *const *grads, const int64_t *sizes, int32_t count,
+                       const NormOut &o, double *part, hipStream_t s) {
+  int64_t total = 0;
+  int32_t used = 0;
+  for (int32_t i = 0; i < count; ++i) {
+    total = std::min<int64_t>(total + sizes[i], kNormOne + 1);
+    used += sizes[i] > 0;
+  }
+  NormTable t;
+  t.chunk = norm_chunk(sizes, count);
+  t.part = part;
+  t.count = 0;
+  const bool one = total <= kNormOne && used <= 16;
+  uint32_t blocks = 0;
+  int64_t parts = 0;
+  for (int32_t i = 0; i < count; ++i) {
+    if (sizes[i] == 0) continue;
+    t.grad[t.count] = grads[i];
+    t.n[t.count] = sizes[i];
+    t.first[t.count++] = blocks;
+    blocks += (uint32_t)((sizes[i] + t.chunk - 1) / t.chunk);
+    if (!one && t.count == kNormTensors) {
+      square_kernel<T><<<blocks, kThreads, 0, s>>>(t);
+      parts += blocks;
+      t.part += blocks;
+      t.count = 0;
+      blocks = 0;
+    }
+  }
+  if (one) {
+    norm_one_kernel<T><<<1, 1024, 0, s>>>(t, o);
+    return hipGetLastError();
+  }
+  if (t.count > 0) square_kernel<T><<<blocks, kThreads, 0, s>>>(t);
+  finish_kernel<<<1, 1024, 0, s>>>(part, parts + blocks, o);
+  return hipGetLastError();
+}
+
+// ---- step ------------------------------------------------------------------------
+
+constexpr int kTensors = 48;
+constexpr int kTile = 2048;  // elements of a workgroup and turn
+
+struct StepTable {
+  void *param[kTensors];
+  const void *grad[kTensors];
+  void *m[kTensors], *v[kTensors];
+  void *param_out[kTensors], *m_out[kTensors], *v_out[kTensors];
+  void *copy[kTensors];
+  int64_t n[kTensors];
+  float decay[kTensors];
+  uint32_t first[kTensors];  // workgroup
+};
+
+struct StepShared {
+  int64_t tiles;          // of a workgroup
+  double log_b1, log_b2;
+  const float *lr_device;
+  const int32_t *step_device;
+  const float *factor;
+  float lr, b1, b2, a1, a2, eps;  // a: 1 - b
+  float rate, root;       // lr / (1 - b1^t), 1 / sqrt(1 - b2^t)
+  uint32_t step, key;     // key: of the seed
+  int32_t count, place;   // place: of the table's first tensor
+};
+static_assert(sizeof(StepTable) + sizeof(StepShared) <= 4096, "kernel arguments");
+
+constexpr uint32_t kPhi = 0x9E3779B9u, kPlastic = 0xC13FA9A9u;  // 2^32 over those numbers
+
+__host__ __device__ __forceinline__ uint32_t fold_word(uint32_t k, uint32_t word) {
+  k += word + kPhi;
+  k = (k ^ (k >> 16)) * kPhi;
+  k = (k ^ (k >> 15)) * kPlastic;
+  return k ^ (k >> 16);
+}
+
+__host__ __device__ __forceinline__ void rates(double lr, double step, double log_b1,
+                                               double log_b2, float *rate, float *root) {
+  *rate = (float)(lr / -expm1(step * log_b1));
+  *root = (float)(1.0 / sqrt(-expm1(step * log_b2)));
+}
+
+// What a workgroup needs of the step: the same in all its threads.
+struct Step {
+  float f, lr, rate, root, b1, b2, a1, a2, eps;
+  bool taken;  // the factor is finite
+  uint32_t step;
+};
+
+__device__ __forceinline__ Step read_step(const StepShared &o) {
+  Step s;
+  s.f = o.factor ? *o.factor : 1.0f;
+  s.taken = fabsf(s.f) < __builtin_inff();
+  s.lr = o.lr;
+  s.rate = o.rate;
+  s.root = o.root;
+  s.step = o.step;
+  if (o.lr_device || o.step_device) {
+    if (o.lr_device) s.lr = *o.lr_device;
+    if (o.step_device) s.step = (uint32_t)max(1, *o.step_device);
+    rates(s.lr, (double)s.step, o.log_b1, o.log_b2, &s.rate, &s.root);
+  }
+  s.b1 = o.b1;
+  s.b2 = o.b2;
+  s.a1 = o.a1;
+  s.a2 = o.a2;
+  s.eps = o.eps;
+  return s;
+}
+
+// One element; r is the root of the new v.
+__device__ __forceinline__ void update(const Step &s, float decay, float grad, float &p, float &m,
+                                       float &v, float &r) {
+  const float g = grad * s.f;
+  m = fmaf(s.b1, m, s.a1 * g);
+  v = fmaf(s.b2, v, s.a2 * g * g);
+  r = sqrtf(v);
+  p -= fmaf(decay, p, s.rate * m / fmaf(r, s.root, s.eps));
+}
+
+// LEN elements from i on of an array of n, and back.
+template <typename T, int LEN>
+struct Some {
+  typedef T type __attribute__((ext_vector_type(LEN), aligned(sizeof(T))));
+};
+
+template <typename T, int LEN>
+__device__ __forceinline__ void load_some(const void *a, int64_t i, int64_t n, float *x) {
+  const T *p = static_cast<const T *>(a) + i;
+  if (i + LEN <= n) {
+    const typename Some<T, LEN>::type v = *reinterpret_cast<const typename Some<T, LEN>::type *>(p);
+#pragma unroll
+    for (int j = 0; j < LEN; ++j) x[j] = (float)v[j];
+  } else {
+#pragma unroll
+    for (int j = 0; j < LEN; ++j) x[j] = i + j < n ? (float)p[j] : 0.0f;
+  }
+}
+
+template <typename T, int LEN>
+__device__ __forceinline__ void store_some(void *a, int64_t i, int64_t n, const float *x) {
+  T *p = static_cast<T *>(a) + i;
+  if (i + LEN <= n) {
+    typename Some<T, LEN>::type v;
+#pragma unroll
+    for (int j = 0; j < LEN; ++j) v[j] = narrow<T>(x[j]);
+    *reinterpret_cast<typename Some<T, LEN>::type *>(p) = v;
+  } else {
+#pragma unroll
+    for (int j = 0; j < LEN; ++j)
+      if (i + j < n) p[j] = narrow<T>(x[j]);
+  }
+}
+
+template <typename P, typename G>
+__global__ __launch_bounds__(kThreads) void step_kernel(StepTable t, StepShared o) {
+  constexpr int kLen = 4, kVecs = kTile / kThreads / kLen;
+  const int at = find_tensor(t.first, o.count, blockIdx.x);
+  const int64_t n = t.n[at];
+  const Step s = read_step(o);
+  const float decay = s.lr * t.decay[at];
+  const int64_t tile0 = (int64_t)(blockIdx.x - t.first[at]) * o.tiles;
+  for (int64_t tile = tile0; tile < tile0 + o.tiles && tile * kTile < n; ++tile) {
+    const int64_t i0 = tile * kTile + (int64_t)threadIdx.x * kLen;
+    float p[kVecs][kLen], g[kVecs][kLen], m[kVecs][kLen], v[kVecs][kLen];
+#pragma unroll
+    for (int k = 0; k < kVecs; ++k) {
+      const int64_t i = i0 + k * kThreads * kLen;
+      load_some<P, kLen>(t.param[at], i, n, p[k]);
+      load_some<G, kLen>(t.grad[at], i, n, g[k]);
+      load_some<float, kLen>(t.m[at], i, n, m[k]);
+      load_some<float, kLen>(t.v[at], i, n, v[k]);
+    }
+#pragma unroll
+    for (int k = 0; k < kVecs; ++k) {
+      const int64_t i = i0 + k * kThreads * kLen;
+      if (s.taken) {
+#pragma unroll
+        for (int j = 0; j < kLen; ++j) {
+          float r;
+          update(s, decay, g[k][j], p[k][j], m[k][j], v[k][j], r);
+        }
+      }
+      store_some<P, kLen>(t.param_out[at], i, n, p[k]);
+      store_some<float, kLen>(t.m_out[at], i, n, m[k]);
+      store_some<float, kLen>(t.v_out[at], i, n, v[k]);
+      if (t.copy[at]) store_some<G, kLen>(t.copy[at], i, n, p[k]);
+    }
+  }
+}
+
+// ---- states in 8 bits ----------------------------------------------------------------
+//
+// Half a wave holds a block of 256 elements, a lane 8 neighbouring ones, so the
+// block's largest value is found without LDS.
+//
+// An e4m3 number is a float32 number 2^120 times as small without its last 20
+// bits, denormals included; adding 20 random bits before they are cut off rounds up
+// as often as the part cut off asks for.
+
+constexpr int kLane = 8;
+static_assert(ML2_STATE_BLOCK == 32 * kLane, "half a wave holds a block");
+constexpr float kTop = 448.0f;
+
+typedef uint32_t Codes __attribute__((ext_vector_type(2), aligned(4)));
+
+// 8 codes from i on; 0 behind n.
+__device__ __forceinline__ Codes load_codes(const uint8_t *p, int64_t i, int64_t n) {
+  if (i + kLane <= n) return *reinterpret_cast<const Codes *>(p + i);
+  Codes c = {0, 0};
+#pragma unroll
+  for (int j = 0; j < kLane; ++j)
+    if (i + j < n) c[j >> 2] |= (uint32_t)p[i + j] << (8 * (j & 3));
+  return c;
+}
+
+__device__ __forceinline__ void store_codes(uint8_t *p, int64_t i, int64_t n, Codes c) {
+  if (i + kLane <= n) {
+    *reinterpret_cast<Codes *>(p + i) = c;
+  } else {
+#pragma unroll
+    for (int j = 0; j < kLane; ++j)
+      if (i + j < n) p[i + j] = (uint8_t)(c[j >> 2] >> (8 * (j & 3)));
+  }
+}
+
+__device__ __forceinline__ void decode(Codes c, float scale, float (&x)[kLane]) {
+#pragma unroll
+  for (int w = 0; w < 2; ++w) {
+    const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)c[w], false);
+    const auto hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)c[w], true);
+    x[4 * w] = lo[0] * scale;
+    x[4 * w + 1] = lo[1] * scale;
+    x[4 * w + 2] = hi[0] * scale;
+    x[4 * w + 3] = hi[1] * scale;
+  }
+}
+
+// A block's scale, and what brings its elements to units of it: a NaN or an
+// infinity makes it NaN.  (The quotient of the largest itself is rounded once less
+// than the scale's reciprocal.)
+struct Scale {
+  float scale, over;
+};
+
+__device__ __forceinline__ Scale block_scale(const float (&x)[kLane]) {
+  uint32_t most = 0;  // sizes as bits are ordered as the sizes are, NaN last
+#pragma unroll
+  for (int j = 0; j < kLane; ++j) most = max(most, __float_as_uint(x[j]) & 0x7FFFFFFFu);
+  const float top = group_fold(__uint_as_float(most), 5, [](float a, float b) {
+    return __uint_as_float(max(__float_as_uint(a), __float_as_uint(b)));
+  });
+  if (!(top < __builtin_inff())) return {__builtin_nanf(""), 0.0f};
+  const float scale = top / kTop;
+  return scale > 0x1p-100f ? Scale{scale, kTop / top} : Scale{0x1p-100f, 0x1p100f};
+}
+
+// The code of a size in units of its scale; bits: 16 random ones, least: the
+// smallest code of what is not 0.
+__device__ __forceinline__ uint32_t encode(float size, uint32_t bits, uint32_t least) {
+  const uint32_t y = __float_as_uint(size * 0x1p-120f) + (bits << 4 | 8u);
+  const uint32_t code = min(y >> 20, 0x7Eu);
+  return size > 0.0f ? max(code, least) : code;
+}
+
+template <typename P, typename G>
+__global__ __launch_bounds__(kThreads) void step8_kernel(StepTable t, StepShared o) {
+  const int at = find_tensor(t.first, o.count, blockIdx.x);
+  const int64_t n = t.n[at];
+  const Step s = read_step(o);
+  const float decay = s.lr * t.decay[at];
+  const uint32_t key = fold_word(fold_word(o.key, s.step), (uint32_t)(o.place + at));
+  const int64_t codes = (n + ML2_STATE_BLOCK - 1) / ML2_STATE_BLOCK * ML2_STATE_BLOCK;
+  const uint8_t *m0 = static_cast<const uint8_t *>(t.m[at]);
+  const uint8_t *r0 = static_cast<const uint8_t *>(t.v[at]);
+  uint8_t *m1 = static_cast<uint8_t *>(t.m_out[at]), *r1 = static_cast<uint8_t *>(t.v_out[at]);
+  const int64_t tile0 = (int64_t)(blockIdx.x - t.first[at]) * o.tiles;
+  for (int64_t tile = tile0; tile < tile0 + o.tiles && tile * kTile < n; ++tile) {
+    const int64_t i = tile * kTile + (int64_t)threadIdx.x * kLane;
+    const int64_t block = i / ML2_STATE_BLOCK;
+    const bool in = block * ML2_STATE_BLOCK < n;  // the whole half wave, or none of it
+    float p[kLane], g[kLane], m[kLane], r[kLane], ms = 0.0f, rs = 0.0f;
+    load_some<P, kLane>(t.param[at], i, n, p);
+    load_some<G, kLane>(t.grad[at], i, n, g);
+    const Codes mc = load_codes(m0, i, n), rc = load_codes(r0, i, n);
+    if (in) {
+      ms = reinterpret_cast<const float *>(m0 + codes)[block];
+      rs = reinterpret_cast<const float *>(r0 + codes)[block];
+    }
+    if (!s.taken) {
+      store_some<P, kLane>(t.param_out[at], i, n, p);
+      if (t.copy[at]) store_some<G, kLane>(t.copy[at], i, n, p);
+      store_codes(m1, i, n, mc);
+      store_codes(r1, i, n, rc);
+      if (in && (threadIdx.x & 31) == 0) {
+        reinterpret_cast<float *>(m1 + codes)[block] = ms;
+        reinterpret_cast<float *>(r1 + codes)[block] = rs;
+      }
+      continue;
+    }
+    decode(mc, ms, m);
+    decode(rc, rs, r);
+#pragma unroll
+    for (int j = 0; j < kLane; ++j) {
+      float v = r[j] * r[j];
+      update(s, decay, g[j], p[j], m[j], v, r[j]);
+      if (i + j >= n) m[j] = r[j] = 0.0f;
+    }
+    store_some<P, kLane>(t.param_out[at], i, n, p);
+    if (t.copy[at]) store_some<G, kLane>(t.copy[at], i, n, p);
+    const Scale to_m = block_scale(m), to_r = block_scale(r);
+    const uint32_t high = (uint32_t)(i >> 32);
+    const uint32_t k = high ? fold_word(key, high) : key;
+    Codes mo = {0, 0}, ro = {0, 0};
+#pragma unroll
+    for (int j = 0; j < kLane; ++j) {
+      uint32_t h = k + ((uint32_t)i + (uint32_t)j) * kPhi;
+      h = (h ^ (h >> 15)) * kPlastic;
+      h ^= h >> 16;
+      const uint32_t a = encode(fabsf(m[j]) * to_m.over, h >> 16, 0) | (m[j] < 0.0f ? 0x80u : 0u);
+      const uint32_t b = encode(r[j] * to_r.over, h & 0xFFFFu, 1);
+      mo[j >> 2] |= a << (8 * (j & 3));
+      ro[j >> 2] |= b << (8 * (j & 3));
+    }
+    store_codes(m1, i, n, mo);
+    store_codes(r1, i, n, ro);
+    if (in && (threadIdx.x & 31) == 0) {
+      reinterpret_cast<float *>(m1 + codes)[block] = to_m.scale;
+      reinterpret_cast<float *>(r1 + codes)[block] = to_r.scale;
+    }
+  }
+}
+
+typedef void (*StepFn)(StepTable, StepShared);
+
+template <typename P>
+StepFn step_of(int grad_dtype, int bits) {
+  if (grad_dtype == ML2_F32) return bits == 8 ? step8_kernel<P, float> : step_kernel<P, float>;
+  if (grad_dtype == ML2_BF16) return bits == 8 ? step8_kernel<P, __bf16> : step_kernel<P, __bf16>;
+  return bits == 8 ? step8_kernel<P, _Float16> : step_kernel<P, _Float16>;
+}
+
+}  // namespace
+
+size_t grad_norm_workspace_bytes(const int64_t *sizes, int32_t count) {
+  return (size_t)norm_parts(sizes, count, norm_chunk(sizes, count)) * sizeof(double);
+}
+
+hipError_t launch_grad_norm(int dtype, const void *const *grads, const int64_t *sizes,
+                            int32_t count, float scale, float max_norm, float *norm,
+                            float *factor, int32_t *step, void *ws, hipStream_t s) {
+  const NormOut o = {scale, max_norm, norm, factor, step};
+  double *part = static_cast<double *>(ws);
+  if (dtype == ML2_F32) return launch_norm<float>(grads, sizes, count, o, part, s);
+  if (dtype == ML2_BF16) return launch_norm<__bf16>(grads, sizes, count, o, part, s);
+  return launch_norm<_Float16>(grads, sizes, count, o, part, s);
+}
+
+hipError_t launch_adamw(int param_dtype, int grad_dtype, int state_bits,
+                        const ml2_adamw_tensor *tensors, int32_t count,
+                        const ml2_adamw_options &o, hipStream_t s) {
+  const StepFn fn = param_dtype == ML2_F32    ? step_of<float>(grad_dtype, state_bits)
+                    : param_dtype == ML2_BF16 ? step_of<__bf16>(grad_dtype, state_bits)
+                                              : step_of<_Float16>(grad_dtype, state_bits);
+  StepTable t;
+  StepShared c = {};
+  c.log_b1 = log(o.beta1);
+  c.log_b2 = log(o.beta2);
+  c.lr_device = o.lr_device;
+  c.step_device = o.step_device;
+  c.factor = o.factor;
+  c.lr = (float)o.lr;
+  c.b1 = (float)o.beta1;
+  c.b2 = (float)o.beta2;
+  c.a1 = (float)(1.0 - o.beta1);
+  c.a2 = (float)(1.0 - o.beta2);
+  c.eps = (float)o.eps;
+  c.step = (uint32_t)o.step;
+  if (!o.step_device) rates(o.lr, (double)o.step, c.log_b1, c.log_b2, &c.rate, &c.root);
+  c.key = fold_word(fold_word(0, (uint32_t)o.seed), (uint32_t)(o.seed >> 32));
+  hipError_t e = hipSuccess;
+  for (int32_t i0 = 0; i0 < count && e == hipSuccess; i0 += kTensors) {
+    c.place = i0;
+    c.count = std::min(count - i0, kTensors);
+    int64_t tiles = 0;
+    for (int32_t i = 0; i < c.count; ++i) tiles += (tensors[i0 + i].n + kTile - 1) / kTile;
+    if (tiles == 0) continue;
+    c.tiles = (tiles + kMostBlocks - 1) / kMostBlocks;
+    uint32_t blocks = 0;
+    for (int32_t i = 0; i < c.count; ++i) {
+      const ml2_adamw_tensor &e = tensors[i0 + i];
+      t.param[i] = e.param;
+      t.grad[i] = e.grad;
+      t.m[i] = e.m;
+      t.v[i] = e.v;
+      t.param_out[i] = e.param_out ? e.param_out : e.param;
+      t.m_out[i] = e.m_out ? e.m_out : e.m;
+      t.v_out[i] = e.v_out ? e.v_out : e.v;
+      t.copy[i] = e.copy;
+      t.n[i] = e.n;
+      t.decay[i] = e.weight_decay;
+      t.first[i] = blocks;
+      blocks += (uint32_t)(((e.n + kTile - 1) / kTile + c.tiles - 1) / c.tiles);
+    }
+    fn<<<blocks, kThreads, 0, s>>>(t, c);
+    e = hipGetLastError();
+  }
+  return e;
+}
+
+}  // namespace ml2

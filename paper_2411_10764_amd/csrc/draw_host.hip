@@ -1,22 +1,17 @@
 // C-ABI entry points of the operators over rows of scores and over tables:
 // argument validation and the launches.
+#include "args.h"
 #include "draw.h"
 #include "ml2_internal.h"
 
+using ml2::aligned;
+using ml2::element_size;
 using ml2::fail;
 using ml2::hip_fail;
+using ml2::overlap;
+using ml2::size_ok;
 
 namespace {
-
-bool element_size(int32_t dtype, size_t *size) {
-  if (dtype != ML2_F32 && dtype != ML2_BF16 && dtype != ML2_F16) return false;
-  *size = dtype == ML2_F32 ? 4 : 2;
-  return true;
-}
-
-bool aligned(const void *p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
-
-bool size_ok(int64_t v) { return v >= 0 && v <= (int64_t)INT32_MAX; }
 
 ml2_status check_rows(const char *call, int32_t dtype, const ml2::ScoreRows &s, int32_t per_row,
                       const void *ws, size_t ws_bytes, size_t need) {
@@ -46,31 +41,6 @@ ml2_status check_rows(const char *call, int32_t dtype, const ml2::ScoreRows &s, 
   if (ws_bytes < need)
     return fail(ML2_ERR_INVALID_ARG, "%s: workspace %zu < %zu bytes", call, ws_bytes, need);
   return ML2_OK;
-}
-
-// Whether two matrices of `rows` rows of n elements of `size` bytes, lda and ldb
-// elements apart and aligned to their elements, have one in common.  Columns of
-// one buffer lie between one another without that.
-bool overlap(const void *a, int64_t lda, const void *b, int64_t ldb, int64_t rows, int64_t n,
-             size_t size) {
-  if (!a || !b || rows <= 0 || n <= 0) return false;
-  const uintptr_t pa = reinterpret_cast<uintptr_t>(a), pb = reinterpret_cast<uintptr_t>(b);
-  if (pa > pb) return overlap(b, ldb, a, lda, rows, n, size);
-  const uint64_t d = (pb - pa) / size;  // b's first element, counted from a's
-  const uint64_t la = (uint64_t)lda, lb = (uint64_t)ldb, len = (uint64_t)n;
-  if (d >= (uint64_t)(rows - 1) * la + len) return false;
-  if (la == lb) {
-    // row r of b begins in row r + d / la of a, or behind its end and reaches on
-    // into the next
-    const uint64_t at = d % la, row = d / la;
-    return at < len || (row + 1 < (uint64_t)rows && at + len > la);
-  }
-  for (uint64_t i = 0, j = 0; i < (uint64_t)rows && j < (uint64_t)rows;) {
-    const uint64_t x = i * la, y = d + j * lb;
-    if (x < y + len && y < x + len) return true;
-    if (x < y) ++i; else ++j;
-  }
-  return false;
 }
 
 // n, rows and per_row of a workspace query.

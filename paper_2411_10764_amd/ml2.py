@@ -29,6 +29,8 @@ ML2_MAX_STREAM_K = 4096
 ML2_MAX_ROWS = 2097152
 ML2_MAX_TOKENS = 1073741824
 ML2_MAX_WIDTH = 65536
+ML2_MAX_TENSORS = 65536
+ML2_STATE_BLOCK = 256
 ML2_F32, ML2_BF16, ML2_F16 = 0, 1, 2
 
 EXPORTED = (
@@ -43,6 +45,8 @@ EXPORTED = (
     "ml2_stream_explorer_chunk", "ml2_stream_explorer_end", "ml2_last_error",
     "ml2_sample_workspace_bytes", "ml2_sample", "ml2_logprob_workspace_bytes", "ml2_logprob",
     "ml2_logprob_grad", "ml2_embed", "ml2_embed_grad_workspace_bytes", "ml2_embed_grad",
+    "ml2_layer_norm", "ml2_layer_norm_grad_workspace_bytes", "ml2_layer_norm_grad",
+    "ml2_grad_norm_workspace_bytes", "ml2_grad_norm", "ml2_adamw_state_bytes", "ml2_adamw",
 )
 # include/ml2_probe.h: microbenchmarks behind the roofline figures
 EXPORTED_PROBE = ("ml2_probe_visit", "ml2_probe_lds", "ml2_probe_valu", "ml2_tune_walk_plan",
@@ -68,6 +72,19 @@ class ml2_ensemble_desc(ctypes.Structure):
         ("leaf_value", ctypes.c_void_p),
         ("default_left", ctypes.c_void_p),
     ]
+
+
+class ml2_adamw_tensor(ctypes.Structure):
+    _fields_ = [(f, ctypes.c_void_p) for f in
+                ("param", "grad", "m", "v", "param_out", "m_out", "v_out", "copy")] + [
+        ("n", ctypes.c_int64), ("weight_decay", ctypes.c_float)]
+
+
+class ml2_adamw_options(ctypes.Structure):
+    _fields_ = [("lr", ctypes.c_double), ("beta1", ctypes.c_double), ("beta2", ctypes.c_double),
+                ("eps", ctypes.c_double), ("step", ctypes.c_int64), ("lr_device", ctypes.c_void_p),
+                ("step_device", ctypes.c_void_p), ("factor", ctypes.c_void_p),
+                ("seed", ctypes.c_uint64)]
 
 
 class ml2_walk_info(ctypes.Structure):
@@ -146,7 +163,15 @@ def lib():
                                       SZ, P]),
                 ("ml2_embed", [I32, P, I64, I64, I64, P, I64, F32, P, I64, P]),
                 ("ml2_embed_grad_workspace_bytes", [I64, I64, I64, ctypes.POINTER(SZ)]),
-                ("ml2_embed_grad", [I32, P, I64, I64, I64, P, F32, I32, P, I64, I64, P, SZ, P])):
+                ("ml2_embed_grad", [I32, P, I64, I64, I64, P, F32, I32, P, I64, I64, P, SZ, P]),
+                ("ml2_layer_norm", [I32, P, I64, I64, I64, I32, P, P, F32, P, I64, P, P, P]),
+                ("ml2_layer_norm_grad_workspace_bytes", [I64, I64, ctypes.POINTER(SZ)]),
+                ("ml2_layer_norm_grad", [I32, P, I64, I64, I64, P, I64, I32, P, P, P, P, I64, I32,
+                                         P, P, P, SZ, P]),
+                ("ml2_grad_norm_workspace_bytes", [P, I32, ctypes.POINTER(SZ)]),
+                ("ml2_grad_norm", [I32, P, P, I32, F32, F32, P, P, P, P, SZ, P]),
+                ("ml2_adamw_state_bytes", [I32, I64, ctypes.POINTER(SZ)]),
+                ("ml2_adamw", [I32, I32, I32, P, I32, P, P])):
             getattr(L, f).restype = I32
             getattr(L, f).argtypes = types
         L.ml2_last_error.restype = ctypes.c_char_p
@@ -704,6 +729,277 @@ class EmbeddingGrad:
         """grad [table_rows][width]: this object's own buffer."""
         ml2_embed_grad(dout, ids, self.grad, self.ws, scale, stream)
         return self.grad
+
+
+# ---- a training step: normalisation, gradient norms, the optimizer ----------
+
+def _param(x, name: str, dtype, width: int):
+    """(pointer, type) of a parameter [width] of a row type or float32, or (None, the row type)."""
+    if x is None:
+        return None, _dtype(dtype)
+    if x.dtype is not dtype and x.dtype is not _t().f32:
+        raise ValueError(f"{name} must be {dtype} or float32, not {x.dtype}")
+    return _flat(x, name, x.dtype, (width,)), _dtype(x.dtype)
+
+
+def _same_type(a, b, names: str):
+    """The type of two parameters of which each may be None."""
+    if a is not None and b is not None and a.dtype is not b.dtype:
+        raise ValueError(f"{names} must have one type")
+    return a if a is not None else b
+
+
+def ml2_layer_norm(x, weight, bias, out, mean=None, rstd=None, eps: float = 1e-5,
+                   stream=None) -> None:
+    """Layer norm of every row of x [rows][width]; weight and bias may be None."""
+    xp, rows, width, ld = _matrix(x, "x")
+    op, orows, owidth, out_ld = _matrix(out, "out")
+    if (orows, owidth) != (rows, width) or out.dtype is not x.dtype:
+        raise ValueError("out must have the shape and type of x")
+    _same_type(weight, bias, "weight and bias")
+    wp, code = _param(weight, "weight", x.dtype, width)
+    bp, bcode = _param(bias, "bias", x.dtype, width)
+    f32 = _t().f32
+    _check(lib().ml2_layer_norm(_dtype(x.dtype), xp, rows, width, ld, bcode if wp is None else code,
+                                wp, bp, eps, op, out_ld, _flat(mean, "mean", f32, (rows,)),
+                                _flat(rstd, "rstd", f32, (rows,)), _stream(stream)))
+
+
+def ml2_layer_norm_grad_workspace_bytes(rows: int, width: int) -> int:
+    return _bytes(lib().ml2_layer_norm_grad_workspace_bytes, rows, width)
+
+
+def ml2_layer_norm_grad(x, dout, weight, mean, rstd, workspace, dx=None, dweight=None, dbias=None,
+                        stream=None) -> None:
+    """The gradients of ml2_layer_norm to its rows, weight and bias (each may be None)."""
+    xp, rows, width, ld = _matrix(x, "x")
+    dp, drows, dwidth, dout_ld = _matrix(dout, "dout")
+    if (drows, dwidth) != (rows, width) or dout.dtype is not x.dtype:
+        raise ValueError("dout must have the shape and type of x")
+    dxp, dx_ld = None, width
+    if dx is not None:
+        dxp, r, w, dx_ld = _matrix(dx, "dx")
+        if (r, w) != (rows, width) or dx.dtype is not x.dtype:
+            raise ValueError("dx must have the shape and type of x")
+    wp, code = _param(weight, "weight", x.dtype, width)
+    _same_type(dweight, dbias, "dweight and dbias")
+    gwp, gcode = _param(dweight, "dweight", x.dtype, width)
+    gbp, bcode = _param(dbias, "dbias", x.dtype, width)
+    f32 = _t().f32
+    _check(lib().ml2_layer_norm_grad(
+        _dtype(x.dtype), xp, rows, width, ld, dp, dout_ld, code, wp,
+        _flat(mean, "mean", f32, (rows,)), _flat(rstd, "rstd", f32, (rows,)), dxp, dx_ld,
+        bcode if gwp is None else gcode, gwp, gbp, *_space(workspace), _stream(stream)))
+
+
+def _tensors(xs, name: str):
+    """The type of a list of contiguous device tensors of one type."""
+    xs = list(xs)
+    if not xs:
+        raise ValueError(f"{name} must hold a tensor")
+    for x in xs:
+        if not x.is_cuda or not x.is_contiguous() or x.dtype is not xs[0].dtype:
+            raise ValueError(f"{name} must be contiguous device tensors of one type")
+        if x.device != xs[0].device:
+            raise ValueError(f"{name} must be on one device")
+    return xs, xs[0].dtype
+
+
+def ml2_grad_norm_workspace_bytes(sizes) -> int:
+    array = (ctypes.c_int64 * len(sizes))(*sizes)
+    return _bytes(lib().ml2_grad_norm_workspace_bytes, array, len(sizes))
+
+
+def ml2_adamw_state_bytes(state_bits: int, n: int) -> int:
+    return _bytes(lib().ml2_adamw_state_bytes, state_bits, n)
+
+
+def ml2_grad_norm(grads, norm, factor, workspace, max_norm: float = float("inf"),
+                  scale: float = 1.0, step=None, stream=None) -> None:
+    """The norm of all gradients together, and what a step multiplies them by (norm and factor:
+    float32 [1], either may be None; step: int32 [1], raised by one where the norm is finite)."""
+    grads, dtype = _tensors(grads, "grads")
+    n = len(grads)
+    t = _t()
+    _check(lib().ml2_grad_norm(
+        _dtype(dtype), (ctypes.c_void_p * n)(*[g.data_ptr() for g in grads]),
+        (ctypes.c_int64 * n)(*[g.numel() for g in grads]), n, scale, max_norm,
+        _flat(norm, "norm", t.f32, (1,)), _flat(factor, "factor", t.f32, (1,)),
+        _flat(step, "step", t.i32, (1,)), *_space(workspace), _stream(stream)))
+
+
+def ml2_adamw(param_dtype, grad_dtype, state_bits: int, tensors, count: int,
+              options: ml2_adamw_options, stream=None) -> None:
+    """A step of AdamW over an array of ml2_adamw_tensor."""
+    _check(lib().ml2_adamw(_dtype(param_dtype), _dtype(grad_dtype), state_bits, tensors, count,
+                           ctypes.byref(options), _stream(stream)))
+
+
+class LayerNorm:
+    """Buffers of ml2_layer_norm for rows of one width."""
+
+    def __init__(self, rows: int, width: int, dtype, device=None):
+        import torch
+        device = _on(device)
+        self.out = torch.empty(rows, width, dtype=dtype, device=device)
+        self.mean = torch.empty(rows, dtype=torch.float32, device=device)
+        self.rstd = torch.empty(rows, dtype=torch.float32, device=device)
+
+    def run(self, x, weight=None, bias=None, eps: float = 1e-5, stream=None):
+        """(out, mean, rstd): this object's own buffers."""
+        ml2_layer_norm(x, weight, bias, self.out, self.mean, self.rstd, eps, stream)
+        return self.out, self.mean, self.rstd
+
+
+class LayerNormGrad:
+    """Buffers of ml2_layer_norm_grad for rows of one width: dx in the rows' type, dweight and
+    dbias (without bias: None) in grad_dtype."""
+
+    def __init__(self, rows: int, width: int, dtype, grad_dtype=None, bias: bool = True,
+                 device=None):
+        import torch
+        device = _on(device)
+        grad_dtype = dtype if grad_dtype is None else grad_dtype
+        self.dx = torch.empty(rows, width, dtype=dtype, device=device)
+        self.dweight = torch.empty(width, dtype=grad_dtype, device=device)
+        self.dbias = torch.empty(width, dtype=grad_dtype, device=device) if bias else None
+        self.ws = _workspace(ml2_layer_norm_grad_workspace_bytes(rows, width), device)
+
+    def run(self, x, dout, weight, mean, rstd, stream=None):
+        """(dx, dweight, dbias): this object's own buffers."""
+        ml2_layer_norm_grad(x, dout, weight, mean, rstd, self.ws, self.dx, self.dweight,
+                            self.dbias, stream)
+        return self.dx, self.dweight, self.dbias
+
+
+class GradNorm:
+    """ml2_grad_norm over a program's gradient buffers, which it keeps: norm and factor are
+    this object's own buffers, and step, where given, the program's counter."""
+
+    def __init__(self, grads, max_norm: float = float("inf"), scale: float = 1.0, step=None):
+        import torch
+        self.grads, self.dtype = _tensors(grads, "grads")
+        self.count, self.scale, self.max_norm, self.step = len(self.grads), scale, max_norm, step
+        device = self.grads[0].device
+        self.norm = torch.empty(1, dtype=torch.float32, device=device)
+        self.factor = torch.empty(1, dtype=torch.float32, device=device)
+        sizes = [g.numel() for g in self.grads]
+        self.at = (ctypes.c_void_p * self.count)(*[g.data_ptr() for g in self.grads])
+        self.sizes = (ctypes.c_int64 * self.count)(*sizes)
+        self.ws = _workspace(ml2_grad_norm_workspace_bytes(sizes), device)
+        self.args = (_dtype(self.dtype), self.at, self.sizes, self.count, scale, max_norm,
+                     self.norm.data_ptr(), self.factor.data_ptr(),
+                     _flat(step, "step", torch.int32, (1,)), *_space(self.ws))
+
+    def run(self, stream=None):
+        """(norm, factor), both float32 [1]: this object's own buffers."""
+        _check(lib().ml2_grad_norm(*self.args, _stream(stream)))
+        return self.norm, self.factor
+
+
+class AdamW:
+    """ml2_adamw over a program's parameters and gradient buffers, which it keeps.
+
+    state_bits 32 or 8; m and v: lists of states (by default zeros: adamw_state); copies: a list
+    of tensors of the gradients' type that get the new parameters too; weight_decay: one, or one
+    for each tensor.  out: lists of parameters, m and v that a step writes instead of the own ones,
+    which then stay as they were until accept() exchanges the two; None: in place."""
+
+    def __init__(self, params, grads, state_bits: int = 32, m=None, v=None, copies=None,
+                 weight_decay=0.01, betas=(0.9, 0.999), eps: float = 1e-8, seed: int = 0,
+                 out=None):
+        import torch
+        self.params, self.dtype = _tensors(params, "params")
+        self.grads, self.grad_dtype = _tensors(grads, "grads")
+        self.state_bits, self.count = state_bits, len(self.params)
+        sizes = [p.numel() for p in self.params]
+        device = self.params[0].device
+
+        def states(xs, name):
+            if xs is None:
+                return [adamw_state(n, state_bits, device) for n in sizes]
+            xs, dtype = _tensors(xs, name)
+            want = torch.float32 if state_bits == 32 else torch.uint8
+            need = [ml2_adamw_state_bytes(state_bits, n) // want.itemsize for n in sizes]
+            if dtype is not want or [x.numel() for x in xs] != need:
+                raise ValueError(f"{name} must be {want} of adamw_state's sizes")
+            return xs
+
+        self.m, self.v = states(m, "m"), states(v, "v")
+        self.copies = None if copies is None else _tensors(copies, "copies")[0]
+        self.out = None
+        if out is not None:
+            self.out = (_tensors(out[0], "params of out")[0], states(out[1], "m of out"),
+                        states(out[2], "v of out"))
+        if self.copies is not None and self.copies[0].dtype is not self.grad_dtype:
+            raise ValueError("copies must have the gradients' type")
+        if self.out is not None and self.out[0][0].dtype is not self.dtype:
+            raise ValueError("params of out must have the parameters' type")
+        for xs in (self.grads, self.copies, self.out and self.out[0]):
+            if xs is not None and [x.numel() for x in xs] != sizes:
+                raise ValueError("grads, copies and out must have the parameters' sizes")
+        for xs in (self.grads, self.copies, self.m, self.v, *(self.out or ())):
+            if xs is not None and xs[0].device != device:
+                raise ValueError("all tensors must be on one device")
+        decay = list(weight_decay) if hasattr(weight_decay, "__len__") else (
+            [weight_decay] * self.count)
+        if len(decay) != self.count:
+            raise ValueError("weight_decay must be one number, or one for each tensor")
+        self.options = ml2_adamw_options(0.0, betas[0], betas[1], eps, 1, None, None, None, seed)
+        self.tensors = (ml2_adamw_tensor * self.count)()
+        for t, n, d in zip(self.tensors, sizes, decay):
+            t.n, t.weight_decay = n, d
+        self._fill()
+
+    def _fill(self) -> None:
+        outs = self.out or (self.params, self.m, self.v)
+        for i, t in enumerate(self.tensors):
+            t.param, t.grad = self.params[i].data_ptr(), self.grads[i].data_ptr()
+            t.m, t.v = self.m[i].data_ptr(), self.v[i].data_ptr()
+            t.param_out, t.m_out, t.v_out = (x[i].data_ptr() for x in outs)
+            t.copy = self.copies[i].data_ptr() if self.copies is not None else None
+
+    def accept(self) -> None:
+        """The last step's results become the state, and the old state's memory the next
+        step's output (without `out` the step was in place)."""
+        if self.out is not None:
+            old = (self.params, self.m, self.v)
+            (self.params, self.m, self.v), self.out = self.out, old
+            self._fill()
+
+    def run(self, lr, step, factor=None, stream=None):
+        """The new parameters.  lr: a number, or float32 [1] on the device; step: a number, or
+        int32 [1] on the device; factor: float32 [1] on the device, as GradNorm's, or None."""
+        o, t = self.options, _t()
+        o.lr_device = o.step_device = None
+        if isinstance(lr, (int, float)):
+            o.lr = lr
+        else:
+            o.lr_device = _flat(lr, "lr", t.f32, (1,))
+        if isinstance(step, int):
+            o.step = step
+        else:
+            o.step_device = _flat(step, "step", t.i32, (1,))
+        o.factor = _flat(factor, "factor", t.f32, (1,))
+        ml2_adamw(self.dtype, self.grad_dtype, self.state_bits, self.tensors, self.count, o,
+                  stream)
+        return self.out[0] if self.out is not None else self.params
+
+
+def adamw_state(n: int, state_bits: int = 32, device=None):
+    """A state of zeros for n elements: float32 [n], or the bytes of an 8-bit state."""
+    import torch
+    dtype = torch.float32 if state_bits == 32 else torch.uint8
+    size = ml2_adamw_state_bytes(state_bits, n) // dtype.itemsize
+    return torch.zeros(size, dtype=dtype, device=_on(device))
+
+
+def adamw_state_parts(state, n: int):
+    """An 8-bit state's numbers (float8_e4m3fn [n], in units of their block's scale) and scales
+    (float32, one for each ML2_STATE_BLOCK elements), as views."""
+    import torch
+    codes = -(-n // ML2_STATE_BLOCK) * ML2_STATE_BLOCK
+    return state[:n].view(torch.float8_e4m3fn), state[codes:].view(torch.float32)
 
 
 # ---- microbenchmarks (include/ml2_probe.h) ---------------------------------
