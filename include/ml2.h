@@ -593,7 +593,7 @@ typedef struct ml2_adamw_tensor {
 
 /*
  * What a step's tensors share.
- *   beta1, beta2   in [0, 1);  eps: positive and finite, in float32 too
+ *   beta1, beta2   in [0, 1);  eps: from 2^-126 on, finite in float32
  *   lr, step       the learning rate (finite) and the number t of this step, 1 to
  *                  INT32_MAX; where
  *                  lr_device (float32 [1]) or step_device (int32 [1]) is not

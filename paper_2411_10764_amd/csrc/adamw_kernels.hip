@@ -196,11 +196,11 @@ struct StepTable {
 
 struct StepShared {
   int64_t tiles;          // of a workgroup
-  double log_b1, log_b2;
+  double b1, b2, log_b1, log_b2;
   const float *lr_device;
   const int32_t *step_device;
   const float *factor;
-  float lr, b1, b2, a1, a2, eps;  // a: 1 - b
+  float lr, eps;
   float rate, root;       // lr / (1 - b1^t), 1 / sqrt(1 - b2^t)
   uint32_t step, key;     // key: of the seed
   int32_t count, place;   // place: of the table's first tensor
@@ -224,7 +224,7 @@ __host__ __device__ __forceinline__ void rates(double lr, double step, double lo
 
 // What a workgroup needs of the step: the same in all its threads.
 struct Step {
-  float f, lr, rate, root, b1, b2, a1, a2, eps;
+  float f, lr, rate, root, eps;
   bool taken;  // the factor is finite
   uint32_t step;
 };
@@ -242,22 +242,13 @@ __device__ __forceinline__ Step read_step(const StepShared &o) {
     if (o.step_device) s.step = (uint32_t)max(1, *o.step_device);
     rates(s.lr, (double)s.step, o.log_b1, o.log_b2, &s.rate, &s.root);
   }
-  s.b1 = o.b1;
-  s.b2 = o.b2;
-  s.a1 = o.a1;
-  s.a2 = o.a2;
   s.eps = o.eps;
   return s;
 }
 
-// One element; r is the root of the new v.
-__device__ __forceinline__ void update(const Step &s, float decay, float grad, float &p, float &m,
-                                       float &v, float &r) {
-  const float g = grad * s.f;
-  m = fmaf(s.b1, m, s.a1 * g);
-  v = fmaf(s.b2, v, s.a2 * g * g);
-  r = sqrtf(v);
-  p -= fmaf(decay, p, s.rate * m / fmaf(r, s.root, s.eps));
+// A parameter after its step; m and r = sqrt(v) are the new ones.
+__device__ __forceinline__ float moved(const Step &s, float decay, float p, float m, float r) {
+  return p - fmaf(decay, p, s.rate * m / fmaf(r, s.root, s.eps));
 }
 
 // LEN elements from i on of an array of n, and back.
@@ -301,6 +292,8 @@ __global__ __launch_bounds__(kThreads) void step_kernel(StepTable t, StepShared 
   const int64_t n = t.n[at];
   const Step s = read_step(o);
   const float decay = s.lr * t.decay[at];
+  const float b1 = (float)o.b1, b2 = (float)o.b2, a1 = (float)(1.0 - o.b1),
+              a2 = (float)(1.0 - o.b2);
   const int64_t tile0 = (int64_t)(blockIdx.x - t.first[at]) * o.tiles;
   for (int64_t tile = tile0; tile < tile0 + o.tiles && tile * kTile < n; ++tile) {
     const int64_t i0 = tile * kTile + (int64_t)threadIdx.x * kLen;
@@ -319,8 +312,10 @@ __global__ __launch_bounds__(kThreads) void step_kernel(StepTable t, StepShared 
       if (s.taken) {
 #pragma unroll
         for (int j = 0; j < kLen; ++j) {
-          float r;
-          update(s, decay, g[k][j], p[k][j], m[k][j], v[k][j], r);
+          const float gj = g[k][j] * s.f;
+          m[k][j] = fmaf(b1, m[k][j], a1 * gj);
+          v[k][j] = fmaf(b2, v[k][j], a2 * gj * gj);
+          p[k][j] = moved(s, decay, p[k][j], m[k][j], sqrtf(v[k][j]));
         }
       }
       store_some<P, kLen>(t.param_out[at], i, n, p[k]);
@@ -339,6 +334,11 @@ __global__ __launch_bounds__(kThreads) void step_kernel(StepTable t, StepShared 
 // An e4m3 number is a float32 number 2^120 times as small without its last 20
 // bits, denormals included; adding 20 random bits before they are cut off rounds up
 // as often as the part cut off asks for.
+//
+// What is rounded at random should be the value itself: constants that a block
+// shares (b1 and b2 times its scales, the way to units of the new ones) are sums of
+// two float32 numbers, and r keeps what its root cut off, so that m and v are
+// rounded once and their sizes once more.
 
 constexpr int kLane = 8;
 static_assert(ML2_STATE_BLOCK == 32 * kLane, "half a wave holds a block");
@@ -366,43 +366,57 @@ __device__ __forceinline__ void store_codes(uint8_t *p, int64_t i, int64_t n, Co
   }
 }
 
-__device__ __forceinline__ void decode(Codes c, float scale, float (&x)[kLane]) {
+// The numbers that codes stand for, in units of their scale.
+__device__ __forceinline__ void decode(Codes c, float (&x)[kLane]) {
 #pragma unroll
   for (int w = 0; w < 2; ++w) {
     const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)c[w], false);
     const auto hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)c[w], true);
-    x[4 * w] = lo[0] * scale;
-    x[4 * w + 1] = lo[1] * scale;
-    x[4 * w + 2] = hi[0] * scale;
-    x[4 * w + 3] = hi[1] * scale;
+    x[4 * w] = lo[0];
+    x[4 * w + 1] = lo[1];
+    x[4 * w + 2] = hi[0];
+    x[4 * w + 3] = hi[1];
   }
 }
 
-// A block's scale, and what brings its elements to units of it: a NaN or an
-// infinity makes it NaN.  (The quotient of the largest itself is rounded once less
-// than the scale's reciprocal.)
-struct Scale {
-  float scale, over;
+// A factor as the sum of two float32 numbers.
+struct Two {
+  float high, low;
 };
 
-__device__ __forceinline__ Scale block_scale(const float (&x)[kLane]) {
-  uint32_t most = 0;  // sizes as bits are ordered as the sizes are, NaN last
-#pragma unroll
-  for (int j = 0; j < kLane; ++j) most = max(most, __float_as_uint(x[j]) & 0x7FFFFFFFu);
+__device__ __forceinline__ Two two(double x) {
+  const float high = (float)x;
+  return {high, (float)(x - (double)high)};
+}
+
+__device__ __forceinline__ float times(float a, Two b, float add) {
+  return fmaf(a, b.high, fmaf(a, b.low, add));
+}
+
+// A block's scale, and what brings its elements to units of it; `most`: the bits
+// of the lane's largest size, ordered as the sizes are, NaN last.  A NaN or an
+// infinity makes the scale NaN.
+struct Scale {
+  float scale;
+  Two over;
+};
+
+__device__ __forceinline__ Scale block_scale(uint32_t most) {
   const float top = group_fold(__uint_as_float(most), 5, [](float a, float b) {
     return __uint_as_float(max(__float_as_uint(a), __float_as_uint(b)));
   });
-  if (!(top < __builtin_inff())) return {__builtin_nanf(""), 0.0f};
+  if (!(top < __builtin_inff())) return {__builtin_nanf(""), {0.0f, 0.0f}};
   const float scale = top / kTop;
-  return scale > 0x1p-100f ? Scale{scale, kTop / top} : Scale{0x1p-100f, 0x1p100f};
+  if (!(scale > 0x1p-100f)) return {0x1p-100f, {0x1p100f, 0.0f}};
+  const float over = kTop / top;
+  return {scale, {over, fmaf(-over, top, kTop) / top}};
 }
 
-// The code of a size in units of its scale; bits: 16 random ones, least: the
-// smallest code of what is not 0.
-__device__ __forceinline__ uint32_t encode(float size, uint32_t bits, uint32_t least) {
-  const uint32_t y = __float_as_uint(size * 0x1p-120f) + (bits << 4 | 8u);
-  const uint32_t code = min(y >> 20, 0x7Eu);
-  return size > 0.0f ? max(code, least) : code;
+// The code of a size in units of its scale; random: 20 bits, least: the smallest
+// code.
+__device__ __forceinline__ uint32_t encode(float size, uint32_t random, uint32_t least) {
+  const uint32_t code = (__float_as_uint(size * 0x1p-120f) + random) >> 20;
+  return min(max(code, least), 0x7Eu);
 }
 
 template <typename P, typename G>
@@ -411,6 +425,8 @@ __global__ __launch_bounds__(kThreads) void step8_kernel(StepTable t, StepShared
   const int64_t n = t.n[at];
   const Step s = read_step(o);
   const float decay = s.lr * t.decay[at];
+  const Two a1 = two((1.0 - o.b1) * s.f);
+  const float a2 = (float)((1.0 - o.b2) * s.f * s.f);
   const uint32_t key = fold_word(fold_word(o.key, s.step), (uint32_t)(o.place + at));
   const int64_t codes = (n + ML2_STATE_BLOCK - 1) / ML2_STATE_BLOCK * ML2_STATE_BLOCK;
   const uint8_t *m0 = static_cast<const uint8_t *>(t.m[at]);
@@ -440,28 +456,50 @@ __global__ __launch_bounds__(kThreads) void step8_kernel(StepTable t, StepShared
       }
       continue;
     }
-    decode(mc, ms, m);
-    decode(rc, rs, r);
+    decode(mc, m);
+    decode(rc, r);
+    const Two old_m = two(o.b1 * ms), old_v = two(o.b2 * rs * rs);
+    float rest[kLane];  // what the root of v has beyond r
 #pragma unroll
     for (int j = 0; j < kLane; ++j) {
-      float v = r[j] * r[j];
-      update(s, decay, g[j], p[j], m[j], v, r[j]);
-      if (i + j >= n) m[j] = r[j] = 0.0f;
+      m[j] = fmaf(m[j], old_m.high,
+                  fmaf(g[j], a1.high, fmaf(m[j], old_m.low, g[j] * a1.low)));
+      const float square = r[j] * r[j];  // of 4 bits: exact
+      const float v = fmaf(square, old_v.high, fmaf(g[j] * g[j], a2, square * old_v.low));
+      // y: 1 / sqrt(v); v below float32's normal numbers counts as ever less, and
+      // an infinite one gives an infinite root.
+      const float y = __builtin_amdgcn_rsqf(__builtin_amdgcn_fmed3f(v, 0x1p-126f, 0x1.fffffep127f));
+      r[j] = v * y;
+      rest[j] = fmaf(-r[j], r[j], v) * (0.5f * y);
+      p[j] -= fmaf(decay, p[j],
+                   s.rate * m[j] * __builtin_amdgcn_rcpf(fmaf(r[j], s.root, s.eps)));
     }
     store_some<P, kLane>(t.param_out[at], i, n, p);
     if (t.copy[at]) store_some<G, kLane>(t.copy[at], i, n, p);
-    const Scale to_m = block_scale(m), to_r = block_scale(r);
+    if (i + kLane > n) {
+#pragma unroll
+      for (int j = 0; j < kLane; ++j)
+        if (i + j >= n) m[j] = r[j] = 0.0f;
+    }
+    uint32_t most_m = 0, most_r = 0;
+#pragma unroll
+    for (int j = 0; j < kLane; ++j) {
+      most_m = max(most_m, __float_as_uint(m[j]) & 0x7FFFFFFFu);
+      most_r = max(most_r, __float_as_uint(r[j]));
+    }
+    const Scale to_m = block_scale(most_m), to_r = block_scale(most_r);
     const uint32_t high = (uint32_t)(i >> 32);
-    const uint32_t k = high ? fold_word(key, high) : key;
+    const uint32_t k = (high ? fold_word(key, high) : key) + (uint32_t)i * kPhi;
     Codes mo = {0, 0}, ro = {0, 0};
 #pragma unroll
     for (int j = 0; j < kLane; ++j) {
-      uint32_t h = k + ((uint32_t)i + (uint32_t)j) * kPhi;
+      uint32_t h = k + (uint32_t)j * kPhi;
       h = (h ^ (h >> 15)) * kPlastic;
       h ^= h >> 16;
-      const uint32_t a = encode(fabsf(m[j]) * to_m.over, h >> 16, 0) | (m[j] < 0.0f ? 0x80u : 0u);
-      const uint32_t b = encode(r[j] * to_r.over, h & 0xFFFFu, 1);
-      mo[j >> 2] |= a << (8 * (j & 3));
+      const uint32_t a = encode(times(fabsf(m[j]), to_m.over, 0.0f), (h >> 12 & 0xFFFF0u) | 8u, 0);
+      const uint32_t b = encode(times(r[j], to_r.over, rest[j] * to_r.over.high),
+                                (h << 4 & 0xFFFF0u) | 8u, min(__float_as_uint(r[j]), 1u));
+      mo[j >> 2] |= (a | (__float_as_uint(m[j]) >> 24 & 0x80u)) << (8 * (j & 3));
       ro[j >> 2] |= b << (8 * (j & 3));
     }
     store_codes(m1, i, n, mo);
@@ -512,10 +550,8 @@ hipError_t launch_adamw(int param_dtype, int grad_dtype, int state_bits,
   c.step_device = o.step_device;
   c.factor = o.factor;
   c.lr = (float)o.lr;
-  c.b1 = (float)o.beta1;
-  c.b2 = (float)o.beta2;
-  c.a1 = (float)(1.0 - o.beta1);
-  c.a2 = (float)(1.0 - o.beta2);
+  c.b1 = o.beta1;
+  c.b2 = o.beta2;
   c.eps = (float)o.eps;
   c.step = (uint32_t)o.step;
   if (!o.step_device) rates(o.lr, (double)o.step, c.log_b1, c.log_b2, &c.rate, &c.root);

@@ -309,7 +309,7 @@ ml2_status ml2_adamw(int32_t param_dtype, int32_t grad_dtype, int32_t state_bits
     return fail(ML2_ERR_UNSUPPORTED, "%s: count = %d > %d", call, count, ML2_MAX_TENSORS);
   const ml2_adamw_options &o = *options;
   if (!(o.beta1 >= 0.0 && o.beta1 < 1.0) || !(o.beta2 >= 0.0 && o.beta2 < 1.0) ||
-      !((float)o.eps > 0.0f) || !isfinite((float)o.eps) || !isfinite((float)o.lr))
+      !((float)o.eps >= 0x1p-126f) || !isfinite((float)o.eps) || !isfinite((float)o.lr))
     return fail(ML2_ERR_INVALID_ARG, "%s: lr = %g, beta1 = %g, beta2 = %g, eps = %g", call, o.lr,
                 o.beta1, o.beta2, o.eps);
   if (!o.step_device && (o.step < 1 || o.step > (int64_t)INT32_MAX))

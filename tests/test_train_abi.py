@@ -147,7 +147,7 @@ def _adamw(pd=F32, gd=F32, bits=32, tensors=None, count=None, options=None, no_o
     dict(options=o) for o in (
         dict(lr=NAN), dict(lr=INF), dict(lr=1e39), dict(beta1=-0.1), dict(beta1=1.0),
         dict(beta1=NAN), dict(beta2=1.0), dict(beta2=-1e-9), dict(eps=0.0), dict(eps=-1.0),
-        dict(eps=NAN), dict(eps=1e-60), dict(eps=1e60), dict(step=0), dict(step=-1),
+        dict(eps=NAN), dict(eps=1e-60), dict(eps=1e-39), dict(eps=1e60), dict(step=0), dict(step=-1),
         dict(step=1 << 31), dict(lr_device=B + 2), dict(step_device=B + 1), dict(factor=B + 2),
         # an option in memory that the step writes
         dict(lr_device=X), dict(step_device=M + 4 * N - 4), dict(factor=R + 40))] + [
