@@ -23,21 +23,67 @@ namespace {
 constexpr int kWaveBlock = 256;   // threads where a row has at most a wave
 constexpr int kMaxBlock = 1024;
 
-// weight or bias (or `none` where there is none) of columns c .. c + kLen - 1
-template <typename T>
-__device__ __forceinline__ void load_param(const void *p, int f32, float none, int64_t c,
-                                           int64_t width, float *x) {
-  constexpr int kLen = Vec<T>::kLen;
-  if (!p) {
-#pragma unroll
-    for (int j = 0; j < kLen; ++j) x[j] = none;
-  } else if (f32) {
-#pragma unroll
-    for (int j = 0; j < kLen; j += 4) load_floats(static_cast<const float *>(p), c + j, width, x + j);
-  } else {
-    load_floats(static_cast<const T *>(p), c, width, x);
+// A vector of a row, kLen columns from c on.  The one that the row ends in is
+// loaded kLen columns before the end instead, so every load is a whole one; its
+// first columns, and all of a vector behind the row, are another vector's and count
+// for nothing (`skip` of them).  SHORT: rows of fewer than kLen columns, loaded one
+// by one.
+template <typename T, bool SHORT>
+struct Piece {
+  static constexpr int kLen = Vec<T>::kLen;
+  int col, skip;
+  __device__ __forceinline__ Piece(int c, int width) {
+    col = SHORT ? 0 : min(c, width - kLen);
+    skip = SHORT ? (c == 0 ? 0 : kLen) : c - col;
   }
-}
+  __device__ __forceinline__ bool whole() const { return !SHORT && skip == 0; }
+  __device__ __forceinline__ bool has(int j, int width) const {
+    return SHORT ? skip == 0 && j < width : j >= skip;
+  }
+  __device__ __forceinline__ typename Vec<T>::type load(const T *row, int width) const {
+    if (!SHORT) return *reinterpret_cast<const typename Vec<T>::type *>(row + col);
+    typename Vec<T>::type v;
+#pragma unroll
+    for (int j = 0; j < kLen; ++j) v[j] = has(j, width) ? row[j] : (T)0.0f;
+    return v;
+  }
+  __device__ __forceinline__ void store(T *row, int width, const float *x) const {
+    if (whole()) {
+      typename Vec<T>::type v;
+#pragma unroll
+      for (int j = 0; j < kLen; ++j) v[j] = narrow<T>(x[j]);
+      *reinterpret_cast<typename Vec<T>::type *>(row + col) = v;
+    } else if (skip < kLen) {
+#pragma unroll
+      for (int j = 0; j < kLen; ++j)
+        if (has(j, width)) row[col + j] = narrow<T>(x[j]);
+    }
+  }
+  // weight or bias, or `none` where there is none
+  __device__ __forceinline__ void param(const void *p, int f32, float none, int width,
+                                        float *x) const {
+    typedef float F __attribute__((ext_vector_type(4), aligned(4)));
+    if (!p || SHORT) {
+#pragma unroll
+      for (int j = 0; j < kLen; ++j)
+        x[j] = !p || !has(j, width) ? none
+               : f32                ? static_cast<const float *>(p)[j]
+                                    : (float)static_cast<const T *>(p)[j];
+    } else if (f32) {
+#pragma unroll
+      for (int j = 0; j < kLen; j += 4) {
+        const F v = *reinterpret_cast<const F *>(static_cast<const float *>(p) + col + j);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[j + i] = v[i];
+      }
+    } else {
+      const typename Vec<T>::type v =
+          *reinterpret_cast<const typename Vec<T>::type *>(static_cast<const T *>(p) + col);
+#pragma unroll
+      for (int j = 0; j < kLen; ++j) x[j] = (float)v[j];
+    }
+  }
+};
 
 // N sums over the workgroup's waves, in every thread.
 template <int N>
@@ -60,16 +106,19 @@ __device__ __forceinline__ void block_sums(float (&v)[N], float (*lds)[N]) {
 
 // ---- forward --------------------------------------------------------------------
 
-// E columns a lane.  WAVE: 2^log_g lanes share a row, else the workgroup does.
-// Vector k of a lane lies at column (k * lanes + lane) * kLen.
-template <typename T, int E, bool WAVE>
+// E columns a lane, as they came, so that a wide row's fit the registers.  WAVE:
+// 2^log_g lanes share a row, else the workgroup does.  Vector k of a lane lies at
+// column (k * lanes + lane) * kLen.
+template <typename T, int E, bool WAVE, bool SHORT>
 __global__ __launch_bounds__(WAVE ? kWaveBlock : kMaxBlock) void norm_kernel(NormArgs a,
                                                                              int log_g,
                                                                              float over_width) {
   constexpr int kLen = Vec<T>::kLen, kVecs = E / kLen;
   constexpr bool kKeep = E <= 16;  // the parameters stay in registers
+  typedef Piece<T, SHORT> Part;
   __shared__ float first[kMaxBlock / 64][1], second[kMaxBlock / 64][2];
   const int lanes = WAVE ? 1 << log_g : (int)blockDim.x;
+  int width = (int)a.width;
   const int lane = WAVE ? threadIdx.x & (lanes - 1) : threadIdx.x;
   const int64_t per = WAVE ? kWaveBlock >> log_g : 1;
   const int64_t group = WAVE ? threadIdx.x >> log_g : 0;
@@ -77,43 +126,58 @@ __global__ __launch_bounds__(WAVE ? kWaveBlock : kMaxBlock) void norm_kernel(Nor
   if (kKeep) {
 #pragma unroll
     for (int k = 0; k < kVecs; ++k) {
-      const int64_t c = ((int64_t)k * lanes + lane) * kLen;
-      load_param<T>(a.weight, a.param_f32, 1.0f, c, a.width, w + k * kLen);
-      load_param<T>(a.bias, a.param_f32, 0.0f, c, a.width, b + k * kLen);
+      const Part at((k * lanes + lane) * kLen, width);
+      at.param(a.weight, a.param_f32, 1.0f, width, w + k * kLen);
+      at.param(a.bias, a.param_f32, 0.0f, width, b + k * kLen);
     }
   }
   for (int64_t row0 = (int64_t)blockIdx.x * per; row0 < a.rows;
        row0 += (int64_t)gridDim.x * per) {
-    const int64_t row = row0 + group;
-    const bool in = row < a.rows;
-    const T *src = static_cast<const T *>(a.x) + (in ? row : 0) * a.ld;
-    float x[E];
+    // Which columns count is worked out anew for every row: kept, the comparisons
+    // would fill the scalar registers and be spilled.
+    asm("" : "+s"(width));
+    const int64_t row = min(row0 + group, a.rows - 1);
+    const T *src = static_cast<const T *>(a.x) + row * a.ld;
+    typename Vec<T>::type x[kVecs];
 #pragma unroll
     for (int k = 0; k < kVecs; ++k)
-      load_floats(src, ((int64_t)k * lanes + lane) * kLen, in ? a.width : 0, x + k * kLen);
+      x[k] = Part((k * lanes + lane) * kLen, width).load(src, width);
     float s[1] = {0.0f};
 #pragma unroll
-    for (int i = 0; i < E; ++i) s[0] += x[i];
+    for (int k = 0; k < kVecs; ++k) {
+      const Part at((k * lanes + lane) * kLen, width);
+      if (at.whole()) {
+#pragma unroll
+        for (int j = 0; j < kLen; ++j) s[0] += (float)x[k][j];
+      } else {
+#pragma unroll
+        for (int j = 0; j < kLen; ++j) s[0] += at.has(j, width) ? (float)x[k][j] : 0.0f;
+      }
+    }
     if (WAVE)
       s[0] = group_sum(s[0], log_g);
     else
       block_sums(s, first);
     const float m0 = s[0] * over_width;
-#pragma unroll
-    for (int k = 0; k < kVecs; ++k) {
-      const int64_t c = ((int64_t)k * lanes + lane) * kLen;
-      if (c + kLen > a.width) {  // columns behind the row differ from the mean by nothing
-#pragma unroll
-        for (int j = 0; j < kLen; ++j)
-          if (c + j >= a.width) x[k * kLen + j] = m0;
-      }
-    }
     float t[2] = {0.0f, 0.0f};
 #pragma unroll
-    for (int i = 0; i < E; ++i) {
-      x[i] -= m0;
-      t[0] += x[i];
-      t[1] = fmaf(x[i], x[i], t[1]);
+    for (int k = 0; k < kVecs; ++k) {
+      const Part at((k * lanes + lane) * kLen, width);
+      if (at.whole()) {
+#pragma unroll
+        for (int j = 0; j < kLen; ++j) {
+          const float d = (float)x[k][j] - m0;
+          t[0] += d;
+          t[1] = fmaf(d, d, t[1]);
+        }
+      } else {
+#pragma unroll
+        for (int j = 0; j < kLen; ++j) {
+          const float d = at.has(j, width) ? (float)x[k][j] - m0 : 0.0f;
+          t[0] += d;
+          t[1] = fmaf(d, d, t[1]);
+        }
+      }
     }
     if (WAVE) {
       t[0] = group_sum(t[0], log_g);
@@ -125,7 +189,7 @@ __global__ __launch_bounds__(WAVE ? kWaveBlock : kMaxBlock) void norm_kernel(Nor
     const float raw = fmaf(t[1], over_width, -delta * delta);
     const float var = raw < 0.0f ? 0.0f : raw;  // a NaN stays one
     const float rstd = 1.0f / sqrtf(var + a.eps);
-    if (!in) continue;
+    if (row0 + group >= a.rows) continue;
     if (lane == 0) {
       if (a.mean) a.mean[row] = m0 + delta;
       if (a.rstd) a.rstd[row] = rstd;
@@ -133,19 +197,18 @@ __global__ __launch_bounds__(WAVE ? kWaveBlock : kMaxBlock) void norm_kernel(Nor
     T *dst = static_cast<T *>(a.out) + row * a.out_ld;
 #pragma unroll
     for (int k = 0; k < kVecs; ++k) {
-      const int64_t c = ((int64_t)k * lanes + lane) * kLen;
-      if (c >= a.width) continue;
+      const Part at((k * lanes + lane) * kLen, width);
       if (!kKeep) {
-        load_param<T>(a.weight, a.param_f32, 1.0f, c, a.width, w);
-        load_param<T>(a.bias, a.param_f32, 0.0f, c, a.width, b);
+        at.param(a.weight, a.param_f32, 1.0f, width, w);
+        at.param(a.bias, a.param_f32, 0.0f, width, b);
       }
       float y[kLen];
 #pragma unroll
       for (int j = 0; j < kLen; ++j) {
         const int p = kKeep ? k * kLen + j : j;
-        y[j] = fmaf((x[k * kLen + j] - delta) * rstd, w[p], b[p]);
+        y[j] = fmaf(((float)x[k][j] - m0 - delta) * rstd, w[p], b[p]);
       }
-      store_floats(dst, c, a.width, y);
+      at.store(dst, width, y);
     }
   }
 }
@@ -163,55 +226,62 @@ struct GradShape {
 
 // Sums of a lane group over all rows it takes go to part[block][0] (weight) and
 // [1] (bias), float32 [width] each.
-template <typename T, int E>
+template <typename T, int E, bool SHORT>
 __global__ __launch_bounds__(kMaxBlock) void grad_kernel(NormGradArgs a, GradShape g,
                                                          float over_width, float *part) {
   constexpr int kLen = Vec<T>::kLen, kVecs = E / kLen;
+  typedef Piece<T, SHORT> Part;
   __shared__ float lds[kMaxBlock * E];
   float (*sums)[kMaxBlock / 64][3] = reinterpret_cast<float (*)[kMaxBlock / 64][3]>(lds);
   const int lanes = g.lanes, group = (int)threadIdx.x / lanes;
+  int width = (int)a.width;
   const int lane = (int)threadIdx.x - group * lanes;
   const bool wide = lanes > 64;
   float w[E], dw[E], db[E];
 #pragma unroll
   for (int k = 0; k < kVecs; ++k)
-    load_param<T>(a.weight, a.param_f32, 1.0f, ((int64_t)k * lanes + lane) * kLen, a.width,
-                  w + k * kLen);
+    Part((k * lanes + lane) * kLen, width)
+        .param(a.weight, a.param_f32, 1.0f, width, w + k * kLen);
 #pragma unroll
   for (int i = 0; i < E; ++i) dw[i] = db[i] = 0.0f;
   int turn = 0;
   for (int64_t row0 = (int64_t)blockIdx.x * g.per; row0 < a.rows;
        row0 += (int64_t)gridDim.x * g.per, turn ^= 1) {
-    const int64_t row = row0 + group;
-    const bool in = row < a.rows;
-    const int64_t from = in ? row : 0, width = in ? a.width : 0;
-    const float mean = a.mean[from], rstd = a.rstd[from];
-    const T *xs = static_cast<const T *>(a.x) + from * a.ld;
-    const T *ds = static_cast<const T *>(a.dout) + from * a.dout_ld;
-    float x[E], d[E];
+    asm("" : "+s"(width));  // as in norm_kernel
+    const int64_t row = min(row0 + group, a.rows - 1);
+    const float mean = a.mean[row], rstd = a.rstd[row];
+    const T *xs = static_cast<const T *>(a.x) + row * a.ld;
+    const T *ds = static_cast<const T *>(a.dout) + row * a.dout_ld;
+    typename Vec<T>::type x[kVecs], d[kVecs];
 #pragma unroll
     for (int k = 0; k < kVecs; ++k) {
-      const int64_t c = ((int64_t)k * lanes + lane) * kLen;
-      load_floats(xs, c, width, x + k * kLen);
-      load_floats(ds, c, width, d + k * kLen);
-    }
-#pragma unroll
-    for (int k = 0; k < kVecs; ++k) {
-      const int64_t c = ((int64_t)k * lanes + lane) * kLen;
-      if (c + kLen > width) {
-#pragma unroll
-        for (int j = 0; j < kLen; ++j)
-          if (c + j >= width) x[k * kLen + j] = mean;
-      }
+      const Part at((k * lanes + lane) * kLen, width);
+      x[k] = at.load(xs, width);
+      d[k] = at.load(ds, width);
     }
     float s[3] = {0.0f, 0.0f, 0.0f};  // of x - mean, g, g (x - mean)
 #pragma unroll
-    for (int i = 0; i < E; ++i) {
-      x[i] -= mean;
-      const float gi = d[i] * w[i];
-      s[0] += x[i];
-      s[1] += gi;
-      s[2] = fmaf(gi, x[i], s[2]);
+    for (int k = 0; k < kVecs; ++k) {
+      const Part at((k * lanes + lane) * kLen, width);
+      if (at.whole()) {
+#pragma unroll
+        for (int j = 0; j < kLen; ++j) {
+          const float xj = (float)x[k][j] - mean, gj = (float)d[k][j] * w[k * kLen + j];
+          s[0] += xj;
+          s[1] += gj;
+          s[2] = fmaf(gj, xj, s[2]);
+        }
+      } else {
+#pragma unroll
+        for (int j = 0; j < kLen; ++j) {
+          const bool has = at.has(j, width);
+          const float xj = has ? (float)x[k][j] - mean : 0.0f;
+          const float gj = has ? (float)d[k][j] * w[k * kLen + j] : 0.0f;
+          s[0] += xj;
+          s[1] += gj;
+          s[2] = fmaf(gj, xj, s[2]);
+        }
+      }
     }
     const int log_g = wide ? 6 : g.log_g;
 #pragma unroll
@@ -235,21 +305,20 @@ __global__ __launch_bounds__(kMaxBlock) void grad_kernel(NormGradArgs a, GradSha
     }
     const float delta = s[0] * over_width, g_avg = s[1] * over_width;
     const float along = (s[2] - delta * s[1]) * over_width * rstd;  // avg(g xhat)
-    if (in) {
+    if (row0 + group < a.rows) {
       T *dst = a.dx ? static_cast<T *>(a.dx) + row * a.dx_ld : nullptr;
 #pragma unroll
       for (int k = 0; k < kVecs; ++k) {
-        const int64_t c = ((int64_t)k * lanes + lane) * kLen;
         float y[kLen];
 #pragma unroll
         for (int j = 0; j < kLen; ++j) {
           const int i = k * kLen + j;
-          const float xhat = (x[i] - delta) * rstd;
-          dw[i] = fmaf(d[i], xhat, dw[i]);
-          db[i] += d[i];
-          y[j] = rstd * (fmaf(d[i], w[i], -g_avg) - xhat * along);
+          const float dj = (float)d[k][j], xhat = ((float)x[k][j] - mean - delta) * rstd;
+          dw[i] = fmaf(dj, xhat, dw[i]);
+          db[i] += dj;
+          y[j] = rstd * (fmaf(dj, w[i], -g_avg) - xhat * along);
         }
-        if (dst) store_floats(dst, c, a.width, y);
+        if (dst) Part((k * lanes + lane) * kLen, width).store(dst, width, y);
       }
     }
   }
@@ -277,24 +346,25 @@ __global__ __launch_bounds__(kMaxBlock) void grad_kernel(NormGradArgs a, GradSha
   const int parts = wide ? g.per : (int)blockDim.x >> 6;
   const int own = wide ? group : (int)threadIdx.x >> 6;
   const bool has = wide || (int)(threadIdx.x & 63) < lanes;
-  const int span = lanes * E;  // columns that a part holds, the row's and some behind it
-  float *to = part + (int64_t)blockIdx.x * 2 * a.width;
+  float *to = part + (int64_t)blockIdx.x * 2 * width;
 #pragma unroll
   for (int q = 0; q < 2; ++q) {
     __syncthreads();
     if (has) {
 #pragma unroll
       for (int k = 0; k < kVecs; ++k) {
+        const Part at((k * lanes + lane) * kLen, width);
+        float *row = lds + own * width + at.col;  // at most lanes * E columns
 #pragma unroll
         for (int j = 0; j < kLen; ++j)
-          lds[own * span + (k * lanes + lane) * kLen + j] = q ? db[k * kLen + j] : dw[k * kLen + j];
+          if (at.has(j, width)) row[j] = q ? db[k * kLen + j] : dw[k * kLen + j];
       }
     }
     __syncthreads();
-    for (int64_t c = threadIdx.x; c < a.width; c += blockDim.x) {
+    for (int c = threadIdx.x; c < width; c += blockDim.x) {
       float v = lds[c];
-      for (int p = 1; p < parts; ++p) v += lds[p * span + c];
-      to[q * a.width + c] = v;
+      for (int p = 1; p < parts; ++p) v += lds[p * width + c];
+      to[q * width + c] = v;
     }
   }
 }
@@ -310,34 +380,36 @@ template <typename T>
 __global__ __launch_bounds__(kStatThreads) void stat_kernel(NormGradArgs a, int64_t pieces,
                                                             float *stat) {
   constexpr int kLen = Vec<T>::kLen;
+  typedef Piece<T, false> Part;
   __shared__ float lds[2][kStatThreads / 64][3];
+  const int width = (int)a.width;
   int turn = 0;
   for (int64_t item = blockIdx.x; item < a.rows * pieces; item += gridDim.x, turn ^= 1) {
     const int64_t row = item / pieces, piece = item - row * pieces;
     const float mean = a.mean[row];
     const T *xs = static_cast<const T *>(a.x) + row * a.ld;
     const T *ds = static_cast<const T *>(a.dout) + row * a.dout_ld;
-    float x[kStatVecs][kLen], d[kStatVecs][kLen];
-    const int64_t c0 = (piece * kStatVecs * kStatThreads + threadIdx.x) * kLen;
+    typename Vec<T>::type x[kStatVecs], d[kStatVecs];
+    const int c0 = ((int)piece * kStatVecs * kStatThreads + (int)threadIdx.x) * kLen;
 #pragma unroll
     for (int k = 0; k < kStatVecs; ++k) {
-      load_floats(xs, c0 + k * kStatThreads * kLen, a.width, x[k]);
-      load_floats(ds, c0 + k * kStatThreads * kLen, a.width, d[k]);
+      const Part at(c0 + k * kStatThreads * kLen, width);
+      x[k] = at.load(xs, width);
+      d[k] = at.load(ds, width);
     }
     float s[3] = {0.0f, 0.0f, 0.0f};
 #pragma unroll
     for (int k = 0; k < kStatVecs; ++k) {
-      const int64_t c = c0 + k * kStatThreads * kLen;
+      const Part at(c0 + k * kStatThreads * kLen, width);
       float w[kLen];
-      if (c < a.width) {
-        load_param<T>(a.weight, a.param_f32, 1.0f, c, a.width, w);
+      at.param(a.weight, a.param_f32, 1.0f, width, w);
 #pragma unroll
-        for (int j = 0; j < kLen; ++j) {
-          const float v = c + j < a.width ? x[k][j] - mean : 0.0f, g = d[k][j] * w[j];
-          s[0] += v;
-          s[1] += g;
-          s[2] = fmaf(g, v, s[2]);
-        }
+      for (int j = 0; j < kLen; ++j) {
+        const bool has = at.has(j, width);
+        const float v = has ? (float)x[k][j] - mean : 0.0f, g = has ? (float)d[k][j] * w[j] : 0.0f;
+        s[0] += v;
+        s[1] += g;
+        s[2] = fmaf(g, v, s[2]);
       }
     }
     block_sums(s, lds[turn]);
@@ -351,12 +423,14 @@ __global__ __launch_bounds__(kWideThreads) void wide_kernel(NormGradArgs a, int6
                                                             int64_t chunk, float over_width,
                                                             const float *stat, float *part) {
   constexpr int kLen = Vec<T>::kLen, kVecs = kWideColumns / kLen;
-  const int64_t c0 = ((int64_t)blockIdx.x * kVecs * kWideThreads + threadIdx.x) * kLen;
+  typedef Piece<T, false> Part;
+  const int width = (int)a.width;
+  const int c0 = ((int)blockIdx.x * kVecs * kWideThreads + (int)threadIdx.x) * kLen;
   const int64_t r0 = (int64_t)blockIdx.y * chunk, r1 = min(a.rows, r0 + chunk);
   float w[kVecs][kLen], dw[kVecs][kLen], db[kVecs][kLen];
 #pragma unroll
   for (int k = 0; k < kVecs; ++k) {
-    load_param<T>(a.weight, a.param_f32, 1.0f, c0 + k * kWideThreads * kLen, a.width, w[k]);
+    Part(c0 + k * kWideThreads * kLen, width).param(a.weight, a.param_f32, 1.0f, width, w[k]);
 #pragma unroll
     for (int j = 0; j < kLen; ++j) dw[k][j] = db[k][j] = 0.0f;
   }
@@ -371,37 +445,38 @@ __global__ __launch_bounds__(kWideThreads) void wide_kernel(NormGradArgs a, int6
     const float along = (s[2] - delta * s[1]) * over_width * rstd;
     const T *xs = static_cast<const T *>(a.x) + row * a.ld;
     const T *ds = static_cast<const T *>(a.dout) + row * a.dout_ld;
-    float x[kVecs][kLen], d[kVecs][kLen];
+    typename Vec<T>::type x[kVecs], d[kVecs];
 #pragma unroll
     for (int k = 0; k < kVecs; ++k) {
-      load_floats(xs, c0 + k * kWideThreads * kLen, a.width, x[k]);
-      load_floats(ds, c0 + k * kWideThreads * kLen, a.width, d[k]);
+      const Part at(c0 + k * kWideThreads * kLen, width);
+      x[k] = at.load(xs, width);
+      d[k] = at.load(ds, width);
     }
 #pragma unroll
     for (int k = 0; k < kVecs; ++k) {
       float y[kLen];
 #pragma unroll
       for (int j = 0; j < kLen; ++j) {
-        const float xhat = (x[k][j] - mean - delta) * rstd;
-        dw[k][j] = fmaf(d[k][j], xhat, dw[k][j]);
-        db[k][j] += d[k][j];
-        y[j] = rstd * (fmaf(d[k][j], w[k][j], -g_avg) - xhat * along);
+        const float dj = (float)d[k][j], xhat = ((float)x[k][j] - mean - delta) * rstd;
+        dw[k][j] = fmaf(dj, xhat, dw[k][j]);
+        db[k][j] += dj;
+        y[j] = rstd * (fmaf(dj, w[k][j], -g_avg) - xhat * along);
       }
       if (a.dx)
-        store_floats(static_cast<T *>(a.dx) + row * a.dx_ld, c0 + k * kWideThreads * kLen, a.width,
-                     y);
+        Part(c0 + k * kWideThreads * kLen, width)
+            .store(static_cast<T *>(a.dx) + row * a.dx_ld, width, y);
     }
   }
   if (!part) return;
-  float *to = part + (int64_t)blockIdx.y * 2 * a.width;
+  float *to = part + (int64_t)blockIdx.y * 2 * width;
 #pragma unroll
   for (int k = 0; k < kVecs; ++k) {
+    const Part at(c0 + k * kWideThreads * kLen, width);
 #pragma unroll
     for (int j = 0; j < kLen; ++j) {
-      const int64_t c = c0 + k * kWideThreads * kLen + j;
-      if (c < a.width) {
-        to[c] = dw[k][j];
-        to[a.width + c] = db[k][j];
+      if (at.has(j, width)) {
+        to[at.col + j] = dw[k][j];
+        to[width + at.col + j] = db[k][j];
       }
     }
   }
@@ -454,12 +529,12 @@ int log2_up(int64_t v) {
 }
 
 // Rows of at most a wave, and of a workgroup.
-template <typename T, int E>
+template <typename T, int E, bool SHORT>
 hipError_t launch_narrow(const NormArgs &a, int cu_count, hipStream_t s) {
   const int log_g = log2_up((a.width + E - 1) / E);
   const int64_t per = kWaveBlock >> log_g;
   const int64_t grid = std::min<int64_t>((a.rows + per - 1) / per, (int64_t)cu_count * 8);
-  norm_kernel<T, E, true><<<(uint32_t)grid, kWaveBlock, 0, s>>>(a, log_g, 1.0f / (float)a.width);
+  norm_kernel<T, E, true, SHORT><<<(uint32_t)grid, kWaveBlock, 0, s>>>(a, log_g, 1.0f / (float)a.width);
   return hipGetLastError();
 }
 
@@ -467,14 +542,15 @@ template <typename T, int E>
 hipError_t launch_wide(const NormArgs &a, int cu_count, hipStream_t s) {
   const int threads = (int)((a.width + 64 * E - 1) / (64 * E) * 64);
   const int64_t grid = std::min<int64_t>(a.rows, (int64_t)cu_count * (2048 / threads));
-  norm_kernel<T, E, false><<<(uint32_t)grid, threads, 0, s>>>(a, 0, 1.0f / (float)a.width);
+  norm_kernel<T, E, false, false><<<(uint32_t)grid, threads, 0, s>>>(a, 0, 1.0f / (float)a.width);
   return hipGetLastError();
 }
 
 template <typename T>
 hipError_t launch_norm(const NormArgs &a, int cu_count, hipStream_t s) {
-  if (a.width <= 64 * 8) return launch_narrow<T, 8>(a, cu_count, s);
-  if (a.width <= 64 * 16) return launch_narrow<T, 16>(a, cu_count, s);
+  if (a.width < Vec<T>::kLen) return launch_narrow<T, 8, true>(a, cu_count, s);
+  if (a.width <= 64 * 8) return launch_narrow<T, 8, false>(a, cu_count, s);
+  if (a.width <= 64 * 16) return launch_narrow<T, 16, false>(a, cu_count, s);
   if (a.width <= kMaxBlock * 16) return launch_wide<T, 16>(a, cu_count, s);
   if (a.width <= kMaxBlock * 32) return launch_wide<T, 32>(a, cu_count, s);
   return launch_wide<T, 64>(a, cu_count, s);
@@ -522,10 +598,12 @@ hipError_t launch_grad(const NormGradArgs &a, void *ws, hipStream_t s) {
   if (a.rows > 0 && a.width <= kGradWidth) {
     const GradShape g = grad_shape(a.rows, a.width);
     parts = g.blocks;
-    if (grad_columns(a.width) == 8)
-      grad_kernel<T, 8><<<g.blocks, g.threads, 0, s>>>(a, g, over, sums ? part : nullptr);
+    if (a.width < Vec<T>::kLen)
+      grad_kernel<T, 8, true><<<g.blocks, g.threads, 0, s>>>(a, g, over, sums ? part : nullptr);
+    else if (grad_columns(a.width) == 8)
+      grad_kernel<T, 8, false><<<g.blocks, g.threads, 0, s>>>(a, g, over, sums ? part : nullptr);
     else
-      grad_kernel<T, 16><<<g.blocks, g.threads, 0, s>>>(a, g, over, sums ? part : nullptr);
+      grad_kernel<T, 16, false><<<g.blocks, g.threads, 0, s>>>(a, g, over, sums ? part : nullptr);
   } else if (a.rows > 0) {
     const int64_t each = (int64_t)kStatVecs * kStatThreads * Vec<T>::kLen;
     const int64_t pieces = (a.width + each - 1) / each;
