@@ -14,6 +14,7 @@
 // their digits that way.  The gradient takes the stored mean as m0 and finds
 // delta beside its own two sums.
 #include <algorithm>
+#include <type_traits>
 
 #include "train.h"
 
@@ -28,6 +29,15 @@ constexpr int kMaxBlock = 1024;
 // first columns, and all of a vector behind the row, are another vector's and count
 // for nothing (`skip` of them).  SHORT: rows of fewer than kLen columns, loaded one
 // by one.
+//
+// Offsets are unsigned and in bytes, so that they are one register beside a row's
+// address, which all lanes share.
+template <typename A, typename T>
+__device__ __forceinline__ A *at_column(T *row, int col) {
+  typedef typename std::conditional<std::is_const<T>::value, const char, char>::type Byte;
+  return reinterpret_cast<A *>(reinterpret_cast<Byte *>(row) + (uint32_t)col * (uint32_t)sizeof(T));
+}
+
 template <typename T, bool SHORT>
 struct Piece {
   static constexpr int kLen = Vec<T>::kLen;
@@ -41,7 +51,7 @@ struct Piece {
     return SHORT ? skip == 0 && j < width : j >= skip;
   }
   __device__ __forceinline__ typename Vec<T>::type load(const T *row, int width) const {
-    if (!SHORT) return *reinterpret_cast<const typename Vec<T>::type *>(row + col);
+    if (!SHORT) return *at_column<const typename Vec<T>::type>(row, col);
     typename Vec<T>::type v;
 #pragma unroll
     for (int j = 0; j < kLen; ++j) v[j] = has(j, width) ? row[j] : (T)0.0f;
@@ -52,38 +62,58 @@ struct Piece {
       typename Vec<T>::type v;
 #pragma unroll
       for (int j = 0; j < kLen; ++j) v[j] = narrow<T>(x[j]);
-      *reinterpret_cast<typename Vec<T>::type *>(row + col) = v;
+      *at_column<typename Vec<T>::type>(row, col) = v;
     } else if (skip < kLen) {
 #pragma unroll
       for (int j = 0; j < kLen; ++j)
-        if (has(j, width)) row[col + j] = narrow<T>(x[j]);
+        if (has(j, width)) *at_column<T>(row, col + j) = narrow<T>(x[j]);
     }
   }
-  // weight or bias, or `none` where there is none
-  __device__ __forceinline__ void param(const void *p, int f32, float none, int width,
-                                        float *x) const {
+  // weight or bias of columns j .. j + 3 of the vector, or `none` where there is none
+  __device__ __forceinline__ void param4(const void *p, int f32, float none, int width, int j,
+                                         float *x) const {
     typedef float F __attribute__((ext_vector_type(4), aligned(4)));
+    typedef T H __attribute__((ext_vector_type(4), aligned(sizeof(T))));
     if (!p || SHORT) {
 #pragma unroll
-      for (int j = 0; j < kLen; ++j)
-        x[j] = !p || !has(j, width) ? none
-               : f32                ? static_cast<const float *>(p)[j]
-                                    : (float)static_cast<const T *>(p)[j];
+      for (int i = 0; i < 4; ++i)
+        x[i] = !p || !has(j + i, width) ? none
+               : f32                    ? static_cast<const float *>(p)[j + i]
+                                        : (float)static_cast<const T *>(p)[j + i];
     } else if (f32) {
+      const F v = *at_column<const F>(static_cast<const float *>(p), col + j);
 #pragma unroll
-      for (int j = 0; j < kLen; j += 4) {
-        const F v = *reinterpret_cast<const F *>(static_cast<const float *>(p) + col + j);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) x[j + i] = v[i];
-      }
+      for (int i = 0; i < 4; ++i) x[i] = v[i];
     } else {
-      const typename Vec<T>::type v =
-          *reinterpret_cast<const typename Vec<T>::type *>(static_cast<const T *>(p) + col);
+      const H v = *at_column<const H>(static_cast<const T *>(p), col + j);
 #pragma unroll
-      for (int j = 0; j < kLen; ++j) x[j] = (float)v[j];
+      for (int i = 0; i < 4; ++i) x[i] = (float)v[i];
     }
   }
+  __device__ __forceinline__ void param(const void *p, int f32, float none, int width,
+                                        float *x) const {
+#pragma unroll
+    for (int j = 0; j < kLen; j += 4) param4(p, f32, none, width, j, x + j);
+  }
 };
+
+// A vector whose elements are widened again where they are used again: the
+// compiler would keep them in float32, in twice the registers.
+template <typename V>
+__device__ __forceinline__ V anew(V v) {
+  typedef int Bits __attribute__((ext_vector_type(4)));
+  Bits b = __builtin_bit_cast(Bits, v);
+  asm("" : "+v"(b));
+  return __builtin_bit_cast(V, b);
+}
+
+// The same number, of which the compiler does not know it: where a vector lies and
+// which of its columns count is worked out anew then.  Kept, all of that would fill
+// the registers.
+__device__ __forceinline__ int anew(int v) {
+  asm volatile("" : "+s"(v));
+  return v;
+}
 
 // N sums over the workgroup's waves, in every thread.
 template <int N>
@@ -106,23 +136,24 @@ __device__ __forceinline__ void block_sums(float (&v)[N], float (*lds)[N]) {
 
 // ---- forward --------------------------------------------------------------------
 
-// E columns a lane, as they came, so that a wide row's fit the registers.  WAVE:
+// E columns a lane, as they came, so that a wide row's fit the registers, and those
+// of two rows where they are at most 128 bytes a lane (hence the bound of 8 waves a
+// SIMD: a compute unit loads one row while it writes another).  WAVE:
 // 2^log_g lanes share a row, else the workgroup does.  Vector k of a lane lies at
 // column (k * lanes + lane) * kLen.
 template <typename T, int E, bool WAVE, bool SHORT>
-__global__ __launch_bounds__(WAVE ? kWaveBlock : kMaxBlock) void norm_kernel(NormArgs a,
-                                                                             int log_g,
-                                                                             float over_width) {
+__global__ __launch_bounds__(WAVE ? kWaveBlock : kMaxBlock,
+                             E >= 32 && E * sizeof(T) <= 128 ? 8 : 1) void norm_kernel(
+    NormArgs a, int log_g, float over_width) {
   constexpr int kLen = Vec<T>::kLen, kVecs = E / kLen;
   constexpr bool kKeep = E <= 16;  // the parameters stay in registers
   typedef Piece<T, SHORT> Part;
   __shared__ float first[kMaxBlock / 64][1], second[kMaxBlock / 64][2];
-  const int lanes = WAVE ? 1 << log_g : (int)blockDim.x;
-  int width = (int)a.width;
+  const int lanes = WAVE ? 1 << log_g : (int)blockDim.x, width = (int)a.width;
   const int lane = WAVE ? threadIdx.x & (lanes - 1) : threadIdx.x;
   const int64_t per = WAVE ? kWaveBlock >> log_g : 1;
   const int64_t group = WAVE ? threadIdx.x >> log_g : 0;
-  float w[kKeep ? E : kLen], b[kKeep ? E : kLen];
+  float w[kKeep ? E : 4], b[kKeep ? E : 4];
   if (kKeep) {
 #pragma unroll
     for (int k = 0; k < kVecs; ++k) {
@@ -133,19 +164,16 @@ __global__ __launch_bounds__(WAVE ? kWaveBlock : kMaxBlock) void norm_kernel(Nor
   }
   for (int64_t row0 = (int64_t)blockIdx.x * per; row0 < a.rows;
        row0 += (int64_t)gridDim.x * per) {
-    // Which columns count is worked out anew for every row: kept, the comparisons
-    // would fill the scalar registers and be spilled.
-    asm("" : "+s"(width));
     const int64_t row = min(row0 + group, a.rows - 1);
     const T *src = static_cast<const T *>(a.x) + row * a.ld;
     typename Vec<T>::type x[kVecs];
 #pragma unroll
     for (int k = 0; k < kVecs; ++k)
-      x[k] = Part((k * lanes + lane) * kLen, width).load(src, width);
+      x[k] = Part((k * lanes + lane) * kLen, anew(width)).load(src, width);
     float s[1] = {0.0f};
 #pragma unroll
     for (int k = 0; k < kVecs; ++k) {
-      const Part at((k * lanes + lane) * kLen, width);
+      const Part at((k * lanes + lane) * kLen, anew(width));
       if (at.whole()) {
 #pragma unroll
         for (int j = 0; j < kLen; ++j) s[0] += (float)x[k][j];
@@ -162,7 +190,8 @@ __global__ __launch_bounds__(WAVE ? kWaveBlock : kMaxBlock) void norm_kernel(Nor
     float t[2] = {0.0f, 0.0f};
 #pragma unroll
     for (int k = 0; k < kVecs; ++k) {
-      const Part at((k * lanes + lane) * kLen, width);
+      x[k] = anew(x[k]);
+      const Part at((k * lanes + lane) * kLen, anew(width));
       if (at.whole()) {
 #pragma unroll
         for (int j = 0; j < kLen; ++j) {
@@ -197,16 +226,21 @@ __global__ __launch_bounds__(WAVE ? kWaveBlock : kMaxBlock) void norm_kernel(Nor
     T *dst = static_cast<T *>(a.out) + row * a.out_ld;
 #pragma unroll
     for (int k = 0; k < kVecs; ++k) {
-      const Part at((k * lanes + lane) * kLen, width);
-      if (!kKeep) {
-        at.param(a.weight, a.param_f32, 1.0f, width, w);
-        at.param(a.bias, a.param_f32, 0.0f, width, b);
-      }
+      const Part at((k * lanes + lane) * kLen, anew(width));
+      x[k] = anew(x[k]);
       float y[kLen];
 #pragma unroll
-      for (int j = 0; j < kLen; ++j) {
-        const int p = kKeep ? k * kLen + j : j;
-        y[j] = fmaf(((float)x[k][j] - m0 - delta) * rstd, w[p], b[p]);
+      for (int j = 0; j < kLen; j += 4) {
+        if (!kKeep) {
+          at.param4(a.weight, a.param_f32, 1.0f, width, j, w);
+          at.param4(a.bias, a.param_f32, 0.0f, width, j, b);
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int p = kKeep ? k * kLen + j + i : i;
+          y[j + i] = fmaf(((float)x[k][j + i] - m0 - delta) * rstd, w[p], b[p]);
+        }
+        if (!kKeep) __builtin_amdgcn_sched_barrier(0);  // few parameters at a time
       }
       at.store(dst, width, y);
     }
@@ -217,11 +251,22 @@ __global__ __launch_bounds__(WAVE ? kWaveBlock : kMaxBlock) void norm_kernel(Nor
 
 constexpr int kGradBlocks = 256;   // at most: each leaves a part of the parameters' sums
 constexpr int kGradWidth = 16 * kMaxBlock;
+constexpr int kDirectTurns = 4;
+
+__device__ __forceinline__ void store_as(int dtype, void *p, int64_t i, float v) {
+  if (dtype == ML2_F32)
+    static_cast<float *>(p)[i] = v;
+  else if (dtype == ML2_BF16)
+    static_cast<__bf16 *>(p)[i] = narrow<__bf16>(v);
+  else
+    static_cast<_Float16 *>(p)[i] = narrow<_Float16>(v);
+}
 
 struct GradShape {
   int lanes, log_g;   // of a row; log_g: where they are at most a wave
   int per, threads;   // rows at a time, threads of a workgroup
   int blocks;
+  bool direct;        // one workgroup: it writes the parameters' sums itself
 };
 
 // Sums of a lane group over all rows it takes go to part[block][0] (weight) and
@@ -233,8 +278,7 @@ __global__ __launch_bounds__(kMaxBlock) void grad_kernel(NormGradArgs a, GradSha
   typedef Piece<T, SHORT> Part;
   __shared__ float lds[kMaxBlock * E];
   float (*sums)[kMaxBlock / 64][3] = reinterpret_cast<float (*)[kMaxBlock / 64][3]>(lds);
-  const int lanes = g.lanes, group = (int)threadIdx.x / lanes;
-  int width = (int)a.width;
+  const int lanes = g.lanes, group = (int)threadIdx.x / lanes, width = (int)a.width;
   const int lane = (int)threadIdx.x - group * lanes;
   const bool wide = lanes > 64;
   float w[E], dw[E], db[E];
@@ -247,7 +291,6 @@ __global__ __launch_bounds__(kMaxBlock) void grad_kernel(NormGradArgs a, GradSha
   int turn = 0;
   for (int64_t row0 = (int64_t)blockIdx.x * g.per; row0 < a.rows;
        row0 += (int64_t)gridDim.x * g.per, turn ^= 1) {
-    asm("" : "+s"(width));  // as in norm_kernel
     const int64_t row = min(row0 + group, a.rows - 1);
     const float mean = a.mean[row], rstd = a.rstd[row];
     const T *xs = static_cast<const T *>(a.x) + row * a.ld;
@@ -255,14 +298,14 @@ __global__ __launch_bounds__(kMaxBlock) void grad_kernel(NormGradArgs a, GradSha
     typename Vec<T>::type x[kVecs], d[kVecs];
 #pragma unroll
     for (int k = 0; k < kVecs; ++k) {
-      const Part at((k * lanes + lane) * kLen, width);
+      const Part at((k * lanes + lane) * kLen, anew(width));
       x[k] = at.load(xs, width);
       d[k] = at.load(ds, width);
     }
     float s[3] = {0.0f, 0.0f, 0.0f};  // of x - mean, g, g (x - mean)
 #pragma unroll
     for (int k = 0; k < kVecs; ++k) {
-      const Part at((k * lanes + lane) * kLen, width);
+      const Part at((k * lanes + lane) * kLen, anew(width));
       if (at.whole()) {
 #pragma unroll
         for (int j = 0; j < kLen; ++j) {
@@ -309,6 +352,8 @@ __global__ __launch_bounds__(kMaxBlock) void grad_kernel(NormGradArgs a, GradSha
       T *dst = a.dx ? static_cast<T *>(a.dx) + row * a.dx_ld : nullptr;
 #pragma unroll
       for (int k = 0; k < kVecs; ++k) {
+        x[k] = anew(x[k]);
+        d[k] = anew(d[k]);
         float y[kLen];
 #pragma unroll
         for (int j = 0; j < kLen; ++j) {
@@ -318,7 +363,7 @@ __global__ __launch_bounds__(kMaxBlock) void grad_kernel(NormGradArgs a, GradSha
           db[i] += dj;
           y[j] = rstd * (fmaf(dj, w[i], -g_avg) - xhat * along);
         }
-        if (dst) Part((k * lanes + lane) * kLen, width).store(dst, width, y);
+        if (dst) Part((k * lanes + lane) * kLen, anew(width)).store(dst, width, y);
       }
     }
   }
@@ -346,6 +391,7 @@ __global__ __launch_bounds__(kMaxBlock) void grad_kernel(NormGradArgs a, GradSha
   const int parts = wide ? g.per : (int)blockDim.x >> 6;
   const int own = wide ? group : (int)threadIdx.x >> 6;
   const bool has = wide || (int)(threadIdx.x & 63) < lanes;
+  typedef float F4 __attribute__((ext_vector_type(4), aligned(4)));
   float *to = part + (int64_t)blockIdx.x * 2 * width;
 #pragma unroll
   for (int q = 0; q < 2; ++q) {
@@ -355,16 +401,30 @@ __global__ __launch_bounds__(kMaxBlock) void grad_kernel(NormGradArgs a, GradSha
       for (int k = 0; k < kVecs; ++k) {
         const Part at((k * lanes + lane) * kLen, width);
         float *row = lds + own * width + at.col;  // at most lanes * E columns
+        if (at.whole()) {
 #pragma unroll
-        for (int j = 0; j < kLen; ++j)
-          if (at.has(j, width)) row[j] = q ? db[k * kLen + j] : dw[k * kLen + j];
+          for (int j = 0; j < kLen; j += 4) {
+            const int i = k * kLen + j;
+            *reinterpret_cast<F4 *>(row + j) = q ? F4{db[i], db[i + 1], db[i + 2], db[i + 3]}
+                                                 : F4{dw[i], dw[i + 1], dw[i + 2], dw[i + 3]};
+          }
+        } else {
+#pragma unroll
+          for (int j = 0; j < kLen; ++j)
+            if (at.has(j, width)) row[j] = q ? db[k * kLen + j] : dw[k * kLen + j];
+        }
       }
     }
     __syncthreads();
+    void *out = q ? a.dbias : a.dweight;
     for (int c = threadIdx.x; c < width; c += blockDim.x) {
       float v = lds[c];
+#pragma unroll 8
       for (int p = 1; p < parts; ++p) v += lds[p * width + c];
-      to[q * width + c] = v;
+      if (!g.direct)
+        to[q * width + c] = v;
+      else if (out)
+        store_as(a.grad_dtype, out, c, v);
     }
   }
 }
@@ -434,6 +494,19 @@ __global__ __launch_bounds__(kWideThreads) void wide_kernel(NormGradArgs a, int6
 #pragma unroll
     for (int j = 0; j < kLen; ++j) dw[k][j] = db[k][j] = 0.0f;
   }
+  // The next row is loaded before this one's gradient is written.
+  typename Vec<T>::type x[kVecs], d[kVecs], x1[kVecs], d1[kVecs];
+  const auto load = [&](int64_t row) {
+    const T *xs = static_cast<const T *>(a.x) + row * a.ld;
+    const T *ds = static_cast<const T *>(a.dout) + row * a.dout_ld;
+#pragma unroll
+    for (int k = 0; k < kVecs; ++k) {
+      const Part at(c0 + k * kWideThreads * kLen, width);
+      x1[k] = at.load(xs, width);
+      d1[k] = at.load(ds, width);
+    }
+  };
+  load(r0);
   for (int64_t row = r0; row < r1; ++row) {
     float s[3] = {0.0f, 0.0f, 0.0f};
     for (int64_t p = 0; p < pieces; ++p) {
@@ -443,15 +516,12 @@ __global__ __launch_bounds__(kWideThreads) void wide_kernel(NormGradArgs a, int6
     const float mean = a.mean[row], rstd = a.rstd[row];
     const float delta = s[0] * over_width, g_avg = s[1] * over_width;
     const float along = (s[2] - delta * s[1]) * over_width * rstd;
-    const T *xs = static_cast<const T *>(a.x) + row * a.ld;
-    const T *ds = static_cast<const T *>(a.dout) + row * a.dout_ld;
-    typename Vec<T>::type x[kVecs], d[kVecs];
 #pragma unroll
     for (int k = 0; k < kVecs; ++k) {
-      const Part at(c0 + k * kWideThreads * kLen, width);
-      x[k] = at.load(xs, width);
-      d[k] = at.load(ds, width);
+      x[k] = x1[k];
+      d[k] = d1[k];
     }
+    if (row + 1 < r1) load(row + 1);
 #pragma unroll
     for (int k = 0; k < kVecs; ++k) {
       float y[kLen];
@@ -485,15 +555,7 @@ __global__ __launch_bounds__(kWideThreads) void wide_kernel(NormGradArgs a, int6
 // ---- the parameters' sums ------------------------------------------------------------
 
 constexpr int kJoinColumns = 64, kJoinSlices = 16;
-
-__device__ __forceinline__ void store_as(int dtype, void *p, int64_t i, float v) {
-  if (dtype == ML2_F32)
-    static_cast<float *>(p)[i] = v;
-  else if (dtype == ML2_BF16)
-    static_cast<__bf16 *>(p)[i] = narrow<__bf16>(v);
-  else
-    static_cast<_Float16 *>(p)[i] = narrow<_Float16>(v);
-}
+constexpr int kJoinAhead = 16;  // parts in flight
 
 // blockIdx.y = 0: weight, 1: bias.  Slices of threads add the parts one after the
 // other, then the slices.
@@ -509,8 +571,14 @@ __global__ __launch_bounds__(kJoinColumns *kJoinSlices) void join_kernel(NormGra
   const int p1 = min(parts, (slice + 1) * each);
   float v = 0.0f;
   if (c < a.width) {
-#pragma unroll 8
-    for (int p = slice * each; p < p1; ++p) v += part[((int64_t)p * 2 + blockIdx.y) * a.width + c];
+    for (int p = slice * each; p < p1; p += kJoinAhead) {
+      float x[kJoinAhead];
+#pragma unroll
+      for (int i = 0; i < kJoinAhead; ++i)
+        x[i] = p + i < p1 ? part[((int64_t)(p + i) * 2 + blockIdx.y) * a.width + c] : 0.0f;
+#pragma unroll
+      for (int i = 0; i < kJoinAhead; ++i) v += x[i];
+    }
   }
   lds[slice][lane] = v;
   __syncthreads();
@@ -571,7 +639,9 @@ GradShape grad_shape(int64_t rows, int64_t width) {
     g.threads = kMaxBlock / g.lanes * g.lanes;
   }
   g.per = g.threads / g.lanes;
-  g.blocks = (int)std::min<int64_t>((rows + g.per - 1) / g.per, kGradBlocks);
+  const int64_t turns = (rows + g.per - 1) / g.per;
+  g.direct = turns <= kDirectTurns;
+  g.blocks = g.direct ? 1 : (int)std::min<int64_t>(turns, kGradBlocks);
   return g;
 }
 
@@ -595,9 +665,11 @@ hipError_t launch_grad(const NormGradArgs &a, void *ws, hipStream_t s) {
   const float over = 1.0f / (float)a.width;
   float *part = static_cast<float *>(ws);
   int parts = 0;
+  bool done = false;
   if (a.rows > 0 && a.width <= kGradWidth) {
     const GradShape g = grad_shape(a.rows, a.width);
     parts = g.blocks;
+    done = g.direct;
     if (a.width < Vec<T>::kLen)
       grad_kernel<T, 8, true><<<g.blocks, g.threads, 0, s>>>(a, g, over, sums ? part : nullptr);
     else if (grad_columns(a.width) == 8)
@@ -618,7 +690,7 @@ hipError_t launch_grad(const NormGradArgs &a, void *ws, hipStream_t s) {
     wide_kernel<T><<<grid, kWideThreads, 0, s>>>(a, pieces, chunk, over, stat,
                                                  sums ? part : nullptr);
   }
-  if (sums) {
+  if (sums && !done) {
     const dim3 grid((uint32_t)((a.width + kJoinColumns - 1) / kJoinColumns), 2);
     join_kernel<<<grid, kJoinColumns * kJoinSlices, 0, s>>>(a, part, parts);
   }

@@ -844,10 +844,19 @@ class LayerNorm:
         self.out = torch.empty(rows, width, dtype=dtype, device=device)
         self.mean = torch.empty(rows, dtype=torch.float32, device=device)
         self.rstd = torch.empty(rows, dtype=torch.float32, device=device)
+        self.shape, self.dtype, self.code = (rows, width), dtype, _dtype(dtype)
+        self.buffers = (self.out.data_ptr(), width, self.mean.data_ptr(), self.rstd.data_ptr())
 
     def run(self, x, weight=None, bias=None, eps: float = 1e-5, stream=None):
         """(out, mean, rstd): this object's own buffers."""
-        ml2_layer_norm(x, weight, bias, self.out, self.mean, self.rstd, eps, stream)
+        xp, rows, width, ld = _matrix(x, "x")
+        if (rows, width) != self.shape or x.dtype is not self.dtype:
+            raise ValueError("x must have the rows, width and type that this object was made for")
+        _same_type(weight, bias, "weight and bias")
+        wp, code = _param(weight, "weight", self.dtype, width)
+        bp, bcode = _param(bias, "bias", self.dtype, width)
+        _check(lib().ml2_layer_norm(self.code, xp, rows, width, ld, bcode if wp is None else code,
+                                    wp, bp, eps, *self.buffers, _stream(stream)))
         return self.out, self.mean, self.rstd
 
 
@@ -864,11 +873,24 @@ class LayerNormGrad:
         self.dweight = torch.empty(width, dtype=grad_dtype, device=device)
         self.dbias = torch.empty(width, dtype=grad_dtype, device=device) if bias else None
         self.ws = _workspace(ml2_layer_norm_grad_workspace_bytes(rows, width), device)
+        self.shape, self.dtype, self.code = (rows, width), dtype, _dtype(dtype)
+        self.buffers = (self.dx.data_ptr(), width, _dtype(grad_dtype), self.dweight.data_ptr(),
+                        _ptr(self.dbias), *_space(self.ws))
 
     def run(self, x, dout, weight, mean, rstd, stream=None):
         """(dx, dweight, dbias): this object's own buffers."""
-        ml2_layer_norm_grad(x, dout, weight, mean, rstd, self.ws, self.dx, self.dweight,
-                            self.dbias, stream)
+        xp, rows, width, ld = _matrix(x, "x")
+        dp, drows, dwidth, dout_ld = _matrix(dout, "dout")
+        if (rows, width) != self.shape or (drows, dwidth) != self.shape or (
+                x.dtype is not self.dtype or dout.dtype is not self.dtype):
+            raise ValueError("x and dout must have the rows, width and type that this object was "
+                             "made for")
+        wp, code = _param(weight, "weight", self.dtype, width)
+        f32 = _t().f32
+        _check(lib().ml2_layer_norm_grad(
+            self.code, xp, rows, width, ld, dp, dout_ld, code, wp,
+            _flat(mean, "mean", f32, (rows,)), _flat(rstd, "rstd", f32, (rows,)), *self.buffers,
+            _stream(stream)))
         return self.dx, self.dweight, self.dbias
 
 
