@@ -153,7 +153,7 @@ __global__ __launch_bounds__(WAVE ? kWaveBlock : kMaxBlock,
   const int lane = WAVE ? threadIdx.x & (lanes - 1) : threadIdx.x;
   const int64_t per = WAVE ? kWaveBlock >> log_g : 1;
   const int64_t group = WAVE ? threadIdx.x >> log_g : 0;
-  float w[kKeep ? E : 4], b[kKeep ? E : 4];
+  float w[kKeep ? E : kLen], b[kKeep ? E : kLen];
   if (kKeep) {
 #pragma unroll
     for (int k = 0; k < kVecs; ++k) {
@@ -232,17 +232,17 @@ __global__ __launch_bounds__(WAVE ? kWaveBlock : kMaxBlock,
 #pragma unroll
       for (int j = 0; j < kLen; j += 4) {
         if (!kKeep) {
-          at.param4(a.weight, a.param_f32, 1.0f, width, j, w);
-          at.param4(a.bias, a.param_f32, 0.0f, width, j, b);
+          at.param4(a.weight, a.param_f32, 1.0f, width, j, w + j);
+          at.param4(a.bias, a.param_f32, 0.0f, width, j, b + j);
         }
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          const int p = kKeep ? k * kLen + j + i : i;
+          const int p = kKeep ? k * kLen + j + i : j + i;
           y[j + i] = fmaf(((float)x[k][j + i] - m0 - delta) * rstd, w[p], b[p]);
         }
-        if (!kKeep) __builtin_amdgcn_sched_barrier(0);  // few parameters at a time
       }
       at.store(dst, width, y);
+      if (!kKeep) __builtin_amdgcn_sched_barrier(0);  // one vector's parameters at a time
     }
   }
 }
@@ -269,6 +269,17 @@ struct GradShape {
   bool direct;        // one workgroup: it writes the parameters' sums itself
 };
 
+// The sum over a wave's groups of 2^log_g lanes, in the lanes of the first.
+__device__ __forceinline__ float fold_groups(float v, int log_g) {
+  const auto add = [](float p, float r) { return p + r; };
+  if (log_g <= 3) v += lane_swap<0x128>(v);  // row_ror 8
+  if (log_g <= 2) v += lane_swap<0x124>(v);  // row_ror 4
+  if (log_g <= 1) v += lane_swap<0x122>(v);  // row_ror 2
+  if (log_g <= 0) v += lane_swap<0x121>(v);  // row_ror 1
+  if (log_g <= 4) v = join_rows(v, add);
+  return join_halves(v, add);
+}
+
 // Sums of a lane group over all rows it takes go to part[block][0] (weight) and
 // [1] (bias), float32 [width] each.
 template <typename T, int E, bool SHORT>
@@ -276,7 +287,7 @@ __global__ __launch_bounds__(kMaxBlock) void grad_kernel(NormGradArgs a, GradSha
                                                          float over_width, float *part) {
   constexpr int kLen = Vec<T>::kLen, kVecs = E / kLen;
   typedef Piece<T, SHORT> Part;
-  __shared__ float lds[kMaxBlock * E];
+  __shared__ float lds[2][kMaxBlock * E];  // weight and bias
   float (*sums)[kMaxBlock / 64][3] = reinterpret_cast<float (*)[kMaxBlock / 64][3]>(lds);
   const int lanes = g.lanes, group = (int)threadIdx.x / lanes, width = (int)a.width;
   const int lane = (int)threadIdx.x - group * lanes;
@@ -370,62 +381,53 @@ __global__ __launch_bounds__(kMaxBlock) void grad_kernel(NormGradArgs a, GradSha
   if (!part) return;
   // The groups of a wave, then the waves: lane i of a wave holds the columns of
   // lane i % lanes.
-  if (!wide) {
+  if (!wide && g.log_g < 6) {
 #pragma unroll
     for (int i = 0; i < E; ++i) {
-      float v[2] = {dw[i], db[i]};
-#pragma unroll
-      for (int q = 0; q < 2; ++q) {
-        if (g.log_g <= 3) v[q] += lane_swap<0x128>(v[q]);  // row_ror 8
-        if (g.log_g <= 2) v[q] += lane_swap<0x124>(v[q]);  // row_ror 4
-        if (g.log_g <= 1) v[q] += lane_swap<0x122>(v[q]);  // row_ror 2
-        if (g.log_g <= 0) v[q] += lane_swap<0x121>(v[q]);  // row_ror 1
-        const auto add = [](float p, float r) { return p + r; };
-        if (g.log_g <= 4) v[q] = join_rows(v[q], add);
-        if (g.log_g <= 5) v[q] = join_halves(v[q], add);
-      }
-      dw[i] = v[0];
-      db[i] = v[1];
+      dw[i] = fold_groups(dw[i], g.log_g);
+      db[i] = fold_groups(db[i], g.log_g);
     }
   }
   const int parts = wide ? g.per : (int)blockDim.x >> 6;
   const int own = wide ? group : (int)threadIdx.x >> 6;
-  const bool has = wide || (int)(threadIdx.x & 63) < lanes;
   typedef float F4 __attribute__((ext_vector_type(4), aligned(4)));
-  float *to = part + (int64_t)blockIdx.x * 2 * width;
+  __syncthreads();
+  if (wide || (int)(threadIdx.x & 63) < lanes) {
 #pragma unroll
-  for (int q = 0; q < 2; ++q) {
-    __syncthreads();
-    if (has) {
+    for (int k = 0; k < kVecs; ++k) {
+      const Part at((k * lanes + lane) * kLen, width);
+      float *row = lds[0] + own * width + at.col;  // at most lanes * E columns
+      if (at.whole()) {
 #pragma unroll
-      for (int k = 0; k < kVecs; ++k) {
-        const Part at((k * lanes + lane) * kLen, width);
-        float *row = lds + own * width + at.col;  // at most lanes * E columns
-        if (at.whole()) {
+        for (int j = 0; j < kLen; j += 4) {
+          const int i = k * kLen + j;
+          *reinterpret_cast<F4 *>(row + j) = F4{dw[i], dw[i + 1], dw[i + 2], dw[i + 3]};
+          *reinterpret_cast<F4 *>(row + kMaxBlock * E + j) =
+              F4{db[i], db[i + 1], db[i + 2], db[i + 3]};
+        }
+      } else {
 #pragma unroll
-          for (int j = 0; j < kLen; j += 4) {
-            const int i = k * kLen + j;
-            *reinterpret_cast<F4 *>(row + j) = q ? F4{db[i], db[i + 1], db[i + 2], db[i + 3]}
-                                                 : F4{dw[i], dw[i + 1], dw[i + 2], dw[i + 3]};
+        for (int j = 0; j < kLen; ++j) {
+          if (at.has(j, width)) {
+            row[j] = dw[k * kLen + j];
+            row[kMaxBlock * E + j] = db[k * kLen + j];
           }
-        } else {
-#pragma unroll
-          for (int j = 0; j < kLen; ++j)
-            if (at.has(j, width)) row[j] = q ? db[k * kLen + j] : dw[k * kLen + j];
         }
       }
     }
-    __syncthreads();
-    void *out = q ? a.dbias : a.dweight;
-    for (int c = threadIdx.x; c < width; c += blockDim.x) {
-      float v = lds[c];
+  }
+  __syncthreads();
+  float *to = part + (int64_t)blockIdx.x * 2 * width;
+  for (int i = threadIdx.x; i < 2 * width; i += blockDim.x) {
+    const int q = i >= width, c = q ? i - width : i;
+    float v = lds[q][c];
 #pragma unroll 8
-      for (int p = 1; p < parts; ++p) v += lds[p * width + c];
-      if (!g.direct)
-        to[q * width + c] = v;
-      else if (out)
-        store_as(a.grad_dtype, out, c, v);
-    }
+    for (int p = 1; p < parts; ++p) v += lds[q][p * width + c];
+    void *out = q ? a.dbias : a.dweight;
+    if (!g.direct)
+      to[i] = v;
+    else if (out)
+      store_as(a.grad_dtype, out, c, v);
   }
 }
 
@@ -494,8 +496,12 @@ __global__ __launch_bounds__(kWideThreads) void wide_kernel(NormGradArgs a, int6
 #pragma unroll
     for (int j = 0; j < kLen; ++j) dw[k][j] = db[k][j] = 0.0f;
   }
-  // The next row is loaded before this one's gradient is written.
+  // The next row is loaded before this one's gradient is written.  A lane takes one
+  // piece's sums of the row.
+  static_assert(ML2_MAX_WIDTH <= 16 * kStatVecs * kStatThreads * 4, "16 lanes hold the pieces");
   typename Vec<T>::type x[kVecs], d[kVecs], x1[kVecs], d1[kVecs];
+  float s1[3], mean1, rstd1;
+  const int lane = threadIdx.x & 15;
   const auto load = [&](int64_t row) {
     const T *xs = static_cast<const T *>(a.x) + row * a.ld;
     const T *ds = static_cast<const T *>(a.dout) + row * a.dout_ld;
@@ -505,15 +511,18 @@ __global__ __launch_bounds__(kWideThreads) void wide_kernel(NormGradArgs a, int6
       x1[k] = at.load(xs, width);
       d1[k] = at.load(ds, width);
     }
+#pragma unroll
+    for (int i = 0; i < 3; ++i)
+      s1[i] = lane < pieces ? stat[(row * pieces + lane) * 3 + i] : 0.0f;
+    mean1 = a.mean[row];
+    rstd1 = a.rstd[row];
   };
   load(r0);
   for (int64_t row = r0; row < r1; ++row) {
-    float s[3] = {0.0f, 0.0f, 0.0f};
-    for (int64_t p = 0; p < pieces; ++p) {
+    float s[3];
 #pragma unroll
-      for (int i = 0; i < 3; ++i) s[i] += stat[(row * pieces + p) * 3 + i];
-    }
-    const float mean = a.mean[row], rstd = a.rstd[row];
+    for (int i = 0; i < 3; ++i) s[i] = group_sum(s1[i], 4);
+    const float mean = mean1, rstd = rstd1;
     const float delta = s[0] * over_width, g_avg = s[1] * over_width;
     const float along = (s[2] - delta * s[1]) * over_width * rstd;
 #pragma unroll
