@@ -38,6 +38,11 @@ __device__ __forceinline__ A *at_column(T *row, int col) {
   return reinterpret_cast<A *>(reinterpret_cast<Byte *>(row) + (uint32_t)col * (uint32_t)sizeof(T));
 }
 
+// What is known of a call's weight and bias where its kernel is chosen: that both
+// are there, in float32 or in the rows' type.  Wide rows load them again for every
+// row, and loads behind a branch would wait for one another.
+enum Params { kAny, kFloat, kSame };
+
 template <typename T, bool SHORT>
 struct Piece {
   static constexpr int kLen = Vec<T>::kLen;
@@ -71,17 +76,18 @@ struct Piece {
     }
   }
   // weight or bias of columns j .. j + 3 of the vector, or `none` where there is none
+  template <int HOW = kAny>
   __device__ __forceinline__ void param4(const void *p, int f32, float none, int width, int j,
                                          float *x) const {
     typedef float F __attribute__((ext_vector_type(4), aligned(4)));
     typedef T H __attribute__((ext_vector_type(4), aligned(sizeof(T))));
-    if (!p || SHORT) {
+    if (HOW == kAny && (!p || SHORT)) {
 #pragma unroll
       for (int i = 0; i < 4; ++i)
         x[i] = !p || !has(j + i, width) ? none
                : f32                    ? static_cast<const float *>(p)[j + i]
                                         : (float)static_cast<const T *>(p)[j + i];
-    } else if (f32) {
+    } else if (HOW == kAny ? f32 : HOW == kFloat) {
       const F v = *at_column<const F>(static_cast<const float *>(p), col + j);
 #pragma unroll
       for (int i = 0; i < 4; ++i) x[i] = v[i];
@@ -142,7 +148,7 @@ __device__ __forceinline__ void block_sums(float (&v)[N], float (*lds)[N]) {
 // SIMD: a compute unit loads one row while it writes another).  WAVE:
 // 2^log_g lanes share a row, else the workgroup does.  Vector k of a lane lies at
 // column (k * lanes + lane) * kLen.
-template <typename T, int E, bool WAVE, bool SHORT>
+template <typename T, int E, bool WAVE, bool SHORT, Params HOW>
 __global__ __launch_bounds__(WAVE ? kWaveBlock : kMaxBlock,
                              E >= 32 && E * sizeof(T) <= 128 ? 8 : 1) void norm_kernel(
     NormArgs a, int log_g, float over_width) {
@@ -245,8 +251,8 @@ __global__ __launch_bounds__(WAVE ? kWaveBlock : kMaxBlock,
 #pragma unroll
       for (int j = 0; j < kLen; j += 4) {
         if (!kKeep) {
-          at.param4(a.weight, a.param_f32, 1.0f, width, j, w + j);
-          at.param4(a.bias, a.param_f32, 0.0f, width, j, b + j);
+          at.template param4<HOW>(a.weight, a.param_f32, 1.0f, width, j, w + j);
+          at.template param4<HOW>(a.bias, a.param_f32, 0.0f, width, j, b + j);
         }
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -255,7 +261,6 @@ __global__ __launch_bounds__(WAVE ? kWaveBlock : kMaxBlock,
         }
       }
       at.store(dst, width, y);
-      if (!kKeep) __builtin_amdgcn_sched_barrier(0);  // one vector's parameters at a time
     }
   }
 }
@@ -658,7 +663,8 @@ hipError_t launch_narrow(const NormArgs &a, int cu_count, hipStream_t s) {
   const int log_g = log2_up((a.width + E - 1) / E);
   const int64_t per = kWaveBlock >> log_g;
   const int64_t grid = std::min<int64_t>((a.rows + per - 1) / per, (int64_t)cu_count * 8);
-  norm_kernel<T, E, true, SHORT><<<(uint32_t)grid, kWaveBlock, 0, s>>>(a, log_g, 1.0f / (float)a.width);
+  norm_kernel<T, E, true, SHORT, kAny><<<(uint32_t)grid, kWaveBlock, 0, s>>>(
+      a, log_g, 1.0f / (float)a.width);
   return hipGetLastError();
 }
 
@@ -666,7 +672,16 @@ template <typename T, int E>
 hipError_t launch_wide(const NormArgs &a, int cu_count, hipStream_t s) {
   const int threads = (int)((a.width + 64 * E - 1) / (64 * E) * 64);
   const int64_t grid = std::min<int64_t>(a.rows, (int64_t)cu_count * (2048 / threads));
-  norm_kernel<T, E, false, false><<<(uint32_t)grid, threads, 0, s>>>(a, 0, 1.0f / (float)a.width);
+  const float over = 1.0f / (float)a.width;
+  constexpr bool kSplit = E > 16;
+  if (kSplit && a.weight && a.bias && a.param_f32)
+    norm_kernel<T, E, false, false, kSplit ? kFloat : kAny>
+        <<<(uint32_t)grid, threads, 0, s>>>(a, 0, over);
+  else if (kSplit && a.weight && a.bias)
+    norm_kernel<T, E, false, false, kSplit ? kSame : kAny>
+        <<<(uint32_t)grid, threads, 0, s>>>(a, 0, over);
+  else
+    norm_kernel<T, E, false, false, kAny><<<(uint32_t)grid, threads, 0, s>>>(a, 0, over);
   return hipGetLastError();
 }
 
