@@ -115,12 +115,27 @@ __global__ __launch_bounds__(1024) void finish_kernel(const double *part, int64_
   if (threadIdx.x == 0) finish(o, v);
 }
 
-// Few elements in all: one workgroup, one launch.
+// Few elements in all: one workgroup, one launch.  Its waves take chunks of all
+// tensors in turn (t.first: chunks).
 template <typename T>
-__global__ __launch_bounds__(1024) void norm_one_kernel(NormTable t, NormOut o) {
+__global__ __launch_bounds__(1024) void norm_one_kernel(NormTable t, uint32_t chunks, NormOut o) {
+  constexpr int kLen = Vec<T>::kLen;
   __shared__ double lds[16];
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
   double v = 0.0;
-  for (int i = 0; i < t.count; ++i) v += squares(static_cast<const T *>(t.grad[i]), 0, t.n[i]);
+  for (uint32_t c = wave; c < chunks; c += 16) {
+    const int i = find_tensor(t.first, t.count, c);
+    const int64_t at = (int64_t)(c - t.first[i]) * t.chunk + lane * kLen;
+    float x[kNormVecs][kLen];
+#pragma unroll
+    for (int k = 0; k < kNormVecs; ++k)
+      load_floats(static_cast<const T *>(t.grad[i]), at + k * 64 * kLen, t.n[i], x[k]);
+#pragma unroll
+    for (int k = 0; k < kNormVecs; ++k) {
+#pragma unroll
+      for (int j = 0; j < kLen; ++j) v = fma((double)x[k][j], (double)x[k][j], v);
+    }
+  }
   v = block_sum(v, lds);
   if (threadIdx.x == 0) finish(o, v);
 }
@@ -152,7 +167,8 @@ hipError_t launch_norm(const void *const *grads, const int64_t *sizes, int32_t c
   t.chunk = norm_chunk(sizes, count);
   t.part = part;
   t.count = 0;
-  const bool one = total <= kNormOne && used <= 16;
+  const bool one = total <= kNormOne && used <= kNormTensors;
+  if (one) t.chunk = 64 * kNormVecs * Vec<T>::kLen;
   uint32_t blocks = 0;
   int64_t parts = 0;
   for (int32_t i = 0; i < count; ++i) {
@@ -170,7 +186,7 @@ hipError_t launch_norm(const void *const *grads, const int64_t *sizes, int32_t c
     }
   }
   if (one) {
-    norm_one_kernel<T><<<1, 1024, 0, s>>>(t, o);
+    norm_one_kernel<T><<<1, 1024, 0, s>>>(t, blocks, o);
     return hipGetLastError();
   }
   if (t.count > 0) square_kernel<T><<<blocks, kThreads, 0, s>>>(t);
@@ -251,78 +267,111 @@ __device__ __forceinline__ float moved(const Step &s, float decay, float p, floa
   return p - fmaf(decay, p, s.rate * m / fmaf(r, s.root, s.eps));
 }
 
-// LEN elements from i on of an array of n, and back.
+// LEN elements of a tile from place `at` on, and back.  A tile's array is the same
+// in all lanes and a place the same in all tiles, so an address costs nothing; `left`
+// elements of the tile are the tensor's, all of them where WHOLE.
 template <typename T, int LEN>
 struct Some {
   typedef T type __attribute__((ext_vector_type(LEN), aligned(sizeof(T))));
 };
 
-template <typename T, int LEN>
-__device__ __forceinline__ void load_some(const void *a, int64_t i, int64_t n, float *x) {
-  const T *p = static_cast<const T *>(a) + i;
-  if (i + LEN <= n) {
-    const typename Some<T, LEN>::type v = *reinterpret_cast<const typename Some<T, LEN>::type *>(p);
+template <typename T, int LEN, bool WHOLE>
+__device__ __forceinline__ void load_some(const T *tile, uint32_t at, uint32_t left, float *x) {
+  if (WHOLE || at + LEN <= left) {
+    const auto v = *reinterpret_cast<const typename Some<T, LEN>::type *>(tile + at);
 #pragma unroll
     for (int j = 0; j < LEN; ++j) x[j] = (float)v[j];
   } else {
 #pragma unroll
-    for (int j = 0; j < LEN; ++j) x[j] = i + j < n ? (float)p[j] : 0.0f;
+    for (int j = 0; j < LEN; ++j) x[j] = at + j < left ? (float)tile[at + j] : 0.0f;
   }
 }
 
-template <typename T, int LEN>
-__device__ __forceinline__ void store_some(void *a, int64_t i, int64_t n, const float *x) {
-  T *p = static_cast<T *>(a) + i;
-  if (i + LEN <= n) {
+template <typename T, int LEN, bool WHOLE>
+__device__ __forceinline__ void store_some(T *tile, uint32_t at, uint32_t left, const float *x) {
+  if (WHOLE || at + LEN <= left) {
     typename Some<T, LEN>::type v;
 #pragma unroll
     for (int j = 0; j < LEN; ++j) v[j] = narrow<T>(x[j]);
-    *reinterpret_cast<typename Some<T, LEN>::type *>(p) = v;
+    *reinterpret_cast<typename Some<T, LEN>::type *>(tile + at) = v;
   } else {
 #pragma unroll
     for (int j = 0; j < LEN; ++j)
-      if (i + j < n) p[j] = narrow<T>(x[j]);
+      if (at + j < left) tile[at + j] = narrow<T>(x[j]);
+  }
+}
+
+// The arrays of a tensor from element `first` on.
+template <typename P, typename G, typename S>
+struct Arrays {
+  const P *param;
+  const G *grad;
+  const S *m, *v;
+  P *param_out;
+  S *m_out, *v_out;
+  G *copy;  // or null
+  __device__ __forceinline__ Arrays(const StepTable &t, int at, int64_t first)
+      : param(static_cast<const P *>(t.param[at]) + first),
+        grad(static_cast<const G *>(t.grad[at]) + first),
+        m(static_cast<const S *>(t.m[at]) + first),
+        v(static_cast<const S *>(t.v[at]) + first),
+        param_out(static_cast<P *>(t.param_out[at]) + first),
+        m_out(static_cast<S *>(t.m_out[at]) + first),
+        v_out(static_cast<S *>(t.v_out[at]) + first),
+        copy(t.copy[at] ? static_cast<G *>(t.copy[at]) + first : nullptr) {}
+};
+
+struct Rates {
+  float b1, b2, a1, a2;  // a: 1 - b
+};
+
+template <typename P, typename G, bool WHOLE>
+__device__ __forceinline__ void step_tile(const Arrays<P, G, float> &t, uint32_t left,
+                                          const Step &s, const Rates &q, float decay) {
+  constexpr int kLen = 4, kVecs = kTile / kThreads / kLen;
+  float p[kVecs][kLen], g[kVecs][kLen], m[kVecs][kLen], v[kVecs][kLen];
+#pragma unroll
+  for (int k = 0; k < kVecs; ++k) {
+    const uint32_t at = threadIdx.x * kLen + k * kThreads * kLen;
+    load_some<P, kLen, WHOLE>(t.param, at, left, p[k]);
+    load_some<G, kLen, WHOLE>(t.grad, at, left, g[k]);
+    load_some<float, kLen, WHOLE>(t.m, at, left, m[k]);
+    load_some<float, kLen, WHOLE>(t.v, at, left, v[k]);
+  }
+#pragma unroll
+  for (int k = 0; k < kVecs; ++k) {
+    const uint32_t at = threadIdx.x * kLen + k * kThreads * kLen;
+    if (s.taken) {
+#pragma unroll
+      for (int j = 0; j < kLen; ++j) {
+        const float gj = g[k][j] * s.f;
+        m[k][j] = fmaf(q.b1, m[k][j], q.a1 * gj);
+        v[k][j] = fmaf(q.b2, v[k][j], q.a2 * gj * gj);
+        p[k][j] = moved(s, decay, p[k][j], m[k][j], sqrtf(v[k][j]));
+      }
+    }
+    store_some<P, kLen, WHOLE>(t.param_out, at, left, p[k]);
+    store_some<float, kLen, WHOLE>(t.m_out, at, left, m[k]);
+    store_some<float, kLen, WHOLE>(t.v_out, at, left, v[k]);
+    if (t.copy) store_some<G, kLen, WHOLE>(t.copy, at, left, p[k]);
   }
 }
 
 template <typename P, typename G>
 __global__ __launch_bounds__(kThreads) void step_kernel(StepTable t, StepShared o) {
-  constexpr int kLen = 4, kVecs = kTile / kThreads / kLen;
   const int at = find_tensor(t.first, o.count, blockIdx.x);
   const int64_t n = t.n[at];
   const Step s = read_step(o);
   const float decay = s.lr * t.decay[at];
-  const float b1 = (float)o.b1, b2 = (float)o.b2, a1 = (float)(1.0 - o.b1),
-              a2 = (float)(1.0 - o.b2);
+  const Rates q = {(float)o.b1, (float)o.b2, (float)(1.0 - o.b1), (float)(1.0 - o.b2)};
   const int64_t tile0 = (int64_t)(blockIdx.x - t.first[at]) * o.tiles;
   for (int64_t tile = tile0; tile < tile0 + o.tiles && tile * kTile < n; ++tile) {
-    const int64_t i0 = tile * kTile + (int64_t)threadIdx.x * kLen;
-    float p[kVecs][kLen], g[kVecs][kLen], m[kVecs][kLen], v[kVecs][kLen];
-#pragma unroll
-    for (int k = 0; k < kVecs; ++k) {
-      const int64_t i = i0 + k * kThreads * kLen;
-      load_some<P, kLen>(t.param[at], i, n, p[k]);
-      load_some<G, kLen>(t.grad[at], i, n, g[k]);
-      load_some<float, kLen>(t.m[at], i, n, m[k]);
-      load_some<float, kLen>(t.v[at], i, n, v[k]);
-    }
-#pragma unroll
-    for (int k = 0; k < kVecs; ++k) {
-      const int64_t i = i0 + k * kThreads * kLen;
-      if (s.taken) {
-#pragma unroll
-        for (int j = 0; j < kLen; ++j) {
-          const float gj = g[k][j] * s.f;
-          m[k][j] = fmaf(b1, m[k][j], a1 * gj);
-          v[k][j] = fmaf(b2, v[k][j], a2 * gj * gj);
-          p[k][j] = moved(s, decay, p[k][j], m[k][j], sqrtf(v[k][j]));
-        }
-      }
-      store_some<P, kLen>(t.param_out[at], i, n, p[k]);
-      store_some<float, kLen>(t.m_out[at], i, n, m[k]);
-      store_some<float, kLen>(t.v_out[at], i, n, v[k]);
-      if (t.copy[at]) store_some<G, kLen>(t.copy[at], i, n, p[k]);
-    }
+    const Arrays<P, G, float> a(t, at, tile * kTile);
+    const int64_t left = n - tile * kTile;
+    if (left >= kTile)
+      step_tile<P, G, true>(a, kTile, s, q, decay);
+    else
+      step_tile<P, G, false>(a, (uint32_t)left, s, q, decay);
   }
 }
 
@@ -346,23 +395,25 @@ constexpr float kTop = 448.0f;
 
 typedef uint32_t Codes __attribute__((ext_vector_type(2), aligned(4)));
 
-// 8 codes from i on; 0 behind n.
-__device__ __forceinline__ Codes load_codes(const uint8_t *p, int64_t i, int64_t n) {
-  if (i + kLane <= n) return *reinterpret_cast<const Codes *>(p + i);
+// 8 codes of a tile from place `at` on; 0 behind the tensor.
+template <bool WHOLE>
+__device__ __forceinline__ Codes load_codes(const uint8_t *tile, uint32_t at, uint32_t left) {
+  if (WHOLE || at + kLane <= left) return *reinterpret_cast<const Codes *>(tile + at);
   Codes c = {0, 0};
 #pragma unroll
   for (int j = 0; j < kLane; ++j)
-    if (i + j < n) c[j >> 2] |= (uint32_t)p[i + j] << (8 * (j & 3));
+    if (at + j < left) c[j >> 2] |= (uint32_t)tile[at + j] << (8 * (j & 3));
   return c;
 }
 
-__device__ __forceinline__ void store_codes(uint8_t *p, int64_t i, int64_t n, Codes c) {
-  if (i + kLane <= n) {
-    *reinterpret_cast<Codes *>(p + i) = c;
+template <bool WHOLE>
+__device__ __forceinline__ void store_codes(uint8_t *tile, uint32_t at, uint32_t left, Codes c) {
+  if (WHOLE || at + kLane <= left) {
+    *reinterpret_cast<Codes *>(tile + at) = c;
   } else {
 #pragma unroll
     for (int j = 0; j < kLane; ++j)
-      if (i + j < n) p[i + j] = (uint8_t)(c[j >> 2] >> (8 * (j & 3)));
+      if (at + j < left) tile[at + j] = (uint8_t)(c[j >> 2] >> (8 * (j & 3)));
   }
 }
 
@@ -389,13 +440,19 @@ __device__ __forceinline__ Two two(double x) {
   return {high, (float)(x - (double)high)};
 }
 
+__device__ __forceinline__ Two operator*(Two a, float b) {
+  const float high = a.high * b;
+  return {high, fmaf(a.high, b, -high) + a.low * b};
+}
+
 __device__ __forceinline__ float times(float a, Two b, float add) {
   return fmaf(a, b.high, fmaf(a, b.low, add));
 }
 
 // A block's scale, and what brings its elements to units of it; `most`: the bits
 // of the lane's largest size, ordered as the sizes are, NaN last.  A NaN or an
-// infinity makes the scale NaN.
+// infinity makes the scale NaN.  (The reciprocal is taken of 2^-20 as much: that of
+// the largest numbers would be flushed.  What it is off by is found exactly.)
 struct Scale {
   float scale;
   Two over;
@@ -405,11 +462,12 @@ __device__ __forceinline__ Scale block_scale(uint32_t most) {
   const float top = group_fold(__uint_as_float(most), 5, [](float a, float b) {
     return __uint_as_float(max(__float_as_uint(a), __float_as_uint(b)));
   });
-  if (!(top < __builtin_inff())) return {__builtin_nanf(""), {0.0f, 0.0f}};
-  const float scale = top / kTop;
-  if (!(scale > 0x1p-100f)) return {0x1p-100f, {0x1p100f, 0.0f}};
-  const float over = kTop / top;
-  return {scale, {over, fmaf(-over, top, kTop) / top}};
+  const Two scale = Two{1.0f / kTop, (float)(1.0 / kTop - (double)(1.0f / kTop))} * top;
+  const float r = __builtin_amdgcn_rcpf(top * 0x1p-20f) * 0x1p-20f, over = kTop * r;
+  Scale s = {scale.high + scale.low, {over, fmaf(-over, top, kTop) * r}};
+  if (!(s.scale > 0x1p-100f)) s = {0x1p-100f, {0x1p100f, 0.0f}};
+  if (!(top < __builtin_inff())) s = {__builtin_nanf(""), {0.0f, 0.0f}};
+  return s;
 }
 
 // The code of a size in units of its scale; random: 20 bits, least: the smallest
@@ -419,95 +477,115 @@ __device__ __forceinline__ uint32_t encode(float size, uint32_t random, uint32_t
   return min(max(code, least), 0x7Eu);
 }
 
+// Scales of a tile's blocks, of m and of r: read and written.
+struct Scales {
+  const float *m, *r;
+  float *m_out, *r_out;
+};
+
+// What a workgroup needs of the step beside that.
+struct Rates8 {
+  Two b1, b2, a1;  // a1: (1 - b1) factor
+  float a2;        // (1 - b2) factor^2
+};
+
+template <typename P, typename G, bool WHOLE>
+__device__ __forceinline__ void step8_tile(const Arrays<P, G, uint8_t> &t, const Scales &c,
+                                           uint32_t left, const Step &s, const Rates8 &q,
+                                           float decay, uint32_t key) {
+  const uint32_t at = threadIdx.x * kLane, block = at / ML2_STATE_BLOCK;
+  const bool in = WHOLE || block * ML2_STATE_BLOCK < left;  // the half wave, or none of it
+  float p[kLane], g[kLane], m[kLane], r[kLane], ms = 0.0f, rs = 0.0f;
+  load_some<P, kLane, WHOLE>(t.param, at, left, p);
+  load_some<G, kLane, WHOLE>(t.grad, at, left, g);
+  const Codes mc = load_codes<WHOLE>(t.m, at, left), rc = load_codes<WHOLE>(t.v, at, left);
+  if (in) {
+    ms = c.m[block];
+    rs = c.r[block];
+  }
+  if (!s.taken) {
+    store_some<P, kLane, WHOLE>(t.param_out, at, left, p);
+    if (t.copy) store_some<G, kLane, WHOLE>(t.copy, at, left, p);
+    store_codes<WHOLE>(t.m_out, at, left, mc);
+    store_codes<WHOLE>(t.v_out, at, left, rc);
+    if (in && (threadIdx.x & 31) == 0) {
+      c.m_out[block] = ms;
+      c.r_out[block] = rs;
+    }
+    return;
+  }
+  decode(mc, m);
+  decode(rc, r);
+  const Two old_m = q.b1 * ms, old_v = q.b2 * rs * rs;
+  float rest[kLane];  // what the root of v has beyond r
+#pragma unroll
+  for (int j = 0; j < kLane; ++j) {
+    m[j] = fmaf(m[j], old_m.high, fmaf(g[j], q.a1.high, fmaf(m[j], old_m.low, g[j] * q.a1.low)));
+    const float square = r[j] * r[j];  // of 4 bits: exact
+    const float v = fmaf(square, old_v.high, fmaf(g[j] * g[j], q.a2, square * old_v.low));
+    // y: 1 / sqrt(v); v below float32's normal numbers counts as ever less, and an
+    // infinite one gives an infinite root.
+    const float y = __builtin_amdgcn_rsqf(__builtin_amdgcn_fmed3f(v, 0x1p-126f, 0x1.fffffep127f));
+    r[j] = v * y;
+    rest[j] = fmaf(-r[j], r[j], v) * (0.5f * y);
+    p[j] -= fmaf(decay, p[j],
+                 s.rate * m[j] * __builtin_amdgcn_rcpf(fmaf(r[j], s.root, s.eps)));
+    if (!WHOLE && at + j >= left) m[j] = r[j] = 0.0f;
+  }
+  store_some<P, kLane, WHOLE>(t.param_out, at, left, p);
+  if (t.copy) store_some<G, kLane, WHOLE>(t.copy, at, left, p);
+  uint32_t most_m = 0, most_r = 0;
+#pragma unroll
+  for (int j = 0; j < kLane; ++j) {
+    most_m = max(most_m, __float_as_uint(m[j]) & 0x7FFFFFFFu);
+    most_r = max(most_r, __float_as_uint(r[j]));
+  }
+  const Scale to_m = block_scale(most_m), to_r = block_scale(most_r);
+  Codes mo = {0, 0}, ro = {0, 0};
+#pragma unroll
+  for (int j = 0; j < kLane; ++j) {
+    uint32_t h = key + (at + (uint32_t)j) * kPhi;
+    h = (h ^ (h >> 15)) * kPlastic;
+    h ^= h >> 16;
+    const uint32_t a = encode(times(fabsf(m[j]), to_m.over, 0.0f), (h >> 12 & 0xFFFF0u) | 8u, 0);
+    const uint32_t b = encode(times(r[j], to_r.over, rest[j] * to_r.over.high),
+                              (h << 4 & 0xFFFF0u) | 8u, min(__float_as_uint(r[j]), 1u));
+    mo[j >> 2] |= (a | (__float_as_uint(m[j]) >> 24 & 0x80u)) << (8 * (j & 3));
+    ro[j >> 2] |= b << (8 * (j & 3));
+  }
+  store_codes<WHOLE>(t.m_out, at, left, mo);
+  store_codes<WHOLE>(t.v_out, at, left, ro);
+  if (in && (threadIdx.x & 31) == 0) {
+    c.m_out[block] = to_m.scale;
+    c.r_out[block] = to_r.scale;
+  }
+}
+
 template <typename P, typename G>
 __global__ __launch_bounds__(kThreads) void step8_kernel(StepTable t, StepShared o) {
   const int at = find_tensor(t.first, o.count, blockIdx.x);
   const int64_t n = t.n[at];
   const Step s = read_step(o);
   const float decay = s.lr * t.decay[at];
-  const Two a1 = two((1.0 - o.b1) * s.f);
-  const float a2 = (float)((1.0 - o.b2) * s.f * s.f);
+  const Rates8 q = {two(o.b1), two(o.b2), two((1.0 - o.b1) * s.f),
+                    (float)((1.0 - o.b2) * s.f * s.f)};
   const uint32_t key = fold_word(fold_word(o.key, s.step), (uint32_t)(o.place + at));
   const int64_t codes = (n + ML2_STATE_BLOCK - 1) / ML2_STATE_BLOCK * ML2_STATE_BLOCK;
-  const uint8_t *m0 = static_cast<const uint8_t *>(t.m[at]);
-  const uint8_t *r0 = static_cast<const uint8_t *>(t.v[at]);
-  uint8_t *m1 = static_cast<uint8_t *>(t.m_out[at]), *r1 = static_cast<uint8_t *>(t.v_out[at]);
   const int64_t tile0 = (int64_t)(blockIdx.x - t.first[at]) * o.tiles;
   for (int64_t tile = tile0; tile < tile0 + o.tiles && tile * kTile < n; ++tile) {
-    const int64_t i = tile * kTile + (int64_t)threadIdx.x * kLane;
-    const int64_t block = i / ML2_STATE_BLOCK;
-    const bool in = block * ML2_STATE_BLOCK < n;  // the whole half wave, or none of it
-    float p[kLane], g[kLane], m[kLane], r[kLane], ms = 0.0f, rs = 0.0f;
-    load_some<P, kLane>(t.param[at], i, n, p);
-    load_some<G, kLane>(t.grad[at], i, n, g);
-    const Codes mc = load_codes(m0, i, n), rc = load_codes(r0, i, n);
-    if (in) {
-      ms = reinterpret_cast<const float *>(m0 + codes)[block];
-      rs = reinterpret_cast<const float *>(r0 + codes)[block];
-    }
-    if (!s.taken) {
-      store_some<P, kLane>(t.param_out[at], i, n, p);
-      if (t.copy[at]) store_some<G, kLane>(t.copy[at], i, n, p);
-      store_codes(m1, i, n, mc);
-      store_codes(r1, i, n, rc);
-      if (in && (threadIdx.x & 31) == 0) {
-        reinterpret_cast<float *>(m1 + codes)[block] = ms;
-        reinterpret_cast<float *>(r1 + codes)[block] = rs;
-      }
-      continue;
-    }
-    decode(mc, m);
-    decode(rc, r);
-    const Two old_m = two(o.b1 * ms), old_v = two(o.b2 * rs * rs);
-    float rest[kLane];  // what the root of v has beyond r
-#pragma unroll
-    for (int j = 0; j < kLane; ++j) {
-      m[j] = fmaf(m[j], old_m.high,
-                  fmaf(g[j], a1.high, fmaf(m[j], old_m.low, g[j] * a1.low)));
-      const float square = r[j] * r[j];  // of 4 bits: exact
-      const float v = fmaf(square, old_v.high, fmaf(g[j] * g[j], a2, square * old_v.low));
-      // y: 1 / sqrt(v); v below float32's normal numbers counts as ever less, and
-      // an infinite one gives an infinite root.
-      const float y = __builtin_amdgcn_rsqf(__builtin_amdgcn_fmed3f(v, 0x1p-126f, 0x1.fffffep127f));
-      r[j] = v * y;
-      rest[j] = fmaf(-r[j], r[j], v) * (0.5f * y);
-      p[j] -= fmaf(decay, p[j],
-                   s.rate * m[j] * __builtin_amdgcn_rcpf(fmaf(r[j], s.root, s.eps)));
-    }
-    store_some<P, kLane>(t.param_out[at], i, n, p);
-    if (t.copy[at]) store_some<G, kLane>(t.copy[at], i, n, p);
-    if (i + kLane > n) {
-#pragma unroll
-      for (int j = 0; j < kLane; ++j)
-        if (i + j >= n) m[j] = r[j] = 0.0f;
-    }
-    uint32_t most_m = 0, most_r = 0;
-#pragma unroll
-    for (int j = 0; j < kLane; ++j) {
-      most_m = max(most_m, __float_as_uint(m[j]) & 0x7FFFFFFFu);
-      most_r = max(most_r, __float_as_uint(r[j]));
-    }
-    const Scale to_m = block_scale(most_m), to_r = block_scale(most_r);
-    const uint32_t high = (uint32_t)(i >> 32);
-    const uint32_t k = (high ? fold_word(key, high) : key) + (uint32_t)i * kPhi;
-    Codes mo = {0, 0}, ro = {0, 0};
-#pragma unroll
-    for (int j = 0; j < kLane; ++j) {
-      uint32_t h = k + (uint32_t)j * kPhi;
-      h = (h ^ (h >> 15)) * kPlastic;
-      h ^= h >> 16;
-      const uint32_t a = encode(times(fabsf(m[j]), to_m.over, 0.0f), (h >> 12 & 0xFFFF0u) | 8u, 0);
-      const uint32_t b = encode(times(r[j], to_r.over, rest[j] * to_r.over.high),
-                                (h << 4 & 0xFFFF0u) | 8u, min(__float_as_uint(r[j]), 1u));
-      mo[j >> 2] |= (a | (__float_as_uint(m[j]) >> 24 & 0x80u)) << (8 * (j & 3));
-      ro[j >> 2] |= b << (8 * (j & 3));
-    }
-    store_codes(m1, i, n, mo);
-    store_codes(r1, i, n, ro);
-    if (in && (threadIdx.x & 31) == 0) {
-      reinterpret_cast<float *>(m1 + codes)[block] = to_m.scale;
-      reinterpret_cast<float *>(r1 + codes)[block] = to_r.scale;
-    }
+    const int64_t first = tile * kTile, left = n - first;
+    const Arrays<P, G, uint8_t> a(t, at, first);
+    const auto scales = [&](void *state) {
+      return reinterpret_cast<float *>(static_cast<uint8_t *>(state) + codes) +
+             first / ML2_STATE_BLOCK;
+    };
+    const Scales c = {scales(t.m[at]), scales(t.v[at]), scales(t.m_out[at]), scales(t.v_out[at])};
+    const uint32_t high = (uint32_t)(first >> 32);
+    const uint32_t k = (high ? fold_word(key, high) : key) + (uint32_t)first * kPhi;
+    if (left >= kTile)
+      step8_tile<P, G, true>(a, c, kTile, s, q, decay, k);
+    else
+      step8_tile<P, G, false>(a, c, (uint32_t)left, s, q, decay, k);
   }
 }
 
