@@ -27,8 +27,7 @@ constexpr int kMaxBlock = 1024;
 // A vector of a row, kLen columns from c on.  The one that the row ends in is
 // loaded kLen columns before the end instead, so every load is a whole one; its
 // first columns, and all of a vector behind the row, are another vector's and count
-// for nothing (`skip` of them).  SHORT: rows of fewer than kLen columns, loaded one
-// by one.
+// for nothing (`skip` of them).
 //
 // Offsets are unsigned and in bytes, so that they are one register beside a row's
 // address, which all lanes share.
@@ -43,12 +42,17 @@ __device__ __forceinline__ A *at_column(T *row, int col) {
 // row, and loads behind a branch would wait for one another.
 enum Params { kAny, kFloat, kSame };
 
-template <typename T, bool SHORT>
+// How rows end: anywhere, before the first vector does (its columns are loaded one by
+// one), or with the last lane's last vector.
+enum Ends { kAnywhere, kShort, kWhole };
+
+template <typename T, Ends ENDS>
 struct Piece {
+  static constexpr bool SHORT = ENDS == kShort;
   static constexpr int kLen = Vec<T>::kLen;
   int col, skip;
   __device__ __forceinline__ Piece(int c, int width) {
-    col = SHORT ? 0 : min(c, width - kLen);
+    col = SHORT ? 0 : ENDS == kWhole ? c : min(c, width - kLen);
     skip = SHORT ? (c == 0 ? 0 : kLen) : c - col;
   }
   __device__ __forceinline__ bool whole() const { return !SHORT && skip == 0; }
@@ -126,8 +130,7 @@ __device__ __forceinline__ int anew(int v) {
 template <int N>
 __device__ __forceinline__ void block_sums(float (&v)[N], float (*lds)[N]) {
   const int wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
-#pragma unroll
-  for (int i = 0; i < N; ++i) v[i] = group_sum(v[i], 6);
+  group_sums(v, 6);
   if ((threadIdx.x & 63) == 0) {
 #pragma unroll
     for (int i = 0; i < N; ++i) lds[wave][i] = v[i];
@@ -148,13 +151,13 @@ __device__ __forceinline__ void block_sums(float (&v)[N], float (*lds)[N]) {
 // SIMD: a compute unit loads one row while it writes another).  WAVE:
 // 2^log_g lanes share a row, else the workgroup does.  Vector k of a lane lies at
 // column (k * lanes + lane) * kLen.
-template <typename T, int E, bool WAVE, bool SHORT, Params HOW>
+template <typename T, int E, bool WAVE, Ends ENDS, Params HOW>
 __global__ __launch_bounds__(WAVE ? kWaveBlock : kMaxBlock,
                              E >= 32 && E * sizeof(T) <= 128 ? 8 : 1) void norm_kernel(
     NormArgs a, int log_g, float over_width) {
   constexpr int kLen = Vec<T>::kLen, kVecs = E / kLen;
   constexpr bool kKeep = E <= 16;  // the parameters stay in registers
-  typedef Piece<T, SHORT> Part;
+  typedef Piece<T, ENDS> Part;
   __shared__ float first[kMaxBlock / 64][1], second[kMaxBlock / 64][2];
   const int lanes = WAVE ? 1 << log_g : (int)blockDim.x, width = (int)a.width;
   const int lane = WAVE ? threadIdx.x & (lanes - 1) : threadIdx.x;
@@ -201,7 +204,7 @@ __global__ __launch_bounds__(WAVE ? kWaveBlock : kMaxBlock,
       }
     }
     if (WAVE)
-      s[0] = group_sum(s[0], log_g);
+      group_sums(s, E > 8 ? 6 : log_g);  // more than 8 columns a lane: whole waves
     else
       block_sums(s, first);
     const float m0 = s[0] * over_width;
@@ -227,15 +230,14 @@ __global__ __launch_bounds__(WAVE ? kWaveBlock : kMaxBlock,
       }
     }
     if (WAVE) {
-      t[0] = group_sum(t[0], log_g);
-      t[1] = group_sum(t[1], log_g);
+      group_sums(t, E > 8 ? 6 : log_g);
     } else {
       block_sums(t, second);
     }
     const float delta = t[0] * over_width;
     const float raw = fmaf(t[1], over_width, -delta * delta);
     const float var = raw < 0.0f ? 0.0f : raw;  // a NaN stays one
-    const float rstd = 1.0f / sqrtf(var + a.eps);
+    const float rstd = 1.0f / sqrtf(var + a.eps), shift = -delta * rstd;
     if (row >= a.rows) continue;
     if (lane == 0) {
       if (a.mean) a.mean[row] = m0 + delta;
@@ -257,7 +259,7 @@ __global__ __launch_bounds__(WAVE ? kWaveBlock : kMaxBlock,
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           const int p = kKeep ? k * kLen + j + i : j + i;
-          y[j + i] = fmaf(((float)x[k][j + i] - m0 - delta) * rstd, w[p], b[p]);
+          y[j + i] = fmaf(fmaf((float)x[k][j + i] - m0, rstd, shift), w[p], b[p]);
         }
       }
       at.store(dst, width, y);
@@ -300,11 +302,11 @@ __device__ __forceinline__ float fold_groups(float v, int log_g) {
 
 // Sums of a lane group over all rows it takes go to part[block][0] (weight) and
 // [1] (bias), float32 [width] each.
-template <typename T, int E, bool SHORT>
+template <typename T, int E, Ends ENDS>
 __global__ __launch_bounds__(kMaxBlock) void grad_kernel(NormGradArgs a, GradShape g,
                                                          float over_width, float *part) {
   constexpr int kLen = Vec<T>::kLen, kVecs = E / kLen;
-  typedef Piece<T, SHORT> Part;
+  typedef Piece<T, ENDS> Part;
   // The row's sums and the weight, each lane's four by four, then the parts of the
   // gradients of weight and bias.
   __shared__ float lds[2][kMaxBlock * E];
@@ -361,33 +363,34 @@ __global__ __launch_bounds__(kMaxBlock) void grad_kernel(NormGradArgs a, GradSha
 #pragma unroll
     for (int k = 0; k < kVecs; ++k) {
       const Part at((k * lanes + lane) * kLen, anew(width));
+      float w[kLen];
 #pragma unroll
       for (int j = 0; j < kLen; j += 4) {
-        const F4 w = weight[(k * kLen + j) / 4 * lanes + lane];
-        if (at.whole()) {
+        const F4 v = weight[(k * kLen + j) / 4 * lanes + lane];
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const float xj = (float)x[k][j + i] - mean, gj = (float)d[k][j + i] * w[i];
-            s[0] += xj;
-            s[1] += gj;
-            s[2] = fmaf(gj, xj, s[2]);
-          }
-        } else if (at.any()) {
+        for (int i = 0; i < 4; ++i) w[j + i] = v[i];
+      }
+      if (at.whole()) {
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const bool has = at.has(j + i, width);
-            const float xj = has ? (float)x[k][j + i] - mean : 0.0f;
-            const float gj = has ? (float)d[k][j + i] * w[i] : 0.0f;
-            s[0] += xj;
-            s[1] += gj;
-            s[2] = fmaf(gj, xj, s[2]);
-          }
+        for (int j = 0; j < kLen; ++j) {
+          const float xj = (float)x[k][j] - mean, gj = (float)d[k][j] * w[j];
+          s[0] += xj;
+          s[1] += gj;
+          s[2] = fmaf(gj, xj, s[2]);
+        }
+      } else if (at.any()) {
+#pragma unroll
+        for (int j = 0; j < kLen; ++j) {
+          const bool has = at.has(j, width);
+          const float xj = has ? (float)x[k][j] - mean : 0.0f;
+          const float gj = has ? (float)d[k][j] * w[j] : 0.0f;
+          s[0] += xj;
+          s[1] += gj;
+          s[2] = fmaf(gj, xj, s[2]);
         }
       }
     }
-    const int log_g = wide ? 6 : g.log_g;
-#pragma unroll
-    for (int i = 0; i < 3; ++i) s[i] = group_sum(s[i], log_g);
+    group_sums(s, E > 8 || wide ? 6 : g.log_g);  // more than 8 columns a lane: whole waves
     if (wide) {
       // One barrier a row: the waves that still read the last row's sums have the
       // other half of the buffer.
@@ -407,6 +410,7 @@ __global__ __launch_bounds__(kMaxBlock) void grad_kernel(NormGradArgs a, GradSha
     }
     const float delta = s[0] * over_width, g_avg = s[1] * over_width;
     const float along = (s[2] - delta * s[1]) * over_width * rstd;  // avg(g xhat)
+    const float shift = -delta * rstd;
     const int64_t row = row0 + group;
     if (row < a.rows) {
       T *dst = a.dx ? static_cast<T *>(a.dx) + row * a.dx_ld : nullptr;
@@ -421,10 +425,10 @@ __global__ __launch_bounds__(kMaxBlock) void grad_kernel(NormGradArgs a, GradSha
         for (int j = 0; j < kLen; ++j) {
           const int i = k * kLen + j;
           const float w = weight[i / 4 * lanes + lane][j & 3];
-          const float dj = (float)d[k][j], xhat = ((float)x[k][j] - mean - delta) * rstd;
+          const float dj = (float)d[k][j], xhat = fmaf((float)x[k][j] - mean, rstd, shift);
           dw[i] = fmaf(dj, xhat, dw[i]);
           db[i] += dj;
-          y[j] = rstd * (fmaf(dj, w, -g_avg) - xhat * along);
+          y[j] = rstd * fmaf(-along, xhat, fmaf(dj, w, -g_avg));
         }
         if (dst) at.store(dst, width, y);
       }
@@ -433,7 +437,7 @@ __global__ __launch_bounds__(kMaxBlock) void grad_kernel(NormGradArgs a, GradSha
   if (!part) return;
   // The groups of a wave, then the waves: lane i of a wave holds the columns of
   // lane i % lanes.
-  if (!wide && g.log_g < 6) {
+  if (E == 8 && !wide && g.log_g < 6) {
 #pragma unroll
     for (int i = 0; i < E; ++i) {
       dw[i] = fold_groups(dw[i], g.log_g);
@@ -494,7 +498,7 @@ template <typename T>
 __global__ __launch_bounds__(kStatThreads) void stat_kernel(NormGradArgs a, int64_t pieces,
                                                             float *stat) {
   constexpr int kLen = Vec<T>::kLen;
-  typedef Piece<T, false> Part;
+  typedef Piece<T, kAnywhere> Part;
   __shared__ float lds[2][kStatThreads / 64][3];
   const int width = (int)a.width;
   int turn = 0;
@@ -537,7 +541,7 @@ __global__ __launch_bounds__(kWideThreads) void wide_kernel(NormGradArgs a, int6
                                                             int64_t chunk, float over_width,
                                                             const float *stat, float *part) {
   constexpr int kLen = Vec<T>::kLen, kVecs = kWideColumns / kLen;
-  typedef Piece<T, false> Part;
+  typedef Piece<T, kAnywhere> Part;
   const int width = (int)a.width;
   const int c0 = ((int)blockIdx.x * kVecs * kWideThreads + (int)threadIdx.x) * kLen;
   const int64_t r0 = (int64_t)blockIdx.y * chunk, r1 = min(a.rows, r0 + chunk);
@@ -573,10 +577,12 @@ __global__ __launch_bounds__(kWideThreads) void wide_kernel(NormGradArgs a, int6
   for (int64_t row = r0; row < r1; ++row) {
     float s[3];
 #pragma unroll
-    for (int i = 0; i < 3; ++i) s[i] = group_sum(s1[i], 4);
+    for (int i = 0; i < 3; ++i) s[i] = s1[i];
+    group_sums(s, 4);
     const float mean = mean1, rstd = rstd1;
     const float delta = s[0] * over_width, g_avg = s[1] * over_width;
     const float along = (s[2] - delta * s[1]) * over_width * rstd;
+    const float shift = -delta * rstd;
 #pragma unroll
     for (int k = 0; k < kVecs; ++k) {
       x[k] = x1[k];
@@ -588,10 +594,10 @@ __global__ __launch_bounds__(kWideThreads) void wide_kernel(NormGradArgs a, int6
       float y[kLen];
 #pragma unroll
       for (int j = 0; j < kLen; ++j) {
-        const float dj = (float)d[k][j], xhat = ((float)x[k][j] - mean - delta) * rstd;
+        const float dj = (float)d[k][j], xhat = fmaf((float)x[k][j] - mean, rstd, shift);
         dw[k][j] = fmaf(dj, xhat, dw[k][j]);
         db[k][j] += dj;
-        y[j] = rstd * (fmaf(dj, w[k][j], -g_avg) - xhat * along);
+        y[j] = rstd * fmaf(-along, xhat, fmaf(dj, w[k][j], -g_avg));
       }
       if (a.dx)
         Part(c0 + k * kWideThreads * kLen, width)
@@ -615,7 +621,7 @@ __global__ __launch_bounds__(kWideThreads) void wide_kernel(NormGradArgs a, int6
 
 // ---- the parameters' sums ------------------------------------------------------------
 
-constexpr int kJoinColumns = 32, kJoinSlices = 32;
+constexpr int kJoinColumns = 64, kJoinSlices = 16;
 constexpr int kJoinAhead = 8;  // parts in flight
 
 // blockIdx.y = 0: weight, 1: bias.  Slices of threads add the parts one after the
@@ -628,7 +634,7 @@ __global__ __launch_bounds__(kJoinColumns *kJoinSlices) void join_kernel(NormGra
   if (!to) return;
   const int lane = threadIdx.x & (kJoinColumns - 1), slice = threadIdx.x / kJoinColumns;
   const int64_t c = (int64_t)blockIdx.x * kJoinColumns + lane;
-  const int each = (parts + kJoinSlices - 1) / kJoinSlices;
+  const int slices = blockDim.x / kJoinColumns, each = (parts + slices - 1) / slices;
   const int p1 = min(parts, (slice + 1) * each);
   float v = 0.0f;
   if (c < a.width) {
@@ -644,7 +650,7 @@ __global__ __launch_bounds__(kJoinColumns *kJoinSlices) void join_kernel(NormGra
   lds[slice][lane] = v;
   __syncthreads();
   if (slice == 0 && c < a.width) {
-    for (int k = 1; k < kJoinSlices; ++k) v += lds[k][lane];
+    for (int k = 1; k < slices; ++k) v += lds[k][lane];
     store_as(a.grad_dtype, to, c, v);
   }
 }
@@ -658,12 +664,14 @@ int log2_up(int64_t v) {
 }
 
 // Rows of at most a wave, and of a workgroup.
-template <typename T, int E, bool SHORT>
+template <typename T, int E, Ends ENDS>
 hipError_t launch_narrow(const NormArgs &a, int cu_count, hipStream_t s) {
   const int log_g = log2_up((a.width + E - 1) / E);
+  if (ENDS == kAnywhere && a.width == (int64_t)E << log_g)
+    return launch_narrow<T, E, ENDS == kAnywhere ? kWhole : ENDS>(a, cu_count, s);
   const int64_t per = kWaveBlock >> log_g;
   const int64_t grid = std::min<int64_t>((a.rows + per - 1) / per, (int64_t)cu_count * 8);
-  norm_kernel<T, E, true, SHORT, kAny><<<(uint32_t)grid, kWaveBlock, 0, s>>>(
+  norm_kernel<T, E, true, ENDS, kAny><<<(uint32_t)grid, kWaveBlock, 0, s>>>(
       a, log_g, 1.0f / (float)a.width);
   return hipGetLastError();
 }
@@ -674,22 +682,23 @@ hipError_t launch_wide(const NormArgs &a, int cu_count, hipStream_t s) {
   const int64_t grid = std::min<int64_t>(a.rows, (int64_t)cu_count * (2048 / threads));
   const float over = 1.0f / (float)a.width;
   constexpr bool kSplit = E > 16;
+  const auto launch = [&](auto fn) { fn<<<(uint32_t)grid, threads, 0, s>>>(a, 0, over); };
   if (kSplit && a.weight && a.bias && a.param_f32)
-    norm_kernel<T, E, false, false, kSplit ? kFloat : kAny>
-        <<<(uint32_t)grid, threads, 0, s>>>(a, 0, over);
+    launch(norm_kernel<T, E, false, kAnywhere, kSplit ? kFloat : kAny>);
   else if (kSplit && a.weight && a.bias)
-    norm_kernel<T, E, false, false, kSplit ? kSame : kAny>
-        <<<(uint32_t)grid, threads, 0, s>>>(a, 0, over);
+    launch(norm_kernel<T, E, false, kAnywhere, kSplit ? kSame : kAny>);
+  else if (!kSplit && a.width == (int64_t)E * threads)
+    launch(norm_kernel<T, E, false, kSplit ? kAnywhere : kWhole, kAny>);
   else
-    norm_kernel<T, E, false, false, kAny><<<(uint32_t)grid, threads, 0, s>>>(a, 0, over);
+    launch(norm_kernel<T, E, false, kAnywhere, kAny>);
   return hipGetLastError();
 }
 
 template <typename T>
 hipError_t launch_norm(const NormArgs &a, int cu_count, hipStream_t s) {
-  if (a.width < Vec<T>::kLen) return launch_narrow<T, 8, true>(a, cu_count, s);
-  if (a.width <= 64 * 8) return launch_narrow<T, 8, false>(a, cu_count, s);
-  if (a.width <= 64 * 16) return launch_narrow<T, 16, false>(a, cu_count, s);
+  if (a.width < Vec<T>::kLen) return launch_narrow<T, 8, kShort>(a, cu_count, s);
+  if (a.width <= 64 * 8) return launch_narrow<T, 8, kAnywhere>(a, cu_count, s);
+  if (a.width <= 64 * 16) return launch_narrow<T, 16, kAnywhere>(a, cu_count, s);
   if (a.width <= kMaxBlock * 16) return launch_wide<T, 16>(a, cu_count, s);
   if (a.width <= kMaxBlock * 32) return launch_wide<T, 32>(a, cu_count, s);
   return launch_wide<T, 64>(a, cu_count, s);
@@ -741,12 +750,16 @@ hipError_t launch_grad(const NormGradArgs &a, void *ws, hipStream_t s) {
     const GradShape g = grad_shape(a.rows, a.width);
     parts = g.blocks;
     done = g.direct;
+    const auto launch = [&](auto fn) {
+      fn<<<g.blocks, g.threads, 0, s>>>(a, g, over, sums ? part : nullptr);
+    };
+    const bool eight = grad_columns(a.width) == 8;
     if (a.width < Vec<T>::kLen)
-      grad_kernel<T, 8, true><<<g.blocks, g.threads, 0, s>>>(a, g, over, sums ? part : nullptr);
-    else if (grad_columns(a.width) == 8)
-      grad_kernel<T, 8, false><<<g.blocks, g.threads, 0, s>>>(a, g, over, sums ? part : nullptr);
+      launch(grad_kernel<T, 8, kShort>);
+    else if (a.width == (int64_t)g.lanes * (eight ? 8 : 16))
+      eight ? launch(grad_kernel<T, 8, kWhole>) : launch(grad_kernel<T, 16, kWhole>);
     else
-      grad_kernel<T, 16, false><<<g.blocks, g.threads, 0, s>>>(a, g, over, sums ? part : nullptr);
+      eight ? launch(grad_kernel<T, 8, kAnywhere>) : launch(grad_kernel<T, 16, kAnywhere>);
   } else if (a.rows > 0) {
     const int64_t each = (int64_t)kStatVecs * kStatThreads * Vec<T>::kLen;
     const int64_t pieces = (a.width + each - 1) / each;
@@ -763,7 +776,8 @@ hipError_t launch_grad(const NormGradArgs &a, void *ws, hipStream_t s) {
   }
   if (sums && !done) {
     const dim3 grid((uint32_t)((a.width + kJoinColumns - 1) / kJoinColumns), 2);
-    join_kernel<<<grid, kJoinColumns * kJoinSlices, 0, s>>>(a, part, parts);
+    const int slices = std::max(1, std::min(kJoinSlices, (parts + kJoinAhead - 1) / kJoinAhead));
+    join_kernel<<<grid, kJoinColumns * slices, 0, s>>>(a, part, parts);
   }
   return hipGetLastError();
 }

@@ -86,6 +86,23 @@ __device__ __forceinline__ float group_sum(float v, int log_g) {
   return group_fold(v, log_g, [](float a, float b) { return a + b; });
 }
 
+// The same for N sums at once: one decision a step where log_g is not known when
+// this is compiled, and the steps of one sum between those of another.
+template <int N>
+__device__ __forceinline__ void group_sums(float (&v)[N], int log_g) {
+  const auto add = [](float a, float b) { return a + b; };
+  const auto step = [&](auto f) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = f(v[i]);
+  };
+  if (log_g >= 1) step([](float x) { return x + lane_swap<0xB1>(x); });
+  if (log_g >= 2) step([](float x) { return x + lane_swap<0x4E>(x); });
+  if (log_g >= 3) step([](float x) { return x + lane_swap<0x141>(x); });
+  if (log_g >= 4) step([](float x) { return x + lane_swap<0x140>(x); });
+  if (log_g >= 5) step([&](float x) { return join_rows(x, add); });
+  if (log_g >= 6) step([&](float x) { return join_halves(x, add); });
+}
+
 // Elements c .. c + kLen - 1 of a row of `width`, zeros outside.
 template <typename T>
 __device__ __forceinline__ void load_floats(const T *row, int64_t c, int64_t width, float *x) {
