@@ -267,26 +267,39 @@ Arrays arrays(const ml2_adamw_tensor &t, size_t param_size, size_t grad_size, in
            range(t.v_out ? t.v_out : t.v, s), range(t.copy, g)}};
 }
 
+// The ranges of a list that are not empty, in order.  Tensors mostly lie in the order
+// in which they were made, then nothing is sorted.
+void put_in_order(std::vector<Range> *list, size_t from) {
+  const auto before = [](Range a, Range b) { return a.at < b.at; };
+  const auto begin = list->begin(), middle = begin + (ptrdiff_t)from, end = list->end();
+  if (!std::is_sorted(middle, end, before)) std::sort(middle, end, before);
+  std::inplace_merge(begin, middle, end, before);
+}
+
 // Whether nothing that is written shares memory with anything but its own input.
 bool apart(const ml2_adamw_tensor *tensors, int32_t count, size_t param_size, size_t grad_size,
            int32_t bits) {
-  std::vector<Range> written;
+  std::vector<Range> written, read;
   written.reserve(4 * (size_t)count);
-  for (int32_t i = 0; i < count; ++i)
-    for (const Range &r : arrays(tensors[i], param_size, grad_size, bits).out)
-      if (r.at < r.end) written.push_back(r);
-  std::sort(written.begin(), written.end(), [](Range a, Range b) { return a.at < b.at; });
+  for (int q = 0; q < 4; ++q) {
+    const size_t w0 = written.size(), r0 = read.size();
+    for (int32_t i = 0; i < count; ++i) {
+      const Arrays a = arrays(tensors[i], param_size, grad_size, bits);
+      if (a.out[q].at < a.out[q].end) written.push_back(a.out[q]);
+      if (a.in[q].at < a.in[q].end && (q == 3 || !same(a.in[q], a.out[q])))
+        read.push_back(a.in[q]);
+    }
+    put_in_order(&written, w0);
+    put_in_order(&read, r0);
+  }
   for (size_t i = 1; i < written.size(); ++i)
     if (written[i].at < written[i - 1].end) return false;
-  for (int32_t i = 0; i < count; ++i) {
-    const Arrays a = arrays(tensors[i], param_size, grad_size, bits);
-    for (int q = 0; q < 4; ++q) {
-      if (a.in[q].at == a.in[q].end || (q < 3 && same(a.in[q], a.out[q]))) continue;
-      // the written ones are apart, so their ends are in order too
-      const auto w = std::upper_bound(written.begin(), written.end(), a.in[q].at,
-                                      [](uintptr_t at, Range r) { return at < r.end; });
-      if (w != written.end() && w->at < a.in[q].end) return false;
-    }
+  // The written ones are apart, so their ends are in order too: the first that ends
+  // behind the beginning of a read one is the only one it can meet first.
+  size_t w = 0;
+  for (const Range &r : read) {
+    while (w < written.size() && written[w].end <= r.at) ++w;
+    if (w < written.size() && written[w].at < r.end) return false;
   }
   return true;
 }

@@ -733,6 +733,19 @@ class EmbeddingGrad:
 
 # ---- a training step: normalisation, gradient norms, the optimizer ----------
 
+def _current() -> int:
+    import torch
+    return torch._C._cuda_getDevice()
+
+
+def _here(xs) -> None:
+    """All tensors on the current device, whose stream the call goes to."""
+    at = _current()
+    for x in xs:
+        if x is not None and x.get_device() != at:
+            raise ValueError(f"tensors on device {x.get_device()}, the current one is {at}")
+
+
 def _param(x, name: str, dtype, width: int):
     """(pointer, type) of a parameter [width] of a row type or float32, or (None, the row type)."""
     if x is None:
@@ -759,6 +772,7 @@ def ml2_layer_norm(x, weight, bias, out, mean=None, rstd=None, eps: float = 1e-5
     _same_type(weight, bias, "weight and bias")
     wp, code = _param(weight, "weight", x.dtype, width)
     bp, bcode = _param(bias, "bias", x.dtype, width)
+    _here((x, weight, bias, out, mean, rstd))
     f32 = _t().f32
     _check(lib().ml2_layer_norm(_dtype(x.dtype), xp, rows, width, ld, bcode if wp is None else code,
                                 wp, bp, eps, op, out_ld, _flat(mean, "mean", f32, (rows,)),
@@ -785,6 +799,7 @@ def ml2_layer_norm_grad(x, dout, weight, mean, rstd, workspace, dx=None, dweight
     _same_type(dweight, dbias, "dweight and dbias")
     gwp, gcode = _param(dweight, "dweight", x.dtype, width)
     gbp, bcode = _param(dbias, "dbias", x.dtype, width)
+    _here((x, dout, weight, mean, rstd, dx, dweight, dbias, workspace))
     f32 = _t().f32
     _check(lib().ml2_layer_norm_grad(
         _dtype(x.dtype), xp, rows, width, ld, dp, dout_ld, code, wp,
@@ -821,6 +836,7 @@ def ml2_grad_norm(grads, norm, factor, workspace, max_norm: float = float("inf")
     grads, dtype = _tensors(grads, "grads")
     n = len(grads)
     t = _t()
+    _here((grads[0], norm, factor, step, workspace))
     _check(lib().ml2_grad_norm(
         _dtype(dtype), (ctypes.c_void_p * n)(*[g.data_ptr() for g in grads]),
         (ctypes.c_int64 * n)(*[g.numel() for g in grads]), n, scale, max_norm,
@@ -853,6 +869,7 @@ class LayerNorm:
         if (rows, width) != self.shape or x.dtype is not self.dtype:
             raise ValueError("x must have the rows, width and type that this object was made for")
         _same_type(weight, bias, "weight and bias")
+        _here((x, weight, bias, self.out))
         wp, code = _param(weight, "weight", self.dtype, width)
         bp, bcode = _param(bias, "bias", self.dtype, width)
         _check(lib().ml2_layer_norm(self.code, xp, rows, width, ld, bcode if wp is None else code,
@@ -885,6 +902,7 @@ class LayerNormGrad:
                 x.dtype is not self.dtype or dout.dtype is not self.dtype):
             raise ValueError("x and dout must have the rows, width and type that this object was "
                              "made for")
+        _here((x, dout, weight, mean, rstd, self.dx))
         wp, code = _param(weight, "weight", self.dtype, width)
         f32 = _t().f32
         _check(lib().ml2_layer_norm_grad(
@@ -915,6 +933,7 @@ class GradNorm:
 
     def run(self, stream=None):
         """(norm, factor), both float32 [1]: this object's own buffers."""
+        _here((self.norm, self.step))
         _check(lib().ml2_grad_norm(*self.args, _stream(stream)))
         return self.norm, self.factor
 
@@ -1003,6 +1022,7 @@ class AdamW:
         else:
             o.step_device = _flat(step, "step", t.i32, (1,))
         o.factor = _flat(factor, "factor", t.f32, (1,))
+        _here((self.params[0], factor))
         ml2_adamw(self.dtype, self.grad_dtype, self.state_bits, self.tensors, self.count, o,
                   stream)
         return self.out[0] if self.out is not None else self.params

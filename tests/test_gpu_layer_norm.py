@@ -272,3 +272,32 @@ def test_streams_graph_and_repeats(rows, width):
 def _eager(x, dout, w, b):
     out, mean, rstd = ml2.LayerNorm(*x.shape, x.dtype).run(x, w, b)
     return (out, mean, rstd, *ml2.LayerNormGrad(*x.shape, x.dtype).run(x, dout, w, mean, rstd))
+
+
+def test_tensors_of_another_device_are_refused(monkeypatch):
+    """A call goes to the current device's stream: tensors of another one (here: seen so) raise."""
+    x = torch.zeros(4, 8, device=DEV)
+    ln, grad = ml2.LayerNorm(4, 8, x.dtype), ml2.LayerNormGrad(4, 8, x.dtype)
+    out, mean, rstd = ln.run(x)
+    norm, adam = ml2.GradNorm([x]), ml2.AdamW([x], [x.clone()])
+    monkeypatch.setattr(ml2, "_current", lambda: 1)
+    for call in (lambda: ln.run(x), lambda: grad.run(x, x, None, mean, rstd), norm.run,
+                 lambda: adam.run(1e-3, 1), lambda: ml2.ml2_layer_norm(x, None, None, out),
+                 lambda: ml2.ml2_layer_norm_grad(x, x, None, mean, rstd, grad.ws, grad.dx),
+                 lambda: ml2.ml2_grad_norm([x], norm.norm, norm.factor, norm.ws)):
+        with pytest.raises(ValueError, match="current"):
+            call()
+
+
+def test_objects_refuse_other_rows():
+    x = torch.zeros(4, 8, device=DEV)
+    ln, grad = ml2.LayerNorm(4, 8, x.dtype), ml2.LayerNormGrad(4, 8, x.dtype)
+    _, mean, rstd = ln.run(x)
+    w = torch.ones(8, device=DEV)
+    for call in (lambda: ln.run(x[:3]), lambda: ln.run(x[:, :7]), lambda: ln.run(x.half()),
+                 lambda: ln.run(x, w[:7]), lambda: ln.run(x, w.half(), w),
+                 lambda: grad.run(x, x[:3], w, mean, rstd), lambda: grad.run(x, x.half(), w, mean, rstd),
+                 lambda: grad.run(x, x, w.half(), mean, rstd),
+                 lambda: grad.run(x, x, w, mean[:3], rstd), lambda: ln.run(x.t().contiguous().t())):
+        with pytest.raises(ValueError):
+            call()
