@@ -486,6 +486,8 @@ class _Types:
         self.f32, self.i32 = torch.float32, torch.int32
         self.mask = (torch.uint8, torch.bool)
         self.code = {torch.float32: ML2_F32, torch.bfloat16: ML2_BF16, torch.float16: ML2_F16}
+        self.current = torch._C._cuda_getDevice
+        self.stream = torch._C._cuda_getCurrentRawStream
 
 
 _types = None
@@ -733,17 +735,15 @@ class EmbeddingGrad:
 
 # ---- a training step: normalisation, gradient norms, the optimizer ----------
 
-def _current() -> int:
-    import torch
-    return torch._C._cuda_getDevice()
-
-
-def _here(xs) -> None:
-    """All tensors on the current device, whose stream the call goes to."""
-    at = _current()
+def _here(stream, *xs):
+    """The stream of a call over these tensors (None among them): the current device's, on which
+    they all have to be."""
+    t = _t()
+    at = t.current()
     for x in xs:
         if x is not None and x.get_device() != at:
             raise ValueError(f"tensors on device {x.get_device()}, the current one is {at}")
+    return t.stream(at) if stream is None else _stream(stream)
 
 
 def _param(x, name: str, dtype, width: int):
@@ -772,11 +772,11 @@ def ml2_layer_norm(x, weight, bias, out, mean=None, rstd=None, eps: float = 1e-5
     _same_type(weight, bias, "weight and bias")
     wp, code = _param(weight, "weight", x.dtype, width)
     bp, bcode = _param(bias, "bias", x.dtype, width)
-    _here((x, weight, bias, out, mean, rstd))
     f32 = _t().f32
     _check(lib().ml2_layer_norm(_dtype(x.dtype), xp, rows, width, ld, bcode if wp is None else code,
                                 wp, bp, eps, op, out_ld, _flat(mean, "mean", f32, (rows,)),
-                                _flat(rstd, "rstd", f32, (rows,)), _stream(stream)))
+                                _flat(rstd, "rstd", f32, (rows,)),
+                                _here(stream, x, weight, bias, out, mean, rstd)))
 
 
 def ml2_layer_norm_grad_workspace_bytes(rows: int, width: int) -> int:
@@ -799,12 +799,12 @@ def ml2_layer_norm_grad(x, dout, weight, mean, rstd, workspace, dx=None, dweight
     _same_type(dweight, dbias, "dweight and dbias")
     gwp, gcode = _param(dweight, "dweight", x.dtype, width)
     gbp, bcode = _param(dbias, "dbias", x.dtype, width)
-    _here((x, dout, weight, mean, rstd, dx, dweight, dbias, workspace))
     f32 = _t().f32
     _check(lib().ml2_layer_norm_grad(
         _dtype(x.dtype), xp, rows, width, ld, dp, dout_ld, code, wp,
         _flat(mean, "mean", f32, (rows,)), _flat(rstd, "rstd", f32, (rows,)), dxp, dx_ld,
-        bcode if gwp is None else gcode, gwp, gbp, *_space(workspace), _stream(stream)))
+        bcode if gwp is None else gcode, gwp, gbp, *_space(workspace),
+        _here(stream, x, dout, weight, mean, rstd, dx, dweight, dbias, workspace)))
 
 
 def _tensors(xs, name: str):
@@ -836,12 +836,12 @@ def ml2_grad_norm(grads, norm, factor, workspace, max_norm: float = float("inf")
     grads, dtype = _tensors(grads, "grads")
     n = len(grads)
     t = _t()
-    _here((grads[0], norm, factor, step, workspace))
     _check(lib().ml2_grad_norm(
         _dtype(dtype), (ctypes.c_void_p * n)(*[g.data_ptr() for g in grads]),
         (ctypes.c_int64 * n)(*[g.numel() for g in grads]), n, scale, max_norm,
         _flat(norm, "norm", t.f32, (1,)), _flat(factor, "factor", t.f32, (1,)),
-        _flat(step, "step", t.i32, (1,)), *_space(workspace), _stream(stream)))
+        _flat(step, "step", t.i32, (1,)), *_space(workspace),
+        _here(stream, grads[0], norm, factor, step, workspace)))
 
 
 def ml2_adamw(param_dtype, grad_dtype, state_bits: int, tensors, count: int,
@@ -869,11 +869,11 @@ class LayerNorm:
         if (rows, width) != self.shape or x.dtype is not self.dtype:
             raise ValueError("x must have the rows, width and type that this object was made for")
         _same_type(weight, bias, "weight and bias")
-        _here((x, weight, bias, self.out))
         wp, code = _param(weight, "weight", self.dtype, width)
         bp, bcode = _param(bias, "bias", self.dtype, width)
         _check(lib().ml2_layer_norm(self.code, xp, rows, width, ld, bcode if wp is None else code,
-                                    wp, bp, eps, *self.buffers, _stream(stream)))
+                                    wp, bp, eps, *self.buffers,
+                                    _here(stream, x, weight, bias, self.out)))
         return self.out, self.mean, self.rstd
 
 
@@ -902,13 +902,12 @@ class LayerNormGrad:
                 x.dtype is not self.dtype or dout.dtype is not self.dtype):
             raise ValueError("x and dout must have the rows, width and type that this object was "
                              "made for")
-        _here((x, dout, weight, mean, rstd, self.dx))
         wp, code = _param(weight, "weight", self.dtype, width)
         f32 = _t().f32
         _check(lib().ml2_layer_norm_grad(
             self.code, xp, rows, width, ld, dp, dout_ld, code, wp,
             _flat(mean, "mean", f32, (rows,)), _flat(rstd, "rstd", f32, (rows,)), *self.buffers,
-            _stream(stream)))
+            _here(stream, x, dout, weight, mean, rstd, self.dx)))
         return self.dx, self.dweight, self.dbias
 
 
@@ -933,8 +932,7 @@ class GradNorm:
 
     def run(self, stream=None):
         """(norm, factor), both float32 [1]: this object's own buffers."""
-        _here((self.norm, self.step))
-        _check(lib().ml2_grad_norm(*self.args, _stream(stream)))
+        _check(lib().ml2_grad_norm(*self.args, _here(stream, self.norm, self.step)))
         return self.norm, self.factor
 
 
@@ -1022,9 +1020,8 @@ class AdamW:
         else:
             o.step_device = _flat(step, "step", t.i32, (1,))
         o.factor = _flat(factor, "factor", t.f32, (1,))
-        _here((self.params[0], factor))
         ml2_adamw(self.dtype, self.grad_dtype, self.state_bits, self.tensors, self.count, o,
-                  stream)
+                  _here(stream, self.params[0], factor))
         return self.out[0] if self.out is not None else self.params
 
 

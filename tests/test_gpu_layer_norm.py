@@ -280,7 +280,7 @@ def test_tensors_of_another_device_are_refused(monkeypatch):
     ln, grad = ml2.LayerNorm(4, 8, x.dtype), ml2.LayerNormGrad(4, 8, x.dtype)
     out, mean, rstd = ln.run(x)
     norm, adam = ml2.GradNorm([x]), ml2.AdamW([x], [x.clone()])
-    monkeypatch.setattr(ml2, "_current", lambda: 1)
+    monkeypatch.setattr(ml2._t(), "current", lambda: 1)
     for call in (lambda: ln.run(x), lambda: grad.run(x, x, None, mean, rstd), norm.run,
                  lambda: adam.run(1e-3, 1), lambda: ml2.ml2_layer_norm(x, None, None, out),
                  lambda: ml2.ml2_layer_norm_grad(x, x, None, mean, rstd, grad.ws, grad.dx),
