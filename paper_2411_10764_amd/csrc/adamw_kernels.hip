@@ -35,8 +35,11 @@ __device__ __forceinline__ int find_tensor(const uint32_t (&first)[MOST], int co
 
 constexpr int kNormTensors = 128;
 constexpr int kNormVecs = 4;       // vectors of a thread in flight
-constexpr int kNormParts = 2048;   // about as many parts, and one for each tensor
-constexpr int64_t kNormLeast = 16384;
+// About as many parts, and one for each tensor, of at least so many elements: 4M float32
+// elements in 10 tensors 10.4 us, with half the parts of twice the size 12.7; 134M bf16
+// ones 54 with 2,048 or 4,096 parts, 57 with 1,024.
+constexpr int kNormParts = 4096;
+constexpr int64_t kNormLeast = 8192;
 
 struct NormTable {
   const void *grad[kNormTensors];
@@ -140,7 +143,9 @@ __global__ __launch_bounds__(1024) void norm_one_kernel(NormTable t, uint32_t ch
   if (threadIdx.x == 0) finish(o, v);
 }
 
-constexpr int64_t kNormOne = 65536;  // elements
+// Up to so many chunks: 65,536 float32 elements 7.2 us, in two launches 9.7; 131,072
+// 10.7 and 9.9.  163,840 bf16 ones 9.8 and 8.2.
+constexpr int64_t kNormOne = 64;
 
 int64_t norm_chunk(const int64_t *sizes, int32_t count) {
   int64_t total = 0;
@@ -157,18 +162,15 @@ int64_t norm_parts(const int64_t *sizes, int32_t count, int64_t chunk) {
 template <typename T>
 hipError_t launch_norm(const void *const *grads, const int64_t *sizes, int32_t count,
                        const NormOut &o, double *part, hipStream_t s) {
-  int64_t total = 0;
-  int32_t used = 0;
-  for (int32_t i = 0; i < count; ++i) {
-    total = std::min<int64_t>(total + sizes[i], kNormOne + 1);
-    used += sizes[i] > 0;
-  }
+  constexpr int64_t kChunk = 64 * kNormVecs * Vec<T>::kLen;  // of a wave
+  int64_t chunks = 0;
+  for (int32_t i = 0; i < count && chunks <= kNormOne; ++i)
+    chunks += (sizes[i] + kChunk - 1) / kChunk;
+  const bool one = chunks <= kNormOne;
   NormTable t;
-  t.chunk = norm_chunk(sizes, count);
+  t.chunk = one ? kChunk : norm_chunk(sizes, count);
   t.part = part;
   t.count = 0;
-  const bool one = total <= kNormOne && used <= kNormTensors;
-  if (one) t.chunk = 64 * kNormVecs * Vec<T>::kLen;
   uint32_t blocks = 0;
   int64_t parts = 0;
   for (int32_t i = 0; i < count; ++i) {

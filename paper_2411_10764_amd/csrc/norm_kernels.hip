@@ -271,7 +271,6 @@ __global__ __launch_bounds__(WAVE ? kWaveBlock : kMaxBlock,
 
 constexpr int kGradBlocks = 256;   // at most: each leaves a part of the parameters' sums
 constexpr int kGradWidth = 16 * kMaxBlock;
-constexpr int kDirectTurns = 4;
 
 __device__ __forceinline__ void store_as(int dtype, void *p, int64_t i, float v) {
   if (dtype == ML2_F32)
@@ -720,7 +719,10 @@ GradShape grad_shape(int64_t rows, int64_t width) {
   }
   g.per = g.threads / g.lanes;
   const int64_t turns = (rows + g.per - 1) / g.per;
-  g.direct = turns <= kDirectTurns;
+  // A turn costs less than the launch that joins parts: 256 x 128 float32 (4 turns)
+  // 8.8 us, in two launches 11.3; 512 x 128 (8) 12.5 and 11.5; 32 x 1,024 bf16 (2) 11.3
+  // and 12.8; 48 x 1,024 (3) 13.3 and 12.5; 4 x 4,096 (1) 11.4 and 13.4.
+  g.direct = turns <= (grad_columns(width) == 8 ? 4 : g.lanes == 64 ? 2 : 1);
   g.blocks = g.direct ? 1 : (int)std::min<int64_t>(turns, kGradBlocks);
   return g;
 }
@@ -730,13 +732,26 @@ int64_t stat_pieces(int64_t width) {  // for the smaller vectors
   return (width + each - 1) / each;
 }
 
+// A chunk has at least so many rows, and the chunks of all slabs so many workgroups at
+// most: a chunk costs its part of the parameters' sums, a row of a chunk a turn.  100
+// rows of 20,000 bf16 17 us, in chunks of one row 28, of 12 20; 260 of 50,021 float32
+// 55, with 512 workgroups 53, with 1,024 57; 2,048 of 20,000 bf16 98, 105 and 100.
+constexpr int64_t kLeastChunk = 4, kWideBlocks = 640;
+// Rows of more than half of kGradWidth are read twice where there are few: 5 of 16,384
+// bf16 13 us, in registers 16; 320 22 and 30; 512 28 and 29; 1,024 49 and 38.
+constexpr int64_t kFewRows = 512;
 constexpr int64_t kWideSlab = (int64_t)kWideThreads * kWideColumns;
 
-// Rows of a chunk: enough chunks to fill the device.
+// Rows of a chunk.
 int64_t wide_chunk(int64_t rows, int64_t width) {
   const int64_t slabs = (width + kWideSlab - 1) / kWideSlab;
-  const int64_t chunks = std::max<int64_t>(1, std::min<int64_t>(rows, 1024 / slabs));
+  const int64_t chunks = std::max<int64_t>(1, std::min<int64_t>(rows / kLeastChunk, kWideBlocks / slabs));
   return (rows + chunks - 1) / chunks;
+}
+
+// Whether rows are read twice.
+bool grad_twice(int64_t rows, int64_t width) {
+  return width > kGradWidth || (width > kGradWidth / 2 && rows <= kFewRows);
 }
 
 template <typename T>
@@ -746,7 +761,7 @@ hipError_t launch_grad(const NormGradArgs &a, void *ws, hipStream_t s) {
   float *part = static_cast<float *>(ws);
   int parts = 0;
   bool done = false;
-  if (a.rows > 0 && a.width <= kGradWidth) {
+  if (a.rows > 0 && !grad_twice(a.rows, a.width)) {
     const GradShape g = grad_shape(a.rows, a.width);
     parts = g.blocks;
     done = g.direct;
@@ -792,7 +807,7 @@ hipError_t launch_layer_norm(int dtype, const NormArgs &a, int cu_count, hipStre
 
 size_t layer_norm_grad_workspace_bytes(int64_t rows, int64_t width) {
   if (rows <= 0 || width <= 0) return 0;
-  if (width <= kGradWidth)
+  if (!grad_twice(rows, width))
     return (size_t)grad_shape(rows, width).blocks * 2 * (size_t)width * sizeof(float);
   const int64_t chunk = wide_chunk(rows, width);
   return ((size_t)rows * (size_t)stat_pieces(width) * 3 +

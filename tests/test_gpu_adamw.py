@@ -319,7 +319,8 @@ def _norm_case(sizes, dtype, gap, scale, max_norm, size=1.0):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
-@pytest.mark.parametrize("sizes", [[1], [0, 3], [50000], [65536], [65537], [1000] * 16, [1000] * 17,
+@pytest.mark.parametrize("sizes", [[1], [0, 3], [50000], [65536], [65537], [131072], [131073], [1000] * 16, [1000] * 17,
+                                   [1] * 64, [1] * 65,
                                    [7] * 128, [9] * 129, [333] * 400, [1 << 22, 5, 100001],
                                    [40000001]])
 def test_norms(dtype, sizes):

@@ -106,7 +106,9 @@ def test_strides(dtype, width, pad):
 @pytest.mark.parametrize("rows,width", [(1, 1), (1, 64), (1, 65536), (2, 3), (64, 8), (255, 8),
                                         (257, 17), (1000, 128), (4097, 33), (5000, 512),
                                         (3001, 771), (20000, 5), (300, 2050), (1100, 1040),
-                                        (270, 16384), (100, 16390), (70000, 2)])
+                                        (270, 16384), (512, 8200), (513, 8200),
+                                        (600, 16384), (100, 16390), (70000, 2), (17, 512), (65, 512),
+                                        (32, 1024), (33, 1024), (4, 4096), (5, 4096)])
 def test_rows(dtype, rows, width):
     _both(dtype, rows, width)
 
