@@ -270,7 +270,10 @@ __global__ __launch_bounds__(WAVE ? kWaveBlock : kMaxBlock,
 // ---- gradients of rows that fit a workgroup's registers ---------------------------
 
 constexpr int kGradBlocks = 256;   // at most: each leaves a part of the parameters' sums
-constexpr int kGradWidth = 16 * kMaxBlock;
+// Widest rows that stay in a workgroup's registers, of 32-bit and of 16-bit columns: 24
+// of those a lane fill 126 registers with their sums (32 would spill 34).  2,048 x
+// 24,576 bf16 83 us, read twice 114; 2,048 x 16,384 float32 101, 16,385 146.
+constexpr int kGradWidth = 16 * kMaxBlock, kGradWidth16 = 24 * kMaxBlock;
 
 __device__ __forceinline__ void store_as(int dtype, void *p, int64_t i, float v) {
   if (dtype == ML2_F32)
@@ -307,11 +310,13 @@ __global__ __launch_bounds__(kMaxBlock) void grad_kernel(NormGradArgs a, GradSha
   constexpr int kLen = Vec<T>::kLen, kVecs = E / kLen;
   typedef Piece<T, ENDS> Part;
   // The row's sums and the weight, each lane's four by four, then the parts of the
-  // gradients of weight and bias.
-  __shared__ float lds[2][kMaxBlock * E];
+  // gradients of weight and bias (a row as wide as a workgroup has but one part).
+  constexpr bool kJoins = E <= 16;
+  constexpr int kSpan = kMaxBlock * E, kWeight = kJoins ? kSpan : 128;
+  __shared__ float lds[kWeight + kSpan];
   typedef float F4 __attribute__((ext_vector_type(4)));
-  float (*sums)[kMaxBlock / 64][3] = reinterpret_cast<float (*)[kMaxBlock / 64][3]>(lds[0]);
-  F4 *weight = reinterpret_cast<F4 *>(lds[1]);
+  float (*sums)[kMaxBlock / 64][3] = reinterpret_cast<float (*)[kMaxBlock / 64][3]>(lds);
+  F4 *weight = reinterpret_cast<F4 *>(lds + kWeight);
   const int lanes = g.lanes, group = (int)threadIdx.x / lanes, width = (int)a.width;
   const int lane = (int)threadIdx.x - group * lanes;
   const bool wide = lanes > 64;
@@ -362,6 +367,7 @@ __global__ __launch_bounds__(kMaxBlock) void grad_kernel(NormGradArgs a, GradSha
 #pragma unroll
     for (int k = 0; k < kVecs; ++k) {
       const Part at((k * lanes + lane) * kLen, anew(width));
+      if (!kJoins) __builtin_amdgcn_sched_barrier(0);
       float w[kLen];
 #pragma unroll
       for (int j = 0; j < kLen; j += 4) {
@@ -430,6 +436,7 @@ __global__ __launch_bounds__(kMaxBlock) void grad_kernel(NormGradArgs a, GradSha
           y[j] = rstd * fmaf(-along, xhat, fmaf(dj, w, -g_avg));
         }
         if (dst) at.store(dst, width, y);
+        if (!kJoins) __builtin_amdgcn_sched_barrier(0);  // one vector at a time
       }
     }
   }
@@ -444,40 +451,44 @@ __global__ __launch_bounds__(kMaxBlock) void grad_kernel(NormGradArgs a, GradSha
     }
   }
   const int parts = wide ? g.per : (int)blockDim.x >> 6;
+  float *to = part + (int64_t)blockIdx.x * 2 * width;
   const int own = wide ? group : (int)threadIdx.x >> 6;
   typedef float U4 __attribute__((ext_vector_type(4), aligned(4)));
-  __syncthreads();
-  if (wide || (int)(threadIdx.x & 63) < lanes) {
+  // A lane's columns of `row` and, `apart` floats on, of the bias's.
+  const auto put = [&](float *row, int apart) {
 #pragma unroll
     for (int k = 0; k < kVecs; ++k) {
       const Part at((k * lanes + lane) * kLen, width);
-      float *row = lds[0] + own * width + at.col;  // at most lanes * E columns
+      float *to = row + at.col;
       if (at.whole()) {
 #pragma unroll
         for (int j = 0; j < kLen; j += 4) {
           const int i = k * kLen + j;
-          *reinterpret_cast<U4 *>(row + j) = U4{dw[i], dw[i + 1], dw[i + 2], dw[i + 3]};
-          *reinterpret_cast<U4 *>(row + kMaxBlock * E + j) =
-              U4{db[i], db[i + 1], db[i + 2], db[i + 3]};
+          *reinterpret_cast<U4 *>(to + j) = U4{dw[i], dw[i + 1], dw[i + 2], dw[i + 3]};
+          *reinterpret_cast<U4 *>(to + apart + j) = U4{db[i], db[i + 1], db[i + 2], db[i + 3]};
         }
       } else {
 #pragma unroll
         for (int j = 0; j < kLen; ++j) {
           if (at.has(j, width)) {
-            row[j] = dw[k * kLen + j];
-            row[kMaxBlock * E + j] = db[k * kLen + j];
+            to[j] = dw[k * kLen + j];
+            to[apart + j] = db[k * kLen + j];
           }
         }
       }
     }
-  }
+  };
+  if (!kJoins) return put(to, width);
   __syncthreads();
-  float *to = part + (int64_t)blockIdx.x * 2 * width;
+  // at most lanes * E columns a part
+  if (wide || (int)(threadIdx.x & 63) < lanes) put(lds + own * width, kSpan);
+  __syncthreads();
   for (int i = threadIdx.x; i < 2 * width; i += blockDim.x) {
     const int q = i >= width, c = q ? i - width : i;
-    float v = lds[q][c];
+    const float *from = lds + q * kSpan + c;
+    float v = from[0];
 #pragma unroll 8
-    for (int p = 1; p < parts; ++p) v += lds[q][p * width + c];
+    for (int p = 1; p < parts; ++p) v += from[p * width];
     void *out = q ? a.dbias : a.dweight;
     if (!g.direct)
       to[i] = v;
@@ -703,7 +714,9 @@ hipError_t launch_norm(const NormArgs &a, int cu_count, hipStream_t s) {
   return launch_wide<T, 64>(a, cu_count, s);
 }
 
-int grad_columns(int64_t width) { return width <= 64 * 8 ? 8 : 16; }
+int grad_columns(int64_t width) {
+  return width <= 64 * 8 ? 8 : width <= kGradWidth ? 16 : 24;
+}
 
 GradShape grad_shape(int64_t rows, int64_t width) {
   GradShape g;
@@ -722,7 +735,7 @@ GradShape grad_shape(int64_t rows, int64_t width) {
   // A turn costs less than the launch that joins parts: 256 x 128 float32 (4 turns)
   // 8.8 us, in two launches 11.3; 512 x 128 (8) 12.5 and 11.5; 32 x 1,024 bf16 (2) 11.3
   // and 12.8; 48 x 1,024 (3) 13.3 and 12.5; 4 x 4,096 (1) 11.4 and 13.4.
-  g.direct = turns <= (grad_columns(width) == 8 ? 4 : g.lanes == 64 ? 2 : 1);
+  g.direct = turns <= (grad_columns(width) == 8 ? 4 : g.lanes == 64 ? 2 : width <= kGradWidth);
   g.blocks = g.direct ? 1 : (int)std::min<int64_t>(turns, kGradBlocks);
   return g;
 }
@@ -738,7 +751,8 @@ int64_t stat_pieces(int64_t width) {  // for the smaller vectors
 // 55, with 512 workgroups 53, with 1,024 57; 2,048 of 20,000 bf16 98, 105 and 100.
 constexpr int64_t kLeastChunk = 4, kWideBlocks = 640;
 // Rows of more than half of kGradWidth are read twice where there are few: 5 of 16,384
-// bf16 13 us, in registers 16; 320 22 and 30; 512 28 and 29; 1,024 49 and 38.
+// bf16 13 us, in registers 16; 320 22 and 30; 512 28 and 29; 1,024 49 and 38; 520 of
+// 20,000 36 and 38, 1,000 55 and 44.
 constexpr int64_t kFewRows = 512;
 constexpr int64_t kWideSlab = (int64_t)kWideThreads * kWideColumns;
 
@@ -750,8 +764,9 @@ int64_t wide_chunk(int64_t rows, int64_t width) {
 }
 
 // Whether rows are read twice.
-bool grad_twice(int64_t rows, int64_t width) {
-  return width > kGradWidth || (width > kGradWidth / 2 && rows <= kFewRows);
+bool grad_twice(int64_t rows, int64_t width, size_t size) {
+  return width > (size == 2 ? kGradWidth16 : kGradWidth) ||
+         (width > kGradWidth / 2 && rows <= kFewRows);
 }
 
 template <typename T>
@@ -761,20 +776,22 @@ hipError_t launch_grad(const NormGradArgs &a, void *ws, hipStream_t s) {
   float *part = static_cast<float *>(ws);
   int parts = 0;
   bool done = false;
-  if (a.rows > 0 && !grad_twice(a.rows, a.width)) {
+  if (a.rows > 0 && !grad_twice(a.rows, a.width, sizeof(T))) {
     const GradShape g = grad_shape(a.rows, a.width);
     parts = g.blocks;
     done = g.direct;
     const auto launch = [&](auto fn) {
       fn<<<g.blocks, g.threads, 0, s>>>(a, g, over, sums ? part : nullptr);
     };
-    const bool eight = grad_columns(a.width) == 8;
+    const bool whole = a.width == (int64_t)g.lanes * grad_columns(a.width);
     if (a.width < Vec<T>::kLen)
       launch(grad_kernel<T, 8, kShort>);
-    else if (a.width == (int64_t)g.lanes * (eight ? 8 : 16))
-      eight ? launch(grad_kernel<T, 8, kWhole>) : launch(grad_kernel<T, 16, kWhole>);
+    else if (grad_columns(a.width) == 8)
+      whole ? launch(grad_kernel<T, 8, kWhole>) : launch(grad_kernel<T, 8, kAnywhere>);
+    else if (sizeof(T) == 4 || grad_columns(a.width) == 16)
+      whole ? launch(grad_kernel<T, 16, kWhole>) : launch(grad_kernel<T, 16, kAnywhere>);
     else
-      eight ? launch(grad_kernel<T, 8, kAnywhere>) : launch(grad_kernel<T, 16, kAnywhere>);
+      launch(grad_kernel<T, sizeof(T) == 2 ? 24 : 16, kAnywhere>);
   } else if (a.rows > 0) {
     const int64_t each = (int64_t)kStatVecs * kStatThreads * Vec<T>::kLen;
     const int64_t pieces = (a.width + each - 1) / each;
@@ -807,11 +824,15 @@ hipError_t launch_layer_norm(int dtype, const NormArgs &a, int cu_count, hipStre
 
 size_t layer_norm_grad_workspace_bytes(int64_t rows, int64_t width) {
   if (rows <= 0 || width <= 0) return 0;
-  if (!grad_twice(rows, width))
-    return (size_t)grad_shape(rows, width).blocks * 2 * (size_t)width * sizeof(float);
-  const int64_t chunk = wide_chunk(rows, width);
-  return ((size_t)rows * (size_t)stat_pieces(width) * 3 +
-          (size_t)((rows + chunk - 1) / chunk) * 2 * (size_t)width) * sizeof(float);
+  size_t floats = 0;  // for rows of either size of columns
+  if (!grad_twice(rows, width, 2))
+    floats = (size_t)grad_shape(rows, width).blocks * 2 * (size_t)width;
+  if (grad_twice(rows, width, 4)) {
+    const int64_t chunk = wide_chunk(rows, width);
+    floats = std::max(floats, (size_t)rows * (size_t)stat_pieces(width) * 3 +
+                                  (size_t)((rows + chunk - 1) / chunk) * 2 * (size_t)width);
+  }
+  return floats * sizeof(float);
 }
 
 hipError_t launch_layer_norm_grad(int dtype, const NormGradArgs &a, void *ws, hipStream_t s) {

@@ -813,11 +813,20 @@ def _tensors(xs, name: str):
     if not xs:
         raise ValueError(f"{name} must hold a tensor")
     for x in xs:
-        if not x.is_cuda or not x.is_contiguous() or x.dtype is not xs[0].dtype:
+        if x is None or not x.is_cuda or not x.is_contiguous() or x.dtype is not xs[0].dtype:
             raise ValueError(f"{name} must be contiguous device tensors of one type")
         if x.device != xs[0].device:
             raise ValueError(f"{name} must be on one device")
     return xs, xs[0].dtype
+
+
+def _like(grads, old):
+    """A list of gradients that can take the place of another."""
+    grads, dtype = _tensors(grads, "grads")
+    if dtype is not old[0].dtype or grads[0].device != old[0].device or (
+            [g.numel() for g in grads] != [g.numel() for g in old]):
+        raise ValueError("grads must have the type, sizes and device of those before")
+    return grads
 
 
 def ml2_grad_norm_workspace_bytes(sizes) -> int:
@@ -912,23 +921,28 @@ class LayerNormGrad:
 
 
 class GradNorm:
-    """ml2_grad_norm over a program's gradient buffers, which it keeps: norm and factor are
-    this object's own buffers, and step, where given, the program's counter."""
+    """ml2_grad_norm over a program's gradient buffers, which it keeps (take() names others): norm
+    and factor are this object's own buffers, and step, where given, the program's counter."""
 
     def __init__(self, grads, max_norm: float = float("inf"), scale: float = 1.0, step=None):
         import torch
         self.grads, self.dtype = _tensors(grads, "grads")
-        self.count, self.scale, self.max_norm, self.step = len(self.grads), scale, max_norm, step
-        device = self.grads[0].device
-        self.norm = torch.empty(1, dtype=torch.float32, device=device)
-        self.factor = torch.empty(1, dtype=torch.float32, device=device)
+        count, self.step = len(self.grads), step
+        self.norm, self.factor = (torch.empty(1, dtype=torch.float32, device=self.grads[0].device)
+                                  for _ in range(2))
         sizes = [g.numel() for g in self.grads]
-        self.at = (ctypes.c_void_p * self.count)(*[g.data_ptr() for g in self.grads])
-        self.sizes = (ctypes.c_int64 * self.count)(*sizes)
-        self.ws = _workspace(ml2_grad_norm_workspace_bytes(sizes), device)
-        self.args = (_dtype(self.dtype), self.at, self.sizes, self.count, scale, max_norm,
-                     self.norm.data_ptr(), self.factor.data_ptr(),
+        self.at = (ctypes.c_void_p * count)()
+        self.ws = _workspace(ml2_grad_norm_workspace_bytes(sizes), self.norm.device)
+        self.args = (_dtype(self.dtype), self.at, (ctypes.c_int64 * count)(*sizes), count, scale,
+                     max_norm, self.norm.data_ptr(), self.factor.data_ptr(),
                      _flat(step, "step", torch.int32, (1,)), *_space(self.ws))
+        self.take(self.grads)
+
+    def take(self, grads) -> None:
+        """Other gradients of the same sizes and type from now on."""
+        self.grads = _like(grads, self.grads)
+        for i, g in enumerate(self.grads):
+            self.at[i] = g.data_ptr()
 
     def run(self, stream=None):
         """(norm, factor), both float32 [1]: this object's own buffers."""
@@ -937,7 +951,8 @@ class GradNorm:
 
 
 class AdamW:
-    """ml2_adamw over a program's parameters and gradient buffers, which it keeps.
+    """ml2_adamw over a program's parameters and gradient buffers, which it keeps (take() names
+    other gradients).
 
     state_bits 32 or 8; m and v: lists of states (by default zeros: adamw_state); copies: a list
     of tensors of the gradients' type that get the new parameters too; weight_decay: one, or one
@@ -959,7 +974,8 @@ class AdamW:
                 return [adamw_state(n, state_bits, device) for n in sizes]
             xs, dtype = _tensors(xs, name)
             want = torch.float32 if state_bits == 32 else torch.uint8
-            need = [ml2_adamw_state_bytes(state_bits, n) // want.itemsize for n in sizes]
+            need = sizes if state_bits == 32 else [
+                -(-n // ML2_STATE_BLOCK) * (ML2_STATE_BLOCK + 4) for n in sizes]
             if dtype is not want or [x.numel() for x in xs] != need:
                 raise ValueError(f"{name} must be {want} of adamw_state's sizes")
             return xs
@@ -991,12 +1007,19 @@ class AdamW:
         self._fill()
 
     def _fill(self) -> None:
-        outs = self.out or (self.params, self.m, self.v)
-        for i, t in enumerate(self.tensors):
-            t.param, t.grad = self.params[i].data_ptr(), self.grads[i].data_ptr()
-            t.m, t.v = self.m[i].data_ptr(), self.v[i].data_ptr()
-            t.param_out, t.m_out, t.v_out = (x[i].data_ptr() for x in outs)
-            t.copy = self.copies[i].data_ptr() if self.copies is not None else None
+        lists = (self.params, self.grads, self.m, self.v,
+                 *(self.out or (self.params, self.m, self.v)))
+        at = [[x.data_ptr() for x in xs] for xs in lists]
+        copies = [x.data_ptr() for x in self.copies] if self.copies is not None else (
+            [None] * self.count)
+        for t, *t7, copy in zip(self.tensors, *at, copies):
+            t.param, t.grad, t.m, t.v, t.param_out, t.m_out, t.v_out = t7
+            t.copy = copy
+
+    def take(self, grads) -> None:
+        """Other gradients of the same sizes and type from now on."""
+        self.grads = _like(grads, self.grads)
+        self._fill()
 
     def accept(self) -> None:
         """The last step's results become the state, and the old state's memory the next

@@ -405,3 +405,26 @@ def test_a_captured_step_follows_its_counter(bits):
             assert torch.equal(x, y)
         for x, y in zip((*a.m, *a.v), (*b.m, *b.v)):
             assert torch.equal(x, y)
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_other_gradients(bits):
+    """take(): the next call is that of objects made with those gradients."""
+    a = Case([1000, 3, 700], torch.float32, torch.bfloat16, bits, factor=0.5)
+    b = Case([1000, 3, 700], torch.float32, torch.bfloat16, bits, factor=0.5)
+    fresh = [torch.randn(n, device=DEV).bfloat16() for n in a.sizes]
+    norm = ml2.GradNorm(a.g, 1.0)
+    for to, x in zip(b.g, fresh):
+        to.copy_(x)
+    norm.take(fresh)
+    a.plan.take(fresh)
+    a.run()
+    b.run()
+    for have, want in zip((a.p, a.m, a.v), (b.p, b.m, b.v)):
+        assert all(torch.equal(x, y) for x, y in zip(have, want))
+    assert torch.equal(norm.run()[0], ml2.GradNorm(b.g, 1.0).run()[0])
+    for bad in (fresh[:2], [fresh[0], fresh[1], fresh[2][:-1]], [x.float() for x in fresh],
+                [None] * 3):
+        for taker in (norm, a.plan):
+            with pytest.raises(ValueError):
+                taker.take(bad)

@@ -107,7 +107,7 @@ def test_strides(dtype, width, pad):
                                         (257, 17), (1000, 128), (4097, 33), (5000, 512),
                                         (3001, 771), (20000, 5), (300, 2050), (1100, 1040),
                                         (270, 16384), (512, 8200), (513, 8200),
-                                        (600, 16384), (100, 16390), (70000, 2), (17, 512), (65, 512),
+                                        (600, 16384), (515, 20001), (513, 24576), (100, 16390), (70000, 2), (17, 512), (65, 512),
                                         (32, 1024), (33, 1024), (4, 4096), (5, 4096)])
 def test_rows(dtype, rows, width):
     _both(dtype, rows, width)
@@ -151,28 +151,27 @@ def test_nan_and_infinity_stay_in_their_rows(width):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
-@pytest.mark.parametrize("width", [24, 1000, 3001, 18000])
-def test_in_place(dtype, width):
+@pytest.mark.parametrize("rows,width", [(50, 24), (50, 1000), (50, 3001), (50, 18000), (520, 8300),
+                                        (515, 17001), (700, 24)])
+def test_in_place(dtype, rows, width):
     """The output in the rows' memory, the rows' gradient in x's and in dout's."""
     rng = np.random.default_rng(width)
-    x, dout = (_rows(rng, 50, width, dtype, 3).to(DEV)[:, :width] for _ in range(2))
+    x, dout = (_rows(rng, rows, width, dtype, 3).to(DEV)[:, :width] for _ in range(2))
     w, b = (p.to(DEV) for p in _params(rng, width, torch.float32))
-    ln = ml2.LayerNorm(50, width, dtype)
+    ln = ml2.LayerNorm(rows, width, dtype)
     out, mean, rstd = ln.run(x, w, b)
-    grad = ml2.LayerNormGrad(50, width, dtype, torch.float32)
+    grad = ml2.LayerNormGrad(rows, width, dtype, torch.float32)
     dx, dw, db = grad.run(x, dout, w, mean, rstd)
     for into in ("x", "dout"):
-        a, d = x.clone(), dout.clone()
-        a2, d2 = torch.empty(50, width + 3, dtype=dtype, device=DEV)[:, :width], None
-        a2.copy_(x)
-        d2 = torch.empty(50, width + 5, dtype=dtype, device=DEV)[:, :width]
-        d2.copy_(dout)
-        to = a2 if into == "x" else d2
+        a = torch.empty(rows, width + 3, dtype=dtype, device=DEV)[:, :width]
+        d = torch.empty(rows, width + 5, dtype=dtype, device=DEV)[:, :width]
+        a.copy_(x)
+        d.copy_(dout)
+        to = a if into == "x" else d
         gw, gb = torch.empty_like(dw), torch.empty_like(db)
-        ml2.ml2_layer_norm_grad(a2, d2, w, mean, rstd, grad.ws, to, gw, gb)
+        ml2.ml2_layer_norm_grad(a, d, w, mean, rstd, grad.ws, to, gw, gb)
         torch.cuda.synchronize()
         assert torch.equal(to, dx) and torch.equal(gw, dw) and torch.equal(gb, db)
-        del a, d
     y = x.clone()
     ml2.ml2_layer_norm(y, w, b, y)
     torch.cuda.synchronize()
