@@ -84,32 +84,28 @@ struct Piece {
         if (has(j, width)) *at_column<T>(row, col + j) = narrow<T>(x[j]);
     }
   }
-  // weight or bias of columns j .. j + 3 of the vector, or `none` where there is none
-  template <int HOW = kAny>
-  __device__ __forceinline__ void param4(const void *p, int f32, float none, int width, int j,
-                                         float *x) const {
-    typedef float F __attribute__((ext_vector_type(4), aligned(4)));
-    typedef T H __attribute__((ext_vector_type(4), aligned(sizeof(T))));
-    if (HOW == kAny && (!p || SHORT)) {
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-        x[i] = !p || !has(j + i, width) ? none
-               : f32                    ? static_cast<const float *>(p)[j + i]
-                                        : (float)static_cast<const T *>(p)[j + i];
-    } else if (HOW == kAny ? f32 : HOW == kFloat) {
-      const F v = *at_column<const F>(static_cast<const float *>(p), col + j);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) x[i] = v[i];
-    } else {
-      const H v = *at_column<const H>(static_cast<const T *>(p), col + j);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) x[i] = (float)v[i];
-    }
-  }
+  // weight or bias, or `none` where there is none
   __device__ __forceinline__ void param(const void *p, int f32, float none, int width,
                                         float *x) const {
+    typedef float F __attribute__((ext_vector_type(4), aligned(4)));
+    if (!p || SHORT) {
 #pragma unroll
-    for (int j = 0; j < kLen; j += 4) param4(p, f32, none, width, j, x + j);
+      for (int j = 0; j < kLen; ++j)
+        x[j] = !p || !has(j, width) ? none
+               : f32                ? static_cast<const float *>(p)[j]
+                                    : (float)static_cast<const T *>(p)[j];
+    } else if (f32) {
+#pragma unroll
+      for (int j = 0; j < kLen; j += 4) {
+        const F v = *at_column<const F>(static_cast<const float *>(p), col + j);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[j + i] = v[i];
+      }
+    } else {
+      const auto v = *at_column<const typename Vec<T>::type>(static_cast<const T *>(p), col);
+#pragma unroll
+      for (int j = 0; j < kLen; ++j) x[j] = (float)v[j];
+    }
   }
 };
 
@@ -168,7 +164,19 @@ __global__ __launch_bounds__(WAVE ? kWaveBlock : kMaxBlock,
   const int lane = WAVE ? threadIdx.x & (lanes - 1) : threadIdx.x;
   const int64_t per = WAVE ? kWaveBlock >> log_g : 1;
   const int64_t group = WAVE ? threadIdx.x >> log_g : 0;
-  float w[kKeep ? E : kLen], b[kKeep ? E : kLen];
+  float w[kKeep ? E : kLen], b[kKeep ? E : kLen], y[kLen];
+  // The parameters of kStep columns at a time, in their type, the next ones loaded
+  // before these are used.
+  typedef typename std::conditional<HOW == kSame, T, float>::type Param;
+  constexpr int kStep = HOW == kSame ? kLen : 4, kSteps = E / kStep;
+  typedef Param ParamVec __attribute__((ext_vector_type(kStep), aligned(sizeof(Param))));
+  ParamVec w1, b1;
+  const auto fetch = [&](int q) {
+    const Part at((q * kStep / kLen * lanes + lane) * kLen, anew(width));
+    const int c = at.col + q * kStep % kLen;
+    w1 = *at_column<const ParamVec>(static_cast<const Param *>(a.weight), c);
+    b1 = *at_column<const ParamVec>(static_cast<const Param *>(a.bias), c);
+  };
   if (kKeep) {
 #pragma unroll
     for (int k = 0; k < kVecs; ++k) {
@@ -234,11 +242,11 @@ __global__ __launch_bounds__(WAVE ? kWaveBlock : kMaxBlock,
         }
       }
     }
-    if (WAVE) {
+    if (HOW != kAny) fetch(0);
+    if (WAVE)
       group_sums(t, E > 8 ? 6 : log_g);
-    } else {
+    else
       block_sums(t, second);
-    }
     const float delta = t[0] * over_width;
     const float raw = fmaf(t[1], over_width, -delta * delta);
     const float var = raw < 0.0f ? 0.0f : raw;  // a NaN stays one
@@ -249,25 +257,36 @@ __global__ __launch_bounds__(WAVE ? kWaveBlock : kMaxBlock,
       if (a.rstd) a.rstd[row] = rstd;
     }
     T *dst = static_cast<T *>(a.out) + row * a.out_ld;
+    if constexpr (HOW != kAny) {
 #pragma unroll
-    for (int k = 0; k < kVecs; ++k) {
-      const Part at((k * lanes + lane) * kLen, anew(width));
-      x[k] = anew(x[k]);
-      if (kKeep && !at.any()) continue;
-      float y[kLen];
+      for (int q = 0; q < kSteps; ++q) {
+        const int k = q * kStep / kLen, j0 = q * kStep % kLen;
+        const ParamVec wq = w1, bq = b1;
+        if (q + 1 < kSteps) fetch(q + 1);
+        const Part at((k * lanes + lane) * kLen, anew(width));
+        if (j0 == 0) x[k] = anew(x[k]);
 #pragma unroll
-      for (int j = 0; j < kLen; j += 4) {
-        if (!kKeep) {
-          at.template param4<HOW>(a.weight, a.param_f32, 1.0f, width, j, w + j);
-          at.template param4<HOW>(a.bias, a.param_f32, 0.0f, width, j, b + j);
-        }
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int p = kKeep ? k * kLen + j + i : j + i;
-          y[j + i] = fmaf(fmaf((float)x[k][j + i] - m0, rstd, shift), w[p], b[p]);
-        }
+        for (int j = 0; j < kStep; ++j)
+          y[j0 + j] = fmaf(fmaf((float)x[k][j0 + j] - m0, rstd, shift), (float)wq[j], (float)bq[j]);
+        if (j0 + kStep == kLen) at.store(dst, width, y);
       }
-      at.store(dst, width, y);
+    } else {
+#pragma unroll
+      for (int k = 0; k < kVecs; ++k) {
+        const Part at((k * lanes + lane) * kLen, anew(width));
+        x[k] = anew(x[k]);
+        if (kKeep && !at.any()) continue;
+        if (!kKeep) {
+          at.param(a.weight, a.param_f32, 1.0f, width, w);
+          at.param(a.bias, a.param_f32, 0.0f, width, b);
+        }
+#pragma unroll
+        for (int j = 0; j < kLen; ++j) {
+          const int p = kKeep ? k * kLen + j : j;
+          y[j] = fmaf(fmaf((float)x[k][j] - m0, rstd, shift), w[p], b[p]);
+        }
+        at.store(dst, width, y);
+      }
     }
   }
 }
