@@ -626,25 +626,32 @@ typedef struct ml2_adamw_options {
  *
  * state_bits 32: m and v as they are.  state_bits 8: m and r = sqrt(v) as
  * e4m3 numbers (1 sign, 4 exponent and 3 mantissa bits, bias 7) times a float32
- * scale that each block of ML2_STATE_BLOCK consecutive elements has of its own:
- * scale = max(largest size in the block / 448, 2^-100).  A state of n elements
- * is one array, aligned to 4 bytes, of ceil(n / 256) * 256 bytes (those behind
- * the n-th are neither read nor written) followed by ceil(n / 256) scales;
- * ml2_adamw_state_bytes(8, n).  All bytes 0 stand for zeros.
+ * scale that each block of ML2_STATE_BLOCK consecutive elements has of its own.
+ * A state of n elements is one array, aligned to 4 bytes, of ceil(n / 256) * 256
+ * bytes (those behind the n-th are neither read nor written) followed by
+ * ceil(n / 256) scales; ml2_adamw_state_bytes(8, n).  All bytes 0 stand for zeros.
  * Rounding to the nearest of so few numbers would stop a slow average for good,
- * so sizes are rounded up or down at random, unbiased: up where the 20 bits
- * below the last one kept, plus 16 hashed bits times 16, plus 8, pass 2^20
- * (at most 448; an r that is not 0 does not become 0, so that no element loses
- * its denominator).  The hashed bits depend on seed, t, the tensor's place in
- * `tensors` and the element's index alone: m takes the upper 16 and r the lower
- * 16 bits of
+ * so sizes are rounded up or down at random, unbiased, by bits hashed from seed,
+ * t, the tensor's place in `tensors` and the element's index alone.  In float32,
+ * every operation rounded to the nearest, with b1 = beta1, a1 = 1 - beta1, b2 and
+ * a2 likewise (each rounded once from float64):
+ *   m' = (code_m * scale_m) * b1 + g * a1
+ *   r' = sqrt(((code_r * scale_r) ^ 2) * b2 + (g * a2) * g)
+ *   scale' = max(largest size in the block * (1 / 448), 2^-100)
+ *   size   = |m'| or r' times (1 / scale'),  code = a number of 7 bits:
+ *   (bits of size * 2^-120, a float32 number, + 16 * hashed + 8) >> 20, at most
+ *   126 (448), and at least 1 for an r' that is not 0, so that no element loses its
+ *   denominator; m' gives its sign.
+ * (A root or 1 / scale' may be the number next to the nearest; v' below 2^-126
+ * counts as less than it is.)  The hashed 16 bits are for m the upper and for r the
+ * lower ones of
  *   h = (K + index * 0x9E3779B9) mod 2^32;  h ^= h >> 15;
  *   h = h * 0xC13FA9A9 mod 2^32;            h ^= h >> 16
  * with K from folding the words seed mod 2^32, seed >> 32, t, the place and
  * (from index 2^32 on) index >> 32, by K = mix(K + word + 0x9E3779B9) from 0,
  * mix(k): k ^= k >> 16; k *= 0x9E3779B9; k ^= k >> 15; k *= 0xC13FA9A9;
- * k ^= k >> 16.  A block with a gradient that is NaN or infinite gets a scale of
- * NaN.
+ * k ^= k >> 16.  A block with an m' or r' that is NaN or infinite gets a scale of
+ * NaN for that state.
  *
  * A tensor's arrays share no memory with one another or with another tensor's,
  * but for an output that is its own input, and gradients.

@@ -9,7 +9,7 @@
 //
 // Measured: norm of 134M bf16 elements 53 us (268 MB, 5.1 TB/s); steps of 33.5M
 // float32 parameters 170 us (940 MB, 5.5 TB/s), of 12M in 60 tensors with a bf16 copy
-// 75, of 134M bf16 ones with 8-bit states 280 (1.35 GB, 4.8 TB/s).
+// 75, of 134M bf16 ones with 8-bit states 250 (1.35 GB, 5.4 TB/s).
 #include <math.h>
 
 #include <algorithm>
@@ -393,10 +393,10 @@ __global__ __launch_bounds__(kThreads) void step_kernel(StepTable t, StepShared 
 // bits, denormals included; adding 20 random bits before they are cut off rounds up
 // as often as the part cut off asks for.
 //
-// What is rounded at random should be the value itself: constants that a block
-// shares (b1 and b2 times its scales, the way to units of the new ones) are sums of
-// two float32 numbers, and r keeps what its root cut off, so that m and v are
-// rounded once and their sizes once more.
+// Every operation is float32's own, rounded once, as ml2.h says it: a state's codes
+// are the same wherever they are worked out.  (Constants and products carried as sums
+// of two numbers, so that little is rounded before the codes are, took 281 us for
+// 134M bf16 elements against 250 and changed a code in two million.)
 
 constexpr int kLane = 8;
 static_assert(ML2_STATE_BLOCK == 32 * kLane, "half a wave holds a block");
@@ -439,44 +439,20 @@ __device__ __forceinline__ void decode(Codes c, float (&x)[kLane]) {
   }
 }
 
-// A factor as the sum of two float32 numbers.
-struct Two {
-  float high, low;
-};
-
-__device__ __forceinline__ Two two(double x) {
-  const float high = (float)x;
-  return {high, (float)(x - (double)high)};
-}
-
-__device__ __forceinline__ Two operator*(Two a, float b) {
-  const float high = a.high * b;
-  return {high, fmaf(a.high, b, -high) + a.low * b};
-}
-
-__device__ __forceinline__ float times(float a, Two b, float add) {
-  return fmaf(a, b.high, fmaf(a, b.low, add));
-}
-
-// A block's scale, and what brings its elements to units of it; `most`: the bits
-// of the lane's largest size, ordered as the sizes are, NaN last.  A NaN or an
-// infinity makes the scale NaN.  (The reciprocal is taken of 2^-20 as much: that of
-// the largest numbers would be flushed.  What it is off by is found exactly.)
+// A block's scale, and its reciprocal; `most`: the bits of the lane's largest size,
+// ordered as the sizes are, NaN last.  A NaN or an infinity makes the scale NaN.
 struct Scale {
-  float scale;
-  Two over;
+  float scale, over;
 };
 
 __device__ __forceinline__ Scale block_scale(uint32_t most) {
   const float top = group_fold(__uint_as_float(most), 5, [](float a, float b) {
     return __uint_as_float(max(__float_as_uint(a), __float_as_uint(b)));
   });
-  const Two scale = Two{1.0f / kTop, (float)(1.0 / kTop - (double)(1.0f / kTop))} * top;
-  const float r = __builtin_amdgcn_rcpf(top * 0x1p-20f) * 0x1p-20f, over = kTop * r;
-  Scale s = {scale.high + scale.low, {over, fmaf(-over, top, kTop) * r}};
-  if (!(s.scale > 0x1p-100f)) s = {0x1p-100f, {0x1p100f, 0.0f}};
-  if (!(top < __builtin_inff())) s = {__builtin_nanf(""), {0.0f, 0.0f}};
-  return s;
+  const float scale = fmaxf(top * (1.0f / kTop), 0x1p-100f);
+  const float r = __builtin_amdgcn_rcpf(scale);  // and what it is off by
+  const float over = fmaf(fmaf(-scale, r, 1.0f), r, r);
+  return top < __builtin_inff() ? Scale{scale, over} : Scale{__builtin_nanf(""), 0.0f};
 }
 
 // The code of a size in units of its scale; random: 20 bits, least: the smallest
@@ -492,15 +468,9 @@ struct Scales {
   float *m_out, *r_out;
 };
 
-// What a workgroup needs of the step beside that.
-struct Rates8 {
-  Two b1, b2, a1;  // a1: (1 - b1) factor
-  float a2;        // (1 - b2) factor^2
-};
-
 template <typename P, typename G, bool WHOLE>
 __device__ __forceinline__ void step8_tile(const Arrays<P, G, uint8_t> &t, const Scales &c,
-                                           uint32_t left, const Step &s, const Rates8 &q,
+                                           uint32_t left, const Step &s, const Rates &q,
                                            float decay, uint32_t key) {
   const uint32_t at = threadIdx.x * kLane, block = at / ML2_STATE_BLOCK;
   const bool in = WHOLE || block * ML2_STATE_BLOCK < left;  // the half wave, or none of it
@@ -525,18 +495,16 @@ __device__ __forceinline__ void step8_tile(const Arrays<P, G, uint8_t> &t, const
   }
   decode(mc, m);
   decode(rc, r);
-  const Two old_m = q.b1 * ms, old_v = q.b2 * rs * rs;
-  float rest[kLane];  // what the root of v has beyond r
 #pragma unroll
   for (int j = 0; j < kLane; ++j) {
-    m[j] = fmaf(m[j], old_m.high, fmaf(g[j], q.a1.high, fmaf(m[j], old_m.low, g[j] * q.a1.low)));
-    const float square = r[j] * r[j];  // of 4 bits: exact
-    const float v = fmaf(square, old_v.high, fmaf(g[j] * g[j], q.a2, square * old_v.low));
-    // y: 1 / sqrt(v); v below float32's normal numbers counts as ever less, and an
-    // infinite one gives an infinite root.
+    const float gj = g[j] * s.f, old = r[j] * rs;
+    m[j] = m[j] * ms * q.b1 + gj * q.a1;
+    const float v = old * old * q.b2 + gj * q.a2 * gj;
+    // The root from its reciprocal and what v lacks of its square, which the fused
+    // operation finds exactly.  An infinite v gives an infinite root.
     const float y = __builtin_amdgcn_rsqf(__builtin_amdgcn_fmed3f(v, 0x1p-126f, 0x1.fffffep127f));
-    r[j] = v * y;
-    rest[j] = fmaf(-r[j], r[j], v) * (0.5f * y);
+    const float root = v * y, lacks = fmaf(-root, root, v);
+    r[j] = v < __builtin_inff() ? fmaf(lacks, 0.5f * y, root) : v;
     p[j] -= fmaf(decay, p[j],
                  s.rate * m[j] * __builtin_amdgcn_rcpf(fmaf(r[j], s.root, s.eps)));
     if (!WHOLE && at + j >= left) m[j] = r[j] = 0.0f;
@@ -556,9 +524,9 @@ __device__ __forceinline__ void step8_tile(const Arrays<P, G, uint8_t> &t, const
     uint32_t h = key + (at + (uint32_t)j) * kPhi;
     h = (h ^ (h >> 15)) * kPlastic;
     h ^= h >> 16;
-    const uint32_t a = encode(times(fabsf(m[j]), to_m.over, 0.0f), (h >> 12 & 0xFFFF0u) | 8u, 0);
-    const uint32_t b = encode(times(r[j], to_r.over, rest[j] * to_r.over.high),
-                              (h << 4 & 0xFFFF0u) | 8u, min(__float_as_uint(r[j]), 1u));
+    const uint32_t a = encode(fabsf(m[j]) * to_m.over, (h >> 12 & 0xFFFF0u) | 8u, 0);
+    const uint32_t b = encode(r[j] * to_r.over, (h << 4 & 0xFFFF0u) | 8u,
+                              min(__float_as_uint(r[j]), 1u));
     mo[j >> 2] |= (a | (__float_as_uint(m[j]) >> 24 & 0x80u)) << (8 * (j & 3));
     ro[j >> 2] |= b << (8 * (j & 3));
   }
@@ -576,8 +544,7 @@ __global__ __launch_bounds__(kThreads) void step8_kernel(StepTable t, StepShared
   const int64_t n = t.n[at];
   const Step s = read_step(o);
   const float decay = s.lr * t.decay[at];
-  const Rates8 q = {two(o.b1), two(o.b2), two((1.0 - o.b1) * s.f),
-                    (float)((1.0 - o.b2) * s.f * s.f)};
+  const Rates q = {(float)o.b1, (float)o.b2, (float)(1.0 - o.b1), (float)(1.0 - o.b2)};
   const uint32_t key = fold_word(fold_word(o.key, s.step), (uint32_t)(o.place + at));
   const int64_t codes = (n + ML2_STATE_BLOCK - 1) / ML2_STATE_BLOCK * ML2_STATE_BLOCK;
   const int64_t tile0 = (int64_t)(blockIdx.x - t.first[at]) * o.tiles;

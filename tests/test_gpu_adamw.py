@@ -234,6 +234,36 @@ def test_extreme_sizes_of_gradients():
         assert np.allclose(m[512:768], 1e14, rtol=1e-6) and np.allclose(v[512:768], 1e27, rtol=1e-5)
 
 
+@pytest.mark.parametrize("step", [1, 7])
+def test_states_in_8_bits_code_for_code(step):
+    """The documented float32 arithmetic, worked out by numpy.  A size is other than numpy's only
+    where a root or a block's 1 / scale is the number next to the nearest: by at most 2 of its last
+    bits, so that its code is another one with a chance of 2 in 2^20 (the bits that decide are
+    spread evenly over them): 0.5 of the 2^18 elements on average, were every one of them off.
+    Fewer than 8 differ, by one code, but for a chance of 1e-7."""
+    n, f32 = 1 << 18, np.float32
+    c = Case([n], torch.float32, torch.float32, 8, step=step)
+    c.run()
+    b1, b2, a1, a2 = (f32(x) for x in (0.9, 0.999, 1 - 0.9, 1 - 0.999))
+    g = c.g[0].cpu().numpy()
+    m, r = (t.values(codes).astype(f32) * np.repeat(scale.astype(f32), t.BLOCK)[:n]
+            for codes, scale in (t.split(x[0], n) for x in c.old[1:]))
+    m = m * b1 + g * a1
+    r = np.sqrt(r * r * b2 + g * a2 * g)
+    h = t.hashed(c.seed, step, 0, np.arange(n))
+    for x, state, bits, least in ((m, c.m[0], h >> 16, 0), (r, c.v[0], h & 0xFFFF, 1)):
+        assert x.dtype == f32
+        scale = np.maximum(np.abs(x).reshape(-1, t.BLOCK).max(1) * f32(1 / 448), f32(2.0 ** -100))
+        size = np.abs(x) * np.repeat(f32(1) / scale, t.BLOCK)
+        want = (size * f32(2.0 ** -120)).view(np.uint32).astype(np.int64) + bits * 16 + 8 >> 20
+        want = np.minimum(np.maximum(want, least * (x != 0)), 126)
+        codes, got_scale = t.split(state, n)
+        assert np.all(np.abs(got_scale - scale) <= 4 * U * scale)
+        off = np.abs((codes & 127).astype(np.int64) - want)
+        assert off.max() <= 1 and off.sum() < 8
+        assert np.array_equal(codes >= 128, np.signbit(x))
+
+
 def test_slow_averages_move_in_8_bits():
     """3,000 steps of one gradient a tensor's element: both averages arrive at it.  The mean of
     4,096 unbiased chains is off by far less than the 5 % asked for; rounding to the nearest would
