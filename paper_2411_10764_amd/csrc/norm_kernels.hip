@@ -15,9 +15,9 @@
 // delta beside its own two sums.
 //
 // Measured: 32,768 x 1,024 bf16 27 us (134 MB, 4.9 TB/s; a copy reaches 4.65 to
-// 4.7), 8,192 x 4,096 float32 44 us (6.1 TB/s), 515 x 50,021 fp16 40 us; gradients of
+// 4.7), 8,192 x 4,096 float32 44 us (6.1 TB/s), 515 x 50,021 fp16 39 us; gradients of
 // 32,768 x 1,024 bf16 43 to 47 us (201 MB), of 8,192 x 20,000 bf16 207 us (4.75 TB/s),
-// of 260 x 50,021 float32 57 us, of 96 x 128 float32 7 us.
+// of 260 x 50,021 float32 58 us, of 96 x 128 float32 7 us.
 #include <algorithm>
 #include <type_traits>
 
@@ -719,8 +719,8 @@ hipError_t launch_wide(const NormArgs &a, int cu_count, hipStream_t s) {
   const auto launch = [&](auto fn) { fn<<<(uint32_t)grid, threads, 0, s>>>(a, 0, over); };
   if (kSplit && a.weight && a.bias && a.param_f32)
     launch(norm_kernel<T, E, false, kAnywhere, kSplit ? kFloat : kAny>);
-  else if (kSplit && a.weight && a.bias)
-    launch(norm_kernel<T, E, false, kAnywhere, kSplit ? kSame : kAny>);
+  else if (kSplit && sizeof(T) == 2 && a.weight && a.bias)
+    launch(norm_kernel<T, E, false, kAnywhere, kSplit && sizeof(T) == 2 ? kSame : kAny>);
   else if (!kSplit && a.width == (int64_t)E * threads)
     launch(norm_kernel<T, E, false, kSplit ? kAnywhere : kWhole, kAny>);
   else

@@ -1034,17 +1034,20 @@ class AdamW:
         int32 [1] on the device; factor: float32 [1] on the device, as GradNorm's, or None."""
         o, t = self.options, _t()
         o.lr_device = o.step_device = None
+        used = [self.params[0], factor]
         if isinstance(lr, (int, float)):
             o.lr = lr
         else:
             o.lr_device = _flat(lr, "lr", t.f32, (1,))
+            used.append(lr)
         if isinstance(step, int):
             o.step = step
         else:
             o.step_device = _flat(step, "step", t.i32, (1,))
+            used.append(step)
         o.factor = _flat(factor, "factor", t.f32, (1,))
         ml2_adamw(self.dtype, self.grad_dtype, self.state_bits, self.tensors, self.count, o,
-                  _here(stream, self.params[0], factor))
+                  _here(stream, *used))
         return self.out[0] if self.out is not None else self.params
 
 

@@ -458,3 +458,19 @@ def test_other_gradients(bits):
         for taker in (norm, a.plan):
             with pytest.raises(ValueError):
                 taker.take(bad)
+
+
+@pytest.mark.parametrize("which", ["lr", "step", "factor"])
+def test_rates_of_another_device_are_refused(which):
+    """(here: seen so)"""
+    class Far(torch.Tensor):
+        def get_device(self):
+            return torch.cuda.current_device() + 1
+
+    args = dict(lr=torch.ones(1, device=DEV), step=torch.ones(1, dtype=torch.int32, device=DEV),
+                factor=torch.ones(1, device=DEV))
+    c = Case([5], torch.float32, torch.float32, 32)
+    c.plan.run(**args)
+    args[which] = args[which].as_subclass(Far)
+    with pytest.raises(ValueError, match="current"):
+        c.plan.run(**args)
