@@ -507,11 +507,13 @@ ml2_status ml2_embed_grad(int32_t dtype, const void *dout, int64_t n, int64_t wi
  * the columns 0..width-1 of row r, and rstd = 1 / sqrt(V + eps),
  *   out_i = (x_i - m) * rstd * weight_i + bias_i
  * in float32, sums and squares among it (m to more than its precision), rounded
- * once at the end.  x: [rows][ld] of dtype, out: [rows][out_ld] of dtype.  weight, bias: [width] of param_dtype, which is dtype or
- * ML2_F32, or NULL (1 and 0).  mean, rstd: float32 [rows], what the gradient
- * takes, or NULL.  eps: a positive finite number.  A row that holds a NaN or an
- * infinity, or whose sum passes float32, gives NaN throughout; a row of one value
- * gives bias.
+ * once at the end.  x: [rows][ld] of dtype, out: [rows][out_ld] of dtype.
+ * weight, bias: [width] of param_dtype, which is dtype or ML2_F32, or NULL (1
+ * and 0).  mean, rstd: float32 [rows], what the gradient takes, or NULL.  eps: a
+ * positive finite number.  A row that holds a NaN or an infinity, or whose sum
+ * passes float32, gives NaN throughout; one whose sum of squared distances from m
+ * passes it (distances of 2^56 and more) has an rstd of 0, and gives bias as a row of
+ * one value does.
  * out may be x itself (the same pointer and row stride), and shares no other
  * memory with what the call reads or writes.
  * Errors: INVALID_ARG (unknown dtype or param_dtype, NULL x or out that is

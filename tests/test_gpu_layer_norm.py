@@ -279,12 +279,14 @@ def _eager(x, dout, w, b):
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 def test_rows_whose_sum_passes_float32(width, dtype):
     """2^127 and another number of 2^127 are 2^128: such a row is NaN, the one beside it is not."""
-    x = torch.zeros(2, width, device=DEV, dtype=dtype)
+    x = torch.zeros(3, width, device=DEV, dtype=dtype)
     x[0, :2] = 2.0 ** 127
     x[1, :1] = 2.0 ** 60
-    out, mean, rstd = ml2.LayerNorm(2, width, dtype).run(x)
+    x[2, 0], x[2, 1] = 2.0 ** 64, -2.0 ** 64  # squares that pass it: an rstd of 0
+    out, mean, rstd = ml2.LayerNorm(3, width, dtype).run(x)
     assert out[0].isnan().all() and mean[0].isnan() and rstd[0].isnan()
     assert out[1].isfinite().all() and mean[1].isfinite() and rstd[1] > 0
+    assert (out[2] == 0).all() and mean[2] == 0 and rstd[2] == 0
 
 
 def test_tensors_of_another_device_are_refused(monkeypatch):
