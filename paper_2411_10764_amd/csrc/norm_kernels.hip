@@ -315,15 +315,20 @@ struct GradShape {
   bool direct;        // one workgroup: it writes the parameters' sums itself
 };
 
-// The sum over a wave's groups of 2^log_g lanes, in the lanes of the first.
-__device__ __forceinline__ float fold_groups(float v, int log_g) {
+// Sums over a wave's groups of 2^log_g lanes, in the lanes of the first.
+template <int N>
+__device__ __forceinline__ void fold_groups(float (&v)[N], int log_g) {
+  const auto each = [&](auto fn) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = fn(v[i]);
+  };
   const auto add = [](float p, float r) { return p + r; };
-  if (log_g <= 3) v += lane_swap<0x128>(v);  // row_ror 8
-  if (log_g <= 2) v += lane_swap<0x124>(v);  // row_ror 4
-  if (log_g <= 1) v += lane_swap<0x122>(v);  // row_ror 2
-  if (log_g <= 0) v += lane_swap<0x121>(v);  // row_ror 1
-  if (log_g <= 4) v = join_rows(v, add);
-  return join_halves(v, add);
+  if (log_g <= 3) each([](float x) { return x + lane_swap<0x128>(x); });  // row_ror 8
+  if (log_g <= 2) each([](float x) { return x + lane_swap<0x124>(x); });  // row_ror 4
+  if (log_g <= 1) each([](float x) { return x + lane_swap<0x122>(x); });  // row_ror 2
+  if (log_g <= 0) each([](float x) { return x + lane_swap<0x121>(x); });  // row_ror 1
+  if (log_g <= 4) each([&](float x) { return join_rows(x, add); });
+  each([&](float x) { return join_halves(x, add); });
 }
 
 // Sums of a lane group over all rows it takes go to part[block][0] (weight) and
@@ -468,56 +473,63 @@ __global__ __launch_bounds__(kMaxBlock) void grad_kernel(NormGradArgs a, GradSha
   // The groups of a wave, then the waves: lane i of a wave holds the columns of
   // lane i % lanes.
   if (E == 8 && !wide && g.log_g < 6) {
-#pragma unroll
-    for (int i = 0; i < E; ++i) {
-      dw[i] = fold_groups(dw[i], g.log_g);
-      db[i] = fold_groups(db[i], g.log_g);
-    }
+    fold_groups(dw, g.log_g);
+    fold_groups(db, g.log_g);
   }
   const int parts = wide ? g.per : (int)blockDim.x >> 6;
   float *to = part + (int64_t)blockIdx.x * 2 * width;
   const int own = wide ? group : (int)threadIdx.x >> 6;
   typedef float U4 __attribute__((ext_vector_type(4), aligned(4)));
-  // A lane's columns of `row` and, `apart` floats on, of the bias's.
-  const auto put = [&](float *row, int apart) {
+  // Four sums of a piece, from its column j on.
+  const auto put = [&](const Part &at, int j, F4 v, float *row) {
+    float *p = row + at.col + j;
+    if (at.whole()) {
+      *reinterpret_cast<U4 *>(p) = v;
+    } else {
 #pragma unroll
-    for (int k = 0; k < kVecs; ++k) {
-      const Part at((k * lanes + lane) * kLen, width);
-      float *to = row + at.col;
-      if (at.whole()) {
-#pragma unroll
-        for (int j = 0; j < kLen; j += 4) {
-          const int i = k * kLen + j;
-          *reinterpret_cast<U4 *>(to + j) = U4{dw[i], dw[i + 1], dw[i + 2], dw[i + 3]};
-          *reinterpret_cast<U4 *>(to + apart + j) = U4{db[i], db[i + 1], db[i + 2], db[i + 3]};
-        }
-      } else {
-#pragma unroll
-        for (int j = 0; j < kLen; ++j) {
-          if (at.has(j, width)) {
-            to[j] = dw[k * kLen + j];
-            to[apart + j] = db[k * kLen + j];
-          }
-        }
-      }
+      for (int i = 0; i < 4; ++i)
+        if (at.has(j + i, width)) p[i] = v[i];
     }
   };
-  if (!kJoins) return put(to, width);
+  const auto four = [](const float *v) { return F4{v[0], v[1], v[2], v[3]}; };
+  if (!kJoins) {
+#pragma unroll
+    for (int i = 0; i < E; i += 4) {
+      const Part at((i / kLen * lanes + lane) * kLen, width);
+      put(at, i % kLen, four(dw + i), to);
+      put(at, i % kLen, four(db + i), to + width);
+    }
+    return;
+  }
+  // A part lies in LDS as the weight does, a lane's vectors `lanes` apart: stored by
+  // columns, 32 bytes from lane to lane, 16 parts of 771 took 3.0 us.
+  const int vecs = E / 4 * lanes;  // of a part
+  F4 *joined = reinterpret_cast<F4 *>(lds);
   __syncthreads();
-  // at most lanes * E columns a part
-  if (wide || (int)(threadIdx.x & 63) < lanes) put(lds + own * width, kSpan);
+  if (wide || (int)(threadIdx.x & 63) < lanes) {  // at most kSpan / 4 of all parts
+    F4 *mine = joined + own * vecs + lane;
+#pragma unroll
+    for (int i = 0; i < E; i += 4) {
+      mine[i / 4 * lanes] = four(dw + i);
+      mine[i / 4 * lanes + kSpan / 4] = four(db + i);
+    }
+  }
   __syncthreads();
-  for (int i = threadIdx.x; i < 2 * width; i += blockDim.x) {
-    const int q = i >= width, c = q ? i - width : i;
-    const float *from = lds + q * kSpan + c;
-    float v = from[0];
+  for (int i = threadIdx.x; i < 2 * vecs; i += blockDim.x) {
+    const int q = i >= vecs, slot = q ? i - vecs : i, nth = slot / lanes;
+    const F4 *from = joined + q * (kSpan / 4) + slot;
+    F4 v = from[0];
 #pragma unroll 8
-    for (int p = 1; p < parts; ++p) v += from[p * width];
-    void *out = q ? a.dbias : a.dweight;
-    if (!g.direct)
-      to[i] = v;
-    else if (out)
-      store_as(a.grad_dtype, out, c, v);
+    for (int p = 1; p < parts; ++p) v += from[p * vecs];
+    const Part at((nth * 4 / kLen * lanes + slot - nth * lanes) * kLen, width);
+    const int j = nth * 4 % kLen;
+    if (!g.direct) {
+      put(at, j, v, to + q * width);
+    } else if (void *out = q ? a.dbias : a.dweight) {
+#pragma unroll
+      for (int n = 0; n < 4; ++n)
+        if (at.has(j + n, width)) store_as(a.grad_dtype, out, at.col + j + n, v[n]);
+    }
   }
 }
 
@@ -760,7 +772,16 @@ GradShape grad_shape(int64_t rows, int64_t width) {
   // 8.8 us, in two launches 11.3; 512 x 128 (8) 12.5 and 11.5; 32 x 1,024 bf16 (2) 11.3
   // and 12.8; 48 x 1,024 (3) 13.3 and 12.5; 4 x 4,096 (1) 11.4 and 13.4.
   g.direct = turns <= (grad_columns(width) == 8 ? 4 : g.lanes == 64 ? 2 : width <= kGradWidth);
-  g.blocks = g.direct ? 1 : (int)std::min<int64_t>(turns, kGradBlocks);
+  // Waves of a SIMD follow one another: where all rows are taken at once, as few of
+  // them as make as many workgroups as there may be.  3,001 x 771 fp16 13.2 us, 16 rows a
+  // workgroup 13.8; 2,048 12.0 and 12.5.  (Not where that doubles the parts, or where
+  // they are wider: 256 x 4,096 bf16 13.7 and 11.6, 700 x 4,096 15.4 and 14.9.)
+  if (g.lanes <= 64 && turns >= kGradBlocks / 2 && turns < kGradBlocks) {
+    const int64_t few = (rows + kGradBlocks - 1) / kGradBlocks, wave = 64 / g.lanes;
+    g.per = (int)((few + wave - 1) / wave * wave);
+    g.threads = g.per * g.lanes;
+  }
+  g.blocks = g.direct ? 1 : (int)std::min<int64_t>((rows + g.per - 1) / g.per, kGradBlocks);
   return g;
 }
 
