@@ -536,7 +536,15 @@ __global__ __launch_bounds__(kMaxBlock) void grad_kernel(NormGradArgs a, GradSha
 // ---- gradients of wider rows -------------------------------------------------------
 
 constexpr int kStatThreads = 256, kStatVecs = 4;
-constexpr int kWideThreads = 256, kWideColumns = 8;  // a thread's columns
+
+// A wave a workgroup, with two vectors of a row a lane: 2,048 x 30,000 float32 234 us, of
+// four waves 253, of one wave with four vectors 235; 512 x 65,536 bf16 79, 85 (and
+// with one vector 79), 79.
+template <typename T>
+struct Wide {
+  static constexpr int kThreads = 64, kVecs = 2;
+  static constexpr int64_t kSlab = (int64_t)kThreads * kVecs * Vec<T>::kLen;
+};
 
 // Row sums of x - mean, g and g (x - mean) over a piece of kStatVecs vectors a
 // thread: stat[row][piece][3].
@@ -581,20 +589,20 @@ __global__ __launch_bounds__(kStatThreads) void stat_kernel(NormGradArgs a, int6
   }
 }
 
-// A workgroup takes kWideThreads * kWideColumns columns of `chunk` rows.
+// A workgroup takes a slab of columns of `chunk` rows.
 template <typename T>
-__global__ __launch_bounds__(kWideThreads) void wide_kernel(NormGradArgs a, int64_t pieces,
+__global__ __launch_bounds__(Wide<T>::kThreads) void wide_kernel(NormGradArgs a, int64_t pieces,
                                                             int64_t chunk, float over_width,
                                                             const float *stat, float *part) {
-  constexpr int kLen = Vec<T>::kLen, kVecs = kWideColumns / kLen;
+  constexpr int kLen = Vec<T>::kLen, kVecs = Wide<T>::kVecs, kThreads = Wide<T>::kThreads;
   typedef Piece<T, kAnywhere> Part;
   const int width = (int)a.width;
-  const int c0 = ((int)blockIdx.x * kVecs * kWideThreads + (int)threadIdx.x) * kLen;
+  const int c0 = ((int)blockIdx.x * kVecs * kThreads + (int)threadIdx.x) * kLen;
   const int64_t r0 = (int64_t)blockIdx.y * chunk, r1 = min(a.rows, r0 + chunk);
   float w[kVecs][kLen], dw[kVecs][kLen], db[kVecs][kLen];
 #pragma unroll
   for (int k = 0; k < kVecs; ++k) {
-    Part(c0 + k * kWideThreads * kLen, width).param(a.weight, a.param_f32, 1.0f, width, w[k]);
+    Part(c0 + k * kThreads * kLen, width).param(a.weight, a.param_f32, 1.0f, width, w[k]);
 #pragma unroll
     for (int j = 0; j < kLen; ++j) dw[k][j] = db[k][j] = 0.0f;
   }
@@ -609,7 +617,7 @@ __global__ __launch_bounds__(kWideThreads) void wide_kernel(NormGradArgs a, int6
     const T *ds = static_cast<const T *>(a.dout) + row * a.dout_ld;
 #pragma unroll
     for (int k = 0; k < kVecs; ++k) {
-      const Part at(c0 + k * kWideThreads * kLen, width);
+      const Part at(c0 + k * kThreads * kLen, width);
       x1[k] = at.load(xs, width);
       d1[k] = at.load(ds, width);
     }
@@ -646,7 +654,7 @@ __global__ __launch_bounds__(kWideThreads) void wide_kernel(NormGradArgs a, int6
         y[j] = rstd * fmaf(-along, xhat, fmaf(dj, w[k][j], -g_avg));
       }
       if (a.dx)
-        Part(c0 + k * kWideThreads * kLen, width)
+        Part(c0 + k * kThreads * kLen, width)
             .store(static_cast<T *>(a.dx) + row * a.dx_ld, width, y);
     }
   }
@@ -654,7 +662,7 @@ __global__ __launch_bounds__(kWideThreads) void wide_kernel(NormGradArgs a, int6
   float *to = part + (int64_t)blockIdx.y * 2 * width;
 #pragma unroll
   for (int k = 0; k < kVecs; ++k) {
-    const Part at(c0 + k * kWideThreads * kLen, width);
+    const Part at(c0 + k * kThreads * kLen, width);
 #pragma unroll
     for (int j = 0; j < kLen; ++j) {
       if (at.has(j, width)) {
@@ -792,18 +800,18 @@ int64_t stat_pieces(int64_t width) {  // for the smaller vectors
 
 // A chunk has at least so many rows, and the chunks of all slabs so many workgroups at
 // most: a chunk costs its part of the parameters' sums, a row of a chunk a turn.  100
-// rows of 20,000 bf16 17 us, in chunks of one row 28, of 12 20; 260 of 50,021 float32
-// 55, with 512 workgroups 53, with 1,024 57; 2,048 of 20,000 bf16 98, 105 and 100.
-constexpr int64_t kLeastChunk = 4, kWideBlocks = 640;
+// rows of 20,000 bf16 17 us, in chunks of one row 28, of 12 20; 2,048 of 30,000 float32
+// 234, with 960 or 2,048 workgroups 246; 512 of 65,536 bf16 79, 82 and 82.
+constexpr int64_t kLeastChunk = 4, kWideBlocks = 1280;
 // Rows of more than half of kGradWidth are read twice where there are few: 5 of 16,384
 // bf16 13 us, in registers 16; 320 22 and 30; 512 28 and 29; 1,024 49 and 38; 520 of
 // 20,000 36 and 38, 1,000 55 and 44.
 constexpr int64_t kFewRows = 512;
-constexpr int64_t kWideSlab = (int64_t)kWideThreads * kWideColumns;
 
 // Rows of a chunk.
+template <typename T>
 int64_t wide_chunk(int64_t rows, int64_t width) {
-  const int64_t slabs = (width + kWideSlab - 1) / kWideSlab;
+  const int64_t slabs = (width + Wide<T>::kSlab - 1) / Wide<T>::kSlab;
   const int64_t chunks = std::max<int64_t>(1, std::min<int64_t>(rows / kLeastChunk, kWideBlocks / slabs));
   return (rows + chunks - 1) / chunks;
 }
@@ -844,11 +852,11 @@ hipError_t launch_grad(const NormGradArgs &a, void *ws, hipStream_t s) {
     part += (size_t)a.rows * stat_pieces(a.width) * 3;
     const int64_t items = std::min<int64_t>(a.rows * pieces, 1 << 20);
     stat_kernel<T><<<(uint32_t)items, kStatThreads, 0, s>>>(a, pieces, stat);
-    const int64_t chunk = wide_chunk(a.rows, a.width);
-    const dim3 grid((uint32_t)((a.width + kWideSlab - 1) / kWideSlab),
+    const int64_t chunk = wide_chunk<T>(a.rows, a.width);
+    const dim3 grid((uint32_t)((a.width + Wide<T>::kSlab - 1) / Wide<T>::kSlab),
                     (uint32_t)((a.rows + chunk - 1) / chunk));
     parts = (int)grid.y;
-    wide_kernel<T><<<grid, kWideThreads, 0, s>>>(a, pieces, chunk, over, stat,
+    wide_kernel<T><<<grid, Wide<T>::kThreads, 0, s>>>(a, pieces, chunk, over, stat,
                                                  sums ? part : nullptr);
   }
   if (sums && !done) {
@@ -873,7 +881,8 @@ size_t layer_norm_grad_workspace_bytes(int64_t rows, int64_t width) {
   if (!grad_twice(rows, width, 2))
     floats = (size_t)grad_shape(rows, width).blocks * 2 * (size_t)width;
   if (grad_twice(rows, width, 4)) {
-    const int64_t chunk = wide_chunk(rows, width);
+    const int64_t chunk =
+        std::min(wide_chunk<float>(rows, width), wide_chunk<__bf16>(rows, width));
     floats = std::max(floats, (size_t)rows * (size_t)stat_pieces(width) * 3 +
                                   (size_t)((rows + chunk - 1) / chunk) * 2 * (size_t)width);
   }
