@@ -777,9 +777,11 @@ GradShape grad_shape(int64_t rows, int64_t width) {
   g.per = g.threads / g.lanes;
   const int64_t turns = (rows + g.per - 1) / g.per;
   // A turn costs less than the launch that joins parts: 256 x 128 float32 (4 turns)
-  // 8.8 us, in two launches 11.3; 512 x 128 (8) 12.5 and 11.5; 32 x 1,024 bf16 (2) 11.3
-  // and 12.8; 48 x 1,024 (3) 13.3 and 12.5; 4 x 4,096 (1) 11.4 and 13.4.
-  g.direct = turns <= (grad_columns(width) == 8 ? 4 : g.lanes == 64 ? 2 : width <= kGradWidth);
+  // 8.8 us, in two launches 10.1; 512 x 128 (8) 12.5 and 10.2; 32 x 1,024 bf16 (2) 8.5
+  // and 9.8; 64 x 1,024 (4) 12.3 and 11.3; 8 x 4,096 (2) 10.2 and 11.7; 2 x 8,192 (1) 9.9
+  // and 11.6; 4 x 8,192 (2) 12.2 and 11.4; 1 x 10,000 (1) 10.6 and 12.2; 1 x 16,384 14.2
+  // and 12.2.
+  g.direct = turns <= (grad_columns(width) == 8 ? 4 : g.lanes <= 256 ? 2 : width <= 12 * kMaxBlock);
   // Waves of a SIMD follow one another: where all rows are taken at once, as few of
   // them as make as many workgroups as there may be.  3,001 x 771 fp16 13.2 us, 16 rows a
   // workgroup 13.8; 2,048 12.0 and 12.5.  (Not where that doubles the parts, or where
@@ -803,10 +805,11 @@ int64_t stat_pieces(int64_t width) {  // for the smaller vectors
 // rows of 20,000 bf16 17 us, in chunks of one row 28, of 12 20; 2,048 of 30,000 float32
 // 234, with 960 or 2,048 workgroups 246; 512 of 65,536 bf16 79, 82 and 82.
 constexpr int64_t kLeastChunk = 4, kWideBlocks = 1280;
-// Rows of more than half of kGradWidth are read twice where there are few: 5 of 16,384
-// bf16 13 us, in registers 16; 320 22 and 30; 512 28 and 29; 1,024 49 and 38; 520 of
-// 20,000 36 and 38, 1,000 55 and 44.
-constexpr int64_t kFewRows = 512;
+// Rows of more than half of kGradWidth, of which a compute unit has one or two, are read
+// twice too: 200 of 10,000 bf16 19 us, in registers 21; 300 21 and 23; 400 24 and 23; of
+// 16,384 float32 60 rows 15 and 15, 200 19 and 21, 300 25 and 30, 512 35 and 34.  Very
+// few are done sooner with fewer launches: 5 of 10,000 14 and 12.
+constexpr int64_t kTwiceFrom = 64, kTwiceTo = 320;
 
 // Rows of a chunk.
 template <typename T>
@@ -819,7 +822,7 @@ int64_t wide_chunk(int64_t rows, int64_t width) {
 // Whether rows are read twice.
 bool grad_twice(int64_t rows, int64_t width, size_t size) {
   return width > (size == 2 ? kGradWidth16 : kGradWidth) ||
-         (width > kGradWidth / 2 && rows <= kFewRows);
+         (width > kGradWidth / 2 && rows > kTwiceFrom && rows <= kTwiceTo);
 }
 
 template <typename T>
