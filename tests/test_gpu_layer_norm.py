@@ -114,6 +114,16 @@ def test_rows(dtype, rows, width):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,width", [
+    (64, 8193), (65, 8193), (320, 8193), (321, 8193), (64, 20001), (65, 20001),  # read twice
+    (2, 8192), (3, 8192), (8, 4096), (9, 4096), (1, 12288), (1, 12289), (2, 12288),  # launches
+    (2032, 1024), (2033, 1001), (4080, 600), (4081, 600), (16257, 60), (20000, 9),  # waves
+    (12400, 100), (9000, 200), (4100, 257)])
+def test_rows_at_the_gradients_borders(dtype, rows, width):
+    _both(dtype, rows, width)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("kind", ["far", "outlier", "one", "small"])
 @pytest.mark.parametrize("width", [6, 64, 771, 3000, 17000])
 def test_values(dtype, kind, width):
