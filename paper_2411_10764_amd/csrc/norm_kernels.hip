@@ -16,8 +16,8 @@
 //
 // Measured: 32,768 x 1,024 bf16 27 us (134 MB, 4.9 TB/s; a copy reaches 4.65 to
 // 4.7), 8,192 x 4,096 float32 44 us (6.1 TB/s), 515 x 50,021 fp16 39 us; gradients of
-// 32,768 x 1,024 bf16 43 to 47 us (201 MB), of 8,192 x 20,000 bf16 207 us (4.75 TB/s),
-// of 260 x 50,021 float32 58 us, of 96 x 128 float32 7 us.
+// 32,768 x 1,024 bf16 41 to 44 us (201 MB), of 8,192 x 20,000 bf16 208 us (4.7 TB/s),
+// of 260 x 50,021 float32 57 us, of 96 x 128 float32 7 us.
 #include <algorithm>
 #include <type_traits>
 
@@ -296,7 +296,7 @@ __global__ __launch_bounds__(WAVE ? kWaveBlock : kMaxBlock,
 constexpr int kGradBlocks = 256;   // at most: each leaves a part of the parameters' sums
 // Widest rows that stay in a workgroup's registers, of 32-bit and of 16-bit columns: 24
 // of those a lane fill 126 registers with their sums (32 would spill 34).  2,048 x
-// 24,576 bf16 83 us, read twice 114; 2,048 x 16,384 float32 101, 16,385 146.
+// 24,576 bf16 82 us, read twice 114; 2,048 x 16,384 float32 95, 16,385 136.
 constexpr int kGradWidth = 16 * kMaxBlock, kGradWidth16 = 24 * kMaxBlock;
 
 __device__ __forceinline__ void store_as(int dtype, void *p, int64_t i, float v) {
@@ -704,7 +704,8 @@ __global__ __launch_bounds__(kJoinColumns *kJoinSlices) void join_kernel(NormGra
   lds[slice][lane] = v;
   __syncthreads();
   if (slice == 0 && c < a.width) {
-    for (int k = 1; k < slices; ++k) v += lds[k][lane];
+#pragma unroll
+    for (int k = 1; k < kJoinSlices; ++k) v += k < slices ? lds[k][lane] : 0.0f;
     store_as(a.grad_dtype, to, c, v);
   }
 }
@@ -730,10 +731,22 @@ hipError_t launch_narrow(const NormArgs &a, int cu_count, hipStream_t s) {
   return hipGetLastError();
 }
 
+// Workgroups of a row of so many waves: as many as a compute unit holds, of which each
+// SIMD takes a fourth of the waves, rounded up.  (12,000 x 10,000 bf16, of ten waves: 94
+// us, three a compute unit 114; 12,000 x 5,000, of five: 49, six 51; 4,096 x 9,000 31 and
+// 29.)  Rows whose parameters do not stay in registers lose nothing with a workgroup of
+// their own, and then a row's loads do not wait for the last one's stores: 16,384 x 20,000
+// bf16 235, as above 258; 4,096 x 40,000 fp16 128 and 136.  It pays after some rows:
+// 2,048 x 32,768 50 and 56, 1,536 x 50,024 70 and 68, 1,024 x 50,021 62 and 55.
+int64_t wide_grid(int64_t rows, int waves, bool own, int cu_count) {
+  const int64_t fit = (int64_t)cu_count * (waves <= 4 ? 32 / waves : 8 / ((waves + 3) / 4));
+  return std::min(rows, own && rows > 3 * fit ? (int64_t)1 << 20 : fit);
+}
+
 template <typename T, int E>
 hipError_t launch_wide(const NormArgs &a, int cu_count, hipStream_t s) {
   const int threads = (int)((a.width + 64 * E - 1) / (64 * E) * 64);
-  const int64_t grid = std::min<int64_t>(a.rows, (int64_t)cu_count * (2048 / threads));
+  const int64_t grid = wide_grid(a.rows, threads / 64, E > 16, cu_count);
   const float over = 1.0f / (float)a.width;
   constexpr bool kSplit = E > 16;
   const auto launch = [&](auto fn) { fn<<<(uint32_t)grid, threads, 0, s>>>(a, 0, over); };
