@@ -32,11 +32,28 @@ Range range(const void *p, int64_t bytes) {
   return {at, p && bytes > 0 ? at + (uintptr_t)bytes : at};
 }
 
-Range matrix(const void *p, int64_t rows, int64_t width, int64_t ld, size_t size) {
-  return range(p, rows > 0 && width > 0 ? ((rows - 1) * ld + width) * (int64_t)size : 0);
+bool meet(Range a, Range b) { return a.at < b.end && b.at < a.end && a.at < a.end && b.at < b.end; }
+
+// Rows of `bytes` bytes, `pitch` bytes apart; what lies between them is not theirs.
+struct Rows {
+  uintptr_t at;
+  uint64_t rows, bytes, pitch;
+};
+
+Rows matrix(const void *p, int64_t rows, int64_t width, int64_t ld, size_t size) {
+  const bool any = p && rows > 0 && width > 0;
+  return {reinterpret_cast<uintptr_t>(p), any ? (uint64_t)rows : 0, (uint64_t)width * size,
+          (uint64_t)ld * size};
 }
 
-bool meet(Range a, Range b) { return a.at < b.end && b.at < a.end && a.at < a.end && b.at < b.end; }
+// The row in which b begins, or behind which, or else the next one.  No end of the
+// matrix is worked out: with the largest sizes it lies beyond 64 bits.
+bool meet(const Rows &a, Range b) {
+  if (a.rows == 0 || b.at >= b.end || b.end <= a.at) return false;
+  const uint64_t from = b.at > a.at ? b.at - a.at : 0, row = from / a.pitch, in = from % a.pitch;
+  if (row >= a.rows) return false;
+  return in < a.bytes || (row + 1 < a.rows && b.end - b.at > a.pitch - in);
+}
 
 bool same(Range a, Range b) { return a.at == b.at && a.end == b.end; }
 
@@ -91,11 +108,11 @@ ml2_status ml2_layer_norm(int32_t dtype, const void *x, int64_t rows, int64_t wi
     return fail(ML2_ERR_INVALID_ARG, "ml2_layer_norm: an array is not aligned to its type");
   const Range params[2] = {range(weight, width * (int64_t)param_size),
                            range(bias, width * (int64_t)param_size)};
-  const Range in = matrix(x, rows, width, ld, size), to = matrix(out, rows, width, out_ld, size);
+  const Rows in = matrix(x, rows, width, ld, size), to = matrix(out, rows, width, out_ld, size);
   const Range stats[2] = {range(mean, rows * 4), range(rstd, rows * 4)};
   bool bad = shares(x, ld, out, out_ld, rows, width, size) || meet(stats[0], stats[1]);
-  for (const Range &p : params) bad = bad || meet(p, to) || meet(p, stats[0]) || meet(p, stats[1]);
-  for (const Range &p : stats) bad = bad || meet(p, in) || meet(p, to);
+  for (const Range &p : params) bad = bad || meet(to, p) || meet(p, stats[0]) || meet(p, stats[1]);
+  for (const Range &p : stats) bad = bad || meet(in, p) || meet(to, p);
   if (bad)
     return fail(ML2_ERR_INVALID_ARG, "ml2_layer_norm: out, mean or rstd shares memory with "
                 "another array");
@@ -147,22 +164,23 @@ ml2_status ml2_layer_norm_grad(int32_t dtype, const void *x, int64_t rows, int64
   const size_t need = ml2::layer_norm_grad_workspace_bytes(rows, width);
   if (workspace_bytes < need)
     return fail(ML2_ERR_INVALID_ARG, "%s: workspace %zu < %zu bytes", call, workspace_bytes, need);
-  const Range read[5] = {matrix(x, rows, width, ld, size), matrix(dout, rows, width, dout_ld, size),
-                         range(weight, width * (int64_t)param_size), range(mean, rows * 4),
+  const Rows in[2] = {matrix(x, rows, width, ld, size), matrix(dout, rows, width, dout_ld, size)};
+  const Range read[3] = {range(weight, width * (int64_t)param_size), range(mean, rows * 4),
                          range(rstd, rows * 4)};
   const Range ws = range(workspace, (int64_t)need);
-  const Range to = dx ? matrix(dx, rows, width, dx_ld, size) : range(nullptr, 0);
+  const Rows to = matrix(dx, rows, width, dx_ld, size);
   const Range sums[2] = {range(dweight, width * (int64_t)grad_size),
                          range(dbias, width * (int64_t)grad_size)};
   bool bad = dx && (shares(x, ld, dx, dx_ld, rows, width, size) ||
                     shares(dout, dout_ld, dx, dx_ld, rows, width, size));
   bad = bad || meet(to, ws) || meet(sums[0], sums[1]);
-  for (const Range &p : sums) bad = bad || meet(p, ws) || meet(p, to);
-  for (const Range &p : read) {
-    bad = bad || meet(p, ws);
-    for (const Range &q : sums) bad = bad || meet(p, q);
+  for (const Range &q : sums) {
+    bad = bad || meet(q, ws) || meet(to, q);
+    for (const Rows &p : in) bad = bad || meet(p, q);
+    for (const Range &p : read) bad = bad || meet(p, q);
   }
-  for (int i = 2; i < 5; ++i) bad = bad || meet(read[i], to);
+  for (const Rows &p : in) bad = bad || meet(p, ws);
+  for (const Range &p : read) bad = bad || meet(p, ws) || meet(to, p);
   if (bad)
     return fail(ML2_ERR_INVALID_ARG, "%s: dx, dweight, dbias or workspace shares memory with "
                 "another array", call);

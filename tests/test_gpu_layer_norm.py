@@ -326,3 +326,50 @@ def test_objects_refuse_other_rows():
                  lambda: grad.run(x, x, w, mean[:3], rstd), lambda: ln.run(x.t().contiguous().t())):
         with pytest.raises(ValueError):
             call()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,width", [(9, 24), (70, 1000), (9, 17000)])
+def test_arrays_between_the_rows(dtype, rows, width):
+    """Parameters, statistics, sums and the workspace in the columns behind the rows of one buffer:
+    the same bits as in memory of their own."""
+    print(f"[layer_norm] between rows: {dtype} {rows} x {width}", flush=True)
+    rng = np.random.default_rng(rows + width)
+    x, dout = (_rows(rng, rows, width, dtype).to(DEV) for _ in range(2))
+    w, b = (p.to(DEV) for p in _params(rng, width, torch.float32))
+    need = ml2.ml2_layer_norm_grad_workspace_bytes(rows, width)
+    span = -(-width * 4 // 256) * 256  # bytes of a row and of each array in a row's gap
+    pitch = 2 * span + -(-need // 256) * 256
+    whole = torch.full((5 * rows * pitch,), 77, dtype=torch.uint8, device=DEV)
+    free = torch.ones(5 * rows, pitch, dtype=torch.bool, device=DEV)
+
+    def rows_of(i):  # the rows i, i + 5, ... of the buffer
+        view = whole.view(dtype).view(5 * rows, -1)[i::5, :width]
+        free[i::5, :width * dtype.itemsize] = False
+        return view
+
+    def behind(row, n):
+        at = row * pitch + span
+        free.view(-1)[at: at + 4 * n] = False
+        return whole[at: at + 4 * n].view(torch.float32)
+
+    xs, ds, out, dx = (rows_of(i) for i in range(4))
+    ws, bs, dw, db = (behind(row, width) for row in (0, 1, 2, 3))
+    mean, rstd = (behind(row, rows) for row in (4, 5))
+    at = 7 * pitch + 2 * span
+    space = whole[at: at + max(need, 1)]
+    free.view(-1)[at: at + max(need, 1)] = False
+    for to, v in ((xs, x), (ds, dout), (ws, w), (bs, b)):
+        to.copy_(v)
+    ml2.ml2_layer_norm(xs, ws, bs, out, mean, rstd)
+    ml2.ml2_layer_norm_grad(xs, ds, ws, mean, rstd, space, dx, dw, db)
+    ln, grad = ml2.LayerNorm(rows, width, dtype), ml2.LayerNormGrad(rows, width, dtype, torch.float32)
+    want = ln.run(x, w, b)
+    want += grad.run(x, dout, w, want[1], want[2])
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, v) for a, v in zip((out, mean, rstd, dx, dw, db), want))
+    assert torch.equal(xs, x) and torch.equal(ds, dout) and torch.equal(ws, w)
+    assert torch.all(whole[free.view(-1)] == 77)
+    inside = whole[2 * pitch: 2 * pitch + 4 * rows].view(torch.float32)  # out's first row
+    with pytest.raises(ml2.Ml2Error, match="shares memory"):
+        ml2.ml2_layer_norm(xs, ws, bs, out, inside, rstd)

@@ -1,6 +1,7 @@
 """The operators of a training step without a GPU: bad arguments are refused synchronously with
 the documented status, before any HIP call, and size queries answer."""
 import ctypes
+import random
 
 import pytest
 
@@ -194,3 +195,51 @@ def test_the_binding_refuses():
     for make in (lambda: ml2.GradNorm([]), lambda: ml2.AdamW([], [])):
         with pytest.raises(ValueError, match="hold"):
             make()
+
+
+# ---- memory between the rows ---------------------------------------------------------
+
+@pytest.mark.parametrize("name", ["x", "dout"])
+def test_a_workspace_meets_rows_only_in_their_elements(name):
+    """A call that has nothing to write ends after its checks: OK where the workspace has no
+    element of the rows, between them too, and refused where it has one."""
+    rng = random.Random(5)
+    seen = {True: 0, False: 0}
+    for _ in range(4000):
+        dtype, size = rng.choice(((F32, 4), (BF16, 2), (F16, 2)))
+        rows, width = rng.randint(0, 6), rng.randint(1, 7)
+        need = ml2.ml2_layer_norm_grad_workspace_bytes(rows, width)
+        ld = width + rng.randint(0, 3 * need // size + 4)
+        off = rng.randint(-(rows * ld + 10), need // size + 10)
+        at = WS + off * size
+        used = {at + r * ld * size + i for r in range(rows) for i in range(width * size)}
+        want = any(WS <= b < WS + need for b in used)
+        rest = dict(dict(ld=8, dout_ld=8), **{name: at, "ld" if name == "x" else "dout_ld": ld})
+        got = _grad(dtype, rows=rows, width=width, pd=dtype, gd=dtype, dx=None, dw=None, db=None,
+                    ws_bytes=need, **rest)
+        assert got == (INVALID if want else OK), (dtype, rows, width, ld, off)
+        seen[want] += 1
+    assert min(seen.values()) > 500
+
+
+FAR = dict(rows=(1 << 31) - 1, width=8, ld=1 << 32)  # the last row lies beyond 64 bits
+PITCH, P = 1 << 34, 1 << 40
+
+
+@pytest.mark.parametrize("at", [P, P + 28, P - 4 * FAR["rows"] + 4, P + PITCH, P + 2 * PITCH + 28])
+def test_statistics_in_rows_that_reach_far(at):
+    """No other two arrays meet: out's rows lie behind the statistics' 8.6 GB."""
+    for name in ("mean", "rstd"):
+        assert _norm(**FAR, **dict(dict(x=P, w=None, b=None, mean=None, rstd=None), out=P + (3 << 32),
+                                   out_ld=1 << 32, **{name: at})) == INVALID
+        assert "shares memory" in ml2.lib().ml2_last_error().decode()
+
+
+@pytest.mark.parametrize("bad", [
+    dict(dw=P + 7 * PITCH), dict(dw=P + 7 * PITCH + 64 + 28), dict(db=P + 7 * PITCH + 28),
+    dict(ws=P + 5 * PITCH), dict(dx=P + 3 * PITCH + 512, dx_ld=1 << 32, dw=P + 9 * PITCH + 512)])
+def test_sums_and_a_workspace_in_rows_that_reach_far(bad):
+    args = dict(x=P, dout=P + 64, dout_ld=1 << 32, w=None, mean=P + 1024, rstd=P + PITCH + 1024,
+                dx=None, dw=None, db=None, ws=P + 5 * PITCH + 256)
+    assert _grad(**FAR, **dict(args, **bad)) == INVALID
+    assert "shares memory" in ml2.lib().ml2_last_error().decode()
