@@ -1030,18 +1030,18 @@ class AdamW:
             self._fill()
 
     def run(self, lr, step, factor=None, stream=None):
-        """The new parameters.  lr: a number, or float32 [1] on the device; step: a number, or
+        """The new parameters.  lr: a number, or float32 [1] on the device; step: a whole number, or
         int32 [1] on the device; factor: float32 [1] on the device, as GradNorm's, or None."""
         o, t = self.options, _t()
         o.lr_device = o.step_device = None
         used = [self.params[0], factor]
-        if isinstance(lr, (int, float)):
-            o.lr = lr
+        if isinstance(lr, (int, float, np.integer, np.floating)):
+            o.lr = float(lr)
         else:
             o.lr_device = _flat(lr, "lr", t.f32, (1,))
             used.append(lr)
-        if isinstance(step, int):
-            o.step = step
+        if isinstance(step, (int, np.integer)):
+            o.step = int(step)
         else:
             o.step_device = _flat(step, "step", t.i32, (1,))
             used.append(step)

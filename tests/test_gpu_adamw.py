@@ -474,3 +474,16 @@ def test_rates_of_another_device_are_refused(which):
     args[which] = args[which].as_subclass(Far)
     with pytest.raises(ValueError, match="current"):
         c.plan.run(**args)
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_rates_of_numpy(bits):
+    """numpy's numbers are numbers: the same bits as Python's."""
+    a, b = (Case([3000, 70], torch.float32, torch.float32, bits, step=7) for _ in range(2))
+    a.run(lr=2.0 ** -10, step=7)
+    b.run(lr=np.float32(2.0 ** -10), step=np.int64(7))
+    for x, y in zip((*a.p, *a.m, *a.v), (*b.p, *b.m, *b.v)):
+        assert torch.equal(x, y)
+    for bad in (7.0, np.float64(7), "7"):
+        with pytest.raises((ValueError, AttributeError)):
+            a.plan.run(2.0 ** -10, bad)
