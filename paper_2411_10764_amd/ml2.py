@@ -1032,6 +1032,8 @@ class AdamW:
     def run(self, lr, step, factor=None, stream=None):
         """The new parameters.  lr: a number, or float32 [1] on the device; step: a whole number, or
         int32 [1] on the device; factor: float32 [1] on the device, as GradNorm's, or None."""
+        if lr is None or step is None:  # _flat() lets None pass, and the last call's would stay
+            raise ValueError("lr and step must be given")
         o, t = self.options, _t()
         o.lr_device = o.step_device = None
         used = [self.params[0], factor]

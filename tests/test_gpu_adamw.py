@@ -487,3 +487,15 @@ def test_rates_of_numpy(bits):
     for bad in (7.0, np.float64(7), "7"):
         with pytest.raises((ValueError, AttributeError)):
             a.plan.run(2.0 ** -10, bad)
+
+
+def test_a_step_without_its_rates_is_refused():
+    """None is not the rate or the step of the call before."""
+    c = Case([50], torch.float32, torch.float32, 32)
+    c.run()
+    kept = c.p[0].clone()
+    for lr, step in ((None, 3), (1e-3, None), (None, None)):
+        with pytest.raises(ValueError, match="given"):
+            c.plan.run(lr, step)
+    torch.cuda.synchronize()
+    assert torch.equal(c.p[0], kept)
