@@ -82,11 +82,7 @@ __device__ __forceinline__ float group_fold(float v, int log_g, F f) {
   return v;
 }
 
-__device__ __forceinline__ float group_sum(float v, int log_g) {
-  return group_fold(v, log_g, [](float a, float b) { return a + b; });
-}
-
-// The same for N sums at once: one decision a step where log_g is not known when
+// That for N sums at once: one decision a step where log_g is not known when
 // this is compiled, and the steps of one sum between those of another.
 template <int N>
 __device__ __forceinline__ void group_sums(float (&v)[N], int log_g) {
@@ -114,22 +110,6 @@ __device__ __forceinline__ void load_floats(const T *row, int64_t c, int64_t wid
   } else {
 #pragma unroll
     for (int j = 0; j < kLen; ++j) x[j] = c + j < width ? (float)row[c + j] : 0.0f;
-  }
-}
-
-// Those places of a row, rounded once.
-template <typename T>
-__device__ __forceinline__ void store_floats(T *row, int64_t c, int64_t width, const float *x) {
-  constexpr int kLen = Vec<T>::kLen;
-  if (c + kLen <= width) {
-    typename Vec<T>::type v;
-#pragma unroll
-    for (int j = 0; j < kLen; ++j) v[j] = narrow<T>(x[j]);
-    *reinterpret_cast<typename Vec<T>::type *>(row + c) = v;
-  } else {
-#pragma unroll
-    for (int j = 0; j < kLen; ++j)
-      if (c + j < width) row[c + j] = narrow<T>(x[j]);
   }
 }
 
