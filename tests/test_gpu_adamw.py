@@ -499,3 +499,61 @@ def test_a_step_without_its_rates_is_refused():
             c.plan.run(lr, step)
     torch.cuda.synchronize()
     assert torch.equal(c.p[0], kept)
+
+
+def _state_bytes(c):
+    """What a step has left of every tensor, without the bytes behind an 8-bit state's elements."""
+    if c.bits == 32:
+        return [*c.p, *c.m, *c.v]
+    return c.p + [torch.cat(ml2_parts(x, n)) for xs in (c.m, c.v) for x, n in zip(xs, c.sizes)]
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("P,G", [(torch.float32, torch.float32), (torch.bfloat16, torch.float16)])
+@pytest.mark.parametrize("step", [1, 7, 1000, 2 ** 31 - 1])
+def test_device_and_host_rates_agree_in_every_bit(bits, P, G, step):
+    """Parameters, and for 8 bits codes and scales, of a step whose rate and number lie on the device
+    are those of the same step from the host: float32 holds the rate, and the two rates are worked
+    out in float64 on both sides, so that they round to other float32 numbers only where the
+    functions' last places decide, with a chance of some 2^-28.  A number off by one gives other
+    parameters (but for steps so late that the corrections are 1) and other codes."""
+    sizes, lr = [3000, 70, 4097], 2.0 ** -10
+
+    def stepped(**rates):
+        c = Case(sizes, P, G, bits, step=step)
+        c.run(**rates)
+        return _state_bytes(c)
+
+    def device(n):
+        return torch.tensor([n], dtype=torch.int32, device=DEV)
+
+    want = stepped(lr=lr, step=step)
+    rate = torch.tensor([lr], device=DEV)
+    for rates in (dict(lr=rate, step=device(step)), dict(lr=rate, step=step),
+                  dict(lr=lr, step=device(step))):
+        assert all(torch.equal(a, b) for a, b in zip(stepped(**rates), want)), rates.keys()
+    other = stepped(lr=rate, step=device(step - 1 if step > 1 else 2))
+    if step < 1000:
+        assert not torch.equal(other[0], want[0])
+    if bits == 8:
+        assert not torch.equal(other[3], want[3]) and not torch.equal(other[6], want[6])
+    assert not torch.equal(stepped(lr=2 * rate, step=device(step))[0], want[0])
+
+
+@pytest.mark.parametrize("step", [3, 1000])
+def test_states_in_8_bits_by_the_devices_step(step):
+    """Parameters, codes and scales against 64 bits, rate and number on the device."""
+    c = Case([3000, 70, 4097], torch.float32, torch.float32, 8, step=step)
+    c.run(lr=torch.tensor([HYPER["lr"]], device=DEV),
+          step=torch.tensor([step], dtype=torch.int32, device=DEV))
+    c.check()
+
+
+@pytest.mark.parametrize("seed", [0, (3 << 32) | 5, 5 << 32, 2 ** 64 - 1])
+def test_seeds_of_64_bits(seed):
+    """Both words of the seed are in the hash."""
+    c, low = (Case([3000, 70], torch.float32, torch.float32, 8, seed=s) for s in (seed, seed & t.LOW))
+    c.run()
+    low.run()
+    c.check()
+    assert torch.equal(c.m[0], low.m[0]) == (seed < 1 << 32)

@@ -373,3 +373,31 @@ def test_arrays_between_the_rows(dtype, rows, width):
     inside = whole[2 * pitch: 2 * pitch + 4 * rows].view(torch.float32)  # out's first row
     with pytest.raises(ml2.Ml2Error, match="shares memory"):
         ml2.ml2_layer_norm(xs, ws, bs, out, inside, rstd)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("params", ["float32", "rows"])
+@pytest.mark.parametrize("rows,width", [(600, 50021), (1700, 33000), (1700, 20001), (4500, 9000),
+                                        (700, 65536)])
+def test_more_rows_than_workgroups(dtype, params, rows, width):
+    """A wide row has the same bits whatever other rows a call has: as one of so many that
+    workgroups take several, or have one each, and among 100.  Some of them, on both sides of
+    where workgroups begin their second row, are held against 64 bits too."""
+    print(f"[layer_norm] many rows: {dtype} {params} {rows} x {width}", flush=True)
+    g = torch.Generator(device=DEV).manual_seed(rows + width)
+    x = torch.empty(rows, width, dtype=dtype, device=DEV)
+    for at in range(0, rows, 100):
+        x[at: at + 100] = torch.randn(min(100, rows - at), width, generator=g, device=DEV) * 1.7 + 0.4
+    w, b = (p.to(DEV) for p in _params(np.random.default_rng(width), width,
+                                       torch.float32 if params == "float32" else dtype))
+    out, mean, rstd = ml2.LayerNorm(rows, width, dtype).run(x, w, b)
+    for at in range(0, rows, 100):
+        few = ml2.LayerNorm(len(x[at: at + 100]), width, dtype).run(x[at: at + 100], w, b)
+        for have, want in zip((out, mean, rstd), few):
+            assert torch.equal(have[at: at + 100], want)
+    some = [r for r in (0, 255, 256, 511, 512, 1023, 1535, 1536) if r < rows - 1] + [rows - 1]
+    y, m, r, xhat = t.layer_norm(wide(x[some]), wide(w), wide(b), float(np.float32(1e-5)))
+    tol, mtol, rtol = t.layer_norm_tolerance(wide(x[some]), wide(w), xhat, y, r, dtype)
+    assert t.close(wide(out[some]), y, tol, dtype)
+    assert np.all(np.abs(wide(mean[some]) - m) <= mtol)
+    assert np.all(np.abs(wide(rstd[some]) - r) <= rtol)
