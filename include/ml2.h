@@ -537,9 +537,11 @@ ml2_status ml2_layer_norm(int32_t dtype, const void *x, int64_t rows, int64_t wi
  * are held in float32 in an order that depends on the sizes and the device
  * alone, so results are the same in every run.  rows = 0 gives zeros.
  * dx may be x or dout itself (the same pointer and row stride); nothing else
- * that is written shares memory with what the call reads or writes.
+ * that is written shares memory with what the call reads or writes.  (Columns
+ * behind width are neither read nor written, so other arrays may lie there.)
  * workspace: at least ml2_layer_norm_grad_workspace_bytes(rows, width) bytes of
- * device memory, 256-byte aligned, used by this call until it completes.
+ * device memory, 256-byte aligned, used by this call until it completes.  Fewer
+ * rows may need more: one for several sizes is as large as the largest of theirs.
  * Errors as ml2_layer_norm; INVALID_ARG for another grad_dtype or a small
  * workspace.
  */

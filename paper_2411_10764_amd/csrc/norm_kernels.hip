@@ -149,7 +149,8 @@ __device__ __forceinline__ void block_sums(float (&v)[N], float (*lds)[N]) {
 
 // E columns a lane, as they came, so that a wide row's fit the registers, and those
 // of two rows where they are at most 128 bytes a lane (hence the bound of 8 waves a
-// SIMD: a compute unit loads one row while it writes another).  WAVE:
+// SIMD: a compute unit loads one row while it writes another; with 64 columns and
+// parameters loaded ahead one to three registers do not fit and lie in scratch).  WAVE:
 // 2^log_g lanes share a row, else the workgroup does.  Vector k of a lane lies at
 // column (k * lanes + lane) * kLen.
 template <typename T, int E, bool WAVE, Ends ENDS, Params HOW>
@@ -731,8 +732,12 @@ hipError_t launch_narrow(const NormArgs &a, int cu_count, hipStream_t s) {
   return hipGetLastError();
 }
 
-// Workgroups of a row of so many waves: as many as a compute unit holds, of which each
-// SIMD takes a fourth of the waves, rounded up.  (12,000 x 10,000 bf16, of ten waves: 94
+// Workgroups of a row of so many waves: as many as a compute unit holds at eight waves a
+// SIMD, which takes a fourth of a workgroup's waves, rounded up.  Float32 rows that fill
+// their 16 columns a lane have 65 registers, so seven, and those of 64 columns a lane 99 or
+// 116, so four: of these, some workgroups begin when others have ended.  2,048 x 16,384
+// float32 takes 54 us, 16,380 columns (63 registers) 48, 15,360 51, 15,350 45; 8,192 x
+// 8,192, of eight waves, 100, 8,190 columns 104.  (12,000 x 10,000 bf16, of ten waves: 94
 // us, three a compute unit 114; 12,000 x 5,000, of five: 49, six 51; 4,096 x 9,000 31 and
 // 29.)  Rows whose parameters do not stay in registers lose nothing with a workgroup of
 // their own, and then a row's loads do not wait for the last one's stores: 16,384 x 20,000

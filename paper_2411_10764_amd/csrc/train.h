@@ -82,7 +82,7 @@ __device__ __forceinline__ float group_fold(float v, int log_g, F f) {
   return v;
 }
 
-// That for N sums at once: one decision a step where log_g is not known when
+// N numbers summed over such groups: one decision a step where log_g is not known when
 // this is compiled, and the steps of one sum between those of another.
 template <int N>
 __device__ __forceinline__ void group_sums(float (&v)[N], int log_g) {

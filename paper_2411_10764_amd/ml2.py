@@ -855,7 +855,8 @@ def ml2_grad_norm(grads, norm, factor, workspace, max_norm: float = float("inf")
 
 def ml2_adamw(param_dtype, grad_dtype, state_bits: int, tensors, count: int,
               options: ml2_adamw_options, stream=None) -> None:
-    """A step of AdamW over an array of ml2_adamw_tensor."""
+    """A step of AdamW over an array of ml2_adamw_tensor.  It holds addresses, as the options do, so
+    that nothing here can tell whether they are the current device's, as they have to be."""
     _check(lib().ml2_adamw(_dtype(param_dtype), _dtype(grad_dtype), state_bits, tensors, count,
                            ctypes.byref(options), _stream(stream)))
 
