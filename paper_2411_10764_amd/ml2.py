@@ -951,6 +951,10 @@ class GradNorm:
         return self.norm, self.factor
 
 
+_WHOLE = (int, np.integer)
+_NUMBER = (float, np.floating, *_WHOLE)
+
+
 class AdamW:
     """ml2_adamw over a program's parameters and gradient buffers, which it keeps (take() names
     other gradients).
@@ -1038,12 +1042,12 @@ class AdamW:
         o, t = self.options, _t()
         o.lr_device = o.step_device = None
         used = [self.params[0], factor]
-        if isinstance(lr, (int, float, np.integer, np.floating)):
-            o.lr = float(lr)
+        if isinstance(lr, _NUMBER):
+            o.lr = lr
         else:
             o.lr_device = _flat(lr, "lr", t.f32, (1,))
             used.append(lr)
-        if isinstance(step, (int, np.integer)):
+        if isinstance(step, _WHOLE):
             o.step = int(step)
         else:
             o.step_device = _flat(step, "step", t.i32, (1,))
